@@ -54,11 +54,17 @@ extern "C" {
 #define CB_MAX_BRANCHES 4     /* branch tensors sharing one residual group */
 #define CB_MAX_NUMEL (1LL << 48) /* elements per branch tensor */
 #define CB_CACHE_ALIGN 256    /* byte alignment of the cache arena and of each tensor in it */
+#define CB_INT8_BLOCK 64      /* consecutive elements that share a scale in a CB_INT8 history */
 #define CB_STATUS_BYTES 256   /* device status block at the end of the cache arena */
 
 typedef struct cb_plan cb_plan; /* opaque, host-owned */
 
-typedef enum { CB_BF16 = 0, CB_FP32 = 1 } cb_dtype;
+typedef enum {
+    CB_BF16 = 0,
+    CB_FP32 = 1,
+    CB_INT8 = 2, /* of the history buffer only: 8-bit codes with block scales (cb_plan_create) */
+    CB_E4M3 = 3  /* of the full step's operators only */
+} cb_dtype;
 
 /* One cached branch tensor (Sec. 3.1: the self-attention, cross-attention
  * and MLP outputs S^l, C^l, M^l of block l). `group` names the hidden state
@@ -124,6 +130,17 @@ int cb_schedule_full(int T, int r, int s0, int s1, int K, uint8_t* is_full, int*
  * App. A, Eq. general_weights, are computed here on the normalised times
  * tau = 2 (t - t_min) / (t_max - t_min) - 1. tensors: host array of n_tensors
  * descriptors (copied). cache_dtype: storage type of the history buffer.
+ *   CB_BF16, CB_FP32: the features, converted by cb_cache_push.
+ *   CB_INT8: half the memory and traffic of CB_BF16. Every block of CB_INT8_BLOCK
+ *       consecutive elements of a tensor is held as integers q in [-127, 127] and one
+ *       bf16 scale s: s = max |x| * fp32(1/127), rounded up to a bf16, at least 2^-126;
+ *       q = x * fp32(1/s), rounded to nearest, ties to even. The value held is s q:
+ *       within s/2 of x. A block with a feature that is not finite has no finite scale,
+ *       and its predictions are NaN. Skipped steps compute sum_j w_j s_j q_j in fp32
+ *       (error: (K + 3) 2^-24 sum_j |w_j s_j q_j|), add hidden states in fp32 and
+ *       round once. An entry whose weight is zero is not read. Every call serves such a
+ *       plan; CB_OPT_KERNEL, CB_OPT_WAIT_NS and CB_OPT_TEST_WITHHOLD do not
+ *       concern it (its kernels wait for nothing).
  * out: receives the new plan. Errors: CB_ERR_ARG (K < 1, n_nodes < K, bad
  * descriptor, t_min >= t_max, non-monotone nodes), CB_ERR_LIMIT (K >
  * CB_MAX_K, more than CB_MAX_TENSORS tensors or CB_MAX_BRANCHES members of
@@ -134,7 +151,10 @@ int cb_plan_create(const double* node_t, int n_nodes, int K, const cb_tensor_des
 
 /* Bytes of device memory the history buffer needs: K slots followed by a
  * CB_STATUS_BYTES status block. Slot p starts at p * slot_bytes; inside it
- * tensor i starts at sum_{k<i} roundup(numel_k * esize, CB_CACHE_ALIGN). */
+ * tensor i starts at sum_{k<i} roundup(numel_k * esize, CB_CACHE_ALIGN). With
+ * CB_INT8 tensor k takes roundup(numel_k, CB_CACHE_ALIGN) bytes of codes, the last
+ * block filled up with zeros, and behind them roundup(2 * ceil(numel_k /
+ * CB_INT8_BLOCK), CB_CACHE_ALIGN) bytes of scales. */
 size_t cb_plan_cache_bytes(const cb_plan* plan);
 
 /* Attach caller-owned device memory as the history buffer (the plan never

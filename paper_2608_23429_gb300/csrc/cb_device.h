@@ -104,6 +104,7 @@ struct ExtrapArgs {
     unsigned i_row[kMaxItems];          // tokens * hidden of the item's tensors
     unsigned long long i_hidden_magic[kMaxItems];  // ceil(2^64 / i_hidden) (0: i_hidden = 1)
     unsigned long long i_row_magic[kMaxItems];     // ceil(2^64 / i_row) (0: i_row = 1)
+    int src_bf16;                       // int8 cache write: the features are bf16 (else fp32)
 };
 
 // One full-step launch: copy/convert every tensor into one ring slot.
@@ -207,6 +208,20 @@ cudaError_t epilogue_blocks_per_sm(int* blocks);
 cudaError_t launch_push(const PushArgs& a, bool src_bf16, bool dst_bf16, int grid, size_t smem, cudaStream_t s);
 // with `smem` bytes of dynamic shared memory, for which the kernel's limit is raised
 cudaError_t push_blocks_per_sm(bool src_bf16, bool dst_bf16, size_t smem, int* blocks);
+
+// The int8 history (quant.cu): codes with one bf16 scale per kQuantBlock
+// elements. `write`: a full step's slot write (m_off the features' addresses, m_out
+// the codes'), with the hidden-state update where `grouped`; otherwise a skipped
+// step. Declared weak: the host side links without them, over stand-ins of
+// the other launchers, and refuses the cache type there.
+constexpr int kQuantBlock = 64;
+long long quant_tile_elems(bool write) __attribute__((weak));
+cudaError_t quant_blocks_per_sm(int K, bool grouped, bool write, int* blocks) __attribute__((weak));
+cudaError_t launch_quant_read(const ExtrapArgs& a, int K, bool grouped, int grid, cudaStream_t s) __attribute__((weak));
+cudaError_t launch_quant_write(const ExtrapArgs& a, bool grouped, int grid, cudaStream_t s) __attribute__((weak));
+
+// Notes a failed CUDA call for cb_last_error_message and returns CB_ERR_CUDA (plan.cpp).
+int cuda_error(cudaError_t e, const char* where);
 
 // Status word of cb_extrapolate_noalloc in the library's own device block
 // (static_status.cu): its device address on `device`, which must be the

@@ -32,6 +32,15 @@ size_t esize(cb_dtype d) { return d == CB_BF16 ? 2 : 4; }
 bool valid_dtype(cb_dtype d) { return d == CB_BF16 || d == CB_FP32; }
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// Bytes of a tensor in a slot: its elements, or its int8 codes and their scales,
+// each padded to CB_CACHE_ALIGN.
+size_t slot_tensor_bytes(long long numel, cb_dtype cache) {
+    if (cache != CB_INT8) return round_up((size_t)numel * esize(cache), CB_CACHE_ALIGN);
+    static_assert(cbk::kQuantBlock == CB_INT8_BLOCK, "one block size");
+    const size_t blocks = ((size_t)numel + CB_INT8_BLOCK - 1) / CB_INT8_BLOCK;
+    return round_up((size_t)numel, CB_CACHE_ALIGN) + round_up(2 * blocks, CB_CACHE_ALIGN);
+}
+
 // Barycentric weights rho_j = 1 / prod_{k != j} (x_j - x_k) (App. A, Eq. general_weights).
 bool rho_of(const double* x, int n, double* rho) {
     for (int j = 0; j < n; ++j) {
@@ -69,6 +78,7 @@ struct DeviceInfo {
     int occ_extrap[2][CB_MAX_K + 1] = {};  // [cache_bf16][K]
     int occ_push[2][2] = {};               // [src_bf16][dst_bf16]
     int occ_epilogue = 0;                  // epilogue kernel (bf16 features, no gates)
+    int occ_quant[2][2][CB_MAX_K + 1] = {};  // int8 history: [write][grouped][K]
     int bulk_stages[2][CB_MAX_K + 1] = {};  // 1 once the kernel's shared-memory limit is raised
     int bulk_gated[2][CB_MAX_K + 1] = {};   // the same for the gated kernel
     int bulk_precise[2][2][CB_MAX_K + 1] = {};  // [gated]: the same for fp32 predictions or hidden states
@@ -439,6 +449,39 @@ int launch_epilogue(Launch& L, cbk::ExtrapArgs& A) {
     return e == cudaSuccess ? CB_OK : cuda_fail(e, "epilogue launch");
 }
 
+// The int8 history's kernels: a full step's slot write or a skipped step.
+int launch_quant(Launch& L, cbk::ExtrapArgs& A) {
+    bool grouped = false;
+    for (int i = 0; i < A.n_items; ++i) grouped = grouped || A.resid[i] != nullptr;
+    const bool write = L.full_step;
+    int K = 1;
+    if (!write) {  // entries of weight zero are not read (a target on a node reads that node alone)
+        K = 0;
+        for (int j = 0; j < L.K; ++j) {
+            if (A.w_hi[j] == 0.0f) continue;
+            A.w_hi[K] = A.w_hi[j];
+            A.slot_off[K++] = A.slot_off[j];
+        }
+        K = std::max(K, 1);
+    }
+    int& occ = L.p->dev.occ_quant[write ? 1 : 0][grouped ? 1 : 0][K];
+    if (occ == 0) {
+        cudaError_t e = cbk::quant_blocks_per_sm(K, grouped, write, &occ);
+        if (e != cudaSuccess || occ <= 0) {
+            occ = 0;
+            return cuda_fail(e == cudaSuccess ? cudaErrorInvalidConfiguration : e, "occupancy");
+        }
+    }
+    int r = cut_tiles(A, cbk::quant_tile_elems(write), false);
+    if (r == CB_OK) r = clear_status(L);
+    if (r != CB_OK) return r;
+    const int grid = (int)std::min<long long>(A.tiles_total, (long long)L.p->dev.sms * occ);
+    A.overlap = 1;
+    const cudaStream_t s = (cudaStream_t)L.stream;
+    const cudaError_t e = write ? cbk::launch_quant_write(A, grouped, grid, s) : cbk::launch_quant_read(A, K, grouped, grid, s);
+    return e == cudaSuccess ? CB_OK : cuda_fail(e, write ? "int8 cache write launch" : "int8 extrapolate launch");
+}
+
 // The bulk-copy pipeline. `strided`: every item is off the 16-byte grid on its
 // way out (see the kernel's STRIDED).
 int launch_bulk(Launch& L, cbk::ExtrapArgs& A, bool strided) {
@@ -608,7 +651,7 @@ int run_launch(cb_plan* p, const Window& win, const double* w, void* const* outs
     if (!ch && !p->cache) return CB_ERR_UNBOUND;
     const int K = win.n;
     if (K < 1 || (!feats && !ch && p->count < K)) return CB_ERR_HISTORY_NOT_FULL;
-    if (!valid_dtype(out_dtype) || !valid_dtype(resid_dtype)) return CB_ERR_ARG;
+    if ((!feats && !valid_dtype(out_dtype)) || !valid_dtype(resid_dtype)) return CB_ERR_ARG;
     const int n = (int)p->tensors.size();
     const int ng = (int)p->groups.size();
     const size_t oes = esize(out_dtype), res = esize(resid_dtype);
@@ -652,6 +695,7 @@ int run_launch(cb_plan* p, const Window& win, const double* w, void* const* outs
         A.w_anchor[j] = anchor_weight(std::fabs((double)hi), K, cb16);
     }
     A.out_bf16 = out_dtype == CB_BF16;
+    A.src_bf16 = cb16 ? 1 : 0;
     A.resid_bf16 = resid_dtype == CB_BF16;
 
     int items = 0, members = 0;
@@ -718,6 +762,7 @@ int run_launch(cb_plan* p, const Window& win, const double* w, void* const* outs
     rc = ensure_device(p);
     if (rc != CB_OK) return rc;
     Launch L{p, K, cb16, feats != nullptr, res, gate_dtype, stream, ch};
+    if (p->cache_dtype == CB_INT8) return launch_quant(L, A);
     if (p->kernel == CB_KERNEL_DIRECT) return launch_direct(L, A);
     auto aligned_items = [&](cbk::ExtrapArgs& B) { return epilogue ? launch_epilogue(L, B) : launch_bulk(L, B, false); };
     int n_strided = 0;
@@ -735,7 +780,18 @@ int run_launch(cb_plan* p, const Window& win, const double* w, void* const* outs
     return aligned_items(B);
 }
 
+// The pair (t, f_t) is in H from now on; the oldest entry was overwritten when full.
+void note_push(cb_plan* p, double t) {
+    p->slot_t[p->next] = t;
+    p->next = (p->next + 1) % p->K;
+    if (p->count < p->K) ++p->count;
+    p->has_last = true;
+    p->last_t = t;
+}
+
 }  // namespace
+
+int cbk::cuda_error(cudaError_t e, const char* where) { return cuda_fail(e, where); }
 
 extern "C" {
 
@@ -763,7 +819,7 @@ int cb_plan_create(const double* node_t, int n_nodes, int K, const cb_tensor_des
     if (K < 1 || K > CB_MAX_K) return K < 1 ? CB_ERR_ARG : CB_ERR_LIMIT;
     if (!node_t || n_nodes < K || !tensors || n_tensors < 1) return CB_ERR_ARG;
     if (n_tensors > CB_MAX_TENSORS) return CB_ERR_LIMIT;
-    if (!valid_dtype(cache_dtype)) return CB_ERR_ARG;
+    if (!valid_dtype(cache_dtype) && !(cache_dtype == CB_INT8 && cbk::launch_quant_read)) return CB_ERR_ARG;
     if (!(std::isfinite(t_min) && std::isfinite(t_max) && t_min < t_max)) return CB_ERR_ARG;
     for (int i = 0; i < n_nodes; ++i)
         if (!std::isfinite(node_t[i])) return CB_ERR_ARG;
@@ -814,7 +870,7 @@ int cb_plan_create(const double* node_t, int n_nodes, int K, const cb_tensor_des
         p->off.resize(n_tensors);
         for (int i = 0; i < n_tensors; ++i) {
             p->off[i] = (long long)o;
-            o = round_up(o + (size_t)p->tensors[i].numel * esize(cache_dtype), CB_CACHE_ALIGN);
+            o += slot_tensor_bytes(p->tensors[i].numel, cache_dtype);
         }
         p->slot_bytes = o;
         p->sh_tokens.assign(n_tensors, 0);
@@ -856,6 +912,15 @@ int cb_cache_push(cb_plan* p, const void* const* feats, cb_dtype feat_dtype, dou
     for (int j = 0; j < p->count; ++j)
         if (p->slot_t[(p->oldest() + j) % p->K] == t) return CB_ERR_NODES_DEGENERATE;
 
+    if (p->cache_dtype == CB_INT8) {  // a one-entry launch without hidden states
+        Window one{};
+        one.n = 1;
+        const double w1[1] = {1.0};
+        const int r = run_launch(p, one, w1, nullptr, p->cache_dtype, nullptr, CB_BF16, stream, nullptr, CB_BF16, feats,
+                                 feat_dtype);
+        if (r == CB_OK) note_push(p, t);
+        return r;
+    }
     cbk::PushArgs& A = *p->pargs;
     const bool sb = feat_dtype == CB_BF16, db = p->cache_dtype == CB_BF16;
     A.slot = p->cache + (size_t)p->next * p->slot_bytes;
@@ -883,12 +948,7 @@ int cb_cache_push(cb_plan* p, const void* const* feats, cb_dtype feat_dtype, dou
     if (rc != CB_OK) return rc;
     cudaError_t e = cbk::launch_push(A, sb, db, grid, smem, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "push launch");
-    // the pair (t, f_t) is now in H; the oldest entry was overwritten when full
-    p->slot_t[p->next] = t;
-    p->next = (p->next + 1) % p->K;
-    if (p->count < p->K) ++p->count;
-    p->has_last = true;
-    p->last_t = t;
+    note_push(p, t);
     return CB_OK;
 }
 
@@ -1050,13 +1110,8 @@ int cb_cache_push_residual(cb_plan* p, const void* const* feats, cb_dtype feat_d
     const double w1[1] = {1.0};
     rc = run_launch(p, one, w1, nullptr, p->cache_dtype, resid, resid_dtype, stream, gates, gate_dtype, feats,
                     feat_dtype);
-    if (rc != CB_OK) return rc;
-    p->slot_t[p->next] = t;
-    p->next = (p->next + 1) % p->K;
-    if (p->count < p->K) ++p->count;
-    p->has_last = true;
-    p->last_t = t;
-    return CB_OK;
+    if (rc == CB_OK) note_push(p, t);
+    return rc;
 }
 
 int cb_weights(const cb_plan* p, double t_target, double* w_logical) {
