@@ -1,0 +1,73 @@
+/*
+ * chebboost_block.h — the full step's operators around the history, in the same
+ * library: the norm that takes a block's hidden state with the last branch added,
+ * and the matrix product whose epilogue makes a branch output and the new hidden
+ * state (paper Sec. 3.1: B(x) = x + S(x) + C(x) + M(x), each branch a norm and
+ * matrix products). Their results are what cb_cache_push stores.
+ *
+ * Conventions are those of chebboost.h: the caller owns every device buffer and
+ * stream, work is enqueued on `stream` asynchronously, all arguments are
+ * checked before anything is enqueued, and a negative status is an error
+ * (cb_status_string, cb_last_error_message). No call allocates device memory.
+ * Buffers given for output must not overlap inputs, but for the one pair that
+ * each call names.
+ *
+ * Rows and samples: a call works on `rows` rows of [batch, tokens, features]
+ * flattened; row r belongs to sample r / tokens, whose line of a gate, scale or
+ * shift it uses.
+ */
+#ifndef CHEBBOOST_BLOCK_H
+#define CHEBBOOST_BLOCK_H
+
+#include "chebboost.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Sizes and types of cb_norm_residual. Strides are in elements from one row (or
+ * sample) to the next; 0 means contiguous. */
+typedef struct {
+    int64_t rows;          /* >= 0; 0 does nothing */
+    int64_t hidden;        /* >= 1 */
+    int64_t tokens;        /* rows of one sample; 0: all rows are one sample */
+    int64_t x_stride;
+    int64_t branch_stride;
+    int64_t x_out_stride;
+    int64_t out_stride;
+    int64_t line_stride;   /* from one sample's gate, scale and shift to the next's */
+    cb_dtype x_dtype;      /* of x and x_out: CB_BF16 or CB_FP32 */
+    cb_dtype branch_dtype; /* CB_BF16 or CB_FP32 */
+    cb_dtype param_dtype;  /* of gate, weight, scale, shift: CB_BF16 or CB_FP32 */
+    cb_dtype out_dtype;    /* CB_BF16, CB_FP32 or CB_E4M3 */
+    float eps;             /* >= 0, finite */
+    int32_t reserved;      /* must be 0 */
+} cb_norm_desc;
+
+/* Root-mean-square norm with the residual's addition. For every row
+ *     h = x + gate * branch
+ *     x_out = round(h)
+ *     n = h / sqrt(mean(h^2) + eps) * weight
+ *     y = n * (1 + scale) + shift
+ * in fp32 (h enters the norm un-rounded), and out = y in bf16 or fp32, or
+ *     out_scale = max(max |y| * fp32(1/448), 2^-126) of the row,
+ *     out = y * fp32(1/out_scale) in e4m3, to nearest even,
+ * so that out * out_scale stands for y. x, branch, x_out, out: rows of `hidden`
+ * elements; gate, scale, shift: a line per sample; weight: one line; out_scale:
+ * one float a row (CB_E4M3 only). branch, gate (with a branch only), weight,
+ * scale, shift and x_out may be NULL: no addition, factors 1, terms 0, h not
+ * stored. x_out may be x itself (same stride). With eps > 0 a row of zeros gives
+ * zeros (with shift: its values). A row that holds a value that is not finite gives NaN,
+ * and no other row does.
+ * Rows and hidden sizes on the 16-byte grid take vector loads, others elements.
+ * Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size), CB_ERR_LIMIT
+ * (rows or hidden beyond 2^31 - 1), CB_ERR_CUDA. */
+int cb_norm_residual(const cb_norm_desc* desc, const void* x, const void* branch, const void* gate,
+                     const void* weight, const void* scale, const void* shift, void* x_out, void* out,
+                     float* out_scale, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* CHEBBOOST_BLOCK_H */
