@@ -66,6 +66,72 @@ int cb_norm_residual(const cb_norm_desc* desc, const void* x, const void* branch
                      const void* weight, const void* scale, const void* shift, void* x_out, void* out,
                      float* out_scale, void* stream);
 
+/* Activations of a matrix product's epilogue. */
+enum {
+    CB_ACT_NONE = 0,
+    CB_ACT_GELU = 1, /* v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))), the form of the blocks' MLPs */
+    CB_ACT_SILU = 2  /* v / (1 + exp(-v)) */
+};
+
+/* A layer: what a program lays out once. w: [out_features, in_features] row-major
+ * (w_stride elements from row to row, 0: contiguous), of `type`. */
+typedef struct {
+    int64_t in_features;   /* >= 1 */
+    int64_t out_features;  /* >= 1 */
+    int64_t w_stride;
+    cb_dtype type;         /* of w and of the rows x: CB_BF16 or CB_E4M3 */
+    cb_dtype bias_dtype;   /* CB_BF16 or CB_FP32 */
+    int32_t activation;    /* CB_ACT_* */
+    int32_t reserved;      /* must be 0 */
+    const void* w;
+    const float* w_scale;  /* CB_E4M3 only: [out_features] (NULL: 1) */
+    const void* bias;      /* [out_features] (NULL: 0) */
+} cb_linear_desc;
+
+/* Sizes and types of one cb_linear_run. Strides are in elements; 0 means contiguous. */
+typedef struct {
+    int64_t rows;             /* >= 0; 0 does nothing */
+    int64_t tokens;           /* rows of one sample; 0: all rows are one sample */
+    int64_t x_stride;
+    int64_t out_stride;
+    int64_t resid_stride;
+    int64_t resid_out_stride;
+    int64_t gate_stride;      /* from one sample's gate to the next's */
+    cb_dtype out_dtype;       /* CB_BF16 or CB_FP32 */
+    cb_dtype resid_dtype;     /* of resid and resid_out: CB_BF16 or CB_FP32 */
+    cb_dtype gate_dtype;      /* CB_BF16 or CB_FP32 */
+    int32_t reserved;         /* must be 0 */
+} cb_linear_io;
+
+typedef struct cb_linear cb_linear; /* opaque, host-owned; holds no device memory */
+
+/* Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size), CB_ERR_LIMIT (features beyond
+ * 2^31 - 1, or a row of w or x beyond 2^31 - 256 bytes). The layer keeps the pointers: its buffers must outlive it. */
+int cb_linear_create(const cb_linear_desc* desc, cb_linear** out);
+void cb_linear_destroy(cb_linear* layer);
+
+/* Matrix product with its epilogue. For every row m and output feature n
+ *     v = act(x_scale[m] * w_scale[n] * sum_k x[m, k] w[n, k] + bias[n])
+ *     out = round(v)                        the branch output, as cb_cache_push takes it
+ *     resid_out = round(resid + gate * v)   the hidden state (gate: a line per sample)
+ * with sums, epilogue and hidden state in fp32 and one rounding to each result.
+ * x_scale: one float a row (CB_E4M3 only, NULL: 1). out may be NULL, resid and resid_out
+ * may be NULL together, gate (with resid only) may be NULL: 1; one result at least
+ * is wanted. resid_out may be resid itself (same stride). The order of a sum depends
+ * on the sizes alone: equal calls give equal bits.
+ * Operands whose rows start on 16-byte boundaries (and whose in_features fill whole
+ * 16 bytes) come by TMA, others by words; both run on the tensor cores.
+ * Every wait of the kernels on one of their barriers has a limit of a second; one that
+ * runs out is noted in the status word of cb_linear_device_status and makes the
+ * kernel return early, with incomplete results.
+ * Errors: CB_ERR_ARG, CB_ERR_ALIGN, CB_ERR_LIMIT (rows beyond 2^31 - 1024), CB_ERR_CUDA. */
+int cb_linear_run(const cb_linear* layer, const cb_linear_io* io, const void* x, const float* x_scale,
+                  const void* resid, const void* gate, void* out, void* resid_out, void* stream);
+
+/* The status word of this device's matrix products (CB_DEV_* codes, 0: nothing noted since the last
+ * read) into *status, and clear it. Synchronises `stream`. Errors: CB_ERR_ARG, CB_ERR_CUDA. */
+int cb_linear_device_status(int* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif
