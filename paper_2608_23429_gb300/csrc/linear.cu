@@ -9,57 +9,71 @@ namespace {
 
 __device__ int g_linear_status;  // CB_DEV_* codes of this device's launches
 
-template <bool FP8>
-__device__ __forceinline__ float operand(const void* p, long long row_bytes, int row, int k) {
-    const char* a = reinterpret_cast<const char*>(p) + row * row_bytes;
-    if constexpr (!FP8) return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(a)[k] << 16);
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t) reinterpret_cast<const uint8_t*>(a)[k]));
-    return __half2float(__ushort_as_half((unsigned short)h));
-}
-
-// 64 x 64 outputs of a CTA, 4 x 4 of a thread, operands staged as fp32.
-template <bool FP8>
-__global__ void __launch_bounds__(256) linear_simple_kernel(const __grid_constant__ LinearArgs A) {
-    __shared__ float xs[16][65], ws[16][65];
-    after_previous();
-    const int K = FP8 ? A.k_bytes : A.k_bytes / 2, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-    const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
-    float4 v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = 0; k0 < K; k0 += 16) {
-        for (int i = threadIdx.x; i < 1024; i += 256) {
-            const int r = i / 16, k = i % 16;
-            xs[k][r] = m0 + r < A.M && k0 + k < K ? operand<FP8>(A.x, A.x_row, m0 + r, k0 + k) : 0.0f;
-            ws[k][r] = n0 + r < A.N && k0 + k < K ? operand<FP8>(A.w, A.w_row, n0 + r, k0 + k) : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = xs[k][tr * 4 + i];
-                v[i].x = fmaf(a, ws[k][tc * 4], v[i].x);
-                v[i].y = fmaf(a, ws[k][tc * 4 + 1], v[i].y);
-                v[i].z = fmaf(a, ws[k][tc * 4 + 2], v[i].z);
-                v[i].w = fmaf(a, ws[k][tc * 4 + 3], v[i].w);
-            }
-        __syncthreads();
-    }
-    if (A.x_scale)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = m0 + tr * 4 + i;
-            const float s = row < A.M ? A.x_scale[row] : 0.0f;
-            v[i] = make_float4(v[i].x * s, v[i].y * s, v[i].z * s, v[i].w * s);
-        }
-    lin_finish<4>(A, m0 + tr * 4, 1, n0 + tc * 4, v);
-}
-
 bool wide_type(cb_dtype t) { return t == CB_BF16 || t == CB_FP32; }
 size_t bytes_of(int t) { return t == CB_BF16 ? 2 : t == CB_FP32 ? 4 : 1; }
 bool on_grid(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
+
+// What the calls need to know of a device, found out by the first one there.
+struct Device {
+    int sms, smem, pairs;
+    int* status;
+};
+std::atomic<const Device*> g_devices[kMaxStatusDevices];
+using Encode = decltype(&cuTensorMapEncodeTiled);
+std::atomic<Encode> g_encode;
+
+int device_info(const Device** out) {
+    int d = 0;
+    cudaError_t e = cudaGetDevice(&d);
+    if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+    if (d >= kMaxStatusDevices) return CB_ERR_LIMIT;
+    if ((*out = g_devices[d].load(std::memory_order_acquire))) return CB_OK;
+    Device v{};
+    e = cudaDeviceGetAttribute(&v.sms, cudaDevAttrMultiProcessorCount, d);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&v.smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, d);
+    if (e == cudaSuccess) e = cudaGetSymbolAddress(reinterpret_cast<void**>(&v.status), g_linear_status);
+    if (e == cudaSuccess) e = prepare_linear((size_t)v.smem, &v.pairs);
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found{};
+    if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+    if (e == cudaSuccess && (!fn || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
+    if (e != cudaSuccess) return cuda_error(e, "linear set-up");
+    g_encode.store(reinterpret_cast<Encode>(fn), std::memory_order_relaxed);
+    const Device* mine = new (std::nothrow) Device(v);  // kept until the process ends
+    if (!mine) return CB_ERR_LIMIT;
+    const Device* none = nullptr;
+    if (!g_devices[d].compare_exchange_strong(none, mine, std::memory_order_acq_rel)) {
+        delete mine;
+        mine = none;
+    }
+    *out = mine;
+    return CB_OK;
+}
+
+// Rows of bytes, in boxes of `box` rows by 128 bytes, 128-byte swizzle; zeros behind the ends.
+int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes, long long stride, int box) {
+    const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
+    const cuuint32_t boxes[2] = {128, (cuuint32_t)box}, steps[2] = {1, 1};
+    const CUresult r = g_encode.load(std::memory_order_relaxed)(
+        map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, boxes, steps,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CB_OK : cuda_error(cudaErrorInvalidValue, "tensor map");
+}
+
+// CTAs per tile and the tile's columns: the fewest rounds of tiles, each as long as its loads (16 KB of x and
+// 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take.
+void choose_tile(const Device& dev, int M, int N, bool words, int* cg, int* tile_n) {
+    double best = 1e300;
+    for (int g = words ? 1 : 2; g >= 1; --g)
+        for (int n = 256; n >= 32; n -= 32) {
+            if (n > 32 && n - 32 >= N) continue;
+            const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n);
+            const long long units = g == 2 ? dev.pairs : dev.sms;
+            const double cost = (double)((tiles + units - 1) / units) * (256.0 + 2.0 * n / g);
+            if (cost < best * 0.999) best = cost, *cg = g, *tile_n = n;
+        }
+}
 
 }  // namespace
 }  // namespace cbk
@@ -142,12 +156,24 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
         if (!on_grid(u.p, s)) return CB_ERR_ALIGN;
         a.wide = a.wide && on_grid(u.p, 4 * s) && u.stride % 4 == 0;
     }
-    const dim3 grid((unsigned)((N + 63) / 64), (unsigned)((a.M + 63) / 64));
-    if (d.type == CB_E4M3)
-        linear_simple_kernel<true><<<grid, 256, 0, (cudaStream_t)stream>>>(a);
-    else
-        linear_simple_kernel<false><<<grid, 256, 0, (cudaStream_t)stream>>>(a);
-    const cudaError_t e = cudaGetLastError();
+    const Device* dev = nullptr;
+    int rc = device_info(&dev);
+    if (rc != CB_OK) return rc;
+    a.status = dev->status;
+    const bool words = !(on_grid(x, 16) && on_grid(d.w, 16) && a.x_row % 16 == 0 && a.w_row % 16 == 0);
+    int cg = 1;
+    choose_tile(*dev, a.M, a.N, words, &cg, &a.tile_n);
+    a.tiles_m = (a.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (a.N + a.tile_n - 1) / a.tile_n;
+    if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
+    a.k_blocks = (a.k_bytes + 127) / 128;
+    a.stages = linear_max_stages((size_t)dev->smem, linear_stage_bytes(cg, a.tile_n));
+    if (!words) {
+        rc = operand_map(&a.x_map, x, a.M, a.k_bytes, a.x_row, 128);
+        if (rc == CB_OK) rc = operand_map(&a.w_map, d.w, a.N, a.k_bytes, a.w_row, a.tile_n / cg);
+        if (rc != CB_OK) return rc;
+    }
+    const int tiles = a.tiles_m * a.tiles_n, units = cg == 2 ? dev->pairs : dev->sms;
+    const cudaError_t e = launch_linear(a, cg, d.type == CB_E4M3, words, cg * (tiles < units ? tiles : units), (cudaStream_t)stream);
     return e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
 }
 

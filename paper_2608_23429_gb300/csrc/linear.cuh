@@ -11,7 +11,7 @@
 namespace cbk {
 
 struct LinearArgs {
-    alignas(64) CUtensorMap x_map, w_map;  // where the operands come by TMA
+    CUtensorMap x_map, w_map;  // where the operands come by TMA
     int overlap;
     int M, N;              // rows, output features
     int k_bytes;           // bytes of a row of x and of w
@@ -29,6 +29,13 @@ struct LinearArgs {
     void *out, *resid_out;
     int* status;
 };
+
+// The tensor-core kernels (linear_tc.cu): cg CTAs per tile of 128 cg rows; `words`: operands off the 16-byte grid
+// (cg = 1 only). prepare_linear raises the kernels' shared-memory limit and tells how many pairs of CTAs run at once.
+size_t linear_stage_bytes(int cg, int tile_n);
+int linear_max_stages(size_t smem, size_t stage_bytes);
+cudaError_t prepare_linear(size_t smem, int* pairs);
+cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, bool words, int grid, cudaStream_t s);
 
 #ifdef __CUDACC__
 namespace {
