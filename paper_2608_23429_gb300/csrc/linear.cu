@@ -50,14 +50,15 @@ int device_info(const Device** out) {
     return CB_OK;
 }
 
-// Rows of bytes, in boxes of `box` rows by 128 bytes, 128-byte swizzle; zeros behind the ends.
-int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes, long long stride, int box) {
+// Rows of bytes, in boxes of `box` rows by `wide` bytes (128, or 64), swizzled by as much; behind the ends zeros come in
+// and nothing goes out.
+int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes, long long stride, int box, int wide = 128) {
     const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
-    const cuuint32_t boxes[2] = {128, (cuuint32_t)box}, steps[2] = {1, 1};
+    const cuuint32_t boxes[2] = {(cuuint32_t)wide, (cuuint32_t)box}, steps[2] = {1, 1};
     const CUresult r = g_encode.load(std::memory_order_relaxed)(
         map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, boxes, steps,
-        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        CU_TENSOR_MAP_INTERLEAVE_NONE, wide == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? CB_OK : cuda_error(cudaErrorInvalidValue, "tensor map");
 }
 
@@ -128,33 +129,35 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
 
     LinearArgs a{};
     a.overlap = 1;
-    a.M = (int)io->rows, a.N = (int)N;
     a.k_bytes = (int)(K * es);
-    a.act = d.activation;
-    a.tokens = io->tokens == 0 || io->tokens > io->rows ? (unsigned)io->rows : (unsigned)io->tokens;
-    a.out_dtype = io->out_dtype, a.resid_bf16 = io->resid_dtype == CB_BF16;
-    a.bias_bf16 = d.bias_dtype == CB_BF16, a.gate_bf16 = io->gate_dtype == CB_BF16;
-    a.out_stride = io->out_stride ? io->out_stride : N;
-    a.resid_stride = io->resid_stride ? io->resid_stride : N;
-    a.resid_out_stride = io->resid_out_stride ? io->resid_out_stride : N;
-    a.gate_stride = io->gate_stride ? io->gate_stride : N;
     a.x_row = (io->x_stride ? io->x_stride : K) * es, a.w_row = d.w_stride * es;
-    a.x = x, a.w = d.w, a.x_scale = x_scale, a.w_scale = d.w_scale, a.bias = d.bias;
-    a.resid = resid, a.gate = gate, a.out = out, a.resid_out = resid_out;
+    a.x = x, a.w = d.w;
+    LinearEpilogue& ep = a.e;
+    ep.M = (int)io->rows, ep.N = (int)N;
+    ep.act = d.activation;
+    ep.tokens = io->tokens == 0 || io->tokens > io->rows ? (unsigned)io->rows : (unsigned)io->tokens;
+    ep.out_bf16 = io->out_dtype == CB_BF16, ep.resid_bf16 = io->resid_dtype == CB_BF16;
+    ep.bias_bf16 = d.bias_dtype == CB_BF16, ep.gate_bf16 = io->gate_dtype == CB_BF16;
+    ep.out_stride = io->out_stride ? io->out_stride : N;
+    ep.resid_stride = io->resid_stride ? io->resid_stride : N;
+    ep.resid_out_stride = io->resid_out_stride ? io->resid_out_stride : N;
+    ep.gate_stride = io->gate_stride ? io->gate_stride : N;
+    ep.x_scale = x_scale, ep.w_scale = d.w_scale, ep.bias = d.bias;
+    ep.resid = resid, ep.gate = gate, ep.out = out, ep.resid_out = resid_out;
     if (!on_grid(x, es) || !on_grid(x_scale, 4)) return CB_ERR_ALIGN;
     const struct {
         const void* p;
         int dtype;
         long long stride;
-    } used[] = {{out, io->out_dtype, a.out_stride},     {resid, io->resid_dtype, a.resid_stride},
-                {gate, io->gate_dtype, a.gate_stride},  {resid_out, io->resid_dtype, a.resid_out_stride},
+    } used[] = {{out, io->out_dtype, ep.out_stride},     {resid, io->resid_dtype, ep.resid_stride},
+                {gate, io->gate_dtype, ep.gate_stride},  {resid_out, io->resid_dtype, ep.resid_out_stride},
                 {d.bias, d.bias_dtype, 0},              {d.w_scale, CB_FP32, 0}};
-    a.wide = N % 4 == 0;
+    ep.wide = N % 4 == 0;
     for (const auto& u : used) {
         if (!u.p) continue;
         const size_t s = bytes_of(u.dtype);
         if (!on_grid(u.p, s)) return CB_ERR_ALIGN;
-        a.wide = a.wide && on_grid(u.p, 4 * s) && u.stride % 4 == 0;
+        ep.wide = ep.wide && on_grid(u.p, 4 * s) && u.stride % 4 == 0;
     }
     const Device* dev = nullptr;
     int rc = device_info(&dev);
@@ -162,15 +165,21 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.status = dev->status;
     const bool words = !(on_grid(x, 16) && on_grid(d.w, 16) && a.x_row % 16 == 0 && a.w_row % 16 == 0);
     int cg = 1;
-    choose_tile(*dev, a.M, a.N, words, &cg, &a.tile_n);
-    a.tiles_m = (a.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (a.N + a.tile_n - 1) / a.tile_n;
+    choose_tile(*dev, ep.M, ep.N, words, &cg, &a.tile_n);
+    a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
     a.k_blocks = (a.k_bytes + 127) / 128;
     a.stages = linear_max_stages((size_t)dev->smem, linear_stage_bytes(cg, a.tile_n));
     if (!words) {
-        rc = operand_map(&a.x_map, x, a.M, a.k_bytes, a.x_row, 128);
-        if (rc == CB_OK) rc = operand_map(&a.w_map, d.w, a.N, a.k_bytes, a.w_row, a.tile_n / cg);
+        rc = operand_map(&a.x_map, x, ep.M, a.k_bytes, a.x_row, 128);
+        if (rc == CB_OK) rc = operand_map(&a.w_map, d.w, ep.N, a.k_bytes, a.w_row, a.tile_n / cg);
         if (rc != CB_OK) return rc;
+    }
+    const long long out_row = ep.out_stride * (long long)bytes_of(io->out_dtype);
+    if (out && !resid_out && on_grid(out, 16) && out_row % 16 == 0 && out_row < 1LL << 40) {
+        rc = operand_map(&a.out_map, out, ep.M, N * (long long)bytes_of(io->out_dtype), out_row, 32, 64);
+        if (rc != CB_OK) return rc;
+        a.tma_out = 1;
     }
     const int tiles = a.tiles_m * a.tiles_n, units = cg == 2 ? dev->pairs : dev->sms;
     const cudaError_t e = launch_linear(a, cg, d.type == CB_E4M3, words, cg * (tiles < units ? tiles : units), (cudaStream_t)stream);

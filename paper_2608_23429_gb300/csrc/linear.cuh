@@ -10,23 +10,31 @@
 
 namespace cbk {
 
-struct LinearArgs {
-    CUtensorMap x_map, w_map;  // where the operands come by TMA
-    int overlap;
+// What the epilogue needs. The kernels copy it out of their arguments first: these stay in registers, while
+// arguments would be read again behind every store.
+struct LinearEpilogue {
     int M, N;              // rows, output features
-    int k_bytes;           // bytes of a row of x and of w
-    int tiles_m, tiles_n, k_blocks, stages;
-    int tile_n;            // output columns of a tile
     int act;
     unsigned tokens;       // rows of one sample
-    int out_dtype, resid_bf16, bias_bf16, gate_bf16;
+    int out_bf16, resid_bf16, bias_bf16, gate_bf16;
     int wide;              // four columns of every operand of the epilogue are one aligned vector
     long long out_stride, resid_stride, resid_out_stride, gate_stride;  // elements
-    long long x_row, w_row;                                              // bytes from row to row
-    const void *x, *w;
     const float *x_scale, *w_scale;
     const void *bias, *resid, *gate;
     void *out, *resid_out;
+};
+
+struct LinearArgs {
+    CUtensorMap x_map, w_map;  // where the operands come by TMA
+    CUtensorMap out_map;       // where the output leaves by TMA
+    int tma_out;
+    LinearEpilogue e;
+    int overlap;
+    int k_bytes;           // bytes of a row of x and of w
+    int tiles_m, tiles_n, k_blocks, stages;
+    int tile_n;            // output columns of a tile
+    long long x_row, w_row;  // bytes from row to row
+    const void *x, *w;
     int* status;
 };
 
@@ -45,98 +53,97 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     return *reinterpret_cast<uint32_t*>(&h);
 }
 
-__device__ __forceinline__ float lin_value(const void* p, long long e, int bf16) {
-    return bf16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(p)[e] << 16)
-                : reinterpret_cast<const float*>(p)[e];
+// Loads that no store of the kernel is ordered against: inputs do not overlap outputs, and a hidden state that is
+// updated in place is read by the thread that writes it.
+__device__ __forceinline__ uint4 lin_ld16(const void* p) {
+    uint4 r;
+    asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ uint2 lin_ld8(const void* p) {
+    uint2 r;
+    asm("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
+    return r;
+}
+// One element as fp32 bits, or its half of them.
+__device__ __forceinline__ uint32_t lin_ld1(const void* p, long long e, int bf16) {
+    uint32_t r = 0;
+    if (bf16) {
+        uint16_t h;
+        asm("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(reinterpret_cast<const uint16_t*>(p) + e));
+        r = (uint32_t)h << 16;
+    } else {
+        asm("ld.global.u32 %0, [%1];" : "=r"(r) : "l"(reinterpret_cast<const uint32_t*>(p) + e));
+    }
+    return r;
 }
 
-// Four consecutive columns from element e, `n` of them within the row (vectors where `wide`, with n = 4).
-__device__ __forceinline__ float4 lin_load4(const void* p, long long e, int bf16, int wide, int n) {
-    if (wide) {
-        if (n <= 0) return make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!bf16) return *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + e);
-        const uint2 r = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(p) + e);
-        return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y << 16),
-                           __uint_as_float(r.y & 0xFFFF0000u));
-    }
-    float v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < n ? lin_value(p, e + i, bf16) : 0.0f;
-    return make_float4(v[0], v[1], v[2], v[3]);
+// Four consecutive elements of an aligned row, as they lie in memory, and their values.
+__device__ __forceinline__ uint4 lin_raw4(const void* p, long long e, int bf16) {
+    if (!bf16) return lin_ld16(reinterpret_cast<const float*>(p) + e);
+    const uint2 r = lin_ld8(reinterpret_cast<const uint16_t*>(p) + e);
+    return make_uint4(r.x, r.y, 0, 0);
+}
+__device__ __forceinline__ float4 lin_val4(uint4 r, int bf16) {
+    if (bf16) r = make_uint4(r.x << 16, r.x & 0xFFFF0000u, r.y << 16, r.y & 0xFFFF0000u);
+    return make_float4(__uint_as_float(r.x), __uint_as_float(r.y), __uint_as_float(r.z), __uint_as_float(r.w));
+}
+__device__ __forceinline__ void lin_put4(void* p, long long e, int bf16, float4 v) {
+    if (bf16)
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p) + e) = make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
+    else
+        *reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + e) = v;
+}
+__device__ __forceinline__ void lin_put1(void* p, long long e, int bf16, float v) {
+    if (bf16)
+        reinterpret_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(v);
+    else
+        reinterpret_cast<float*>(p)[e] = v;
 }
 
-__device__ __forceinline__ void lin_store4(void* p, long long e, int bf16, int wide, int n, float4 v) {
-    if (wide) {
-        if (n <= 0) return;
-        if (bf16)
-            *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p) + e) = make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
-        else
-            *reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + e) = v;
-        return;
-    }
-    const float a[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (i >= n) continue;
-        if (bf16)
-            reinterpret_cast<__nv_bfloat16*>(p)[e + i] = __float2bfloat16_rn(a[i]);
-        else
-            reinterpret_cast<float*>(p)[e + i] = a[i];
-    }
+// Two fp32 values in one register pair, for the units that take them together.
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 both(Two v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
-// v / (1 + exp(-t)): SiLU with t = v, the tanh form of GELU with t = 2 sqrt(2/pi) (v + 0.044715 v^3), since
-// (1 + tanh(t/2)) / 2 = 1 / (1 + exp(-t)).
-__device__ __forceinline__ float lin_act(float v, int act) {
-    const float t = act == CB_ACT_GELU ? v * fmaf(0.0713548163f, v * v, 1.59576912f) : v;
-    return __fdividef(v, 1.0f + __expf(-t));
-}
-
-// Eight rows by four columns of a thread: v[i] belongs to row0 + step * i and the
-// columns from col. Bias, activation, output and hidden state.
-template <int ROWS>
-__device__ __forceinline__ void lin_finish(const LinearArgs& A, int row0, int step, int col, float4* v) {
-    const int n = A.N - col < 4 ? A.N - col : 4;  // columns of this thread (<= 0: none)
-    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
-    float4 r[ROWS];
-    if (A.resid_out)
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const int row = row0 + step * i;
-            r[i] = row < A.M ? lin_load4(A.resid, row * A.resid_stride + col, A.resid_bf16, A.wide, n) : none;
-        }
-    if (A.w_scale) {
-        const float4 s = lin_load4(A.w_scale, col, 0, A.wide, n);
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) v[i] = make_float4(v[i].x * s.x, v[i].y * s.y, v[i].z * s.z, v[i].w * s.w);
-    }
-    if (A.bias) {
-        const float4 b = lin_load4(A.bias, col, A.bias_bf16, A.wide, n);
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) v[i] = make_float4(v[i].x + b.x, v[i].y + b.y, v[i].z + b.z, v[i].w + b.w);
-    }
-    if (A.act != CB_ACT_NONE)
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i)
-            v[i] = make_float4(lin_act(v[i].x, A.act), lin_act(v[i].y, A.act), lin_act(v[i].z, A.act), lin_act(v[i].w, A.act));
-    if (A.out)
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const int row = row0 + step * i;
-            if (row < A.M) lin_store4(A.out, row * A.out_stride + col, A.out_dtype == CB_BF16, A.wide, n, v[i]);
-        }
-    if (A.resid_out)
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const int row = row0 + step * i;
-            if (row >= A.M) continue;
-            float4 g = make_float4(1.f, 1.f, 1.f, 1.f);
-            if (A.gate)
-                g = lin_load4(A.gate, (long long)((unsigned)row / A.tokens) * A.gate_stride + col, A.gate_bf16, A.wide, n);
-            lin_store4(A.resid_out, row * A.resid_out_stride + col, A.resid_bf16, A.wide, n,
-                       make_float4(fmaf(g.x, v[i].x, r[i].x), fmaf(g.y, v[i].y, r[i].y), fmaf(g.z, v[i].z, r[i].z),
-                                   fmaf(g.w, v[i].w, r[i].w)));
-        }
+// v / (1 + 2^t): SiLU with t = -v log2(e), the tanh form of GELU with t = -2 log2(e) sqrt(2/pi) (v + 0.044715 v^3),
+// since (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z)).
+template <int ACT>
+__device__ __forceinline__ Two lin_act(Two v) {
+    if constexpr (ACT == CB_ACT_NONE) return v;
+    constexpr float kSilu = -1.44269504f, kGelu1 = -2.30220820f, kGelu3 = -0.102943239f;
+    const Two t = ACT == CB_ACT_SILU ? mul2(v, two(kSilu, kSilu))
+                                     : mul2(v, fma2(two(kGelu3, kGelu3), mul2(v, v), two(kGelu1, kGelu1)));
+    float2 e = both(t);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    float2 d = both(add2(two(e.x, e.y), two(1.0f, 1.0f)));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d.y));
+    return mul2(v, two(d.x, d.y));
 }
 
 }  // namespace

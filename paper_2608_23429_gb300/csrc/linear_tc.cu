@@ -2,15 +2,15 @@
 //
 // A persistent grid of CTAs (CG = 1) or of pairs of CTAs on two SMs (CG = 2) works through output tiles of 128 CG
 // rows by tile_n columns. In a CTA
-//   one warp (TMA) or eight (words) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
+//   one warp (TMA) or seven (words) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
 //     tile_n / CG rows of w, in the 128-byte swizzle that the tensor cores read,
 //   one thread issues tcgen05.mma on them, sums in TMEM (two accumulators of up to 256 columns each),
-//   four warps take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
-//     that their accesses to global memory are rows, and apply the epilogue (lin_finish).
+//   eight warps take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
+//     that their accesses to global memory are rows, and apply the epilogue.
 // A pair of CTAs shares one tile: each loads its 128 rows of x and half of the tile's rows of w, the first one's
 // thread issues for both, and each holds the sums of its own rows.
 //
-// WORDS: operands whose rows do not start on 16-byte boundaries cannot come by TMA. Eight warps load them as
+// WORDS: operands whose rows do not start on 16-byte boundaries cannot come by TMA. Seven warps load them as
 // aligned 32-bit words, a row of a slab per warp and step, shift neighbouring words together and store them where
 // TMA would have put them.
 //
@@ -26,11 +26,13 @@ constexpr int kRows = 128;        // rows of x per CTA
 constexpr int kSlab = 128;        // bytes of K per stage
 constexpr int kMaxLinStages = 12;
 constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the other
-constexpr int kLoadWarps = 8;     // WORDS
+constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes
+constexpr int kLoadWarps = 7;     // WORDS
 constexpr unsigned long long kLimitNs = 1000000000ull;
 
 struct Tail {  // behind the stages
-    float turn[4][32 * 32];
+    float turn[kEpiWarps][32 * 32];
+    float cols[kEpiWarps][2 * 32];  // scales and biases of a chunk's columns
     uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2];
     uint32_t tmem;
     int abort;
@@ -51,7 +53,8 @@ __device__ __forceinline__ uint32_t in_first(uint32_t bar) {
     return r;
 }
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    // relaxed: what it orders are reads of TMEM (tcgen05.wait and fence); a release would wait for the warp's stores
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
     uint32_t ok;
@@ -69,19 +72,22 @@ __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) 
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort, int* status, int code) {
     auto done = [&] { return CLUSTER ? try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity); };
-    if (done()) return true;
-    const unsigned long long t0 = now_ns();
+    unsigned long long t0 = 0;
     while (true) {
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 64; ++i)
             if (done()) return true;
         if (*abort) return false;
-        if (now_ns() - t0 > kLimitNs) {
+        const unsigned long long t = now_ns();
+        if (t0 == 0) t0 = t;
+        if (t - t0 > kLimitNs) {
             *abort = 1;
             record(status, code);
             return false;
         }
     }
 }
+
+__device__ __forceinline__ bool all(bool ok) { return __all_sync(0xFFFFFFFFu, ok) != 0; }
 
 template <int CG>
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -151,6 +157,14 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float* v) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// True in one lane of the warp. The roles' loops are run by whole warps, so that what they compute stays in
+// uniform registers (which the tensor cores' and copies' instructions take), and one lane issues.
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 struct Tile {
     int m, n;
 };
@@ -172,13 +186,222 @@ __device__ __forceinline__ uint32_t word_of(const char* p, int n, int i) {
     return v;
 }
 
+// A place in the ring of stages, and the parity of its present use.
+struct Place {
+    int s = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++s == stages) s = 0, phase ^= 1;
+    }
+};
+
+// Waits until the stages' last fills have been read: no copy and no arrival is under way then. `p`: the place behind
+// them, `fills`: how many there were.
+__device__ __forceinline__ bool drain(Place p, int fills, int stages, uint32_t empty, volatile int* abort, int* status) {
+    for (int i = 0; i < min(fills, stages); ++i) {
+        p.s = p.s == 0 ? (p.phase ^= 1, stages - 1) : p.s - 1;
+        if (!wait(empty + 8 * p.s, p.phase, abort, status, CB_DEV_DRAIN_TIMEOUT)) return false;
+    }
+    return true;
+}
+
+// ---- epilogue of 32 rows by 32 columns of a warp. Wide: a thread has the rows row0 + lane / 8 + 4 i and four columns.
+
+struct Ahead {
+    uint4 scale, bias, gate, resid[8];
+};
+
+// A thread's part of a tile: where its first row and column lie, and the bytes to the row after next but two.
+struct Spot {
+    int row, col;            // of its first element in the tile's first chunk
+    long long gate;          // element of the gate of the warp's first row's sample
+    unsigned next;           // rows from here on belong to other samples
+    const char* resid;
+    char *out, *resid_out;
+    long long resid_step, out_step, resid_out_step;
+};
+
+__device__ __forceinline__ Spot spot_of(const LinearEpilogue& E, int row0, int col0, int lane) {
+    Spot p;
+    p.row = row0 + lane / 8, p.col = col0 + lane % 8 * 4;
+    const int os = E.out_bf16 ? 2 : 4, rs = E.resid_bf16 ? 2 : 4;
+    p.out = reinterpret_cast<char*>(E.out) + (p.row * E.out_stride + p.col) * os;
+    p.resid = reinterpret_cast<const char*>(E.resid) + (p.row * E.resid_stride + p.col) * rs;
+    p.resid_out = reinterpret_cast<char*>(E.resid_out) + (p.row * E.resid_out_stride + p.col) * rs;
+    p.out_step = 4 * E.out_stride * os, p.resid_step = 4 * E.resid_stride * rs, p.resid_out_step = 4 * E.resid_out_stride * rs;
+    const unsigned sample = E.gate ? (unsigned)row0 / E.tokens : 0;
+    p.gate = sample * E.gate_stride + p.col;
+    p.next = (sample + 1) * E.tokens;
+    return p;
+}
+
+// The operands of the chunk that starts `at` columns into the tile. FULL: all 32 rows exist.
+template <bool FULL>
+__device__ __forceinline__ void look_ahead(const LinearEpilogue& E, const Spot& p, int at, Ahead& a) {
+    const int col = p.col + at;
+    if (col >= E.N) return;  // N is a multiple of four
+    if (E.w_scale) a.scale = lin_raw4(E.w_scale, col, 0);
+    if (E.bias) a.bias = lin_raw4(E.bias, col, E.bias_bf16);
+    if (!E.resid_out) return;
+    if (E.gate) a.gate = lin_raw4(E.gate, p.gate + at, E.gate_bf16);
+    if (E.resid_bf16) {
+        const char* q = p.resid + 2 * at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += p.resid_step)
+            if (FULL || p.row + 4 * i < E.M) {
+                const uint2 v = lin_ld8(q);
+                a.resid[i].x = v.x, a.resid[i].y = v.y;
+            }
+    } else {
+        const char* q = p.resid + 4 * at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += p.resid_step)
+            if (FULL || p.row + 4 * i < E.M) a.resid[i] = lin_ld16(q);
+    }
+}
+
+// Eight rows of four columns from q on, `step` bytes apart.
+template <bool FULL>
+__device__ __forceinline__ void put_rows(char* q, long long step, int bf16, int rows, const ulonglong2* v) {
+    if (bf16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += step) {
+            const float2 lo = both(v[i].x), hi = both(v[i].y);
+            if (FULL || 4 * i < rows) *reinterpret_cast<uint2*>(q) = make_uint2(bf16x2(lo.x, lo.y), bf16x2(hi.x, hi.y));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += step)
+            if (FULL || 4 * i < rows) *reinterpret_cast<ulonglong2*>(q) = v[i];
+    }
+}
+
+template <int ACT>
+__device__ __forceinline__ void activate(const float4& s, const float4& b, ulonglong2* v) {
+    const Two s0 = two(s.x, s.y), s1 = two(s.z, s.w), b0 = two(b.x, b.y), b1 = two(b.z, b.w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i].x = lin_act<ACT>(fma2(v[i].x, s0, b0));
+        v[i].y = lin_act<ACT>(fma2(v[i].y, s1, b1));
+    }
+}
+
+template <bool FULL>
+__device__ __forceinline__ void finish(const LinearEpilogue& E, const Spot& p, int at, const Ahead& a, ulonglong2* v) {
+    const int col = p.col + at, rows = E.M - p.row;
+    if (col >= E.N) return;
+    const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+    const float4 s = E.w_scale ? lin_val4(a.scale, 0) : one;
+    const float4 b = E.bias ? lin_val4(a.bias, E.bias_bf16) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (E.act == CB_ACT_NONE) activate<CB_ACT_NONE>(s, b, v);
+    else if (E.act == CB_ACT_GELU) activate<CB_ACT_GELU>(s, b, v);
+    else activate<CB_ACT_SILU>(s, b, v);
+    if (E.out) put_rows<FULL>(p.out + at * (E.out_bf16 ? 2 : 4), p.out_step, E.out_bf16, rows, v);
+    if (!E.resid_out) return;
+    float4 g = E.gate ? lin_val4(a.gate, E.gate_bf16) : one;
+    const bool mixed = E.gate && (unsigned)(p.row - p.row % 4 + 31) >= p.next;  // the warp's rows are of several samples
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned row = (unsigned)(p.row + 4 * i);
+        if (mixed && row >= p.next && (FULL || row < (unsigned)E.M))
+            g = lin_val4(lin_raw4(E.gate, (long long)(row / E.tokens) * E.gate_stride + col, E.gate_bf16), E.gate_bf16);
+        const float4 r = lin_val4(a.resid[i], E.resid_bf16);
+        v[i].x = fma2(two(g.x, g.y), v[i].x, two(r.x, r.y));
+        v[i].y = fma2(two(g.z, g.w), v[i].y, two(r.z, r.w));
+    }
+    put_rows<FULL>(p.resid_out + at * (E.resid_bf16 ? 2 : 4), p.resid_out_step, E.resid_bf16, rows, v);
+}
+
+// Output by TMA, where there is nothing to add it to: a row per lane, as the sums come from TMEM. Columns' operands are
+// read from shared memory by all lanes alike, and 32 rows of 64 bytes leave at a time, through two buffers in turn.
+template <int ACT>
+__device__ __forceinline__ void finish_tma(const LinearArgs& A, const LinearEpilogue& E, const float* cols, Two xs2, float* v,
+                                           uint8_t* buf, int& next, int row0, int col0, int lane) {
+    Two x[16];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(cols + 4 * j);
+        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(cols + 32 + 4 * j);
+        Two p = two(v[4 * j], v[4 * j + 1]), q = two(v[4 * j + 2], v[4 * j + 3]);
+        if (E.x_scale) p = mul2(p, xs2), q = mul2(q, xs2);
+        x[2 * j] = lin_act<ACT>(fma2(p, s.x, b.x));
+        x[2 * j + 1] = lin_act<ACT>(fma2(q, s.y, b.y));
+    }
+    const int turns = E.out_bf16 ? 1 : 2;
+    for (int h = 0; h < turns; ++h) {
+        // the store before the last has left this buffer
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+        uint8_t* const to = buf + 2048 * next + lane * 64;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint4 piece;
+            if (E.out_bf16) {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 f = both(x[4 * j + k]);
+                    w[k] = bf16x2(f.x, f.y);
+                }
+                piece = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                const ulonglong2 f = h == 0 ? make_ulonglong2(x[2 * j], x[2 * j + 1]) : make_ulonglong2(x[2 * j + 8], x[2 * j + 9]);
+                piece = *reinterpret_cast<const uint4*>(&f);
+            }
+            *reinterpret_cast<uint4*>(to + (j ^ (lane / 2 % 4)) * 16) = piece;
+        }
+        fence_generic_to_async();
+        __syncwarp();
+        const int at = col0 + 16 * h;
+        if (at < E.N && lane == 0)
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&A.out_map),
+                         "r"(at * (E.out_bf16 ? 2 : 4)), "r"(row0), "r"(smem_addr(buf) + 2048 * next)
+                         : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        next ^= 1;
+    }
+}
+
+// The same by elements, a column per lane, for rows that are not made of aligned fours.
+__device__ __forceinline__ void finish_elements(const LinearEpilogue& A, int row0, int col0, int lane, const float* turn) {
+    const int col = col0 + lane;
+    if (col >= A.N) return;
+    const float s = A.w_scale ? A.w_scale[col] : 1.0f;
+    const float b = A.bias ? __uint_as_float(lin_ld1(A.bias, col, A.bias_bf16)) : 0.0f;
+    const int rows = min(32, A.M - row0);
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        float x[8], g[8];
+        if (A.resid_out)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = row0 + r0 + i;
+                if (r0 + i >= rows) continue;
+                x[i] = __uint_as_float(lin_ld1(A.resid, row * A.resid_stride + col, A.resid_bf16));
+                g[i] = 1.0f;
+                if (A.gate)
+                    g[i] = __uint_as_float(
+                        lin_ld1(A.gate, (long long)((unsigned)row / A.tokens) * A.gate_stride + col, A.gate_bf16));
+            }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + i, row = row0 + r;
+            if (r >= rows) continue;
+            float v = fmaf(turn[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + lane % 4], s, b);
+            if (A.act == CB_ACT_GELU) v = both(lin_act<CB_ACT_GELU>(two(v, v))).x;
+            if (A.act == CB_ACT_SILU) v = both(lin_act<CB_ACT_SILU>(two(v, v))).x;
+            if (A.out) lin_put1(A.out, row * A.out_stride + col, A.out_bf16, v);
+            if (A.resid_out) lin_put1(A.resid_out, row * A.resid_out_stride + col, A.resid_bf16, fmaf(g[i], v, x[i]));
+        }
+    }
+}
+
 template <int CG, bool FP8, bool WORDS>
-__global__ void __launch_bounds__(32 * (5 + (WORDS ? kLoadWarps : 1)), 1)
+__global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)), 1)
     linear_kernel(const __grid_constant__ LinearArgs A) {
     static_assert(CG == 1 || !WORDS, "pairs of CTAs load by TMA");
     extern __shared__ uint8_t raw[];
     uint8_t* const base = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int w_rows = A.tile_n / CG, stage_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
     Tail& T = *reinterpret_cast<Tail*>(base + stages * stage_bytes);
@@ -194,13 +417,13 @@ __global__ void __launch_bounds__(32 * (5 + (WORDS ? kLoadWarps : 1)), 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, 4 * CG);
+            mbar_init(acc_empty + 8 * i, kEpiWarps * CG);
         }
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_generic_to_async();
     }
-    if (warp == 4) {
+    if (warp == kEpiWarps) {
         const uint32_t at = smem_addr(&T.tmem);
         if constexpr (CG == 1) {
             asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(at) : "memory");
@@ -219,109 +442,159 @@ __global__ void __launch_bounds__(32 * (5 + (WORDS ? kLoadWarps : 1)), 1)
     after_previous();
 
     const int first = blockIdx.x / CG, step = gridDim.x / CG, total = A.tiles_m * A.tiles_n;
-    if (warp < 4) {  // ---- epilogue
+    if (warp < kEpiWarps) {  // ---- epilogue
+        const LinearEpilogue E = A.e;
         float* const turn = T.turn[warp];
-        int n_done = 0;
+        const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
+        int n_done = 0, next_buf = 0;
         for (int t = first; t < total; t += step, ++n_done) {
             const Tile tile = tile_at(A, t);
             const int acc = n_done & 1;
-            if (!__all_sync(0xFFFFFFFFu, wait(acc_full + 8 * acc, (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT)))
-                break;
+            const int row0 = (tile.m * CG + (int)rank) * kRows + quarter * 32, col0 = tile.n * A.tile_n;
+            const float xs = E.x_scale && row0 + lane < E.M ? E.x_scale[row0 + lane] : 1.0f;
+            const Two xs2 = two(xs, xs);
+            const int chunks = row0 < E.M ? (min(A.tile_n, E.N - col0) + 31) / 32 : 0;
+            // the epilogue's operands of a chunk are loaded while the one before it is worked on
+            Ahead ahead;
+            const Spot spot = spot_of(E, row0, col0, lane);
+            const bool rows_full = row0 + 32 <= E.M;
+            auto look = [&](int c) {
+                if (rows_full) look_ahead<true>(E, spot, c * 32, ahead);
+                else look_ahead<false>(E, spot, c * 32, ahead);
+            };
+            float scale = 1.0f, bias = 0.0f;  // of this lane's column of the next chunk
+            auto look_column = [&](int c) {
+                const int col = col0 + c * 32 + lane;
+                if (col >= E.N) return;
+                if (E.w_scale) scale = __uint_as_float(lin_ld1(E.w_scale, col, 0));
+                if (E.bias) bias = __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16));
+            };
+            if (half < chunks) {
+                if (A.tma_out) look_column(half);
+                else if (E.wide) look(half);
+            }
+            if (!all(wait(acc_full + 8 * acc, (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT))) break;
             fence_after();
-            const int row0 = (tile.m * CG + (int)rank) * kRows + warp * 32, col0 = tile.n * A.tile_n;
-            const float xs = A.x_scale && row0 + lane < A.M ? A.x_scale[row0 + lane] : 1.0f;
-            const int chunks = (min(A.tile_n, A.N - col0) + 31) / 32;
-            for (int c = 0; c < chunks; ++c) {
-                float v[32];
-                tmem_load(tmem + ((uint32_t)(warp * 32) << 16) + acc * kAccStride + c * 32, v);
-                if (c + 1 == chunks) {  // all of it has been read
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 1) mbar_arrive(acc_empty + 8 * acc);
-                        else arrive_at(in_first(acc_empty + 8 * acc));
-                    }
+            auto release = [&] {  // the warp has read its part of the accumulator
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 1) mbar_arrive(acc_empty + 8 * acc);
+                    else arrive_at(in_first(acc_empty + 8 * acc));
                 }
-                // a row per lane to rows of 32 columns across eight lanes: 16-byte pieces, swizzled against bank conflicts
+            };
+            if (half >= chunks) release();
+            for (int c = half; c < chunks; c += 2) {
+                float v[32];
+                tmem_load(tmem + ((uint32_t)(quarter * 32) << 16) + acc * kAccStride + c * 32, v);
+                if (c + 2 >= chunks) release();
+                if (A.tma_out) {
+                    float* const cols = T.cols[warp];
+                    cols[lane] = scale, cols[32 + lane] = bias;
+                    __syncwarp();
+                    if (c + 2 < chunks) look_column(c + 2);
+                    uint8_t* const buf = reinterpret_cast<uint8_t*>(turn);
+                    const int col = col0 + c * 32;
+                    if (E.act == CB_ACT_NONE) finish_tma<CB_ACT_NONE>(A, E, cols, xs2, v, buf, next_buf, row0, col, lane);
+                    else if (E.act == CB_ACT_GELU) finish_tma<CB_ACT_GELU>(A, E, cols, xs2, v, buf, next_buf, row0, col, lane);
+                    else finish_tma<CB_ACT_SILU>(A, E, cols, xs2, v, buf, next_buf, row0, col, lane);
+                    continue;
+                }
+                // a row per lane to rows of 32 columns: 16-byte pieces, swizzled against bank conflicts
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<float4*>(&turn[lane * 32 + (j ^ (lane & 7)) * 4]) =
-                        make_float4(v[4 * j] * xs, v[4 * j + 1] * xs, v[4 * j + 2] * xs, v[4 * j + 3] * xs);
+                    *reinterpret_cast<ulonglong2*>(&turn[lane * 32 + (j ^ (lane & 7)) * 4]) =
+                        make_ulonglong2(mul2(two(v[4 * j], v[4 * j + 1]), xs2), mul2(two(v[4 * j + 2], v[4 * j + 3]), xs2));
                 __syncwarp();
-                float4 u[8];
+                if (E.wide) {
+                    ulonglong2 u[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = 4 * i + lane / 8;
-                    u[i] = *reinterpret_cast<const float4*>(&turn[r * 32 + ((lane & 7) ^ (r & 7)) * 4]);
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = 4 * i + lane / 8;
+                        u[i] = *reinterpret_cast<const ulonglong2*>(&turn[r * 32 + ((lane & 7) ^ (r & 7)) * 4]);
+                    }
+                    const Ahead now = ahead;
+                    if (c + 2 < chunks) look(c + 2);
+                    if (rows_full) finish<true>(E, spot, c * 32, now, u);
+                    else finish<false>(E, spot, c * 32, now, u);
+                } else {
+                    finish_elements(E, row0, col0 + c * 32, lane, turn);
                 }
                 __syncwarp();
-                lin_finish<8>(A, row0 + lane / 8, 4, col0 + c * 32 + (lane & 7) * 4, u);
             }
         }
-    } else if (warp == 4) {  // ---- products
-        if (lane == 0 && rank == 0) {
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    } else if (warp == kEpiWarps) {  // ---- products
+        if (rank == 0) {
             // fp32 sums; A and B bf16 (kind f16) or e4m3 (kind f8f6f4), both with K innermost; N / 8, M / 16
             const uint32_t idesc =
                 1u << 4 | (FP8 ? 0u : 1u << 7 | 1u << 10) | (uint32_t)(A.tile_n / 8) << 17 | (uint32_t)(kRows * CG / 16) << 24;
-            int it = 0, n_done = 0;
+            const uint64_t desc0 = operand_desc(ring);
+            const int last_steps = (A.k_bytes - (A.k_blocks - 1) * kSlab + 31) / 32;  // of 32 bytes of K
+            Place at;
+            int n_done = 0;
             bool ok = true;
             for (int t = first; t < total && ok; t += step, ++n_done) {
                 const int acc = n_done & 1;
-                ok = wait<CG == 2>(acc_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT);
+                const uint32_t sums = tmem + acc * kAccStride;
+                ok = all(wait<CG == 2>(acc_empty + 8 * acc, ((n_done >> 1) & 1) ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
                 fence_after();
-                for (int kb = 0; kb < A.k_blocks && ok; ++kb, ++it) {
-                    const int s = it % stages;
-                    ok = wait(full + 8 * s, (it / stages) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT);
+                for (int kb = 0; kb < A.k_blocks && ok; ++kb) {
+                    const uint64_t a = desc0 + (uint32_t)(at.s * stage_bytes) / 16, b = a + kRows * kSlab / 16;
+                    ok = all(wait(full + 8 * at.s, at.phase, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
                     if (!ok) break;
                     fence_after();
-                    const uint64_t a = operand_desc(ring + s * stage_bytes), b = operand_desc(ring + s * stage_bytes + kRows * kSlab);
-                    const int steps = min(4, (A.k_bytes - kb * kSlab + 31) / 32);  // of 32 bytes of K
-                    for (int j = 0; j < steps; ++j)
-                        mma<CG, FP8>(tmem + acc * kAccStride, a + 2 * j, b + 2 * j, idesc, kb + j > 0);
-                    commit<CG>(empty + 8 * s);
+                    const int steps = kb + 1 < A.k_blocks ? 4 : last_steps;
+                    if (elected()) {
+                        mma<CG, FP8>(sums, a, b, idesc, kb > 0);
+                        if (steps > 1) mma<CG, FP8>(sums, a + 2, b + 2, idesc, true);
+                        if (steps > 2) mma<CG, FP8>(sums, a + 4, b + 4, idesc, true);
+                        if (steps > 3) mma<CG, FP8>(sums, a + 6, b + 6, idesc, true);
+                        commit<CG>(empty + 8 * at.s);
+                        if (kb + 1 == A.k_blocks) commit<CG>(acc_full + 8 * acc);
+                    }
+                    at.next(stages);
                 }
-                if (ok) commit<CG>(acc_full + 8 * acc);
             }
         }
     } else if constexpr (!WORDS) {  // ---- copies
-        if (lane == 0) {
-            int it = 0;
+        {
+            Place at;
+            int fills = 0;
             bool ok = true;
+            const uint32_t bar0 = CG == 2 ? in_first(full) : full;
             for (int t = first; t < total && ok; t += step) {
                 const Tile tile = tile_at(A, t);
                 const int row = (tile.m * CG + (int)rank) * kRows, col = tile.n * A.tile_n + (int)rank * w_rows;
-                for (int kb = 0; kb < A.k_blocks; ++kb, ++it) {
-                    const int s = it % stages;
-                    ok = wait(empty + 8 * s, ((it / stages) & 1) ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT);
+                for (int kb = 0; kb < A.k_blocks; ++kb, ++fills) {
+                    ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
                     if (!ok) break;
-                    if (rank == 0) mbar_expect_tx(full + 8 * s, CG * stage_bytes);
-                    const uint32_t bar = CG == 2 ? in_first(full + 8 * s) : full + 8 * s;
-                    const uint32_t dst = ring + s * stage_bytes;
-                    tma_2d<CG>(dst, &A.x_map, kb * kSlab, row, bar);
-                    tma_2d<CG>(dst + kRows * kSlab, &A.w_map, kb * kSlab, col, bar);
+                    const uint32_t dst = ring + at.s * stage_bytes;
+                    if (elected()) {
+                        if (rank == 0) mbar_expect_tx(full + 8 * at.s, CG * stage_bytes);
+                        tma_2d<CG>(dst, &A.x_map, kb * kSlab, row, bar0 + 8 * at.s);
+                        tma_2d<CG>(dst + kRows * kSlab, &A.w_map, kb * kSlab, col, bar0 + 8 * at.s);
+                    }
+                    at.next(stages);
                 }
             }
-            // the stages' last fills have been read, so no copy and no arrival is still under way
-            for (int i = max(0, it - stages); i < it; ++i)
-                if (!wait(empty + 8 * (i % stages), (i / stages) & 1, abort, A.status, CB_DEV_DRAIN_TIMEOUT)) {
-                    const unsigned long long t0 = now_ns();  // given up: copies under way land in microseconds
-                    while (now_ns() - t0 < kMinDrainNs) {}
-                    break;
-                }
+            if (!drain(at, fills, stages, empty, abort, A.status)) {
+                const unsigned long long t0 = now_ns();  // given up: copies under way land in microseconds
+                while (now_ns() - t0 < kMinDrainNs) {}
+            }
         }
     } else {
-        const int lw = warp - 5;
-        int it = 0;
+        const int lw = warp - kEpiWarps - 1;
+        Place at;
+        int fills = 0;
         bool ok = true;
         for (int t = first; t < total && ok; t += step) {
             const Tile tile = tile_at(A, t);
             const int row0 = tile.m * kRows, col0 = tile.n * A.tile_n;
-            for (int kb = 0; kb < A.k_blocks; ++kb, ++it) {
-                const int s = it % stages;
-                ok = __all_sync(0xFFFFFFFFu, wait(empty + 8 * s, ((it / stages) & 1) ^ 1, abort, A.status,
-                                                  CB_DEV_PRODUCER_TIMEOUT));
+            for (int kb = 0; kb < A.k_blocks; ++kb, ++fills) {
+                ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
                 if (!ok) break;
-                uint8_t* const stage = base + s * stage_bytes;
+                uint8_t* const stage = base + at.s * stage_bytes;
                 const int n = min(kSlab, A.k_bytes - kb * kSlab);
                 constexpr int B = 4;  // rows whose loads are in flight together
                 for (int r0 = lw * B; r0 < kRows + w_rows; r0 += kLoadWarps * B) {
@@ -332,7 +605,7 @@ __global__ void __launch_bounds__(32 * (5 + (WORDS ? kLoadWarps : 1)), 1)
                         const int r = r0 + i;
                         const bool is_x = r < kRows;
                         const int at = is_x ? row0 + r : col0 + r - kRows;
-                        const bool on = at < (is_x ? A.M : A.N);
+                        const bool on = at < (is_x ? A.e.M : A.e.N);
                         const char* p = reinterpret_cast<const char*>(is_x ? A.x : A.w) +
                                         at * (is_x ? A.x_row : A.w_row) + (long long)kb * kSlab;
                         shift[i] = (int)((uintptr_t)p & 3);
@@ -349,18 +622,18 @@ __global__ void __launch_bounds__(32 * (5 + (WORDS ? kLoadWarps : 1)), 1)
                 }
                 fence_generic_to_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(full + 8 * s);
+                if (lane == 0) mbar_arrive(full + 8 * at.s);
+                at.next(stages);
             }
         }
-        for (int i = max(0, it - stages); i < it; ++i)
-            wait(empty + 8 * (i % stages), (i / stages) & 1, abort, A.status, CB_DEV_DRAIN_TIMEOUT);
+        drain(at, fills, stages, empty, abort, A.status);
     }
     fence_before();
     __syncwarp();
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();  // no CTA leaves while the other may still reach its barriers or TMEM
     fence_after();
-    if (warp == 4) {
+    if (warp == kEpiWarps) {
         if constexpr (CG == 1)
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
         else
@@ -397,7 +670,7 @@ cudaError_t prepare_linear(size_t smem, int* pairs) {
     at.val.clusterDim.x = 2, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(2);
-    c.blockDim = dim3(192);
+    c.blockDim = dim3(32 * (kEpiWarps + 2));
     c.dynamicSmemBytes = smem;
     c.attrs = &at;
     c.numAttrs = 1;
@@ -412,7 +685,7 @@ cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, bool words, int
     at[1].val.clusterDim.x = (unsigned)cg, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)grid);
-    c.blockDim = dim3(words ? 32 * (5 + kLoadWarps) : 192);
+    c.blockDim = dim3(32 * (kEpiWarps + 1 + (words ? kLoadWarps : 1)));
     c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + sizeof(Tail) + 1024;
     c.stream = s;
     c.attrs = at;
