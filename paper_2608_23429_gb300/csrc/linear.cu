@@ -1,4 +1,5 @@
 // cb_linear_*: the layer's handle, the checks of a call and the choice of its kernel.
+#include <algorithm>
 #include <atomic>
 #include <new>
 
@@ -64,10 +65,10 @@ int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes
 
 // CTAs per tile and the tile's columns: the fewest rounds of tiles, each as long as its loads (16 KB of x and
 // 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take.
-void choose_tile(const Device& dev, int M, int N, bool words, int* cg, int* tile_n) {
+void choose_tile(const Device& dev, int M, int N, bool tma, int* cg, int* tile_n) {
     double best = 1e300;
-    for (int g = words ? 1 : 2; g >= 1; --g)
-        for (int n = 256; n >= 32; n -= 32) {
+    for (int g = tma ? 2 : 1; g >= 1; --g)
+        for (int n = tma ? 256 : 128; n >= 32; n -= 32) {
             if (n > 32 && n - 32 >= N) continue;
             const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n);
             const long long units = g == 2 ? dev.pairs : dev.sms;
@@ -163,14 +164,16 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     int rc = device_info(&dev);
     if (rc != CB_OK) return rc;
     a.status = dev->status;
-    const bool words = !(on_grid(x, 16) && on_grid(d.w, 16) && a.x_row % 16 == 0 && a.w_row % 16 == 0);
+    a.grid_bytes = 16;
+    while (((uintptr_t)x | (uintptr_t)d.w | (uintptr_t)a.x_row | (uintptr_t)a.w_row) % a.grid_bytes) a.grid_bytes /= 2;
+    const bool tma = a.grid_bytes == 16;
     int cg = 1;
-    choose_tile(*dev, ep.M, ep.N, words, &cg, &a.tile_n);
+    choose_tile(*dev, ep.M, ep.N, tma, &cg, &a.tile_n);
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
     a.k_blocks = (a.k_bytes + 127) / 128;
-    a.stages = linear_max_stages((size_t)dev->smem, linear_stage_bytes(cg, a.tile_n));
-    if (!words) {
+    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(!tma, a.tile_n)) / linear_stage_bytes(cg, a.tile_n));
+    if (tma) {
         rc = operand_map(&a.x_map, x, ep.M, a.k_bytes, a.x_row, 128);
         if (rc == CB_OK) rc = operand_map(&a.w_map, d.w, ep.N, a.k_bytes, a.w_row, a.tile_n / cg);
         if (rc != CB_OK) return rc;
@@ -182,7 +185,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
         a.tma_out = 1;
     }
     const int tiles = a.tiles_m * a.tiles_n, units = cg == 2 ? dev->pairs : dev->sms;
-    const cudaError_t e = launch_linear(a, cg, d.type == CB_E4M3, words, cg * (tiles < units ? tiles : units), (cudaStream_t)stream);
+    const cudaError_t e = launch_linear(a, cg, d.type == CB_E4M3, cg * (tiles < units ? tiles : units), (cudaStream_t)stream);
     return e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
 }
 

@@ -33,17 +33,19 @@ struct LinearArgs {
     int k_bytes;           // bytes of a row of x and of w
     int tiles_m, tiles_n, k_blocks, stages;
     int tile_n;            // output columns of a tile
+    int grid_bytes;        // grid on which all rows of x and of w start, up to 16 bytes
     long long x_row, w_row;  // bytes from row to row
     const void *x, *w;
     int* status;
 };
 
-// The tensor-core kernels (linear_tc.cu): cg CTAs per tile of 128 cg rows; `words`: operands off the 16-byte grid
-// (cg = 1 only). prepare_linear raises the kernels' shared-memory limit and tells how many pairs of CTAs run at once.
+// The tensor-core kernels (linear_tc.cu): cg CTAs per tile of 128 cg rows; a.grid_bytes below 16: cg = 1
+// only. prepare_linear raises the kernels' shared-memory limit and tells how many pairs of CTAs run at once.
 size_t linear_stage_bytes(int cg, int tile_n);
-int linear_max_stages(size_t smem, size_t stage_bytes);
+size_t linear_fixed_bytes(bool shift, int tile_n);  // shared memory besides the stages
+constexpr int kMaxLinStages = 12;
 cudaError_t prepare_linear(size_t smem, int* pairs);
-cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, bool words, int grid, cudaStream_t s);
+cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s);
 
 #ifdef __CUDACC__
 namespace {

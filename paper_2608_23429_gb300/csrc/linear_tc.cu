@@ -2,20 +2,23 @@
 //
 // A persistent grid of CTAs (CG = 1) or of pairs of CTAs on two SMs (CG = 2) works through output tiles of 128 CG
 // rows by tile_n columns. In a CTA
-//   one warp (TMA) or seven (words) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
+//   one warp (TMA) or eleven (else) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
 //     tile_n / CG rows of w, in the 128-byte swizzle that the tensor cores read,
 //   one thread issues tcgen05.mma on them, sums in TMEM (two accumulators of up to 256 columns each),
-//   eight warps take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
+//   eight warps (four) take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
 //     that their accesses to global memory are rows, and apply the epilogue.
 // A pair of CTAs shares one tile: each loads its 128 rows of x and half of the tile's rows of w, the first one's
 // thread issues for both, and each holds the sums of its own rows.
 //
-// WORDS: operands whose rows do not start on 16-byte boundaries cannot come by TMA. Seven warps load them as
-// aligned 32-bit words, a row of a slab per warp and step, shift neighbouring words together and store them where
-// TMA would have put them.
+// Operands whose rows do not start on 16-byte boundaries cannot come by TMA (SHIFT). Eleven warps copy the aligned
+// 16-byte pieces that a slab's rows touch into a ring of their own, two slabs ahead, and then move each row, shifted by
+// its offset, to where TMA would have put it. A warp moves the rows that it has copied, four at a time, so the warps
+// need no barrier among them.
 //
 // Every wait has a limit (kLimitNs); one that runs out sets the CTA's abort flag, so that all its roles leave, after
 // the copies under way have landed, and frees the TMEM.
+#include <type_traits>
+
 #include "cb_async.cuh"
 #include "linear.cuh"
 
@@ -24,13 +27,16 @@ namespace {
 
 constexpr int kRows = 128;        // rows of x per CTA
 constexpr int kSlab = 128;        // bytes of K per stage
-constexpr int kMaxLinStages = 12;
 constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the other
-constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes
-constexpr int kLoadWarps = 7;     // WORDS
+constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes, with SHIFT one
+constexpr int kLoadWarps = 11;    // SHIFT: as many as 16 warps leave (7, with eight for the epilogue: 1.5 times slower)
+__host__ __device__ constexpr int epi_warps(bool shift) { return shift ? 4 : kEpiWarps; }
+__host__ __device__ constexpr int linear_threads(bool shift) { return 32 * (epi_warps(shift) + 1 + (shift ? kLoadWarps : 1)); }
+constexpr int kRawRow = 144;      // bytes of a row's pieces
+constexpr int kRawSlabs = 3;      // slabs of pieces held
 constexpr unsigned long long kLimitNs = 1000000000ull;
 
-struct Tail {  // behind the stages
+struct alignas(16) Tail {  // behind the stages
     float turn[kEpiWarps][32 * 32];
     float cols[kEpiWarps][2 * 32];  // scales and biases of a chunk's columns
     uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2];
@@ -71,11 +77,10 @@ __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) 
 // Wait for a phase of a barrier, until the limit or the CTA's abort flag.
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort, int* status, int code) {
-    auto done = [&] { return CLUSTER ? try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity); };
     unsigned long long t0 = 0;
     while (true) {
         for (int i = 0; i < 64; ++i)
-            if (done()) return true;
+            if (CLUSTER ? try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
         if (*abort) return false;
         const unsigned long long t = now_ns();
         if (t0 == 0) t0 = t;
@@ -173,17 +178,6 @@ __device__ __forceinline__ Tile tile_at(const LinearArgs& A, int t) {
     const int group = 8 * A.tiles_n, g = t / group, r = t - g * group;
     const int rows = min(8, A.tiles_m - 8 * g);
     return Tile{8 * g + r % rows, r / rows};
-}
-
-// The aligned word i of the bytes [p, p + n): whole where it lies inside, else byte by byte.
-__device__ __forceinline__ uint32_t word_of(const char* p, int n, int i) {
-    const int shift = (int)((uintptr_t)p & 3), at = 4 * i - shift;  // byte of the row that the word starts with
-    if (at >= 0 && at + 4 <= n) return *reinterpret_cast<const uint32_t*>(p + at);
-    uint32_t v = 0;
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-        if (at + b >= 0 && at + b < n) v |= (uint32_t)(uint8_t)p[at + b] << 8 * b;
-    return v;
 }
 
 // A place in the ring of stages, and the parity of its present use.
@@ -363,42 +357,78 @@ __device__ __forceinline__ void finish_tma(const LinearArgs& A, const LinearEpil
 }
 
 // The same by elements, a column per lane, for rows that are not made of aligned fours.
-__device__ __forceinline__ void finish_elements(const LinearEpilogue& A, int row0, int col0, int lane, const float* turn) {
-    const int col = col0 + lane;
-    if (col >= A.N) return;
-    const float s = A.w_scale ? A.w_scale[col] : 1.0f;
-    const float b = A.bias ? __uint_as_float(lin_ld1(A.bias, col, A.bias_bf16)) : 0.0f;
-    const int rows = min(32, A.M - row0);
-    for (int r0 = 0; r0 < rows; r0 += 8) {
-        float x[8], g[8];
-        if (A.resid_out)
+
+__device__ __forceinline__ void look_ahead_elements(const LinearEpilogue& E, int row0, int col, Ahead& a) {
+    if (col >= E.N) return;
+    a.scale.x = E.w_scale ? lin_ld1(E.w_scale, col, 0) : __float_as_uint(1.0f);
+    a.bias.x = E.bias ? lin_ld1(E.bias, col, E.bias_bf16) : 0;
+    if (!E.resid_out) return;
+    a.gate.x = __float_as_uint(1.0f);
+    if (E.gate) a.gate.x = lin_ld1(E.gate, ((unsigned)row0 / E.tokens) * E.gate_stride + col, E.gate_bf16);
+    const int rows = E.M - row0, step = E.resid_bf16 ? 2 : 4;
+    const char* q = reinterpret_cast<const char*>(E.resid) + (row0 * E.resid_stride + col) * step;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = row0 + r0 + i;
-                if (r0 + i >= rows) continue;
-                x[i] = __uint_as_float(lin_ld1(A.resid, row * A.resid_stride + col, A.resid_bf16));
-                g[i] = 1.0f;
-                if (A.gate)
-                    g[i] = __uint_as_float(
-                        lin_ld1(A.gate, (long long)((unsigned)row / A.tokens) * A.gate_stride + col, A.gate_bf16));
-            }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = r0 + i, row = row0 + r;
-            if (r >= rows) continue;
-            float v = fmaf(turn[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + lane % 4], s, b);
-            if (A.act == CB_ACT_GELU) v = both(lin_act<CB_ACT_GELU>(two(v, v))).x;
-            if (A.act == CB_ACT_SILU) v = both(lin_act<CB_ACT_SILU>(two(v, v))).x;
-            if (A.out) lin_put1(A.out, row * A.out_stride + col, A.out_bf16, v);
-            if (A.resid_out) lin_put1(A.resid_out, row * A.resid_out_stride + col, A.resid_bf16, fmaf(g[i], v, x[i]));
+    for (int i = 0; i < 32; ++i, q += E.resid_stride * step)
+        if (i < rows) {
+            uint32_t& w = i % 4 == 0 ? a.resid[i / 4].x : i % 4 == 1 ? a.resid[i / 4].y : i % 4 == 2 ? a.resid[i / 4].z : a.resid[i / 4].w;
+            w = lin_ld1(q, 0, E.resid_bf16);
         }
+}
+
+__device__ __forceinline__ void put_column(void* p, long long e, long long stride, int bf16, int rows, const float* v) {
+    if (bf16) {
+        __nv_bfloat16* q = reinterpret_cast<__nv_bfloat16*>(p) + e;
+#pragma unroll
+        for (int i = 0; i < 32; ++i, q += stride)
+            if (i < rows) *q = __float2bfloat16_rn(v[i]);
+    } else {
+        float* q = reinterpret_cast<float*>(p) + e;
+#pragma unroll
+        for (int i = 0; i < 32; ++i, q += stride)
+            if (i < rows) *q = v[i];
     }
 }
 
-template <int CG, bool FP8, bool WORDS>
-__global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)), 1)
+template <int ACT>
+__device__ __forceinline__ void activate_column(float s, float b, float* v) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        const float2 f = both(lin_act<ACT>(fma2(two(v[i], v[i + 1]), two(s, s), two(b, b))));
+        v[i] = f.x, v[i + 1] = f.y;
+    }
+}
+
+__device__ __forceinline__ void finish_elements(const LinearEpilogue& E, int row0, int col, int lane, const Ahead& a,
+                                                const float* turn) {
+    if (col >= E.N) return;
+    const int rows = E.M - row0;
+    float v[32];
+#pragma unroll
+    for (int r = 0; r < 32; ++r) v[r] = turn[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + lane % 4];
+    const float scale = __uint_as_float(a.scale.x), bias = __uint_as_float(a.bias.x);
+    if (E.act == CB_ACT_NONE) activate_column<CB_ACT_NONE>(scale, bias, v);
+    else if (E.act == CB_ACT_GELU) activate_column<CB_ACT_GELU>(scale, bias, v);
+    else activate_column<CB_ACT_SILU>(scale, bias, v);
+    if (E.out) put_column(E.out, row0 * E.out_stride + col, E.out_stride, E.out_bf16, rows, v);
+    if (!E.resid_out) return;
+    const unsigned next = ((unsigned)row0 / E.tokens + 1) * E.tokens;  // rows from here on belong to other samples
+    float g = __uint_as_float(a.gate.x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const unsigned row = (unsigned)(row0 + i);
+        if (E.gate && row >= next && i < rows)
+            g = __uint_as_float(lin_ld1(E.gate, (long long)(row / E.tokens) * E.gate_stride + col, E.gate_bf16));
+        const uint4& x = a.resid[i / 4];
+        v[i] = fmaf(g, v[i], __uint_as_float(i % 4 == 0 ? x.x : i % 4 == 1 ? x.y : i % 4 == 2 ? x.z : x.w));
+    }
+    put_column(E.resid_out, row0 * E.resid_out_stride + col, E.resid_out_stride, E.resid_bf16, rows, v);
+}
+
+template <int CG, bool FP8, bool SHIFT>
+__global__ void __launch_bounds__(linear_threads(SHIFT), 1)
     linear_kernel(const __grid_constant__ LinearArgs A) {
-    static_assert(CG == 1 || !WORDS, "pairs of CTAs load by TMA");
+    static_assert(CG == 1 || !SHIFT, "pairs of CTAs load by TMA");
+    constexpr int EPI = epi_warps(SHIFT);
     extern __shared__ uint8_t raw[];
     uint8_t* const base = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
@@ -412,18 +442,18 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
-            mbar_init(full + 8 * s, WORDS ? kLoadWarps : 1);
+            mbar_init(full + 8 * s, SHIFT ? kLoadWarps : 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, kEpiWarps * CG);
+            mbar_init(acc_empty + 8 * i, EPI * CG);
         }
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_generic_to_async();
     }
-    if (warp == kEpiWarps) {
+    if (warp == EPI) {
         const uint32_t at = smem_addr(&T.tmem);
         if constexpr (CG == 1) {
             asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(at) : "memory");
@@ -442,7 +472,7 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
     after_previous();
 
     const int first = blockIdx.x / CG, step = gridDim.x / CG, total = A.tiles_m * A.tiles_n;
-    if (warp < kEpiWarps) {  // ---- epilogue
+    if (warp < EPI) {  // ---- epilogue
         const LinearEpilogue E = A.e;
         float* const turn = T.turn[warp];
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
@@ -472,6 +502,7 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
             if (half < chunks) {
                 if (A.tma_out) look_column(half);
                 else if (E.wide) look(half);
+                else look_ahead_elements(E, row0, col0 + half * 32 + lane, ahead);
             }
             if (!all(wait(acc_full + 8 * acc, (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT))) break;
             fence_after();
@@ -484,15 +515,15 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
                 }
             };
             if (half >= chunks) release();
-            for (int c = half; c < chunks; c += 2) {
+            for (int c = half; c < chunks; c += EPI / 4) {
                 float v[32];
                 tmem_load(tmem + ((uint32_t)(quarter * 32) << 16) + acc * kAccStride + c * 32, v);
-                if (c + 2 >= chunks) release();
+                if (c + EPI / 4 >= chunks) release();
                 if (A.tma_out) {
                     float* const cols = T.cols[warp];
                     cols[lane] = scale, cols[32 + lane] = bias;
                     __syncwarp();
-                    if (c + 2 < chunks) look_column(c + 2);
+                    if (c + EPI / 4 < chunks) look_column(c + EPI / 4);
                     uint8_t* const buf = reinterpret_cast<uint8_t*>(turn);
                     const int col = col0 + c * 32;
                     if (E.act == CB_ACT_NONE) finish_tma<CB_ACT_NONE>(A, E, cols, xs2, v, buf, next_buf, row0, col, lane);
@@ -514,17 +545,18 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
                         u[i] = *reinterpret_cast<const ulonglong2*>(&turn[r * 32 + ((lane & 7) ^ (r & 7)) * 4]);
                     }
                     const Ahead now = ahead;
-                    if (c + 2 < chunks) look(c + 2);
+                    if (c + EPI / 4 < chunks) look(c + EPI / 4);
                     if (rows_full) finish<true>(E, spot, c * 32, now, u);
                     else finish<false>(E, spot, c * 32, now, u);
                 } else {
-                    finish_elements(E, row0, col0 + c * 32, lane, turn);
+                    finish_elements(E, row0, col0 + c * 32 + lane, lane, ahead, turn);
+                    if (c + EPI / 4 < chunks) look_ahead_elements(E, row0, col0 + (c + EPI / 4) * 32 + lane, ahead);
                 }
                 __syncwarp();
             }
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    } else if (warp == kEpiWarps) {  // ---- products
+    } else if (warp == EPI) {  // ---- products
         if (rank == 0) {
             // fp32 sums; A and B bf16 (kind f16) or e4m3 (kind f8f6f4), both with K innermost; N / 8, M / 16
             const uint32_t idesc =
@@ -557,7 +589,7 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
                 }
             }
         }
-    } else if constexpr (!WORDS) {  // ---- copies
+    } else if constexpr (!SHIFT) {  // ---- operands
         {
             Place at;
             int fills = 0;
@@ -584,48 +616,126 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
             }
         }
     } else {
-        const int lw = warp - kEpiWarps - 1;
-        Place at;
-        int fills = 0;
-        bool ok = true;
-        for (int t = first; t < total && ok; t += step) {
+        const int M = A.e.M, N = A.e.N, rows = kRows + w_rows, lw = warp - EPI - 1;
+        const long long x_row = A.x_row, w_row = A.w_row;
+        const char *const x0 = reinterpret_cast<const char*>(A.x), *const w0 = reinterpret_cast<const char*>(A.w);
+        const uint32_t raw_at = smem_addr(&T + 1);
+        const int raw_bytes = rows * kRawRow;
+        struct Slab {
+            int t, kb, row0, col0;
+        };
+        auto start = [&](int t) {
+            if (t >= total) return Slab{t, 0, 0, 0};
             const Tile tile = tile_at(A, t);
-            const int row0 = tile.m * kRows, col0 = tile.n * A.tile_n;
-            for (int kb = 0; kb < A.k_blocks; ++kb, ++fills) {
-                ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
-                if (!ok) break;
-                uint8_t* const stage = base + at.s * stage_bytes;
-                const int n = min(kSlab, A.k_bytes - kb * kSlab);
-                constexpr int B = 4;  // rows whose loads are in flight together
-                for (int r0 = lw * B; r0 < kRows + w_rows; r0 += kLoadWarps * B) {
-                    uint32_t lo[B], hi[B];
-                    int shift[B];
-#pragma unroll
-                    for (int i = 0; i < B; ++i) {
-                        const int r = r0 + i;
-                        const bool is_x = r < kRows;
-                        const int at = is_x ? row0 + r : col0 + r - kRows;
-                        const bool on = at < (is_x ? A.e.M : A.e.N);
-                        const char* p = reinterpret_cast<const char*>(is_x ? A.x : A.w) +
-                                        at * (is_x ? A.x_row : A.w_row) + (long long)kb * kSlab;
-                        shift[i] = (int)((uintptr_t)p & 3);
-                        lo[i] = on ? word_of(p, n, lane) : 0;
-                        hi[i] = on && lane == 31 && shift[i] ? word_of(p, n, 32) : 0;
-                    }
-#pragma unroll
-                    for (int i = 0; i < B; ++i) {
-                        const int r = r0 + i;
-                        const uint32_t next = __shfl_down_sync(0xFFFFFFFFu, lo[i], 1);
-                        const uint32_t v = __funnelshift_r(lo[i], lane == 31 ? hi[i] : next, 8 * shift[i]);
-                        *reinterpret_cast<uint32_t*>(stage + r * kSlab + ((lane / 4) ^ (r & 7)) * 16 + (lane % 4) * 4) = v;
+            return Slab{t, 0, tile.m * kRows, tile.n * A.tile_n};
+        };
+        auto next_of = [&](Slab c) { return ++c.kb < A.k_blocks ? c : start(c.t + step); };
+        const int quad_row = lane / 8, j = lane % 8;  // row of four, piece of the eight that every row has
+        // Copies pieces of the stage rows of the quads q, q + kLoadWarps, ... below `end`, rows of an operand from `from` on, the
+        // stage's row 0 being its row `row0`. NINTH: the pieces behind the eighth, a lane for each row of eight quads.
+        // No byte outside of the operand is read: copies end with it (`ends`: this slab may touch its ends), and pieces
+        // that begin before it are read byte by byte.
+        auto copy_quads = [&](auto ninth, int q, int end, const char* from, long long stride, int row0, int count, int kb,
+                              bool ends, uint32_t dst) {
+            constexpr bool NINTH = decltype(ninth)::value;
+            constexpr int S = NINTH ? 8 * kLoadWarps : kLoadWarps;
+            int r = 4 * (NINTH ? q + lane / 4 * kLoadWarps : q) + (NINTH ? lane % 4 : quad_row);
+            const int piece = NINTH ? 8 : j;
+            const char* at = from + (row0 + r) * stride + kb * kSlab + 16 * piece;
+            dst += 16 * piece;
+#pragma unroll 2
+            for (; q < end; q += S, r += 4 * S, at += 4 * S * stride) {
+                const int m = (int)((uintptr_t)at & 15);
+                const char* const p = at - m;
+                bool on = row0 + r < count && r < 4 * end && (!NINTH || m);
+                int size = 16;
+                if (ends) {
+                    const char* const to = from + (count - 1) * stride + A.k_bytes;
+                    size = (int)min(max((long long)(to - p), 0ll), 16ll);
+                    if (on && p < from) {
+#pragma unroll 1
+                        for (int i = 0; i < 16; ++i)
+                            if (p + i >= from && p + i < to)
+                                asm volatile("st.shared.u8 [%0], %1;" ::"r"(dst + r * kRawRow + i), "h"((short)(uint8_t)p[i])
+                                             : "memory");
+                        on = false;
                     }
                 }
-                fence_generic_to_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(full + 8 * at.s);
-                at.next(stages);
+                if (on)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + r * kRawRow), "l"(size > 0 ? p : from),
+                                 "r"(size)
+                                 : "memory");
             }
+        };
+        const int x_quads = kRows / 4, quads = rows / 4;
+        const int w_first = x_quads + (lw + kLoadWarps - x_quads % kLoadWarps) % kLoadWarps;  // this warp's first quad of w
+        auto copy = [&](const Slab& c, int slot) {
+            const uint32_t dst = raw_at + slot * raw_bytes;
+            const bool ends = (c.kb == 0 || c.kb + 2 >= A.k_blocks) &&
+                              (c.row0 == 0 || c.col0 == 0 || c.row0 + kRows + 16 >= M || c.col0 + w_rows + 16 >= N);
+            const std::false_type eight;
+            const std::true_type ninth;
+            copy_quads(eight, lw, x_quads, x0, x_row, c.row0, M, c.kb, ends, dst);
+            copy_quads(eight, w_first, quads, w0, w_row, c.col0 - kRows, N, c.kb, ends, dst);
+            copy_quads(ninth, lw, x_quads, x0, x_row, c.row0, M, c.kb, ends, dst);
+            copy_quads(ninth, w_first, quads, w0, w_row, c.col0 - kRows, N, c.kb, ends, dst);
+        };
+        // The quads' rows from their pieces to the stage: a lane makes 16 bytes out of two pieces, `off` being the address of the
+        // stage's row 0 in the operand (its low bits).
+        auto move_quads = [&](int q, int end, uint32_t off, uint32_t stride, uint32_t raw, uint32_t stage, int left) {
+            off += (4 * q + quad_row) * stride;
+            raw += (4 * q + quad_row) * kRawRow + 16 * j;
+            stage += (4 * q + quad_row) * kSlab;
+#pragma unroll 2
+            for (; q < end; q += kLoadWarps) {
+                uint32_t w[8];
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(raw));
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+16];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(raw));
+#pragma unroll
+                for (int i = 0; i < 6; ++i) w[i] = off & 8 ? w[i + 2] : w[i];
+#pragma unroll
+                for (int i = 0; i < 5; ++i) w[i] = off & 4 ? w[i + 1] : w[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (off & 3));
+                if (left < 16) {  // zeros behind the row's last byte
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (left < 4 * i + 4) w[i] = left <= 4 * i ? 0 : w[i] & ((1u << 8 * (left - 4 * i)) - 1);
+                }
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (j ^ ((4 * q + quad_row) & 7)) * 16), "r"(w[0]),
+                             "r"(w[1]), "r"(w[2]), "r"(w[3])
+                             : "memory");
+                off += 4 * kLoadWarps * stride;
+                raw += 4 * kLoadWarps * kRawRow;
+                stage += 4 * kLoadWarps * kSlab;
+            }
+        };
+        Place at;
+        int fills = 0, slot = 0;
+        Slab now = start(first), ahead = now;
+#pragma unroll 1
+        for (int i = 0; i + 1 < kRawSlabs; ++i) {
+            if (ahead.t < total) copy(ahead, i), ahead = next_of(ahead);
+            asm volatile("cp.async.commit_group;" ::: "memory");
         }
+        for (; now.t < total; now = next_of(now), ++fills) {
+            if (ahead.t < total) copy(ahead, slot == 0 ? kRawSlabs - 1 : slot - 1), ahead = next_of(ahead);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRawSlabs - 1) : "memory");
+            if (!all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT))) break;
+            __syncwarp();
+            const int left = A.k_bytes - now.kb * kSlab - 16 * j;  // bytes of a row from this lane's 16 on
+            const uint32_t raw = raw_at + slot * raw_bytes, stage = ring + at.s * stage_bytes;
+            const uint32_t xs = (uint32_t)x_row, ws = (uint32_t)w_row;
+            move_quads(lw, x_quads, (uint32_t)(uintptr_t)x0 + (uint32_t)now.row0 * xs, xs, raw, stage, left);
+            move_quads(w_first, quads, (uint32_t)(uintptr_t)w0 + (uint32_t)(now.col0 - kRows) * ws, ws, raw, stage, left);
+            fence_generic_to_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + 8 * at.s);
+            at.next(stages);
+            slot = slot + 1 == kRawSlabs ? 0 : slot + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
         drain(at, fills, stages, empty, abort, A.status);
     }
     fence_before();
@@ -633,7 +743,7 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();  // no CTA leaves while the other may still reach its barriers or TMEM
     fence_after();
-    if (warp == kEpiWarps) {
+    if (warp == EPI) {
         if constexpr (CG == 1)
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
         else
@@ -642,8 +752,8 @@ __global__ void __launch_bounds__(32 * (kEpiWarps + 1 + (WORDS ? kLoadWarps : 1)
 }
 
 using Kernel = void (*)(LinearArgs);
-Kernel kernel_of(int cg, bool fp8, bool words) {
-    if (words) return fp8 ? linear_kernel<1, true, true> : linear_kernel<1, false, true>;
+Kernel kernel_of(int cg, bool fp8, bool shift) {
+    if (shift) return fp8 ? linear_kernel<1, true, true> : linear_kernel<1, false, true>;
     if (cg == 2) return fp8 ? linear_kernel<2, true, false> : linear_kernel<2, false, false>;
     return fp8 ? linear_kernel<1, true, false> : linear_kernel<1, false, false>;
 }
@@ -652,32 +762,31 @@ Kernel kernel_of(int cg, bool fp8, bool words) {
 
 size_t linear_stage_bytes(int cg, int tile_n) { return (size_t)(kRows + tile_n / cg) * kSlab; }
 
-int linear_max_stages(size_t smem, size_t stage_bytes) {
-    const size_t room = smem - sizeof(Tail) - 1024;
-    const int n = (int)(room / stage_bytes);
-    return n < kMaxLinStages ? n : kMaxLinStages;
+size_t linear_fixed_bytes(bool shift, int tile_n) {
+    return 1024 + sizeof(Tail) + (shift ? (size_t)kRawSlabs * kRawRow * (kRows + tile_n) : 0);
 }
 
 cudaError_t prepare_linear(size_t smem, int* pairs) {
-    for (int k = 0; k < 6; ++k) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel_of(k / 2 == 1 ? 2 : 1, k % 2 == 1, k / 2 == 2),
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
+    for (int fp8 = 0; fp8 < 2; ++fp8)
+        for (Kernel k : {kernel_of(2, fp8, false), kernel_of(1, fp8, false), kernel_of(1, fp8, true)}) {
+            const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+        }
     // pairs of CTAs that run at once
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim.x = 2, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(2);
-    c.blockDim = dim3(32 * (kEpiWarps + 2));
+    c.blockDim = dim3(linear_threads(false));
     c.dynamicSmemBytes = smem;
     c.attrs = &at;
     c.numAttrs = 1;
     return cudaOccupancyMaxActiveClusters(pairs, reinterpret_cast<const void*>(kernel_of(2, false, false)), &c);
 }
 
-cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, bool words, int grid, cudaStream_t s) {
+cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s) {
+    const bool shift = a.grid_bytes < 16;
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = a.overlap;
@@ -685,13 +794,13 @@ cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, bool words, int
     at[1].val.clusterDim.x = (unsigned)cg, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)grid);
-    c.blockDim = dim3(32 * (kEpiWarps + 1 + (words ? kLoadWarps : 1)));
-    c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + sizeof(Tail) + 1024;
+    c.blockDim = dim3(linear_threads(shift));
+    c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + linear_fixed_bytes(shift, a.tile_n);
     c.stream = s;
     c.attrs = at;
     c.numAttrs = cg == 2 ? 2 : 1;
     void* args[] = {const_cast<void*>(static_cast<const void*>(&a))};
-    const cudaError_t e = cudaLaunchKernelExC(&c, reinterpret_cast<const void*>(kernel_of(cg, fp8, words)), args);
+    const cudaError_t e = cudaLaunchKernelExC(&c, reinterpret_cast<const void*>(kernel_of(cg, fp8, shift)), args);
     if (e != cudaSuccess) (void)cudaGetLastError();
     return e;
 }
