@@ -63,6 +63,11 @@ int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes
     return r == CUDA_SUCCESS ? CB_OK : cuda_error(cudaErrorInvalidValue, "tensor map");
 }
 
+// Rows that linear_few.cu takes. GB300, w in L2, events around one call (about 8 us of them its own), linear_tc.cu ->
+// linear_few.cu: 8 x 6912 x 1152 14.2 -> 10.7 us, 32 x 1152 x 4608 18.5 -> 13.2, 8 x 64 x 16384 45 -> 9.6; with 64 rows
+// 6912 x 1152 13.2 -> 20.8, 1152 x 4608 18.6 -> 18.4, 12288 x 3072 20.3 -> 55.
+constexpr int kFewRows = 32;
+
 // CTAs per tile and the tile's columns: the fewest rounds of tiles, each as long as its loads (16 KB of x and
 // 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take.
 void choose_tile(const Device& dev, int M, int N, bool tma, int* cg, int* tile_n) {
@@ -167,6 +172,11 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.grid_bytes = 16;
     while (((uintptr_t)x | (uintptr_t)d.w | (uintptr_t)a.x_row | (uintptr_t)a.w_row) % a.grid_bytes) a.grid_bytes /= 2;
     const bool tma = a.grid_bytes == 16;
+    if (ep.M <= kFewRows) {
+        const LinearFewArgs f{ep, 1, a.k_bytes, a.x_row, a.w_row, x, d.w};
+        const cudaError_t e = launch_linear_few(f, d.type == CB_E4M3, !tma, dev->sms, (cudaStream_t)stream);
+        return e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
+    }
     int cg = 1;
     choose_tile(*dev, ep.M, ep.N, tma, &cg, &a.tile_n);
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;

@@ -39,6 +39,17 @@ struct LinearArgs {
     int* status;
 };
 
+// Few rows (linear_few.cu).
+struct LinearFewArgs {
+    LinearEpilogue e;
+    int overlap;
+    int k_bytes;             // bytes of a row of x and of w
+    long long x_row, w_row;  // bytes from row to row
+    const void *x, *w;
+};
+// `shift`: rows off the 16-byte grid.
+cudaError_t launch_linear_few(const LinearFewArgs& a, bool fp8, bool shift, int sms, cudaStream_t s);
+
 // The tensor-core kernels (linear_tc.cu): cg CTAs per tile of 128 cg rows; a.grid_bytes below 16: cg = 1
 // only. prepare_linear raises the kernels' shared-memory limit and tells how many pairs of CTAs run at once.
 size_t linear_stage_bytes(int cg, int tile_n);

@@ -21,6 +21,7 @@
 
 #include "cb_async.cuh"
 #include "linear.cuh"
+#include "linear_shift.cuh"
 
 namespace cbk {
 namespace {
@@ -691,19 +692,9 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
                 uint32_t w[8];
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(raw));
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+16];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(raw));
-#pragma unroll
-                for (int i = 0; i < 6; ++i) w[i] = off & 8 ? w[i + 2] : w[i];
-#pragma unroll
-                for (int i = 0; i < 5; ++i) w[i] = off & 4 ? w[i + 1] : w[i];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (off & 3));
-                if (left < 16) {  // zeros behind the row's last byte
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (left < 4 * i + 4) w[i] = left <= 4 * i ? 0 : w[i] & ((1u << 8 * (left - 4 * i)) - 1);
-                }
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (j ^ ((4 * q + quad_row) & 7)) * 16), "r"(w[0]),
-                             "r"(w[1]), "r"(w[2]), "r"(w[3])
+                const uint4 v = first_bytes(shifted(make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), off & 15), left);
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (j ^ ((4 * q + quad_row) & 7)) * 16), "r"(v.x),
+                             "r"(v.y), "r"(v.z), "r"(v.w)
                              : "memory");
                 off += 4 * kLoadWarps * stride;
                 raw += 4 * kLoadWarps * kRawRow;
