@@ -211,14 +211,18 @@ cudaError_t push_blocks_per_sm(bool src_bf16, bool dst_bf16, size_t smem, int* b
 
 // The int8 history (quant.cu): codes with one bf16 scale per kQuantBlock
 // elements. `write`: a full step's slot write (m_off the features' addresses, m_out
-// the codes'), with the hidden-state update where `grouped`; otherwise a skipped
-// step. Declared weak: the host side links without them, over stand-ins of
-// the other launchers, and refuses the cache type there.
+// the codes'), with the hidden-state update; otherwise a skipped step. Declared
+// weak: the host side links without them, over stand-ins of the other launchers,
+// and refuses the cache type there.
 constexpr int kQuantBlock = 64;
+enum QuantForm {
+    kQuantPlain,    // vectors, one tensor per item and no hidden state
+    kQuantGrouped,  // vectors
+    kQuantElements  // items with vec_ok = 0
+};
 long long quant_tile_elems(bool write) __attribute__((weak));
-cudaError_t quant_blocks_per_sm(int K, bool grouped, bool write, int* blocks) __attribute__((weak));
-cudaError_t launch_quant_read(const ExtrapArgs& a, int K, bool grouped, int grid, cudaStream_t s) __attribute__((weak));
-cudaError_t launch_quant_write(const ExtrapArgs& a, bool grouped, int grid, cudaStream_t s) __attribute__((weak));
+cudaError_t quant_blocks_per_sm(int K, QuantForm form, bool write, int* blocks) __attribute__((weak));
+cudaError_t launch_quant(const ExtrapArgs& a, int K, QuantForm form, bool write, int grid, cudaStream_t s) __attribute__((weak));
 
 // Notes a failed CUDA call for cb_last_error_message and returns CB_ERR_CUDA (plan.cpp).
 int cuda_error(cudaError_t e, const char* where);

@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
     uint32_t rank, ranks;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-    const int col0 = blockIdx.y * 16;
+    const int col0 = (int)(blockIdx.x / ranks) * 16;
     const int M = A.e.M, N = A.e.N, k_bytes = A.k_bytes;
     const char *const x = reinterpret_cast<const char*>(A.x), *const w = reinterpret_cast<const char*>(A.w);
     auto line = [&](const char* from, int row, int rows, long long stride) {
@@ -186,7 +186,7 @@ cudaError_t launch_linear_few(const LinearFewArgs& a, bool fp8, bool shift, int 
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3(cluster, cols);
+    c.gridDim = dim3(cluster * cols);
     c.blockDim = dim3(32 * kWarps);
     c.stream = s;
     c.attrs = at;

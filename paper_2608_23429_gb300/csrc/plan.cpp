@@ -78,7 +78,7 @@ struct DeviceInfo {
     int occ_extrap[2][CB_MAX_K + 1] = {};  // [cache_bf16][K]
     int occ_push[2][2] = {};               // [src_bf16][dst_bf16]
     int occ_epilogue = 0;                  // epilogue kernel (bf16 features, no gates)
-    int occ_quant[2][2][CB_MAX_K + 1] = {};  // int8 history: [write][grouped][K]
+    int occ_quant[2][3][CB_MAX_K + 1] = {};  // int8 history: [write][form][K]
     int bulk_stages[2][CB_MAX_K + 1] = {};  // 1 once the kernel's shared-memory limit is raised
     int bulk_gated[2][CB_MAX_K + 1] = {};   // the same for the gated kernel
     int bulk_precise[2][2][CB_MAX_K + 1] = {};  // [gated]: the same for fp32 predictions or hidden states
@@ -450,23 +450,11 @@ int launch_epilogue(Launch& L, cbk::ExtrapArgs& A) {
 }
 
 // The int8 history's kernels: a full step's slot write or a skipped step.
-int launch_quant(Launch& L, cbk::ExtrapArgs& A) {
-    bool grouped = false;
-    for (int i = 0; i < A.n_items; ++i) grouped = grouped || A.resid[i] != nullptr;
+int launch_quant_form(Launch& L, cbk::ExtrapArgs& A, int K, cbk::QuantForm form) {
     const bool write = L.full_step;
-    int K = 1;
-    if (!write) {  // entries of weight zero are not read (a target on a node reads that node alone)
-        K = 0;
-        for (int j = 0; j < L.K; ++j) {
-            if (A.w_hi[j] == 0.0f) continue;
-            A.w_hi[K] = A.w_hi[j];
-            A.slot_off[K++] = A.slot_off[j];
-        }
-        K = std::max(K, 1);
-    }
-    int& occ = L.p->dev.occ_quant[write ? 1 : 0][grouped ? 1 : 0][K];
+    int& occ = L.p->dev.occ_quant[write ? 1 : 0][form][K];
     if (occ == 0) {
-        cudaError_t e = cbk::quant_blocks_per_sm(K, grouped, write, &occ);
+        cudaError_t e = cbk::quant_blocks_per_sm(K, form, write, &occ);
         if (e != cudaSuccess || occ <= 0) {
             occ = 0;
             return cuda_fail(e == cudaSuccess ? cudaErrorInvalidConfiguration : e, "occupancy");
@@ -477,9 +465,39 @@ int launch_quant(Launch& L, cbk::ExtrapArgs& A) {
     if (r != CB_OK) return r;
     const int grid = (int)std::min<long long>(A.tiles_total, (long long)L.p->dev.sms * occ);
     A.overlap = 1;
-    const cudaStream_t s = (cudaStream_t)L.stream;
-    const cudaError_t e = write ? cbk::launch_quant_write(A, grouped, grid, s) : cbk::launch_quant_read(A, K, grouped, grid, s);
+    const cudaError_t e = cbk::launch_quant(A, K, form, write, grid, (cudaStream_t)L.stream);
     return e == cudaSuccess ? CB_OK : cuda_fail(e, write ? "int8 cache write launch" : "int8 extrapolate launch");
+}
+
+// One launch, or two where some items are reached by vectors and others are not.
+int launch_quant(Launch& L, cbk::ExtrapArgs& A) {
+    int K = 1;
+    if (!L.full_step) {  // entries of weight zero are not read (a target on a node reads that node alone)
+        K = 0;
+        for (int j = 0; j < L.K; ++j) {
+            if (A.w_hi[j] == 0.0f) continue;
+            A.w_hi[K] = A.w_hi[j];
+            A.slot_off[K++] = A.slot_off[j];
+        }
+        K = std::max(K, 1);
+    }
+    bool vec[cbk::kMaxItems];
+    int vecs = 0;
+    cbk::QuantForm form = cbk::kQuantPlain;  // of the items reached by vectors
+    for (int i = 0; i < A.n_items; ++i) {
+        vecs += vec[i] = A.vec_ok[i] != 0;
+        if (vec[i] && A.resid[i]) form = cbk::kQuantGrouped;
+    }
+    if (vecs == A.n_items) return launch_quant_form(L, A, K, form);
+    if (vecs == 0) return launch_quant_form(L, A, K, cbk::kQuantElements);
+    if (!L.p->eargs2) L.p->eargs2.reset(new (std::nothrow) cbk::ExtrapArgs());
+    if (!L.p->eargs2) return CB_ERR_LIMIT;
+    cbk::ExtrapArgs& B = *L.p->eargs2;
+    take_items(A, vec, false, B);
+    const int r = launch_quant_form(L, B, K, cbk::kQuantElements);
+    if (r != CB_OK) return r;
+    take_items(A, vec, true, B);
+    return launch_quant_form(L, B, K, form);
 }
 
 // The bulk-copy pipeline. `strided`: every item is off the 16-byte grid on its
@@ -819,7 +837,7 @@ int cb_plan_create(const double* node_t, int n_nodes, int K, const cb_tensor_des
     if (K < 1 || K > CB_MAX_K) return K < 1 ? CB_ERR_ARG : CB_ERR_LIMIT;
     if (!node_t || n_nodes < K || !tensors || n_tensors < 1) return CB_ERR_ARG;
     if (n_tensors > CB_MAX_TENSORS) return CB_ERR_LIMIT;
-    if (!valid_dtype(cache_dtype) && !(cache_dtype == CB_INT8 && cbk::launch_quant_read)) return CB_ERR_ARG;
+    if (!valid_dtype(cache_dtype) && !(cache_dtype == CB_INT8 && cbk::launch_quant)) return CB_ERR_ARG;
     if (!(std::isfinite(t_min) && std::isfinite(t_max) && t_min < t_max)) return CB_ERR_ARG;
     for (int i = 0; i < n_nodes; ++i)
         if (!std::isfinite(node_t[i])) return CB_ERR_ARG;
