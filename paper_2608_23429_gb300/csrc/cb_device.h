@@ -220,7 +220,7 @@ enum QuantForm {
     kQuantGrouped,  // vectors
     kQuantElements  // items with vec_ok = 0
 };
-long long quant_tile_elems(bool write) __attribute__((weak));
+long long quant_tile_elems(QuantForm form, bool write) __attribute__((weak));
 cudaError_t quant_blocks_per_sm(int K, QuantForm form, bool write, int* blocks) __attribute__((weak));
 cudaError_t launch_quant(const ExtrapArgs& a, int K, QuantForm form, bool write, int grid, cudaStream_t s) __attribute__((weak));
 
