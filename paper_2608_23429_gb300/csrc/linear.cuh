@@ -143,20 +143,36 @@ __device__ __forceinline__ Two add2(Two a, Two b) {
 }
 
 // v / (1 + 2^t): SiLU with t = -v log2(e), the tanh form of GELU with t = -2 log2(e) sqrt(2/pi) (v + 0.044715 v^3),
-// since (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z)).
+// since (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z)). Four at a time, with one reciprocal of the product of their
+// denominators, as the unit for special functions is what an epilogue with an activation waits for. t ends at 30,
+// where the result is below 2^-30 |v|, so that the product stays finite (and a NaN stays with its own value).
 template <int ACT>
-__device__ __forceinline__ Two lin_act(Two v) {
-    if constexpr (ACT == CB_ACT_NONE) return v;
-    constexpr float kSilu = -1.44269504f, kGelu1 = -2.30220820f, kGelu3 = -0.102943239f;
-    const Two t = ACT == CB_ACT_SILU ? mul2(v, two(kSilu, kSilu))
-                                     : mul2(v, fma2(two(kGelu3, kGelu3), mul2(v, v), two(kGelu1, kGelu1)));
-    float2 e = both(t);
-    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
-    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
-    float2 d = both(add2(two(e.x, e.y), two(1.0f, 1.0f)));
-    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d.x));
-    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d.y));
-    return mul2(v, two(d.x, d.y));
+__device__ __forceinline__ void lin_act4(Two& v, Two& w) {
+    if constexpr (ACT != CB_ACT_NONE) {
+        constexpr float kSilu = -1.44269504f, kGelu1 = -2.30220820f, kGelu3 = -0.102943239f;
+        auto denominators = [](Two x) {
+            const Two t = ACT == CB_ACT_SILU ? mul2(x, two(kSilu, kSilu))
+                                             : mul2(x, fma2(two(kGelu3, kGelu3), mul2(x, x), two(kGelu1, kGelu1)));
+            float2 e = both(t);
+            e.x = fminf(e.x, 30.0f), e.y = fminf(e.y, 30.0f);
+            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+            return add2(two(e.x, e.y), two(1.0f, 1.0f));
+        };
+        const Two a = denominators(v), b = denominators(w);
+        const float2 p = both(mul2(a, b));
+        float r = p.x * p.y;
+        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
+        const Two q = mul2(two(r, r), two(p.y, p.x));  // 1 / (a b), pair by pair
+        v = mul2(v, mul2(q, b));
+        w = mul2(w, mul2(q, a));
+    }
+}
+template <int ACT>
+__device__ __forceinline__ float lin_act1(float v) {
+    Two a = two(v, v), b = a;
+    lin_act4<ACT>(a, b);
+    return both(a).x;
 }
 
 }  // namespace

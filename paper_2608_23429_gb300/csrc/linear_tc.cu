@@ -2,15 +2,15 @@
 //
 // A persistent grid of CTAs (CG = 1) or of pairs of CTAs on two SMs (CG = 2) works through output tiles of 128 CG
 // rows by tile_n columns. In a CTA
-//   one warp (TMA) or eleven (else) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
+//   one warp (TMA) or several (else) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
 //     tile_n / CG rows of w, in the 128-byte swizzle that the tensor cores read,
 //   one thread issues tcgen05.mma on them, sums in TMEM (two accumulators of up to 256 columns each),
-//   eight warps (four) take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
+//   eight warps (or four) take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
 //     that their accesses to global memory are rows, and apply the epilogue.
 // A pair of CTAs shares one tile: each loads its 128 rows of x and half of the tile's rows of w, the first one's
 // thread issues for both, and each holds the sums of its own rows.
 //
-// Operands whose rows do not start on 16-byte boundaries cannot come by TMA (SHIFT). Eleven warps copy the aligned
+// Operands whose rows do not start on 16-byte boundaries cannot come by TMA (SHIFT). Seven or eleven warps copy the aligned
 // 16-byte pieces that a slab's rows touch into a ring of their own, two slabs ahead, and then move each row, shifted by
 // its offset, to where TMA would have put it. A warp moves the rows that it has copied, four at a time, so the warps
 // need no barrier among them.
@@ -29,18 +29,21 @@ namespace {
 constexpr int kRows = 128;        // rows of x per CTA
 constexpr int kSlab = 128;        // bytes of K per stage
 constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the other
-constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes, with SHIFT one
-constexpr int kLoadWarps = 11;    // SHIFT: as many as 16 warps leave (7, with eight for the epilogue: 1.5 times slower)
-__host__ __device__ constexpr int epi_warps(bool shift) { return shift ? 4 : kEpiWarps; }
-__host__ __device__ constexpr int linear_threads(bool shift) { return 32 * (epi_warps(shift) + 1 + (shift ? kLoadWarps : 1)); }
+constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes
+// Warps that move operands off the 16-byte grid (0: TMA), of the 16 warps that 128 registers a thread allow. Long sums are
+// bound by them and take 11, with four warps for the epilogue; short ones by the epilogue and take 7 and eight
+// (999 x 577 x 1155 31.4 -> 28.7 us; 4096 x 4096 x 4097 867 -> 1004 us).
+constexpr int kFewLoaders = 7, kManyLoaders = 11, kManyFrom = 24;  // slabs
+__host__ __device__ constexpr int epi_warps(int loaders) { return loaders == kManyLoaders ? 4 : kEpiWarps; }
+__host__ __device__ constexpr int linear_threads(int loaders) { return 32 * (epi_warps(loaders) + 1 + (loaders ? loaders : 1)); }
 constexpr int kRawRow = 144;      // bytes of a row's pieces
 constexpr int kRawSlabs = 3;      // slabs of pieces held
 constexpr unsigned long long kLimitNs = 1000000000ull;
 
 struct alignas(16) Tail {  // behind the stages
     float turn[kEpiWarps][32 * 32];
-    float cols[kEpiWarps][2 * 32];  // scales and biases of a chunk's columns
-    uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2];
+    float cols[2][2 * kAccStride];  // scales and biases of a tile's columns (where the output leaves by TMA)
+    uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2], cols_full[2];
     uint32_t tmem;
     int abort;
 };
@@ -276,8 +279,9 @@ __device__ __forceinline__ void activate(const float4& s, const float4& b, ulong
     const Two s0 = two(s.x, s.y), s1 = two(s.z, s.w), b0 = two(b.x, b.y), b1 = two(b.z, b.w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        v[i].x = lin_act<ACT>(fma2(v[i].x, s0, b0));
-        v[i].y = lin_act<ACT>(fma2(v[i].y, s1, b1));
+        v[i].x = fma2(v[i].x, s0, b0);
+        v[i].y = fma2(v[i].y, s1, b1);
+        lin_act4<ACT>(v[i].x, v[i].y);
     }
 }
 
@@ -316,11 +320,12 @@ __device__ __forceinline__ void finish_tma(const LinearArgs& A, const LinearEpil
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(cols + 4 * j);
-        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(cols + 32 + 4 * j);
+        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(cols + kAccStride + 4 * j);
         Two p = two(v[4 * j], v[4 * j + 1]), q = two(v[4 * j + 2], v[4 * j + 3]);
         if (E.x_scale) p = mul2(p, xs2), q = mul2(q, xs2);
-        x[2 * j] = lin_act<ACT>(fma2(p, s.x, b.x));
-        x[2 * j + 1] = lin_act<ACT>(fma2(q, s.y, b.y));
+        x[2 * j] = fma2(p, s.x, b.x);
+        x[2 * j + 1] = fma2(q, s.y, b.y);
+        lin_act4<ACT>(x[2 * j], x[2 * j + 1]);
     }
     const int turns = E.out_bf16 ? 1 : 2;
     for (int h = 0; h < turns; ++h) {
@@ -393,9 +398,11 @@ __device__ __forceinline__ void put_column(void* p, long long e, long long strid
 template <int ACT>
 __device__ __forceinline__ void activate_column(float s, float b, float* v) {
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        const float2 f = both(lin_act<ACT>(fma2(two(v[i], v[i + 1]), two(s, s), two(b, b))));
-        v[i] = f.x, v[i + 1] = f.y;
+    for (int i = 0; i < 32; i += 4) {
+        Two x = fma2(two(v[i], v[i + 1]), two(s, s), two(b, b)), y = fma2(two(v[i + 2], v[i + 3]), two(s, s), two(b, b));
+        lin_act4<ACT>(x, y);
+        const float2 f = both(x), g = both(y);
+        v[i] = f.x, v[i + 1] = f.y, v[i + 2] = g.x, v[i + 3] = g.y;
     }
 }
 
@@ -425,13 +432,17 @@ __device__ __forceinline__ void finish_elements(const LinearEpilogue& E, int row
     put_column(E.resid_out, row0 * E.resid_out_stride + col, E.resid_out_stride, E.resid_bf16, rows, v);
 }
 
-template <int CG, bool FP8, bool SHIFT>
-__global__ void __launch_bounds__(linear_threads(SHIFT), 1)
+template <int CG, bool FP8, int LOADERS>
+__global__ void __launch_bounds__(linear_threads(LOADERS), 1)
     linear_kernel(const __grid_constant__ LinearArgs A) {
+    constexpr bool SHIFT = LOADERS != 0;
     static_assert(CG == 1 || !SHIFT, "pairs of CTAs load by TMA");
-    constexpr int EPI = epi_warps(SHIFT);
-    extern __shared__ uint8_t raw[];
-    uint8_t* const base = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    constexpr int EPI = epi_warps(LOADERS);
+    extern __shared__ __align__(1024) uint8_t base[];
+    if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
+        if (threadIdx.x == 0) record(A.status, CB_DEV_PRODUCER_TIMEOUT);
+        return;
+    }
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int w_rows = A.tile_n / CG, stage_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
@@ -443,12 +454,13 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
-            mbar_init(full + 8 * s, SHIFT ? kLoadWarps : 1);
+            mbar_init(full + 8 * s, SHIFT ? LOADERS : 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(acc_full + 8 * i, 1);
             mbar_init(acc_empty + 8 * i, EPI * CG);
+            mbar_init(smem_addr(T.cols_full) + 8 * i, EPI);
         }
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -478,31 +490,46 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
         float* const turn = T.turn[warp];
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
         int n_done = 0, next_buf = 0;
+        auto first_row = [&](const Tile& tile) { return (tile.m * CG + (int)rank) * kRows + quarter * 32; };
+        // The operands of a tile that do not depend on its sums are loaded a tile ahead: the scale of this lane's row, and
+        // where the output leaves by TMA a column's scale and bias by each thread, which the warps then share.
+        float xs = 1.0f, scale = 1.0f, bias = 0.0f;
+        auto look_tile = [&](int t) {
+            if (t >= total) return;
+            const Tile tile = tile_at(A, t);
+            const int row = first_row(tile) + lane, col = tile.n * A.tile_n + (int)threadIdx.x;
+            if (E.x_scale && row < E.M) xs = __uint_as_float(lin_ld1(E.x_scale, row, 0));
+            if (!A.tma_out || (int)threadIdx.x >= A.tile_n || col >= E.N) return;
+            if (E.w_scale) scale = __uint_as_float(lin_ld1(E.w_scale, col, 0));
+            if (E.bias) bias = __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16));
+        };
+        look_tile(first);
         for (int t = first; t < total; t += step, ++n_done) {
             const Tile tile = tile_at(A, t);
             const int acc = n_done & 1;
-            const int row0 = (tile.m * CG + (int)rank) * kRows + quarter * 32, col0 = tile.n * A.tile_n;
-            const float xs = E.x_scale && row0 + lane < E.M ? E.x_scale[row0 + lane] : 1.0f;
+            const int row0 = first_row(tile), col0 = tile.n * A.tile_n;
             const Two xs2 = two(xs, xs);
             const int chunks = row0 < E.M ? (min(A.tile_n, E.N - col0) + 31) / 32 : 0;
-            // the epilogue's operands of a chunk are loaded while the one before it is worked on
+            const float* const cols = T.cols[acc];
+            if (A.tma_out) {
+                T.cols[acc][threadIdx.x] = scale, T.cols[acc][kAccStride + threadIdx.x] = bias;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(T.cols_full) + 8 * acc);
+            }
+            look_tile(t + step);
+            if (A.tma_out && !all(wait(smem_addr(T.cols_full) + 8 * acc, (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT)))
+                break;
+            // the others' operands of a chunk are loaded while the one before it is worked on
             Ahead ahead;
-            const Spot spot = spot_of(E, row0, col0, lane);
+            Spot spot;
             const bool rows_full = row0 + 32 <= E.M;
             auto look = [&](int c) {
                 if (rows_full) look_ahead<true>(E, spot, c * 32, ahead);
                 else look_ahead<false>(E, spot, c * 32, ahead);
             };
-            float scale = 1.0f, bias = 0.0f;  // of this lane's column of the next chunk
-            auto look_column = [&](int c) {
-                const int col = col0 + c * 32 + lane;
-                if (col >= E.N) return;
-                if (E.w_scale) scale = __uint_as_float(lin_ld1(E.w_scale, col, 0));
-                if (E.bias) bias = __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16));
-            };
-            if (half < chunks) {
-                if (A.tma_out) look_column(half);
-                else if (E.wide) look(half);
+            if (!A.tma_out && E.wide) spot = spot_of(E, row0, col0, lane);
+            if (half < chunks && !A.tma_out) {
+                if (E.wide) look(half);
                 else look_ahead_elements(E, row0, col0 + half * 32 + lane, ahead);
             }
             if (!all(wait(acc_full + 8 * acc, (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT))) break;
@@ -521,15 +548,11 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
                 tmem_load(tmem + ((uint32_t)(quarter * 32) << 16) + acc * kAccStride + c * 32, v);
                 if (c + EPI / 4 >= chunks) release();
                 if (A.tma_out) {
-                    float* const cols = T.cols[warp];
-                    cols[lane] = scale, cols[32 + lane] = bias;
-                    __syncwarp();
-                    if (c + EPI / 4 < chunks) look_column(c + EPI / 4);
                     uint8_t* const buf = reinterpret_cast<uint8_t*>(turn);
                     const int col = col0 + c * 32;
-                    if (E.act == CB_ACT_NONE) finish_tma<CB_ACT_NONE>(A, E, cols, xs2, v, buf, next_buf, row0, col, lane);
-                    else if (E.act == CB_ACT_GELU) finish_tma<CB_ACT_GELU>(A, E, cols, xs2, v, buf, next_buf, row0, col, lane);
-                    else finish_tma<CB_ACT_SILU>(A, E, cols, xs2, v, buf, next_buf, row0, col, lane);
+                    if (E.act == CB_ACT_NONE) finish_tma<CB_ACT_NONE>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
+                    else if (E.act == CB_ACT_GELU) finish_tma<CB_ACT_GELU>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
+                    else finish_tma<CB_ACT_SILU>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
                     continue;
                 }
                 // a row per lane to rows of 32 columns: 16-byte pieces, swizzled against bank conflicts
@@ -632,15 +655,15 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
         };
         auto next_of = [&](Slab c) { return ++c.kb < A.k_blocks ? c : start(c.t + step); };
         const int quad_row = lane / 8, j = lane % 8;  // row of four, piece of the eight that every row has
-        // Copies pieces of the stage rows of the quads q, q + kLoadWarps, ... below `end`, rows of an operand from `from` on, the
+        // Copies pieces of the stage rows of the quads q, q + LOADERS, ... below `end`, rows of an operand from `from` on, the
         // stage's row 0 being its row `row0`. NINTH: the pieces behind the eighth, a lane for each row of eight quads.
         // No byte outside of the operand is read: copies end with it (`ends`: this slab may touch its ends), and pieces
         // that begin before it are read byte by byte.
         auto copy_quads = [&](auto ninth, int q, int end, const char* from, long long stride, int row0, int count, int kb,
                               bool ends, uint32_t dst) {
             constexpr bool NINTH = decltype(ninth)::value;
-            constexpr int S = NINTH ? 8 * kLoadWarps : kLoadWarps;
-            int r = 4 * (NINTH ? q + lane / 4 * kLoadWarps : q) + (NINTH ? lane % 4 : quad_row);
+            constexpr int S = NINTH ? 8 * LOADERS : LOADERS;
+            int r = 4 * (NINTH ? q + lane / 4 * LOADERS : q) + (NINTH ? lane % 4 : quad_row);
             const int piece = NINTH ? 8 : j;
             const char* at = from + (row0 + r) * stride + kb * kSlab + 16 * piece;
             dst += 16 * piece;
@@ -669,7 +692,7 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
             }
         };
         const int x_quads = kRows / 4, quads = rows / 4;
-        const int w_first = x_quads + (lw + kLoadWarps - x_quads % kLoadWarps) % kLoadWarps;  // this warp's first quad of w
+        const int w_first = x_quads + (lw + LOADERS - x_quads % LOADERS) % LOADERS;  // this warp's first quad of w
         auto copy = [&](const Slab& c, int slot) {
             const uint32_t dst = raw_at + slot * raw_bytes;
             const bool ends = (c.kb == 0 || c.kb + 2 >= A.k_blocks) &&
@@ -688,7 +711,7 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
             raw += (4 * q + quad_row) * kRawRow + 16 * j;
             stage += (4 * q + quad_row) * kSlab;
 #pragma unroll 2
-            for (; q < end; q += kLoadWarps) {
+            for (; q < end; q += LOADERS) {
                 uint32_t w[8];
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(raw));
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+16];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(raw));
@@ -696,9 +719,9 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
                 asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (j ^ ((4 * q + quad_row) & 7)) * 16), "r"(v.x),
                              "r"(v.y), "r"(v.z), "r"(v.w)
                              : "memory");
-                off += 4 * kLoadWarps * stride;
-                raw += 4 * kLoadWarps * kRawRow;
-                stage += 4 * kLoadWarps * kSlab;
+                off += 4 * LOADERS * stride;
+                raw += 4 * LOADERS * kRawRow;
+                stage += 4 * LOADERS * kSlab;
             }
         };
         Place at;
@@ -743,10 +766,11 @@ __global__ void __launch_bounds__(linear_threads(SHIFT), 1)
 }
 
 using Kernel = void (*)(LinearArgs);
-Kernel kernel_of(int cg, bool fp8, bool shift) {
-    if (shift) return fp8 ? linear_kernel<1, true, true> : linear_kernel<1, false, true>;
-    if (cg == 2) return fp8 ? linear_kernel<2, true, false> : linear_kernel<2, false, false>;
-    return fp8 ? linear_kernel<1, true, false> : linear_kernel<1, false, false>;
+Kernel kernel_of(int cg, bool fp8, int loaders) {
+    if (loaders == kManyLoaders) return fp8 ? linear_kernel<1, true, kManyLoaders> : linear_kernel<1, false, kManyLoaders>;
+    if (loaders) return fp8 ? linear_kernel<1, true, kFewLoaders> : linear_kernel<1, false, kFewLoaders>;
+    if (cg == 2) return fp8 ? linear_kernel<2, true, 0> : linear_kernel<2, false, 0>;
+    return fp8 ? linear_kernel<1, true, 0> : linear_kernel<1, false, 0>;
 }
 
 }  // namespace
@@ -754,12 +778,12 @@ Kernel kernel_of(int cg, bool fp8, bool shift) {
 size_t linear_stage_bytes(int cg, int tile_n) { return (size_t)(kRows + tile_n / cg) * kSlab; }
 
 size_t linear_fixed_bytes(bool shift, int tile_n) {
-    return 1024 + sizeof(Tail) + (shift ? (size_t)kRawSlabs * kRawRow * (kRows + tile_n) : 0);
+    return sizeof(Tail) + (shift ? (size_t)kRawSlabs * kRawRow * (kRows + tile_n) : 0);
 }
 
 cudaError_t prepare_linear(size_t smem, int* pairs) {
     for (int fp8 = 0; fp8 < 2; ++fp8)
-        for (Kernel k : {kernel_of(2, fp8, false), kernel_of(1, fp8, false), kernel_of(1, fp8, true)}) {
+        for (Kernel k : {kernel_of(2, fp8, 0), kernel_of(1, fp8, 0), kernel_of(1, fp8, kFewLoaders), kernel_of(1, fp8, kManyLoaders)}) {
             const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e != cudaSuccess) return e;
         }
@@ -769,15 +793,16 @@ cudaError_t prepare_linear(size_t smem, int* pairs) {
     at.val.clusterDim.x = 2, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(2);
-    c.blockDim = dim3(linear_threads(false));
+    c.blockDim = dim3(linear_threads(0));
     c.dynamicSmemBytes = smem;
     c.attrs = &at;
     c.numAttrs = 1;
-    return cudaOccupancyMaxActiveClusters(pairs, reinterpret_cast<const void*>(kernel_of(2, false, false)), &c);
+    return cudaOccupancyMaxActiveClusters(pairs, reinterpret_cast<const void*>(kernel_of(2, false, 0)), &c);
 }
 
 cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s) {
     const bool shift = a.grid_bytes < 16;
+    const int loaders = !shift ? 0 : a.k_blocks >= kManyFrom ? kManyLoaders : kFewLoaders;
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = a.overlap;
@@ -785,13 +810,13 @@ cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaS
     at[1].val.clusterDim.x = (unsigned)cg, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)grid);
-    c.blockDim = dim3(linear_threads(shift));
+    c.blockDim = dim3(linear_threads(loaders));
     c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + linear_fixed_bytes(shift, a.tile_n);
     c.stream = s;
     c.attrs = at;
     c.numAttrs = cg == 2 ? 2 : 1;
     void* args[] = {const_cast<void*>(static_cast<const void*>(&a))};
-    const cudaError_t e = cudaLaunchKernelExC(&c, reinterpret_cast<const void*>(kernel_of(cg, fp8, shift)), args);
+    const cudaError_t e = cudaLaunchKernelExC(&c, reinterpret_cast<const void*>(kernel_of(cg, fp8, loaders)), args);
     if (e != cudaSuccess) (void)cudaGetLastError();
     return e;
 }

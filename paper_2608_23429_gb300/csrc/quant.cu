@@ -564,7 +564,8 @@ __global__ void __launch_bounds__(kThreads) quant_write_kernel(const __grid_cons
             const long long e = tile_e + ((long long)part * kThreads + threadIdx.x) * N;  // and, of further parts, kThreads * N on
             const int m0 = A.first[it], m1 = m0 + (GROUPED ? A.nb[it] : 1);
             void* const x = GROUPED ? A.resid[it] : nullptr;
-            if (e - threadIdx.x * N + (long long)P * kThreads * N <= numel) {  // all of the CTA's vectors are whole
+            const long long warp_end = e + (32 - threadIdx.x % 32) * N + (long long)(P - 1) * kThreads * N;
+            if (warp_end <= numel) {  // all of the warp's vectors are whole
                 float acc[N];
                 long long gate[2] = {0, 0};
                 if (GROUPED && x) {
@@ -619,15 +620,15 @@ __global__ void __launch_bounds__(kThreads) quant_write_kernel(const __grid_cons
                     for (int k = 0; k < 8; ++k) v[k] = two(f[2 * k], f[2 * k + 1]);
                     quantise16(v, amax, ei, numel, scales, reinterpret_cast<unsigned char*>(A.m_out[m]));
                 }
-                if (!GROUPED || !x) continue;
-                for (int k = 0; k < left; ++k) {
-                    float a = value_at(x, ei + k, A.resid_bf16);
-                    for (int m = m0; m < m1; ++m) {
-                        const float f = value_at(reinterpret_cast<const void*>(A.m_off[m]), ei + k, A.src_bf16);
-                        a = fmaf(A.m_gate[m] ? value_at(A.m_gate[m], gate_index(A, it, ei + k), A.gate_bf16) : 1.0f, f, a);
+                if constexpr (GROUPED)
+                    for (int k = 0; x && k < left; ++k) {
+                        float a = value_at(x, ei + k, A.resid_bf16);
+                        for (int m = m0; m < m1; ++m) {
+                            const float f = value_at(reinterpret_cast<const void*>(A.m_off[m]), ei + k, A.src_bf16);
+                            a = fmaf(A.m_gate[m] ? value_at(A.m_gate[m], gate_index(A, it, ei + k), A.gate_bf16) : 1.0f, f, a);
+                        }
+                        put(x, ei + k, a, A.resid_bf16);
                     }
-                    put(x, ei + k, a, A.resid_bf16);
-                }
             }
         }
     }
