@@ -57,14 +57,18 @@ typedef struct {
  * one float a row (CB_E4M3 only). branch, gate (with a branch only), weight,
  * scale, shift and x_out may be NULL: no addition, factors 1, terms 0, h not
  * stored. x_out may be x itself (same stride). With eps > 0 a row of zeros gives
- * zeros (with shift: its values). A row that holds a value that is not finite gives NaN,
- * and no other row does.
+ * zeros (with shift: its values). A row that holds a NaN gives NaN; one that holds an
+ * infinity gives NaN in e4m3, otherwise NaN there and what zeros give elsewhere. No
+ * other row is touched by either.
  * Rows and hidden sizes on the 16-byte grid take vector loads, others elements.
  * Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size), CB_ERR_LIMIT
  * (rows or hidden beyond 2^31 - 1), CB_ERR_CUDA. */
 int cb_norm_residual(const cb_norm_desc* desc, const void* x, const void* branch, const void* gate,
                      const void* weight, const void* scale, const void* shift, void* x_out, void* out,
                      float* out_scale, void* stream);
+
+/* Largest in_features: a sum that long takes a fraction of a wait's limit (cb_linear_run). */
+#define CB_MAX_IN_FEATURES (1LL << 22)
 
 /* Activations of a matrix product's epilogue. */
 enum {
@@ -105,8 +109,9 @@ typedef struct {
 
 typedef struct cb_linear cb_linear; /* opaque, host-owned; holds no device memory */
 
-/* Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size), CB_ERR_LIMIT (features beyond
- * 2^31 - 1, or a row of w or x beyond 2^31 - 256 bytes). The layer keeps the pointers: its buffers must outlive it. */
+/* Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size), CB_ERR_LIMIT (out_features
+ * beyond 2^31 - 1024, in_features beyond CB_MAX_IN_FEATURES, or a row stride of w or x
+ * beyond 2^31 - 256 bytes). The layer keeps the pointers: its buffers must outlive it. */
 int cb_linear_create(const cb_linear_desc* desc, cb_linear** out);
 void cb_linear_destroy(cb_linear* layer);
 
@@ -114,7 +119,11 @@ void cb_linear_destroy(cb_linear* layer);
  *     v = act(x_scale[m] * w_scale[n] * sum_k x[m, k] w[n, k] + bias[n])
  *     out = round(v)                        the branch output, as cb_cache_push takes it
  *     resid_out = round(resid + gate * v)   the hidden state (gate: a line per sample)
- * with sums, epilogue and hidden state in fp32 and one rounding to each result.
+ * with sums, epilogue and hidden state in fp32 and one rounding to each result. The
+ * tensor cores cut sums off rather than round them: where a result is fp32 they sum
+ * parts of 512 features (e4m3: 8192), which are added rounded to nearest, so that a
+ * result is off by 5e-7 of the sums' size whatever in_features is (bf16 results: by up
+ * to 1.2e-9 in_features of it before they are rounded).
  * x_scale: one float a row (CB_E4M3 only, NULL: 1). out may be NULL, resid and resid_out
  * may be NULL together, gate (with resid only) may be NULL: 1; one result at least
  * is wanted. resid_out may be resid itself (same stride). The order of a sum depends
@@ -124,7 +133,8 @@ void cb_linear_destroy(cb_linear* layer);
  * Every wait of the kernels on one of their barriers has a limit of a second; one that
  * runs out is noted in the status word of cb_linear_device_status and makes the
  * kernel return early, with incomplete results.
- * Errors: CB_ERR_ARG, CB_ERR_ALIGN, CB_ERR_LIMIT (rows beyond 2^31 - 1024), CB_ERR_CUDA. */
+ * Errors: CB_ERR_ARG, CB_ERR_ALIGN, CB_ERR_LIMIT (rows beyond 2^31 - 1024, or over 2^28
+ * tiles of 128 rows and 32 to 256 columns), CB_ERR_CUDA. */
 int cb_linear_run(const cb_linear* layer, const cb_linear_io* io, const void* x, const float* x_scale,
                   const void* resid, const void* gate, void* out, void* resid_out, void* stream);
 

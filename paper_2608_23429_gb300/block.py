@@ -7,9 +7,18 @@ from __future__ import annotations
 
 import ctypes
 
-from .chebboost import CB_BF16, _addr, _check, _lib, _stream
+from .chebboost import CB_BF16, CbError, _lib, _stream
 
 _P, _I, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+
+
+def _addr(x):
+    """Address of a buffer (tensor, int or None). These calls take a few microseconds in all, so this is kept short."""
+    return x if x is None or x.__class__ is int else x.data_ptr()
+
+
+def _raise(rc: int, call: str):
+    raise CbError(rc, call)
 
 
 class cb_norm_desc(ctypes.Structure):
@@ -33,6 +42,7 @@ class cb_linear_io(ctypes.Structure):
 
 
 CB_ACT_NONE, CB_ACT_GELU, CB_ACT_SILU = 0, 1, 2
+CB_MAX_IN_FEATURES = 1 << 22
 
 _sig = {
     "cb_norm_residual": ([_P] * 11, _I),
@@ -46,14 +56,16 @@ for _name, (_args, _res) in _sig.items():
     _f.argtypes, _f.restype = _args, _res
 
 EXPORTED = tuple(_sig)
+_norm_residual, _linear_run = _lib.cb_norm_residual, _lib.cb_linear_run
 
 
 def cb_norm_residual(desc: cb_norm_desc, x, branch=None, gate=None, weight=None, scale=None, shift=None, x_out=None,
                      out=None, out_scale=None, stream=None) -> None:
     """RMS norm of ``x + gate * branch`` into ``out`` (with ``out_scale`` where it is e4m3), the sum into ``x_out``."""
-    _check(_lib.cb_norm_residual(ctypes.addressof(desc), _addr(x), _addr(branch), _addr(gate), _addr(weight),
-                                 _addr(scale), _addr(shift), _addr(x_out), _addr(out), _addr(out_scale),
-                                 _stream(stream)), "cb_norm_residual")
+    rc = _norm_residual(ctypes.addressof(desc), _addr(x), _addr(branch), _addr(gate), _addr(weight), _addr(scale), _addr(shift),
+                        _addr(x_out), _addr(out), _addr(out_scale), None if stream is None else _stream(stream))
+    if rc < 0:
+        _raise(rc, "cb_norm_residual")
 
 
 def cb_linear_create(w, out_features: int, in_features: int, type: int, w_scale=None, bias=None,
@@ -62,7 +74,9 @@ def cb_linear_create(w, out_features: int, in_features: int, type: int, w_scale=
     d = cb_linear_desc(in_features, out_features, w_stride, type, bias_dtype, activation, 0, _addr(w), _addr(w_scale),
                        _addr(bias))
     layer = _P()
-    _check(_lib.cb_linear_create(ctypes.addressof(d), ctypes.byref(layer)), "cb_linear_create")
+    rc = _lib.cb_linear_create(ctypes.addressof(d), ctypes.byref(layer))
+    if rc < 0:
+        _raise(rc, "cb_linear_create")
     return layer
 
 
@@ -73,11 +87,15 @@ def cb_linear_destroy(layer) -> None:
 def cb_linear_run(layer, io: cb_linear_io, x, x_scale=None, resid=None, gate=None, out=None, resid_out=None,
                   stream=None) -> None:
     """``act(x w^T + bias)`` into ``out`` and/or, gated and added to ``resid``, into ``resid_out``."""
-    _check(_lib.cb_linear_run(layer, ctypes.addressof(io), _addr(x), _addr(x_scale), _addr(resid), _addr(gate), _addr(out),
-                              _addr(resid_out), _stream(stream)), "cb_linear_run")
+    rc = _linear_run(layer, ctypes.addressof(io), _addr(x), _addr(x_scale), _addr(resid), _addr(gate), _addr(out),
+                     _addr(resid_out), None if stream is None else _stream(stream))
+    if rc < 0:
+        _raise(rc, "cb_linear_run")
 
 
 def cb_linear_device_status(stream=None) -> int:
     st = ctypes.c_int(0)
-    _check(_lib.cb_linear_device_status(ctypes.addressof(st), _stream(stream)), "cb_linear_device_status")
+    rc = _lib.cb_linear_device_status(ctypes.addressof(st), _stream(stream))
+    if rc < 0:
+        _raise(rc, "cb_linear_device_status")
     return st.value

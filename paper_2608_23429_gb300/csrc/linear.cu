@@ -68,12 +68,16 @@ int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes
 // 6912 x 1152 13.2 -> 20.8, 1152 x 4608 18.6 -> 18.4, 12288 x 3072 20.3 -> 55.
 constexpr int kFewRows = 32;
 
+// Slabs of 128 bytes of a pass over K, with fp32 results: an error of 5e-7 of a sum (measured: linear_tc.cuh; e4m3's products
+// lose less, 7e-7 at K = 16384).
+constexpr int kPassBf16 = 8, kPassE4m3 = 64;
+
 // CTAs per tile and the tile's columns: the fewest rounds of tiles, each as long as its loads (16 KB of x and
 // 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take.
-void choose_tile(const Device& dev, int M, int N, bool tma, int* cg, int* tile_n) {
+void choose_tile(const Device& dev, int M, int N, bool tma, int most, int* cg, int* tile_n) {
     double best = 1e300;
     for (int g = tma ? 2 : 1; g >= 1; --g)
-        for (int n = tma ? 256 : 128; n >= 32; n -= 32) {
+        for (int n = most; n >= 32; n -= 32) {
             if (n > 32 && n - 32 >= N) continue;
             const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n);
             const long long units = g == 2 ? dev.pairs : dev.sms;
@@ -102,7 +106,7 @@ int cb_linear_create(const cb_linear_desc* d, cb_linear** out) {
     if (d->w_scale && d->type != CB_E4M3) return CB_ERR_ARG;
     if (d->w_stride != 0 && d->w_stride < d->in_features) return CB_ERR_ARG;
     const long long row = 0x7FFFFF00LL / (long long)bytes_of(d->type);
-    if (d->out_features > 0x7FFFFC00LL || d->in_features > row || d->w_stride > row) return CB_ERR_LIMIT;
+    if (d->out_features > 0x7FFFFC00LL || d->in_features > CB_MAX_IN_FEATURES || d->w_stride > row) return CB_ERR_LIMIT;
     if (!on_grid(d->w, bytes_of(d->type)) || !on_grid(d->w_scale, 4)) return CB_ERR_ALIGN;
     if (d->bias && !on_grid(d->bias, bytes_of(d->bias_dtype))) return CB_ERR_ALIGN;
     cb_linear* l = new (std::nothrow) cb_linear;
@@ -178,10 +182,14 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
         return e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
     }
     int cg = 1;
-    choose_tile(*dev, ep.M, ep.N, tma, &cg, &a.tile_n);
+    a.k_blocks = (a.k_bytes + 127) / 128;
+    // fp32 results: passes over K (see linear_tc.cuh)
+    const bool fp32 = (out && !ep.out_bf16) || (resid_out && !ep.resid_bf16);
+    a.pass_blocks = fp32 ? (d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks;
+    a.passes = (a.k_blocks + a.pass_blocks - 1) / a.pass_blocks;
+    choose_tile(*dev, ep.M, ep.N, tma, a.passes > 1 || !tma ? 128 : 256, &cg, &a.tile_n);
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
-    a.k_blocks = (a.k_bytes + 127) / 128;
     a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(!tma, a.tile_n)) / linear_stage_bytes(cg, a.tile_n));
     if (tma) {
         rc = operand_map(&a.x_map, x, ep.M, a.k_bytes, a.x_row, 128);

@@ -33,6 +33,7 @@ struct LinearArgs {
     int k_bytes;           // bytes of a row of x and of w
     int tiles_m, tiles_n, k_blocks, stages;
     int tile_n;            // output columns of a tile
+    int passes, pass_blocks;  // parts of K that are summed by themselves, and their slabs
     int grid_bytes;        // grid on which all rows of x and of w start, up to 16 bytes
     long long x_row, w_row;  // bytes from row to row
     const void *x, *w;
@@ -50,12 +51,13 @@ struct LinearFewArgs {
 // `shift`: rows off the 16-byte grid.
 cudaError_t launch_linear_few(const LinearFewArgs& a, bool fp8, bool shift, int sms, cudaStream_t s);
 
-// The tensor-core kernels (linear_tc.cu): cg CTAs per tile of 128 cg rows; a.grid_bytes below 16: cg = 1
+// The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows; a.grid_bytes below 16: cg = 1
 // only. prepare_linear raises the kernels' shared-memory limit and tells how many pairs of CTAs run at once.
 size_t linear_stage_bytes(int cg, int tile_n);
 size_t linear_fixed_bytes(bool shift, int tile_n);  // shared memory besides the stages
 constexpr int kMaxLinStages = 12;
 cudaError_t prepare_linear(size_t smem, int* pairs);
+void (*linear_passes_kernel(int cg, bool fp8, int loaders))(LinearArgs);  // linear_tc_passes.cu
 cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s);
 
 #ifdef __CUDACC__

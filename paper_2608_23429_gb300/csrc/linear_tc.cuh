@@ -1,0 +1,839 @@
+// Internal: the matrix product of cb_linear_run on the fifth-generation tensor cores (linear_tc.cu, linear_tc_passes.cu).
+//
+// A persistent grid of CTAs (CG = 1) or of pairs of CTAs on two SMs (CG = 2) works through output tiles of 128 CG
+// rows by tile_n columns. In a CTA
+//   one warp (TMA) or several (else) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
+//     tile_n / CG rows of w, in the 128-byte swizzle that the tensor cores read,
+//   one thread issues tcgen05.mma on them, sums in TMEM (two accumulators of up to 256 columns each),
+//   eight warps (or four) take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
+//     that their accesses to global memory are rows, and apply the epilogue.
+// A pair of CTAs shares one tile: each loads its 128 rows of x and half of the tile's rows of w, the first one's
+// thread issues for both, and each holds the sums of its own rows.
+//
+// Operands whose rows do not start on 16-byte boundaries cannot come by TMA (SHIFT). Seven or eleven warps copy the aligned
+// 16-byte pieces that a slab's rows touch into a ring of their own, two slabs ahead, and then move each row, shifted by
+// its offset, to where TMA would have put it. A warp moves the rows that it has copied, four at a time, so the warps
+// need no barrier among them.
+//
+// The tensor cores cut off what a sum loses where it is added to, which adds up over K: 1.1e-9 K of a result (bf16; 1.9e-5 at
+// K = 16384, 2.1e-6 at 2048). Results in fp32 are therefore summed in passes over parts of K, whose sums the epilogue's warps
+// add, rounded to nearest, into a third part of TMEM while the next pass is under way (A.passes > 1, tiles of up to 128
+// columns).
+//
+// Every wait has a limit (kLimitNs); one that runs out sets the CTA's abort flag, so that all its roles leave, after
+// the copies under way have landed, and frees the TMEM.
+#pragma once
+
+#include <type_traits>
+
+#include "cb_async.cuh"
+#include "linear.cuh"
+#include "linear_shift.cuh"
+
+namespace cbk {
+namespace {
+
+constexpr int kRows = 128;        // rows of x per CTA
+constexpr int kSlab = 128;        // bytes of K per stage
+constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the other (half of it where there are passes)
+constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes
+// Warps that move operands off the 16-byte grid (0: TMA), of the 16 warps that 128 registers a thread allow. Long sums are
+// bound by them and take 11, with four warps for the epilogue; short ones by the epilogue and take 7 and eight
+// (999 x 577 x 1155 31.4 -> 28.7 us; 4096 x 4096 x 4097 867 -> 1004 us).
+constexpr int kFewLoaders = 7, kManyLoaders = 11, kManyFrom = 24;  // slabs
+__host__ __device__ constexpr int epi_warps(int loaders) { return loaders == kManyLoaders ? 4 : kEpiWarps; }
+__host__ __device__ constexpr int linear_threads(int loaders) { return 32 * (epi_warps(loaders) + 1 + (loaders ? loaders : 1)); }
+constexpr int kRawRow = 144;      // bytes of a row's pieces
+constexpr int kRawSlabs = 3;      // slabs of pieces held
+constexpr unsigned long long kLimitNs = 1000000000ull;
+
+struct alignas(16) Tail {  // behind the stages
+    float turn[kEpiWarps][32 * 32];
+    float cols[2][2 * kAccStride];  // scales and biases of a tile's columns (where the output leaves by TMA)
+    uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2], cols_full[2];
+    uint32_t tmem;
+    int abort;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// Address of `bar` in the pair's first CTA.
+__device__ __forceinline__ uint32_t in_first(uint32_t bar) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+    return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+    // relaxed: what it orders are reads of TMEM (tcgen05.wait and fence); a release would wait for the warp's stores
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
+// Wait for a phase of a barrier, until the limit or the CTA's abort flag.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort, int* status, int code) {
+    unsigned long long t0 = 0;
+    while (true) {
+        for (int i = 0; i < 64; ++i)
+            if (CLUSTER ? try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
+        if (*abort) return false;
+        const unsigned long long t = now_ns();
+        if (t0 == 0) t0 = t;
+        if (t - t0 > kLimitNs) {
+            *abort = 1;
+            record(status, code);
+            return false;
+        }
+    }
+}
+
+__device__ __forceinline__ bool all(bool ok) { return __all_sync(0xFFFFFFFFu, ok) != 0; }
+
+template <int CG>
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else  // the barrier may be the other CTA's
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, "
+            "%3}], [%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+
+// Operand in shared memory: rows of 128 bytes, K innermost, 128-byte swizzle in groups of eight rows (1024 bytes).
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+template <int CG, bool FP8>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    const uint32_t on = add;
+#define CB_MMA(GROUP, KIND)                                                                         \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"                                   \
+                 "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, p;\n\t}" ::"r"(d), \
+                 "l"(a), "l"(b), "r"(idesc), "r"(on)                                                \
+                 : "memory")
+    if constexpr (CG == 1) {
+        if constexpr (FP8) CB_MMA("1", "f8f6f4");
+        else CB_MMA("1", "f16");
+    } else {
+        if constexpr (FP8) CB_MMA("2", "f8f6f4");
+        else CB_MMA("2", "f16");
+    }
+#undef CB_MMA
+}
+
+// Arrives on `bar` (of both CTAs of a pair) when all products issued so far are done.
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+            "h"((uint16_t)3)
+            : "memory");
+}
+
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+
+// Stores 32 columns of the warp's 32 rows.
+__device__ __forceinline__ void tmem_store(uint32_t addr, const float* v) {
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+        "r"(addr)
+        : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// 32 columns of the warp's 32 rows, a row per lane.
+__device__ __forceinline__ void tmem_load(uint32_t addr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// True in one lane of the warp. The roles' loops are run by whole warps, so that what they compute stays in
+// uniform registers (which the tensor cores' and copies' instructions take), and one lane issues.
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
+// v += what stands at addr, by halves.
+__device__ __forceinline__ void tmem_add(uint32_t addr, float* v) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t r[16];
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+              "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+            : "r"(addr + 16 * h));
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[16 * h + i] += __uint_as_float(r[i]);
+    }
+}
+
+struct Tile {
+    int m, n;
+};
+// Groups of eight rows of tiles, so that tiles worked on together share operands in L2.
+__device__ __forceinline__ Tile tile_at(const LinearArgs& A, int t) {
+    const int group = 8 * A.tiles_n, g = t / group, r = t - g * group;
+    const int rows = min(8, A.tiles_m - 8 * g);
+    return Tile{8 * g + r % rows, r / rows};
+}
+
+// A place in the ring of stages, and the parity of its present use.
+struct Place {
+    int s = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++s == stages) s = 0, phase ^= 1;
+    }
+};
+
+// Waits until the stages' last fills have been read: no copy and no arrival is under way then. `p`: the place behind
+// them, `fills`: how many there were.
+__device__ __forceinline__ bool drain(Place p, int fills, int stages, uint32_t empty, volatile int* abort, int* status) {
+    for (int i = 0; i < min(fills, stages); ++i) {
+        p.s = p.s == 0 ? (p.phase ^= 1, stages - 1) : p.s - 1;
+        if (!wait(empty + 8 * p.s, p.phase, abort, status, CB_DEV_DRAIN_TIMEOUT)) return false;
+    }
+    return true;
+}
+
+// ---- epilogue of 32 rows by 32 columns of a warp. Wide: a thread has the rows row0 + lane / 8 + 4 i and four columns.
+
+struct Ahead {
+    uint4 scale, bias, gate, resid[8];
+};
+
+// A thread's part of a tile: where its first row and column lie, and the bytes to the row after next but two.
+struct Spot {
+    int row, col;            // of its first element in the tile's first chunk
+    long long gate;          // element of the gate of the warp's first row's sample
+    unsigned next;           // rows from here on belong to other samples
+    const char* resid;
+    char *out, *resid_out;
+    long long resid_step, out_step, resid_out_step;
+};
+
+__device__ __forceinline__ Spot spot_of(const LinearEpilogue& E, int row0, int col0, int lane) {
+    Spot p;
+    p.row = row0 + lane / 8, p.col = col0 + lane % 8 * 4;
+    const int os = E.out_bf16 ? 2 : 4, rs = E.resid_bf16 ? 2 : 4;
+    p.out = reinterpret_cast<char*>(E.out) + (p.row * E.out_stride + p.col) * os;
+    p.resid = reinterpret_cast<const char*>(E.resid) + (p.row * E.resid_stride + p.col) * rs;
+    p.resid_out = reinterpret_cast<char*>(E.resid_out) + (p.row * E.resid_out_stride + p.col) * rs;
+    p.out_step = 4 * E.out_stride * os, p.resid_step = 4 * E.resid_stride * rs, p.resid_out_step = 4 * E.resid_out_stride * rs;
+    const unsigned sample = E.gate ? (unsigned)row0 / E.tokens : 0;
+    p.gate = sample * E.gate_stride + p.col;
+    p.next = (sample + 1) * E.tokens;
+    return p;
+}
+
+// The operands of the chunk that starts `at` columns into the tile. FULL: all 32 rows exist.
+template <bool FULL>
+__device__ __forceinline__ void look_ahead(const LinearEpilogue& E, const Spot& p, int at, Ahead& a) {
+    const int col = p.col + at;
+    if (col >= E.N) return;  // N is a multiple of four
+    if (E.w_scale) a.scale = lin_raw4(E.w_scale, col, 0);
+    if (E.bias) a.bias = lin_raw4(E.bias, col, E.bias_bf16);
+    if (!E.resid_out) return;
+    if (E.gate) a.gate = lin_raw4(E.gate, p.gate + at, E.gate_bf16);
+    if (E.resid_bf16) {
+        const char* q = p.resid + 2 * at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += p.resid_step)
+            if (FULL || p.row + 4 * i < E.M) {
+                const uint2 v = lin_ld8(q);
+                a.resid[i].x = v.x, a.resid[i].y = v.y;
+            }
+    } else {
+        const char* q = p.resid + 4 * at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += p.resid_step)
+            if (FULL || p.row + 4 * i < E.M) a.resid[i] = lin_ld16(q);
+    }
+}
+
+// Eight rows of four columns from q on, `step` bytes apart.
+template <bool FULL>
+__device__ __forceinline__ void put_rows(char* q, long long step, int bf16, int rows, const ulonglong2* v) {
+    if (bf16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += step) {
+            const float2 lo = both(v[i].x), hi = both(v[i].y);
+            if (FULL || 4 * i < rows) *reinterpret_cast<uint2*>(q) = make_uint2(bf16x2(lo.x, lo.y), bf16x2(hi.x, hi.y));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i, q += step)
+            if (FULL || 4 * i < rows) *reinterpret_cast<ulonglong2*>(q) = v[i];
+    }
+}
+
+template <int ACT>
+__device__ __forceinline__ void activate(const float4& s, const float4& b, ulonglong2* v) {
+    const Two s0 = two(s.x, s.y), s1 = two(s.z, s.w), b0 = two(b.x, b.y), b1 = two(b.z, b.w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i].x = fma2(v[i].x, s0, b0);
+        v[i].y = fma2(v[i].y, s1, b1);
+        lin_act4<ACT>(v[i].x, v[i].y);
+    }
+}
+
+template <bool FULL>
+__device__ __forceinline__ void finish(const LinearEpilogue& E, const Spot& p, int at, const Ahead& a, ulonglong2* v) {
+    const int col = p.col + at, rows = E.M - p.row;
+    if (col >= E.N) return;
+    const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+    const float4 s = E.w_scale ? lin_val4(a.scale, 0) : one;
+    const float4 b = E.bias ? lin_val4(a.bias, E.bias_bf16) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (E.act == CB_ACT_NONE) activate<CB_ACT_NONE>(s, b, v);
+    else if (E.act == CB_ACT_GELU) activate<CB_ACT_GELU>(s, b, v);
+    else activate<CB_ACT_SILU>(s, b, v);
+    if (E.out) put_rows<FULL>(p.out + at * (E.out_bf16 ? 2 : 4), p.out_step, E.out_bf16, rows, v);
+    if (!E.resid_out) return;
+    float4 g = E.gate ? lin_val4(a.gate, E.gate_bf16) : one;
+    const bool mixed = E.gate && (unsigned)(p.row - p.row % 4 + 31) >= p.next;  // the warp's rows are of several samples
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned row = (unsigned)(p.row + 4 * i);
+        if (mixed && row >= p.next && (FULL || row < (unsigned)E.M))
+            g = lin_val4(lin_raw4(E.gate, (long long)(row / E.tokens) * E.gate_stride + col, E.gate_bf16), E.gate_bf16);
+        const float4 r = lin_val4(a.resid[i], E.resid_bf16);
+        v[i].x = fma2(two(g.x, g.y), v[i].x, two(r.x, r.y));
+        v[i].y = fma2(two(g.z, g.w), v[i].y, two(r.z, r.w));
+    }
+    put_rows<FULL>(p.resid_out + at * (E.resid_bf16 ? 2 : 4), p.resid_out_step, E.resid_bf16, rows, v);
+}
+
+// Output by TMA, where there is nothing to add it to: a row per lane, as the sums come from TMEM. Columns' operands are
+// read from shared memory by all lanes alike, and 32 rows of 64 bytes leave at a time, through two buffers in turn.
+template <int ACT>
+__device__ __forceinline__ void finish_tma(const LinearArgs& A, const LinearEpilogue& E, const float* cols, Two xs2, float* v,
+                                           uint8_t* buf, int& next, int row0, int col0, int lane) {
+    Two x[16];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(cols + 4 * j);
+        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(cols + kAccStride + 4 * j);
+        Two p = two(v[4 * j], v[4 * j + 1]), q = two(v[4 * j + 2], v[4 * j + 3]);
+        if (E.x_scale) p = mul2(p, xs2), q = mul2(q, xs2);
+        x[2 * j] = fma2(p, s.x, b.x);
+        x[2 * j + 1] = fma2(q, s.y, b.y);
+        lin_act4<ACT>(x[2 * j], x[2 * j + 1]);
+    }
+    const int turns = E.out_bf16 ? 1 : 2;
+    for (int h = 0; h < turns; ++h) {
+        // the store before the last has left this buffer
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+        uint8_t* const to = buf + 2048 * next + lane * 64;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint4 piece;
+            if (E.out_bf16) {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 f = both(x[4 * j + k]);
+                    w[k] = bf16x2(f.x, f.y);
+                }
+                piece = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                const ulonglong2 f = h == 0 ? make_ulonglong2(x[2 * j], x[2 * j + 1]) : make_ulonglong2(x[2 * j + 8], x[2 * j + 9]);
+                piece = *reinterpret_cast<const uint4*>(&f);
+            }
+            *reinterpret_cast<uint4*>(to + (j ^ (lane / 2 % 4)) * 16) = piece;
+        }
+        fence_generic_to_async();
+        __syncwarp();
+        const int at = col0 + 16 * h;
+        if (at < E.N && lane == 0)
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&A.out_map),
+                         "r"(at * (E.out_bf16 ? 2 : 4)), "r"(row0), "r"(smem_addr(buf) + 2048 * next)
+                         : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        next ^= 1;
+    }
+}
+
+// The same by elements, a column per lane, for rows that are not made of aligned fours.
+
+__device__ __forceinline__ void look_ahead_elements(const LinearEpilogue& E, int row0, int col, Ahead& a) {
+    if (col >= E.N) return;
+    a.scale.x = E.w_scale ? lin_ld1(E.w_scale, col, 0) : __float_as_uint(1.0f);
+    a.bias.x = E.bias ? lin_ld1(E.bias, col, E.bias_bf16) : 0;
+    if (!E.resid_out) return;
+    a.gate.x = __float_as_uint(1.0f);
+    if (E.gate) a.gate.x = lin_ld1(E.gate, ((unsigned)row0 / E.tokens) * E.gate_stride + col, E.gate_bf16);
+    const int rows = E.M - row0, step = E.resid_bf16 ? 2 : 4;
+    const char* q = reinterpret_cast<const char*>(E.resid) + (row0 * E.resid_stride + col) * step;
+#pragma unroll
+    for (int i = 0; i < 32; ++i, q += E.resid_stride * step)
+        if (i < rows) {
+            uint32_t& w = i % 4 == 0 ? a.resid[i / 4].x : i % 4 == 1 ? a.resid[i / 4].y : i % 4 == 2 ? a.resid[i / 4].z : a.resid[i / 4].w;
+            w = lin_ld1(q, 0, E.resid_bf16);
+        }
+}
+
+__device__ __forceinline__ void put_column(void* p, long long e, long long stride, int bf16, int rows, const float* v) {
+    if (bf16) {
+        __nv_bfloat16* q = reinterpret_cast<__nv_bfloat16*>(p) + e;
+#pragma unroll
+        for (int i = 0; i < 32; ++i, q += stride)
+            if (i < rows) *q = __float2bfloat16_rn(v[i]);
+    } else {
+        float* q = reinterpret_cast<float*>(p) + e;
+#pragma unroll
+        for (int i = 0; i < 32; ++i, q += stride)
+            if (i < rows) *q = v[i];
+    }
+}
+
+template <int ACT>
+__device__ __forceinline__ void activate_column(float s, float b, float* v) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+        Two x = fma2(two(v[i], v[i + 1]), two(s, s), two(b, b)), y = fma2(two(v[i + 2], v[i + 3]), two(s, s), two(b, b));
+        lin_act4<ACT>(x, y);
+        const float2 f = both(x), g = both(y);
+        v[i] = f.x, v[i + 1] = f.y, v[i + 2] = g.x, v[i + 3] = g.y;
+    }
+}
+
+__device__ __forceinline__ void finish_elements(const LinearEpilogue& E, int row0, int col, int lane, const Ahead& a,
+                                                const float* turn) {
+    if (col >= E.N) return;
+    const int rows = E.M - row0;
+    float v[32];
+#pragma unroll
+    for (int r = 0; r < 32; ++r) v[r] = turn[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + lane % 4];
+    const float scale = __uint_as_float(a.scale.x), bias = __uint_as_float(a.bias.x);
+    if (E.act == CB_ACT_NONE) activate_column<CB_ACT_NONE>(scale, bias, v);
+    else if (E.act == CB_ACT_GELU) activate_column<CB_ACT_GELU>(scale, bias, v);
+    else activate_column<CB_ACT_SILU>(scale, bias, v);
+    if (E.out) put_column(E.out, row0 * E.out_stride + col, E.out_stride, E.out_bf16, rows, v);
+    if (!E.resid_out) return;
+    const unsigned next = ((unsigned)row0 / E.tokens + 1) * E.tokens;  // rows from here on belong to other samples
+    float g = __uint_as_float(a.gate.x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const unsigned row = (unsigned)(row0 + i);
+        if (E.gate && row >= next && i < rows)
+            g = __uint_as_float(lin_ld1(E.gate, (long long)(row / E.tokens) * E.gate_stride + col, E.gate_bf16));
+        const uint4& x = a.resid[i / 4];
+        v[i] = fmaf(g, v[i], __uint_as_float(i % 4 == 0 ? x.x : i % 4 == 1 ? x.y : i % 4 == 2 ? x.z : x.w));
+    }
+    put_column(E.resid_out, row0 * E.resid_out_stride + col, E.resid_out_stride, E.resid_bf16, rows, v);
+}
+
+template <int CG, bool FP8, int LOADERS, bool PASSES>
+__global__ void __launch_bounds__(linear_threads(LOADERS), 1)
+    linear_kernel(const __grid_constant__ LinearArgs A) {
+    constexpr bool SHIFT = LOADERS != 0;
+    static_assert(CG == 1 || !SHIFT, "pairs of CTAs load by TMA");
+    constexpr int EPI = epi_warps(LOADERS);
+    extern __shared__ __align__(1024) uint8_t base[];
+    if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
+        after_previous();
+        if (threadIdx.x == 0) record(A.status, CB_DEV_PRODUCER_TIMEOUT);
+        return;
+    }
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int w_rows = A.tile_n / CG, stage_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
+    Tail& T = *reinterpret_cast<Tail*>(base + stages * stage_bytes);
+    const uint32_t ring = smem_addr(base);
+    const uint32_t full = smem_addr(T.full), empty = smem_addr(T.empty);
+    const uint32_t acc_full = smem_addr(T.acc_full), acc_empty = smem_addr(T.acc_empty);
+    volatile int* const abort = &T.abort;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < stages; ++s) {
+            mbar_init(full + 8 * s, SHIFT ? LOADERS : 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(acc_full + 8 * i, 1);
+            mbar_init(acc_empty + 8 * i, EPI * CG);
+            mbar_init(smem_addr(T.cols_full) + 8 * i, EPI);
+        }
+        *abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_generic_to_async();
+    }
+    if (warp == EPI) {
+        const uint32_t at = smem_addr(&T.tmem);
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(at) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(at) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
+    fence_before();
+    __syncwarp();
+    if constexpr (CG == 2) cluster_sync();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = T.tmem;
+    after_previous();
+
+    const int first = blockIdx.x / CG, step = gridDim.x / CG, total = A.tiles_m * A.tiles_n;
+    if (warp < EPI) {  // ---- epilogue
+        const LinearEpilogue E = A.e;
+        float* const turn = T.turn[warp];
+        const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
+        int n_done = 0, pass = 0, next_buf = 0;  // tiles, and accumulators, taken
+        auto first_row = [&](const Tile& tile) { return (tile.m * CG + (int)rank) * kRows + quarter * 32; };
+        // The operands of a tile that do not depend on its sums are loaded a tile ahead: the scale of this lane's row, and
+        // where the output leaves by TMA a column's scale and bias by each thread, which the warps then share.
+        float xs = 1.0f, scale = 1.0f, bias = 0.0f;
+        auto look_tile = [&](int t) {
+            if (t >= total) return;
+            const Tile tile = tile_at(A, t);
+            const int row = first_row(tile) + lane, col = tile.n * A.tile_n + (int)threadIdx.x;
+            if (E.x_scale && row < E.M) xs = __uint_as_float(lin_ld1(E.x_scale, row, 0));
+            if (!A.tma_out || (int)threadIdx.x >= A.tile_n || col >= E.N) return;
+            if (E.w_scale) scale = __uint_as_float(lin_ld1(E.w_scale, col, 0));
+            if (E.bias) bias = __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16));
+        };
+        look_tile(first);
+        for (int t = first; t < total; t += step, ++n_done) {
+            const Tile tile = tile_at(A, t);
+            const int row0 = first_row(tile), col0 = tile.n * A.tile_n;
+            const Two xs2 = two(xs, xs);
+            const int chunks = row0 < E.M ? (min(A.tile_n, E.N - col0) + 31) / 32 : 0;
+            const float* const cols = T.cols[n_done & 1];
+            if (A.tma_out) {
+                T.cols[n_done & 1][threadIdx.x] = scale, T.cols[n_done & 1][kAccStride + threadIdx.x] = bias;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(T.cols_full) + 8 * (n_done & 1));
+            }
+            look_tile(t + step);
+            if (A.tma_out && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT)))
+                break;
+            // the others' operands of a chunk are loaded while the one before it is worked on
+            Ahead ahead;
+            Spot spot;
+            const bool rows_full = row0 + 32 <= E.M;
+            auto look = [&](int c) {
+                if (rows_full) look_ahead<true>(E, spot, c * 32, ahead);
+                else look_ahead<false>(E, spot, c * 32, ahead);
+            };
+            if (!A.tma_out && E.wide) spot = spot_of(E, row0, col0, lane);
+            if (half < chunks && !A.tma_out) {
+                if (E.wide) look(half);
+                else look_ahead_elements(E, row0, col0 + half * 32 + lane, ahead);
+            }
+            const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), total_at = lanes + 256;
+            constexpr int stride = PASSES ? kAccStride / 2 : kAccStride;
+            auto release = [&] {  // the warp has read its part of the accumulator
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 1) mbar_arrive(acc_empty + 8 * (pass & 1));
+                    else arrive_at(in_first(acc_empty + 8 * (pass & 1)));
+                }
+                ++pass;
+            };
+            bool ok = true;
+            for (int i = 0; PASSES && i + 1 < A.passes; ++i) {  // all but the last one's sums are added up
+                ok = all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
+                if (!ok) break;
+                fence_after();
+                for (int c = half; c < chunks; c += EPI / 4) {
+                    float v[32];
+                    tmem_load(lanes + (pass & 1) * stride + c * 32, v);
+                    if (i > 0) tmem_add(total_at + c * 32, v);
+                    tmem_store(total_at + c * 32, v);
+                }
+                release();
+            }
+            if (!ok || !all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT))) break;
+            fence_after();
+            const uint32_t acc_at = lanes + (pass & 1) * stride;
+            if (half >= chunks) release();
+            for (int c = half; c < chunks; c += EPI / 4) {
+                float v[32];
+                tmem_load(acc_at + c * 32, v);
+                if (PASSES) tmem_add(total_at + c * 32, v);
+                if (c + EPI / 4 >= chunks) release();
+                if (A.tma_out) {
+                    uint8_t* const buf = reinterpret_cast<uint8_t*>(turn);
+                    const int col = col0 + c * 32;
+                    if (E.act == CB_ACT_NONE) finish_tma<CB_ACT_NONE>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
+                    else if (E.act == CB_ACT_GELU) finish_tma<CB_ACT_GELU>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
+                    else finish_tma<CB_ACT_SILU>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
+                    continue;
+                }
+                // a row per lane to rows of 32 columns: 16-byte pieces, swizzled against bank conflicts
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<ulonglong2*>(&turn[lane * 32 + (j ^ (lane & 7)) * 4]) =
+                        make_ulonglong2(mul2(two(v[4 * j], v[4 * j + 1]), xs2), mul2(two(v[4 * j + 2], v[4 * j + 3]), xs2));
+                __syncwarp();
+                if (E.wide) {
+                    ulonglong2 u[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = 4 * i + lane / 8;
+                        u[i] = *reinterpret_cast<const ulonglong2*>(&turn[r * 32 + ((lane & 7) ^ (r & 7)) * 4]);
+                    }
+                    const Ahead now = ahead;
+                    if (c + EPI / 4 < chunks) look(c + EPI / 4);
+                    if (rows_full) finish<true>(E, spot, c * 32, now, u);
+                    else finish<false>(E, spot, c * 32, now, u);
+                } else {
+                    finish_elements(E, row0, col0 + c * 32 + lane, lane, ahead, turn);
+                    if (c + EPI / 4 < chunks) look_ahead_elements(E, row0, col0 + (c + EPI / 4) * 32 + lane, ahead);
+                }
+                __syncwarp();
+            }
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    } else if (warp == EPI) {  // ---- products
+        if (rank == 0) {
+            // fp32 sums; A and B bf16 (kind f16) or e4m3 (kind f8f6f4), both with K innermost; N / 8, M / 16
+            const uint32_t idesc =
+                1u << 4 | (FP8 ? 0u : 1u << 7 | 1u << 10) | (uint32_t)(A.tile_n / 8) << 17 | (uint32_t)(kRows * CG / 16) << 24;
+            const uint64_t desc0 = operand_desc(ring);
+            const int last_steps = (A.k_bytes - (A.k_blocks - 1) * kSlab + 31) / 32;  // of 32 bytes of K
+            Place at;
+            constexpr int stride = PASSES ? kAccStride / 2 : kAccStride;
+            int pass = 0;
+            bool ok = true;
+            // (the slabs' loop is kept short: with passes opened and closed inside it, a slab took 260 clocks longer)
+            for (int t = first; t < total && ok; t += step) {
+                for (int kb0 = 0; kb0 < A.k_blocks && ok; ++pass) {
+                    const int end = PASSES ? min(kb0 + A.pass_blocks, A.k_blocks) : A.k_blocks;
+                    const uint32_t sums = tmem + (pass & 1) * stride;
+                    ok = all(wait<CG == 2>(acc_empty + 8 * (pass & 1), ((pass >> 1) & 1) ^ 1, abort, A.status,
+                                           CB_DEV_PRODUCER_TIMEOUT));
+                    fence_after();
+                    for (int kb = kb0; kb < end && ok; ++kb) {
+                        const uint64_t a = desc0 + (uint32_t)(at.s * stage_bytes) / 16, b = a + kRows * kSlab / 16;
+                        ok = all(wait(full + 8 * at.s, at.phase, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
+                        if (!ok) break;
+                        fence_after();
+                        const int steps = kb + 1 < A.k_blocks ? 4 : last_steps;
+                        if (elected()) {
+                            mma<CG, FP8>(sums, a, b, idesc, kb > kb0);
+                            if (steps > 1) mma<CG, FP8>(sums, a + 2, b + 2, idesc, true);
+                            if (steps > 2) mma<CG, FP8>(sums, a + 4, b + 4, idesc, true);
+                            if (steps > 3) mma<CG, FP8>(sums, a + 6, b + 6, idesc, true);
+                            commit<CG>(empty + 8 * at.s);
+                            if (kb + 1 == end) commit<CG>(acc_full + 8 * (pass & 1));
+                        }
+                        at.next(stages);
+                    }
+                    kb0 = end;
+                }
+            }
+        }
+    } else if constexpr (!SHIFT) {  // ---- operands
+        {
+            Place at;
+            int fills = 0;
+            bool ok = true;
+            const uint32_t bar0 = CG == 2 ? in_first(full) : full;
+            for (int t = first; t < total && ok; t += step) {
+                const Tile tile = tile_at(A, t);
+                const int row = (tile.m * CG + (int)rank) * kRows, col = tile.n * A.tile_n + (int)rank * w_rows;
+                for (int kb = 0; kb < A.k_blocks; ++kb, ++fills) {
+                    ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
+                    if (!ok) break;
+                    const uint32_t dst = ring + at.s * stage_bytes;
+                    if (elected()) {
+                        if (rank == 0) mbar_expect_tx(full + 8 * at.s, CG * stage_bytes);
+                        tma_2d<CG>(dst, &A.x_map, kb * kSlab, row, bar0 + 8 * at.s);
+                        tma_2d<CG>(dst + kRows * kSlab, &A.w_map, kb * kSlab, col, bar0 + 8 * at.s);
+                    }
+                    at.next(stages);
+                }
+            }
+            if (!drain(at, fills, stages, empty, abort, A.status)) {
+                const unsigned long long t0 = now_ns();  // given up: copies under way land in microseconds
+                while (now_ns() - t0 < kMinDrainNs) {}
+            }
+        }
+    } else {
+        const int M = A.e.M, N = A.e.N, rows = kRows + w_rows, lw = warp - EPI - 1;
+        const long long x_row = A.x_row, w_row = A.w_row;
+        const char *const x0 = reinterpret_cast<const char*>(A.x), *const w0 = reinterpret_cast<const char*>(A.w);
+        const uint32_t raw_at = smem_addr(&T + 1);
+        const int raw_bytes = rows * kRawRow;
+        struct Slab {
+            int t, kb, row0, col0;
+        };
+        auto start = [&](int t) {
+            if (t >= total) return Slab{t, 0, 0, 0};
+            const Tile tile = tile_at(A, t);
+            return Slab{t, 0, tile.m * kRows, tile.n * A.tile_n};
+        };
+        auto next_of = [&](Slab c) { return ++c.kb < A.k_blocks ? c : start(c.t + step); };
+        const int quad_row = lane / 8, j = lane % 8;  // row of four, piece of the eight that every row has
+        // Copies pieces of the stage rows of the quads q, q + LOADERS, ... below `end`, rows of an operand from `from` on, the
+        // stage's row 0 being its row `row0`. NINTH: the pieces behind the eighth, a lane for each row of eight quads.
+        // No byte outside of the operand is read: copies end with it (`ends`: this slab may touch its ends), and pieces
+        // that begin before it are read byte by byte.
+        auto copy_quads = [&](auto ninth, int q, int end, const char* from, long long stride, int row0, int count, int kb,
+                              bool ends, uint32_t dst) {
+            constexpr bool NINTH = decltype(ninth)::value;
+            constexpr int S = NINTH ? 8 * LOADERS : LOADERS;
+            int r = 4 * (NINTH ? q + lane / 4 * LOADERS : q) + (NINTH ? lane % 4 : quad_row);
+            const int piece = NINTH ? 8 : j;
+            const char* at = from + (row0 + r) * stride + kb * kSlab + 16 * piece;
+            dst += 16 * piece;
+#pragma unroll 2
+            for (; q < end; q += S, r += 4 * S, at += 4 * S * stride) {
+                const int m = (int)((uintptr_t)at & 15);
+                const char* const p = at - m;
+                bool on = row0 + r < count && r < 4 * end && (!NINTH || m);
+                int size = 16;
+                if (ends) {
+                    const char* const to = from + (count - 1) * stride + A.k_bytes;
+                    size = (int)min(max((long long)(to - p), 0ll), 16ll);
+                    if (on && p < from) {
+#pragma unroll 1
+                        for (int i = 0; i < 16; ++i)
+                            if (p + i >= from && p + i < to)
+                                asm volatile("st.shared.u8 [%0], %1;" ::"r"(dst + r * kRawRow + i), "h"((short)(uint8_t)p[i])
+                                             : "memory");
+                        on = false;
+                    }
+                }
+                if (on)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + r * kRawRow), "l"(size > 0 ? p : from),
+                                 "r"(size)
+                                 : "memory");
+            }
+        };
+        const int x_quads = kRows / 4, quads = rows / 4;
+        const int w_first = x_quads + (lw + LOADERS - x_quads % LOADERS) % LOADERS;  // this warp's first quad of w
+        auto copy = [&](const Slab& c, int slot) {
+            const uint32_t dst = raw_at + slot * raw_bytes;
+            const bool ends = (c.kb == 0 || c.kb + 2 >= A.k_blocks) &&
+                              (c.row0 == 0 || c.col0 == 0 || c.row0 + kRows + 16 >= M || c.col0 + w_rows + 16 >= N);
+            const std::false_type eight;
+            const std::true_type ninth;
+            copy_quads(eight, lw, x_quads, x0, x_row, c.row0, M, c.kb, ends, dst);
+            copy_quads(eight, w_first, quads, w0, w_row, c.col0 - kRows, N, c.kb, ends, dst);
+            copy_quads(ninth, lw, x_quads, x0, x_row, c.row0, M, c.kb, ends, dst);
+            copy_quads(ninth, w_first, quads, w0, w_row, c.col0 - kRows, N, c.kb, ends, dst);
+        };
+        // The quads' rows from their pieces to the stage: a lane makes 16 bytes out of two pieces, `off` being the address of the
+        // stage's row 0 in the operand (its low bits).
+        auto move_quads = [&](int q, int end, uint32_t off, uint32_t stride, uint32_t raw, uint32_t stage, int left) {
+            off += (4 * q + quad_row) * stride;
+            raw += (4 * q + quad_row) * kRawRow + 16 * j;
+            stage += (4 * q + quad_row) * kSlab;
+#pragma unroll 2
+            for (; q < end; q += LOADERS) {
+                uint32_t w[8];
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(raw));
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+16];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(raw));
+                const uint4 v = first_bytes(shifted(make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), off & 15), left);
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (j ^ ((4 * q + quad_row) & 7)) * 16), "r"(v.x),
+                             "r"(v.y), "r"(v.z), "r"(v.w)
+                             : "memory");
+                off += 4 * LOADERS * stride;
+                raw += 4 * LOADERS * kRawRow;
+                stage += 4 * LOADERS * kSlab;
+            }
+        };
+        Place at;
+        int fills = 0, slot = 0;
+        Slab now = start(first), ahead = now;
+#pragma unroll 1
+        for (int i = 0; i + 1 < kRawSlabs; ++i) {
+            if (ahead.t < total) copy(ahead, i), ahead = next_of(ahead);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        for (; now.t < total; now = next_of(now), ++fills) {
+            if (ahead.t < total) copy(ahead, slot == 0 ? kRawSlabs - 1 : slot - 1), ahead = next_of(ahead);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRawSlabs - 1) : "memory");
+            if (!all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT))) break;
+            __syncwarp();
+            const int left = A.k_bytes - now.kb * kSlab - 16 * j;  // bytes of a row from this lane's 16 on
+            const uint32_t raw = raw_at + slot * raw_bytes, stage = ring + at.s * stage_bytes;
+            const uint32_t xs = (uint32_t)x_row, ws = (uint32_t)w_row;
+            move_quads(lw, x_quads, (uint32_t)(uintptr_t)x0 + (uint32_t)now.row0 * xs, xs, raw, stage, left);
+            move_quads(w_first, quads, (uint32_t)(uintptr_t)w0 + (uint32_t)(now.col0 - kRows) * ws, ws, raw, stage, left);
+            fence_generic_to_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + 8 * at.s);
+            at.next(stages);
+            slot = slot + 1 == kRawSlabs ? 0 : slot + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        drain(at, fills, stages, empty, abort, A.status);
+    }
+    fence_before();
+    __syncwarp();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();  // no CTA leaves while the other may still reach its barriers or TMEM
+    fence_after();
+    if (warp == EPI) {
+        if constexpr (CG == 1)
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+using LinearKernel = void (*)(LinearArgs);
+template <bool PASSES>
+LinearKernel kernel_of(int cg, bool fp8, int loaders) {
+    if (loaders == kManyLoaders) return fp8 ? linear_kernel<1, true, kManyLoaders, PASSES> : linear_kernel<1, false, kManyLoaders, PASSES>;
+    if (loaders) return fp8 ? linear_kernel<1, true, kFewLoaders, PASSES> : linear_kernel<1, false, kFewLoaders, PASSES>;
+    if (cg == 2) return fp8 ? linear_kernel<2, true, 0, PASSES> : linear_kernel<2, false, 0, PASSES>;
+    return fp8 ? linear_kernel<1, true, 0, PASSES> : linear_kernel<1, false, 0, PASSES>;
+}
+
+}  // namespace
+}  // namespace cbk

@@ -32,6 +32,8 @@ def test_constants_and_structs_match_the_header(lib):
     block, cb = lib
     for name, value in re.findall(r"\b(CB_ACT_\w+)\s*=\s*(-?\d+)", _header()):
         assert getattr(block, name) == int(value), name
+    for name, value in re.findall(r"#define (CB_\w+) \(1LL << (\d+)\)", _header()):
+        assert getattr(block, name) == 1 << int(value), name
     for body, name in re.findall(r"typedef struct \{(.*?)\}\s*(cb_\w+);", _header(), flags=re.S):
         fields = re.findall(r"(\w+)\s*;", body)
         assert fields == [f for f, _ in getattr(block, name)._fields_], name

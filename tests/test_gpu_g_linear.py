@@ -258,3 +258,27 @@ def test_row_offsets_beyond_2_31(lib):
     close(out[:, :n], ref, (k + 4) * U * (xv.double().abs() @ w.double().abs().t()), "bf16")
     assert float(out[:, n:n + 64].abs().max()) == 0.0
     block.cb_linear_destroy(layer)
+
+
+@pytest.mark.parametrize("type", ["bf16", "e4m3"])
+@pytest.mark.parametrize("k", [512, 520, 4096, 16384])
+def test_fp32_sums_do_not_lose_with_their_length(lib, type, k):
+    """fp32 results of long sums. A part of 512 products takes 32 additions on the tensor cores, each of which cuts off half of
+    2^-23 of the running sum on average, and the running sum averages two thirds of the part's: 1.3e-6 of it in all, however
+    many parts are then added rounded to nearest."""
+    block, cb = lib
+    m, n = 384, 200
+    g = torch.Generator(device="cuda").manual_seed(k)
+    for shift in (0.0, 1.0):
+        x = (torch.randn(m, k, generator=g, device="cuda") + shift).to(DT[type])
+        w = torch.randn(n, k, generator=g, device="cuda").to(DT[type])
+        r = torch.zeros(m, n, device="cuda")
+        out, xo = torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda")
+        layer = block.cb_linear_create(w, n, k, cb.CB_BF16 if type == "bf16" else cb.CB_E4M3)
+        io = block.cb_linear_io(rows=m, out_dtype=cb.CB_FP32, resid_dtype=cb.CB_FP32)
+        block.cb_linear_run(layer, io, x, resid=r, out=out, resid_out=xo)
+        torch.cuda.synchronize()
+        ref = f64(x) @ f64(w).t()
+        assert float((out.double() - ref).norm() / ref.norm()) < 1.3e-6
+        assert torch.equal(out, xo)
+        block.cb_linear_destroy(layer)
