@@ -128,8 +128,9 @@ void cb_linear_destroy(cb_linear* layer);
  * may be NULL together, gate (with resid only) may be NULL: 1; one result at least
  * is wanted. resid_out may be resid itself (same stride). The order of a sum depends
  * on the sizes alone: equal calls give equal bits.
- * Operands whose rows start on 16-byte boundaries come by TMA, others through registers, where they are
- * shifted into place; both run on the tensor cores.
+ * Operands whose rows do not start on 16-byte boundaries are copied onto them first where
+ * there are over 32 rows. The copies are allocated and freed in stream order, from a
+ * pool of the library's own that keeps 1 GiB at most between calls; in a graph they belong to the graph.
  * Every wait of the kernels on one of their barriers has a limit of a second; one that
  * runs out is noted in the status word of cb_linear_device_status and makes the
  * kernel return early, with incomplete results.

@@ -18,10 +18,24 @@ bool on_grid(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
 struct Device {
     int sms, smem, pairs;
     int* status;
+    cudaMemPool_t pool;  // for operands copied onto the 16-byte grid
 };
+// What the pool keeps from call to call: an allocation that maps memory anew takes longer than the product it is for.
+constexpr unsigned long long kPoolKeeps = 1ull << 30;
 std::atomic<const Device*> g_devices[kMaxStatusDevices];
 using Encode = decltype(&cuTensorMapEncodeTiled);
 std::atomic<Encode> g_encode;
+
+cudaError_t make_pool(int device, cudaMemPool_t* pool) {
+    cudaMemPoolProps props{};
+    props.allocType = cudaMemAllocationTypePinned;
+    props.location.type = cudaMemLocationTypeDevice;
+    props.location.id = device;
+    cudaError_t e = cudaMemPoolCreate(pool, &props);
+    unsigned long long keeps = kPoolKeeps;
+    if (e == cudaSuccess) e = cudaMemPoolSetAttribute(*pool, cudaMemPoolAttrReleaseThreshold, &keeps);
+    return e;
+}
 
 int device_info(const Device** out) {
     int d = 0;
@@ -34,6 +48,7 @@ int device_info(const Device** out) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&v.smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, d);
     if (e == cudaSuccess) e = cudaGetSymbolAddress(reinterpret_cast<void**>(&v.status), g_linear_status);
     if (e == cudaSuccess) e = prepare_linear((size_t)v.smem, &v.pairs);
+    if (e == cudaSuccess) e = make_pool(d, &v.pool);
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found{};
     if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
@@ -44,11 +59,37 @@ int device_info(const Device** out) {
     if (!mine) return CB_ERR_LIMIT;
     const Device* none = nullptr;
     if (!g_devices[d].compare_exchange_strong(none, mine, std::memory_order_acq_rel)) {
+        (void)cudaMemPoolDestroy(mine->pool);
         delete mine;
         mine = none;
     }
     *out = mine;
     return CB_OK;
+}
+
+// Copies of the operands that are not on the 16-byte grid (x, w: nullptr where they are), in stream order; `pack` then tells
+// where they lie, and the caller gives `copies` back behind the kernel that reads them.
+int make_copies(const Device& dev, const void* x, long long x_row, int M, const void* w, long long w_row, int N, int bytes,
+                LinearPackArgs* pack, char** copies, cudaStream_t s) {
+    const unsigned chunks = (unsigned)(bytes + 31) / 32;
+    const size_t x_size = x ? ((size_t)M * chunks * 32 + 255) / 256 * 256 : 0, w_size = w ? (size_t)N * chunks * 32 : 0;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    void* at = nullptr;
+    cudaError_t e = cudaStreamIsCapturing(s, &capture);
+    if (e == cudaSuccess) e = cudaMallocFromPoolAsync(&at, x_size + w_size, dev.pool, s);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();  // returned here, so not left for a check of the caller's own launches
+        return cuda_error(e, "linear workspace");
+    }
+    *copies = static_cast<char*>(at);
+    if (x) pack->o[0] = {static_cast<const char*>(x), *copies, M, x_row, bytes, chunks};
+    if (w) pack->o[1] = {static_cast<const char*>(w), *copies + x_size, N, w_row, bytes, chunks};
+    pack->overlap = capture == cudaStreamCaptureStatusNone;  // in a graph it follows the allocation, not a kernel
+    e = launch_linear_pack(*pack, s);
+    if (e == cudaSuccess) return CB_OK;
+    (void)cudaFreeAsync(at, s);
+    *copies = nullptr;
+    return cuda_error(e, "linear launch");
 }
 
 // Rows of bytes, in boxes of `box` rows by `wide` bytes (128, or 64), swizzled by as much; behind the ends zeros come in
@@ -74,9 +115,9 @@ constexpr int kPassBf16 = 8, kPassE4m3 = 64;
 
 // CTAs per tile and the tile's columns: the fewest rounds of tiles, each as long as its loads (16 KB of x and
 // 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take.
-void choose_tile(const Device& dev, int M, int N, bool tma, int most, int* cg, int* tile_n) {
+void choose_tile(const Device& dev, int M, int N, int most, int* cg, int* tile_n) {
     double best = 1e300;
-    for (int g = tma ? 2 : 1; g >= 1; --g)
+    for (int g = 2; g >= 1; --g)
         for (int n = most; n >= 32; n -= 32) {
             if (n > 32 && n - 32 >= N) continue;
             const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n);
@@ -140,8 +181,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     LinearArgs a{};
     a.overlap = 1;
     a.k_bytes = (int)(K * es);
-    a.x_row = (io->x_stride ? io->x_stride : K) * es, a.w_row = d.w_stride * es;
-    a.x = x, a.w = d.w;
+    const long long x_row = (io->x_stride ? io->x_stride : K) * es, w_row = d.w_stride * es;
     LinearEpilogue& ep = a.e;
     ep.M = (int)io->rows, ep.N = (int)N;
     ep.act = d.activation;
@@ -173,12 +213,10 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     int rc = device_info(&dev);
     if (rc != CB_OK) return rc;
     a.status = dev->status;
-    a.grid_bytes = 16;
-    while (((uintptr_t)x | (uintptr_t)d.w | (uintptr_t)a.x_row | (uintptr_t)a.w_row) % a.grid_bytes) a.grid_bytes /= 2;
-    const bool tma = a.grid_bytes == 16;
+    const bool x_on = on_grid(x, 16) && x_row % 16 == 0, w_on = on_grid(d.w, 16) && w_row % 16 == 0;
     if (ep.M <= kFewRows) {
-        const LinearFewArgs f{ep, 1, a.k_bytes, a.x_row, a.w_row, x, d.w};
-        const cudaError_t e = launch_linear_few(f, d.type == CB_E4M3, !tma, dev->sms, (cudaStream_t)stream);
+        const LinearFewArgs f{ep, 1, a.k_bytes, x_row, w_row, x, d.w};
+        const cudaError_t e = launch_linear_few(f, d.type == CB_E4M3, !x_on || !w_on, dev->sms, (cudaStream_t)stream);
         return e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
     }
     int cg = 1;
@@ -187,15 +225,10 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     const bool fp32 = (out && !ep.out_bf16) || (resid_out && !ep.resid_bf16);
     a.pass_blocks = fp32 ? (d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks;
     a.passes = (a.k_blocks + a.pass_blocks - 1) / a.pass_blocks;
-    choose_tile(*dev, ep.M, ep.N, tma, a.passes > 1 || !tma ? 128 : 256, &cg, &a.tile_n);
+    choose_tile(*dev, ep.M, ep.N, a.passes > 1 ? 128 : 256, &cg, &a.tile_n);
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
-    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(!tma, a.tile_n)) / linear_stage_bytes(cg, a.tile_n));
-    if (tma) {
-        rc = operand_map(&a.x_map, x, ep.M, a.k_bytes, a.x_row, 128);
-        if (rc == CB_OK) rc = operand_map(&a.w_map, d.w, ep.N, a.k_bytes, a.w_row, a.tile_n / cg);
-        if (rc != CB_OK) return rc;
-    }
+    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes()) / linear_stage_bytes(cg, a.tile_n));
     const long long out_row = ep.out_stride * (long long)bytes_of(io->out_dtype);
     if (out && !resid_out && on_grid(out, 16) && out_row % 16 == 0 && out_row < 1LL << 40) {
         rc = operand_map(&a.out_map, out, ep.M, N * (long long)bytes_of(io->out_dtype), out_row, 32, 64);
@@ -203,8 +236,27 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
         a.tma_out = 1;
     }
     const int tiles = a.tiles_m * a.tiles_n, units = cg == 2 ? dev->pairs : dev->sms;
-    const cudaError_t e = launch_linear(a, cg, d.type == CB_E4M3, cg * (tiles < units ? tiles : units), (cudaStream_t)stream);
-    return e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
+    const int grid = cg * (tiles < units ? tiles : units);
+    const cudaStream_t s = (cudaStream_t)stream;
+    char* copies = nullptr;
+    LinearPackArgs pack{};
+    rc = x_on && w_on ? CB_OK : make_copies(*dev, x_on ? nullptr : x, x_row, ep.M, w_on ? nullptr : d.w, w_row, ep.N, a.k_bytes, &pack, &copies, s);
+    if (rc != CB_OK) return rc;
+    const PackOperand &px = pack.o[0], &pw = pack.o[1];
+    rc = px.dst ? operand_map(&a.x_map, px.dst, ep.M, 32ll * px.chunks, 32ll * px.chunks, 128)
+                : operand_map(&a.x_map, x, ep.M, a.k_bytes, x_row, 128);
+    if (rc == CB_OK)
+        rc = pw.dst ? operand_map(&a.w_map, pw.dst, ep.N, 32ll * pw.chunks, 32ll * pw.chunks, a.tile_n / cg)
+                    : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);
+    if (rc == CB_OK) {
+        const cudaError_t e = launch_linear(a, cg, d.type == CB_E4M3, grid, s);
+        if (e != cudaSuccess) rc = cuda_error(e, "linear launch");
+    }
+    if (copies) {
+        const cudaError_t e = cudaFreeAsync(copies, s);
+        if (e != cudaSuccess && rc == CB_OK) rc = cuda_error(e, "linear workspace");
+    }
+    return rc;
 }
 
 int cb_linear_device_status(int* status, void* stream) {

@@ -25,8 +25,8 @@ struct LinearEpilogue {
 };
 
 struct LinearArgs {
-    CUtensorMap x_map, w_map;  // where the operands come by TMA
-    CUtensorMap out_map;       // where the output leaves by TMA
+    CUtensorMap x_map, w_map;
+    CUtensorMap out_map;  // where the output leaves by TMA
     int tma_out;
     LinearEpilogue e;
     int overlap;
@@ -34,9 +34,6 @@ struct LinearArgs {
     int tiles_m, tiles_n, k_blocks, stages;
     int tile_n;            // output columns of a tile
     int passes, pass_blocks;  // parts of K that are summed by themselves, and their slabs
-    int grid_bytes;        // grid on which all rows of x and of w start, up to 16 bytes
-    long long x_row, w_row;  // bytes from row to row
-    const void *x, *w;
     int* status;
 };
 
@@ -51,13 +48,28 @@ struct LinearFewArgs {
 // `shift`: rows off the 16-byte grid.
 cudaError_t launch_linear_few(const LinearFewArgs& a, bool fp8, bool shift, int sms, cudaStream_t s);
 
-// The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows; a.grid_bytes below 16: cg = 1
-// only. prepare_linear raises the kernels' shared-memory limit and tells how many pairs of CTAs run at once.
+// Rows copied onto a grid of 32 bytes, with zeros behind each (linear_pack.cu).
+struct PackOperand {
+    const char* src;
+    char* dst;                  // nullptr: nothing to copy
+    long long rows, stride;     // bytes from row to row of src
+    int bytes;                  // of a row
+    unsigned chunks;            // of 32 bytes, of a row of dst
+};
+struct LinearPackArgs {
+    PackOperand o[2];
+    unsigned blocks;            // of the first operand
+    int overlap;
+};
+cudaError_t launch_linear_pack(LinearPackArgs& a, cudaStream_t s);
+
+// The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows. prepare_linear raises the kernels' shared-memory
+// limit and tells how many pairs of CTAs run at once.
 size_t linear_stage_bytes(int cg, int tile_n);
-size_t linear_fixed_bytes(bool shift, int tile_n);  // shared memory besides the stages
+size_t linear_fixed_bytes();  // shared memory besides the stages
 constexpr int kMaxLinStages = 12;
 cudaError_t prepare_linear(size_t smem, int* pairs);
-void (*linear_passes_kernel(int cg, bool fp8, int loaders))(LinearArgs);  // linear_tc_passes.cu
+void (*linear_passes_kernel(int cg, bool fp8))(LinearArgs);  // linear_tc_passes.cu
 cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s);
 
 #ifdef __CUDACC__

@@ -2,18 +2,15 @@
 //
 // A persistent grid of CTAs (CG = 1) or of pairs of CTAs on two SMs (CG = 2) works through output tiles of 128 CG
 // rows by tile_n columns. In a CTA
-//   one warp (TMA) or several (else) fill a ring of stages with slabs of 128 bytes of K: 128 rows of x and
-//     tile_n / CG rows of w, in the 128-byte swizzle that the tensor cores read,
+//   one warp fills a ring of stages by TMA with slabs of 128 bytes of K: 128 rows of x and tile_n / CG rows of w, in
+//     the 128-byte swizzle that the tensor cores read,
 //   one thread issues tcgen05.mma on them, sums in TMEM (two accumulators of up to 256 columns each),
-//   eight warps (or four) take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
+//   eight warps take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
 //     that their accesses to global memory are rows, and apply the epilogue.
 // A pair of CTAs shares one tile: each loads its 128 rows of x and half of the tile's rows of w, the first one's
 // thread issues for both, and each holds the sums of its own rows.
 //
-// Operands whose rows do not start on 16-byte boundaries cannot come by TMA (SHIFT). Seven or eleven warps copy the aligned
-// 16-byte pieces that a slab's rows touch into a ring of their own, two slabs ahead, and then move each row, shifted by
-// its offset, to where TMA would have put it. A warp moves the rows that it has copied, four at a time, so the warps
-// need no barrier among them.
+// Operands whose rows do not start on 16-byte boundaries cannot come by TMA; linear_pack.cu copies them onto the grid first.
 //
 // The tensor cores cut off what a sum loses where it is added to, which adds up over K: 1.1e-9 K of a result (bf16; 1.9e-5 at
 // K = 16384, 2.1e-6 at 2048). Results in fp32 are therefore summed in passes over parts of K, whose sums the epilogue's warps
@@ -28,7 +25,6 @@
 
 #include "cb_async.cuh"
 #include "linear.cuh"
-#include "linear_shift.cuh"
 
 namespace cbk {
 namespace {
@@ -37,14 +33,7 @@ constexpr int kRows = 128;        // rows of x per CTA
 constexpr int kSlab = 128;        // bytes of K per stage
 constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the other (half of it where there are passes)
 constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes
-// Warps that move operands off the 16-byte grid (0: TMA), of the 16 warps that 128 registers a thread allow. Long sums are
-// bound by them and take 11, with four warps for the epilogue; short ones by the epilogue and take 7 and eight
-// (999 x 577 x 1155 31.4 -> 28.7 us; 4096 x 4096 x 4097 867 -> 1004 us).
-constexpr int kFewLoaders = 7, kManyLoaders = 11, kManyFrom = 24;  // slabs
-__host__ __device__ constexpr int epi_warps(int loaders) { return loaders == kManyLoaders ? 4 : kEpiWarps; }
-__host__ __device__ constexpr int linear_threads(int loaders) { return 32 * (epi_warps(loaders) + 1 + (loaders ? loaders : 1)); }
-constexpr int kRawRow = 144;      // bytes of a row's pieces
-constexpr int kRawSlabs = 3;      // slabs of pieces held
+constexpr int kLinearThreads = 32 * (kEpiWarps + 2);
 constexpr unsigned long long kLimitNs = 1000000000ull;
 
 struct alignas(16) Tail {  // behind the stages
@@ -469,12 +458,9 @@ __device__ __forceinline__ void finish_elements(const LinearEpilogue& E, int row
     put_column(E.resid_out, row0 * E.resid_out_stride + col, E.resid_out_stride, E.resid_bf16, rows, v);
 }
 
-template <int CG, bool FP8, int LOADERS, bool PASSES>
-__global__ void __launch_bounds__(linear_threads(LOADERS), 1)
-    linear_kernel(const __grid_constant__ LinearArgs A) {
-    constexpr bool SHIFT = LOADERS != 0;
-    static_assert(CG == 1 || !SHIFT, "pairs of CTAs load by TMA");
-    constexpr int EPI = epi_warps(LOADERS);
+template <int CG, bool FP8, bool PASSES>
+__global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_constant__ LinearArgs A) {
+    constexpr int EPI = kEpiWarps;
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
         after_previous();
@@ -492,7 +478,7 @@ __global__ void __launch_bounds__(linear_threads(LOADERS), 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
-            mbar_init(full + 8 * s, SHIFT ? LOADERS : 1);
+            mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -674,144 +660,30 @@ __global__ void __launch_bounds__(linear_threads(LOADERS), 1)
                 }
             }
         }
-    } else if constexpr (!SHIFT) {  // ---- operands
-        {
-            Place at;
-            int fills = 0;
-            bool ok = true;
-            const uint32_t bar0 = CG == 2 ? in_first(full) : full;
-            for (int t = first; t < total && ok; t += step) {
-                const Tile tile = tile_at(A, t);
-                const int row = (tile.m * CG + (int)rank) * kRows, col = tile.n * A.tile_n + (int)rank * w_rows;
-                for (int kb = 0; kb < A.k_blocks; ++kb, ++fills) {
-                    ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
-                    if (!ok) break;
-                    const uint32_t dst = ring + at.s * stage_bytes;
-                    if (elected()) {
-                        if (rank == 0) mbar_expect_tx(full + 8 * at.s, CG * stage_bytes);
-                        tma_2d<CG>(dst, &A.x_map, kb * kSlab, row, bar0 + 8 * at.s);
-                        tma_2d<CG>(dst + kRows * kSlab, &A.w_map, kb * kSlab, col, bar0 + 8 * at.s);
-                    }
-                    at.next(stages);
-                }
-            }
-            if (!drain(at, fills, stages, empty, abort, A.status)) {
-                const unsigned long long t0 = now_ns();  // given up: copies under way land in microseconds
-                while (now_ns() - t0 < kMinDrainNs) {}
-            }
-        }
-    } else {
-        const int M = A.e.M, N = A.e.N, rows = kRows + w_rows, lw = warp - EPI - 1;
-        const long long x_row = A.x_row, w_row = A.w_row;
-        const char *const x0 = reinterpret_cast<const char*>(A.x), *const w0 = reinterpret_cast<const char*>(A.w);
-        const uint32_t raw_at = smem_addr(&T + 1);
-        const int raw_bytes = rows * kRawRow;
-        struct Slab {
-            int t, kb, row0, col0;
-        };
-        auto start = [&](int t) {
-            if (t >= total) return Slab{t, 0, 0, 0};
-            const Tile tile = tile_at(A, t);
-            return Slab{t, 0, tile.m * kRows, tile.n * A.tile_n};
-        };
-        auto next_of = [&](Slab c) { return ++c.kb < A.k_blocks ? c : start(c.t + step); };
-        const int quad_row = lane / 8, j = lane % 8;  // row of four, piece of the eight that every row has
-        // Copies pieces of the stage rows of the quads q, q + LOADERS, ... below `end`, rows of an operand from `from` on, the
-        // stage's row 0 being its row `row0`. NINTH: the pieces behind the eighth, a lane for each row of eight quads.
-        // No byte outside of the operand is read: copies end with it (`ends`: this slab may touch its ends), and pieces
-        // that begin before it are read byte by byte.
-        auto copy_quads = [&](auto ninth, int q, int end, const char* from, long long stride, int row0, int count, int kb,
-                              bool ends, uint32_t dst) {
-            constexpr bool NINTH = decltype(ninth)::value;
-            constexpr int S = NINTH ? 8 * LOADERS : LOADERS;
-            int r = 4 * (NINTH ? q + lane / 4 * LOADERS : q) + (NINTH ? lane % 4 : quad_row);
-            const int piece = NINTH ? 8 : j;
-            const char* at = from + (row0 + r) * stride + kb * kSlab + 16 * piece;
-            dst += 16 * piece;
-#pragma unroll 2
-            for (; q < end; q += S, r += 4 * S, at += 4 * S * stride) {
-                const int m = (int)((uintptr_t)at & 15);
-                const char* const p = at - m;
-                bool on = row0 + r < count && r < 4 * end && (!NINTH || m);
-                int size = 16;
-                if (ends) {
-                    const char* const to = from + (count - 1) * stride + A.k_bytes;
-                    size = (int)min(max((long long)(to - p), 0ll), 16ll);
-                    if (on && p < from) {
-#pragma unroll 1
-                        for (int i = 0; i < 16; ++i)
-                            if (p + i >= from && p + i < to)
-                                asm volatile("st.shared.u8 [%0], %1;" ::"r"(dst + r * kRawRow + i), "h"((short)(uint8_t)p[i])
-                                             : "memory");
-                        on = false;
-                    }
-                }
-                if (on)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + r * kRawRow), "l"(size > 0 ? p : from),
-                                 "r"(size)
-                                 : "memory");
-            }
-        };
-        const int x_quads = kRows / 4, quads = rows / 4;
-        const int w_first = x_quads + (lw + LOADERS - x_quads % LOADERS) % LOADERS;  // this warp's first quad of w
-        auto copy = [&](const Slab& c, int slot) {
-            const uint32_t dst = raw_at + slot * raw_bytes;
-            const bool ends = (c.kb == 0 || c.kb + 2 >= A.k_blocks) &&
-                              (c.row0 == 0 || c.col0 == 0 || c.row0 + kRows + 16 >= M || c.col0 + w_rows + 16 >= N);
-            const std::false_type eight;
-            const std::true_type ninth;
-            copy_quads(eight, lw, x_quads, x0, x_row, c.row0, M, c.kb, ends, dst);
-            copy_quads(eight, w_first, quads, w0, w_row, c.col0 - kRows, N, c.kb, ends, dst);
-            copy_quads(ninth, lw, x_quads, x0, x_row, c.row0, M, c.kb, ends, dst);
-            copy_quads(ninth, w_first, quads, w0, w_row, c.col0 - kRows, N, c.kb, ends, dst);
-        };
-        // The quads' rows from their pieces to the stage: a lane makes 16 bytes out of two pieces, `off` being the address of the
-        // stage's row 0 in the operand (its low bits).
-        auto move_quads = [&](int q, int end, uint32_t off, uint32_t stride, uint32_t raw, uint32_t stage, int left) {
-            off += (4 * q + quad_row) * stride;
-            raw += (4 * q + quad_row) * kRawRow + 16 * j;
-            stage += (4 * q + quad_row) * kSlab;
-#pragma unroll 2
-            for (; q < end; q += LOADERS) {
-                uint32_t w[8];
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(raw));
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+16];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(raw));
-                const uint4 v = first_bytes(shifted(make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), off & 15), left);
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (j ^ ((4 * q + quad_row) & 7)) * 16), "r"(v.x),
-                             "r"(v.y), "r"(v.z), "r"(v.w)
-                             : "memory");
-                off += 4 * LOADERS * stride;
-                raw += 4 * LOADERS * kRawRow;
-                stage += 4 * LOADERS * kSlab;
-            }
-        };
+    } else {  // ---- operands
         Place at;
-        int fills = 0, slot = 0;
-        Slab now = start(first), ahead = now;
-#pragma unroll 1
-        for (int i = 0; i + 1 < kRawSlabs; ++i) {
-            if (ahead.t < total) copy(ahead, i), ahead = next_of(ahead);
-            asm volatile("cp.async.commit_group;" ::: "memory");
+        int fills = 0;
+        bool ok = true;
+        const uint32_t bar0 = CG == 2 ? in_first(full) : full;
+        for (int t = first; t < total && ok; t += step) {
+            const Tile tile = tile_at(A, t);
+            const int row = (tile.m * CG + (int)rank) * kRows, col = tile.n * A.tile_n + (int)rank * w_rows;
+            for (int kb = 0; kb < A.k_blocks; ++kb, ++fills) {
+                ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
+                if (!ok) break;
+                const uint32_t dst = ring + at.s * stage_bytes;
+                if (elected()) {
+                    if (rank == 0) mbar_expect_tx(full + 8 * at.s, CG * stage_bytes);
+                    tma_2d<CG>(dst, &A.x_map, kb * kSlab, row, bar0 + 8 * at.s);
+                    tma_2d<CG>(dst + kRows * kSlab, &A.w_map, kb * kSlab, col, bar0 + 8 * at.s);
+                }
+                at.next(stages);
+            }
         }
-        for (; now.t < total; now = next_of(now), ++fills) {
-            if (ahead.t < total) copy(ahead, slot == 0 ? kRawSlabs - 1 : slot - 1), ahead = next_of(ahead);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            asm volatile("cp.async.wait_group %0;" ::"n"(kRawSlabs - 1) : "memory");
-            if (!all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT))) break;
-            __syncwarp();
-            const int left = A.k_bytes - now.kb * kSlab - 16 * j;  // bytes of a row from this lane's 16 on
-            const uint32_t raw = raw_at + slot * raw_bytes, stage = ring + at.s * stage_bytes;
-            const uint32_t xs = (uint32_t)x_row, ws = (uint32_t)w_row;
-            move_quads(lw, x_quads, (uint32_t)(uintptr_t)x0 + (uint32_t)now.row0 * xs, xs, raw, stage, left);
-            move_quads(w_first, quads, (uint32_t)(uintptr_t)w0 + (uint32_t)(now.col0 - kRows) * ws, ws, raw, stage, left);
-            fence_generic_to_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(full + 8 * at.s);
-            at.next(stages);
-            slot = slot + 1 == kRawSlabs ? 0 : slot + 1;
+        if (!drain(at, fills, stages, empty, abort, A.status)) {
+            const unsigned long long t0 = now_ns();  // given up: copies under way land in microseconds
+            while (now_ns() - t0 < kMinDrainNs) {}
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        drain(at, fills, stages, empty, abort, A.status);
     }
     fence_before();
     __syncwarp();
@@ -828,11 +700,9 @@ __global__ void __launch_bounds__(linear_threads(LOADERS), 1)
 
 using LinearKernel = void (*)(LinearArgs);
 template <bool PASSES>
-LinearKernel kernel_of(int cg, bool fp8, int loaders) {
-    if (loaders == kManyLoaders) return fp8 ? linear_kernel<1, true, kManyLoaders, PASSES> : linear_kernel<1, false, kManyLoaders, PASSES>;
-    if (loaders) return fp8 ? linear_kernel<1, true, kFewLoaders, PASSES> : linear_kernel<1, false, kFewLoaders, PASSES>;
-    if (cg == 2) return fp8 ? linear_kernel<2, true, 0, PASSES> : linear_kernel<2, false, 0, PASSES>;
-    return fp8 ? linear_kernel<1, true, 0, PASSES> : linear_kernel<1, false, 0, PASSES>;
+LinearKernel kernel_of(int cg, bool fp8) {
+    if (cg == 2) return fp8 ? linear_kernel<2, true, PASSES> : linear_kernel<2, false, PASSES>;
+    return fp8 ? linear_kernel<1, true, PASSES> : linear_kernel<1, false, PASSES>;
 }
 
 }  // namespace

@@ -3,6 +3,6 @@
 
 namespace cbk {
 
-void (*linear_passes_kernel(int cg, bool fp8, int loaders))(LinearArgs) { return kernel_of<true>(cg, fp8, loaders); }
+void (*linear_passes_kernel(int cg, bool fp8))(LinearArgs) { return kernel_of<true>(cg, fp8); }
 
 }  // namespace cbk

@@ -282,3 +282,77 @@ def test_fp32_sums_do_not_lose_with_their_length(lib, type, k):
         assert float((out.double() - ref).norm() / ref.norm()) < 1.3e-6
         assert torch.equal(out, xo)
         block.cb_linear_destroy(layer)
+
+
+OFF_GRID = [case(40, 96, 33), case(40, 96, 31, "e4m3"), case(65, 130, 1, "e4m3"), case(300, 200, 17, "e4m3", xoff=9, xpad=2),
+            case(700, 520, 1031, resid="fp32", gate="bf16", tokens=100), case(700, 520, 2063, "e4m3", out="fp32"), case(90, 700, 5494),
+            case(1500, 1100, 2049, act="GELU"), case(333, 64, 4097, "e4m3", xpad=1, resid="bf16"), case(2000, 1000, 40, xoff=1)]
+
+
+@pytest.mark.parametrize("c", OFF_GRID, ids=lambda c: "{m}x{n}x{k}_{type}".format(**c))
+def test_operands_off_the_grid(lib, c):
+    d, want, out, xo = run(lib, c, seed=5)
+    v, e, hidden, he = want
+    if c["out"]:
+        close(out, v, e, c["out"])
+    if c["resid"]:
+        close(xo, hidden, he, c["resid"])
+
+
+@pytest.mark.parametrize("type", ["bf16", "e4m3"])
+@pytest.mark.parametrize("xoff,woff", [(0, 1), (3, 0), (5, 2)])
+def test_only_the_operands_rows_are_summed(lib, type, xoff, woff):
+    """One operand off the grid or both, with NaN before, between and behind the rows: none of it reaches a result."""
+    block, cb = lib
+    m, n, k = 200, 136, 144
+    g = torch.Generator(device="cuda").manual_seed(3)
+    data = {}
+    for name, rows, off in (("x", m, xoff), ("w", n, woff)):
+        buf = torch.full((off + rows * (k + 16) + 16,), float("nan"), device="cuda").to(DT[type])
+        data[name] = buf[off:off + rows * (k + 16)].view(rows, k + 16)[:, :k]
+        data[name].copy_(torch.randint(-4, 5, (rows, k), generator=g, device="cuda").to(DT[type]))
+    out = torch.empty(m, n, device="cuda")
+    layer = block.cb_linear_create(data["w"], n, k, cb.CB_E4M3 if type == "e4m3" else cb.CB_BF16, w_stride=k + 16)
+    block.cb_linear_run(layer, block.cb_linear_io(rows=m, x_stride=k + 16, out_dtype=cb.CB_FP32), data["x"], out=out)
+    assert torch.equal(out.double(), f64(data["x"]) @ f64(data["w"]).t())  # small whole numbers: exact
+    block.cb_linear_destroy(layer)
+
+
+def test_off_the_grid_on_two_streams_and_in_a_graph(lib):
+    """The copies of such operands: calls of several sizes on two streams at once, then some in one graph, whose inputs change."""
+    block, cb = lib
+    g = torch.Generator(device="cuda").manual_seed(9)
+    whole = lambda *s: torch.randint(-4, 5, s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    sets = []
+    for m, n, k in [(100, 77, 333), (1000, 500, 1031), (64, 2000, 65), (513, 129, 4097)]:
+        x, w = whole(m, k), whole(n, k)
+        sets.append((x, w, block.cb_linear_create(w, n, k, cb.CB_BF16), block.cb_linear_io(rows=m, out_dtype=cb.CB_FP32)))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for turn in range(40):
+        for i, (x, w, layer, io) in enumerate(sets):
+            out = torch.empty(x.shape[0], w.shape[0], device="cuda")
+            outs.append((i, out))
+    torch.cuda.synchronize()
+    for j, (i, out) in enumerate(outs):
+        x, w, layer, io = sets[i]
+        block.cb_linear_run(layer, io, x, out=out, stream=streams[j % 2 ^ (j // 4) % 2])
+    torch.cuda.synchronize()
+    for i, out in outs:
+        assert torch.equal(out.double(), f64(sets[i][0]) @ f64(sets[i][1]).t())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(streams[0]), torch.cuda.graph(graph, stream=streams[0]):
+        for i, (x, w, layer, io) in enumerate(sets):
+            block.cb_linear_run(layer, io, x, out=outs[i][1], stream=torch.cuda.current_stream())
+    for turn in range(3):
+        for x, w, layer, io in sets:
+            x.copy_(whole(*x.shape))
+            w.copy_(whole(*w.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (x, w, layer, io) in enumerate(sets):
+            assert torch.equal(outs[i][1].double(), f64(x) @ f64(w).t()), (turn, i)
+    for x, w, layer, io in sets:
+        block.cb_linear_destroy(layer)
+    assert block.cb_linear_device_status() == 0
