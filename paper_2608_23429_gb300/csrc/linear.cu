@@ -104,6 +104,41 @@ int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes
     return r == CUDA_SUCCESS ? CB_OK : cuda_error(cudaErrorInvalidValue, "tensor map");
 }
 
+// Boxes of shared memory of a warp, besides two, for hidden states in bf16 and fp32: [1] where sums are short, as the results are
+// what takes the time then, [0] where they are long and stages are worth more. GB300, {1, 4} -> {4, 7}: 16384 x 8192 x 512 e4m3
+// with a bf16 output and hidden state 178 -> 150 us, fp32 hidden state alone 212 -> 192; 4096 x 1152 x 4608 64.1 -> 66.2 ({2, 5}).
+constexpr int kShortBlocks = 16, kMoreBoxes[2][2] = {{1, 4}, {4, 7}};
+
+// Results and hidden states whose rows lie on the 16-byte grid go by TMA, in boxes of 32 rows by 64 bytes.
+int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
+    const LinearEpilogue& e = a->e;
+    a->results = Results::kDirect;
+    const struct {
+        const void* p;
+        long long row, es;
+        CUtensorMap* map;
+    } used[] = {{e.out, e.out_stride, (long long)bytes_of(io->out_dtype), &a->out_map},
+                {e.resid, e.resid_stride, (long long)bytes_of(io->resid_dtype), &a->resid_map},
+                {e.resid_out, e.resid_out_stride, (long long)bytes_of(io->resid_dtype), &a->resid_out_map}};
+    for (const auto& u : used)
+        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40)) return CB_OK;
+    // a gate's pieces of 16 bytes are read whole
+    const long long gs = (long long)bytes_of(io->gate_dtype);
+    if (e.gate && (!on_grid(e.gate, 16) || e.gate_stride * gs % 16 != 0 || e.N * gs % 16 != 0)) return CB_OK;
+    for (const auto& u : used) {
+        if (!u.p) continue;
+        const int rc = operand_map(u.map, u.p, e.M, e.N * u.es, u.row * u.es, 32, 64);
+        if (rc != CB_OK) return rc;
+    }
+    a->results = e.resid_out ? Results::kHidden : Results::kOut;
+    if (e.resid_out) {
+        const int out = !e.out ? 0 : e.out_bf16 ? 1 : 2, resid = e.resid_bf16 ? 1 : 2;
+        a->more_boxes = std::max(kMoreBoxes[a->k_blocks <= kShortBlocks][resid - 1], out + 2 * resid - 2);
+        a->ring = (2 + a->more_boxes - out) / resid;
+    }
+    return CB_OK;
+}
+
 // Rows that linear_few.cu takes. GB300, w in L2, events around one call (about 8 us of them its own), linear_tc.cu ->
 // linear_few.cu: 8 x 6912 x 1152 14.2 -> 10.7 us, 32 x 1152 x 4608 18.5 -> 13.2, 8 x 64 x 16384 45 -> 9.6; with 64 rows
 // 6912 x 1152 13.2 -> 20.8, 1152 x 4608 18.6 -> 18.4, 12288 x 3072 20.3 -> 55.
@@ -228,13 +263,9 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     choose_tile(*dev, ep.M, ep.N, a.passes > 1 ? 128 : 256, &cg, &a.tile_n);
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
-    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes()) / linear_stage_bytes(cg, a.tile_n));
-    const long long out_row = ep.out_stride * (long long)bytes_of(io->out_dtype);
-    if (out && !resid_out && on_grid(out, 16) && out_row % 16 == 0 && out_row < 1LL << 40) {
-        rc = operand_map(&a.out_map, out, ep.M, N * (long long)bytes_of(io->out_dtype), out_row, 32, 64);
-        if (rc != CB_OK) return rc;
-        a.tma_out = 1;
-    }
+    rc = results_by_tma(io, &a);
+    if (rc != CB_OK) return rc;
+    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.more_boxes)) / linear_stage_bytes(cg, a.tile_n));
     const int tiles = a.tiles_m * a.tiles_n, units = cg == 2 ? dev->pairs : dev->sms;
     const int grid = cg * (tiles < units ? tiles : units);
     const cudaStream_t s = (cudaStream_t)stream;

@@ -24,10 +24,14 @@ struct LinearEpilogue {
     void *out, *resid_out;
 };
 
+// How results leave: an output alone by TMA, a hidden state with or without an output by TMA, or either by the threads.
+enum class Results { kOut, kHidden, kDirect };
+
 struct LinearArgs {
+    Results results;
     CUtensorMap x_map, w_map;
-    CUtensorMap out_map;  // where the output leaves by TMA
-    int tma_out;
+    CUtensorMap out_map, resid_map, resid_out_map;
+    int ring, more_boxes;  // hidden states of chunks that a warp holds; boxes of shared memory that it needs for them besides two
     LinearEpilogue e;
     int overlap;
     int k_bytes;           // bytes of a row of x and of w
@@ -66,10 +70,14 @@ cudaError_t launch_linear_pack(LinearPackArgs& a, cudaStream_t s);
 // The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows. prepare_linear raises the kernels' shared-memory
 // limit and tells how many pairs of CTAs run at once.
 size_t linear_stage_bytes(int cg, int tile_n);
-size_t linear_fixed_bytes();  // shared memory besides the stages
+size_t linear_fixed_bytes(int more_boxes);  // shared memory besides the stages
+constexpr int kBox = 2048, kMaxRing = 6;
 constexpr int kMaxLinStages = 12;
 cudaError_t prepare_linear(size_t smem, int* pairs);
-void (*linear_passes_kernel(int cg, bool fp8))(LinearArgs);  // linear_tc_passes.cu
+using LinearKernel = void (*)(LinearArgs);
+LinearKernel linear_out_kernel(int cg, bool fp8, bool passes);     // linear_tc_out.cu
+LinearKernel linear_hidden_kernel(int cg, bool fp8, bool passes);  // linear_tc_hidden.cu
+LinearKernel linear_direct_kernel(int cg, bool fp8, bool passes);  // linear_tc_direct.cu
 cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s);
 
 #ifdef __CUDACC__

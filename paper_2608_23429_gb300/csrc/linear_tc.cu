@@ -1,16 +1,16 @@
-// The tensor-core kernels whose sums stay in one accumulator, and the launch of all of them (see linear_tc.cuh).
+// The launch of the tensor-core kernels (see linear_tc.cuh).
 #include "linear_tc.cuh"
 
 namespace cbk {
 
 size_t linear_stage_bytes(int cg, int tile_n) { return (size_t)(kRows + tile_n / cg) * kSlab; }
 
-size_t linear_fixed_bytes() { return sizeof(Tail); }
+size_t linear_fixed_bytes(int more_boxes) { return kTailBytes + (size_t)kEpiWarps * more_boxes * kBox; }
 
 cudaError_t prepare_linear(size_t smem, int* pairs) {
-    for (int fp8 = 0; fp8 < 2; ++fp8)
-        for (LinearKernel k : {kernel_of<false>(2, fp8), kernel_of<false>(1, fp8), linear_passes_kernel(2, fp8), linear_passes_kernel(1, fp8)}) {
-            const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    for (int i = 0; i < 8; ++i)
+        for (auto of : {linear_out_kernel, linear_hidden_kernel, linear_direct_kernel}) {
+            const cudaError_t e = cudaFuncSetAttribute(of(1 + i % 2, i & 2, i & 4), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e != cudaSuccess) return e;
         }
     // pairs of CTAs that run at once
@@ -23,7 +23,7 @@ cudaError_t prepare_linear(size_t smem, int* pairs) {
     c.dynamicSmemBytes = smem;
     c.attrs = &at;
     c.numAttrs = 1;
-    return cudaOccupancyMaxActiveClusters(pairs, reinterpret_cast<const void*>(kernel_of<false>(2, false)), &c);
+    return cudaOccupancyMaxActiveClusters(pairs, reinterpret_cast<const void*>(linear_out_kernel(2, false, false)), &c);
 }
 
 cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s) {
@@ -35,11 +35,12 @@ cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaS
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)grid);
     c.blockDim = dim3(kLinearThreads);
-    c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + linear_fixed_bytes();
+    c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + linear_fixed_bytes(a.more_boxes);
     c.stream = s;
     c.attrs = at;
     c.numAttrs = cg == 2 ? 2 : 1;
-    const LinearKernel k = a.passes > 1 ? linear_passes_kernel(cg, fp8) : kernel_of<false>(cg, fp8);
+    const auto of = a.results == Results::kOut ? linear_out_kernel : a.results == Results::kHidden ? linear_hidden_kernel : linear_direct_kernel;
+    const LinearKernel k = of(cg, fp8, a.passes > 1);
     void* args[] = {const_cast<void*>(static_cast<const void*>(&a))};
     const cudaError_t e = cudaLaunchKernelExC(&c, reinterpret_cast<const void*>(k), args);
     if (e != cudaSuccess) (void)cudaGetLastError();

@@ -25,6 +25,7 @@
 
 #include "cb_async.cuh"
 #include "linear.cuh"
+#include "linear_shift.cuh"
 
 namespace cbk {
 namespace {
@@ -40,9 +41,11 @@ struct alignas(16) Tail {  // behind the stages
     float turn[kEpiWarps][32 * 32];
     float cols[2][2 * kAccStride];  // scales and biases of a tile's columns (where the output leaves by TMA)
     uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2], cols_full[2];
+    uint64_t resid_full[kEpiWarps][kMaxRing];
     uint32_t tmem;
     int abort;
 };
+constexpr int kTailBytes = (sizeof(Tail) + 1023) / 1024 * 1024;  // boxes of epilogue's hidden states follow
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -337,12 +340,37 @@ __device__ __forceinline__ void finish(const LinearEpilogue& E, const Spot& p, i
     put_rows<FULL>(p.resid_out + at * (E.resid_bf16 ? 2 : 4), p.resid_out_step, E.resid_bf16, rows, v);
 }
 
-// Output by TMA, where there is nothing to add it to: a row per lane, as the sums come from TMEM. Columns' operands are
-// read from shared memory by all lanes alike, and 32 rows of 64 bytes leave at a time, through two buffers in turn.
+// Results by TMA: a row per lane, as the sums come from TMEM. Columns' scale and bias are read from shared memory by all lanes
+// alike; hidden states come in and results leave in boxes of 32 rows of 64 bytes (a chunk of 32 columns is one of bf16 or two of
+// fp32), swizzled by 64 bytes.
+
+__device__ __forceinline__ uint32_t piece_at(uint32_t box, int lane, int j) { return box + lane * 64 + (j ^ (lane / 2 % 4)) * 16; }
+__device__ __forceinline__ void store_box(const CUtensorMap* map, int x, int y, uint32_t box) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(box)
+                 : "memory");
+}
+__device__ __forceinline__ uint4 packed8(const Two* x) {
+    const float2 a = both(x[0]), b = both(x[1]), c = both(x[2]), d = both(x[3]);
+    return make_uint4(bf16x2(a.x, a.y), bf16x2(b.x, b.y), bf16x2(c.x, c.y), bf16x2(d.x, d.y));
+}
+__device__ __forceinline__ uint4 as_uint4(Two a, Two b) {
+    const float2 f = both(a), g = both(b);
+    return make_uint4(__float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(g.x), __float_as_uint(g.y));
+}
+__device__ __forceinline__ void st_shared16(uint32_t at, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// Two bf16 values of a word.
+__device__ __forceinline__ Two widened(uint32_t w) { return two(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+
+// The 32 sums of a lane's row to values.
 template <int ACT>
-__device__ __forceinline__ void finish_tma(const LinearArgs& A, const LinearEpilogue& E, const float* cols, Two xs2, float* v,
-                                           uint8_t* buf, int& next, int row0, int col0, int lane) {
-    Two x[16];
+__device__ __forceinline__ void values(const LinearEpilogue& E, const float* cols, Two xs2, const float* v, Two* x) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(cols + 4 * j);
@@ -353,38 +381,54 @@ __device__ __forceinline__ void finish_tma(const LinearArgs& A, const LinearEpil
         x[2 * j + 1] = fma2(q, s.y, b.y);
         lin_act4<ACT>(x[2 * j], x[2 * j + 1]);
     }
-    const int turns = E.out_bf16 ? 1 : 2;
-    for (int h = 0; h < turns; ++h) {
-        // the store before the last has left this buffer
-        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-        __syncwarp();
-        uint8_t* const to = buf + 2048 * next + lane * 64;
+}
+
+// A box's worth of values (16 of fp32, 32 of bf16) into shared memory.
+template <bool BF16>
+__device__ __forceinline__ void put_box(uint32_t box, int lane, const Two* x) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint4 piece;
-            if (E.out_bf16) {
-                uint32_t w[4];
+    for (int j = 0; j < 4; ++j) st_shared16(piece_at(box, lane, j), BF16 ? packed8(x + 4 * j) : as_uint4(x[2 * j], x[2 * j + 1]));
+}
+
+// The gate of 32 columns as it lies in memory, `row` being this lane's sample's, and its values (1 where there is none). N gates
+// are whole pieces of 16 bytes.
+__device__ __forceinline__ void look_gate(const LinearEpilogue& E, const char* row, int col, uint4* raw) {
+    if (!E.gate) return;
+    const int step = E.gate_bf16 ? 8 : 4;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 f = both(x[4 * j + k]);
-                    w[k] = bf16x2(f.x, f.y);
-                }
-                piece = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-                const ulonglong2 f = h == 0 ? make_ulonglong2(x[2 * j], x[2 * j + 1]) : make_ulonglong2(x[2 * j + 8], x[2 * j + 9]);
-                piece = *reinterpret_cast<const uint4*>(&f);
-            }
-            *reinterpret_cast<uint4*>(to + (j ^ (lane / 2 % 4)) * 16) = piece;
+    for (int j = 0; j < 8; ++j) raw[j] = ld16_if(row + col * (16 / step) + 16 * j, step * j < 32 && col + step * j < E.N);
+}
+__device__ __forceinline__ void gate_pairs(const LinearEpilogue& E, const uint4* raw, Two* g) {
+    if (!E.gate) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) g[j] = two(1.0f, 1.0f);
+    } else if (E.gate_bf16) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            g[4 * j] = widened(raw[j].x), g[4 * j + 1] = widened(raw[j].y), g[4 * j + 2] = widened(raw[j].z), g[4 * j + 3] = widened(raw[j].w);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            g[2 * j] = two(__uint_as_float(raw[j].x), __uint_as_float(raw[j].y)),
+            g[2 * j + 1] = two(__uint_as_float(raw[j].z), __uint_as_float(raw[j].w));
+    }
+}
+
+// The hidden state in a box plus gate times x, in place.
+template <bool BF16>
+__device__ __forceinline__ void add_box(uint32_t box, int lane, const Two* gate, const Two* x) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t at = piece_at(box, lane, j);
+        const uint4 r = ld_shared16(at);
+        if constexpr (BF16) {
+            const Two h[4] = {fma2(gate[4 * j], x[4 * j], widened(r.x)), fma2(gate[4 * j + 1], x[4 * j + 1], widened(r.y)),
+                              fma2(gate[4 * j + 2], x[4 * j + 2], widened(r.z)), fma2(gate[4 * j + 3], x[4 * j + 3], widened(r.w))};
+            st_shared16(at, packed8(h));
+        } else {
+            st_shared16(at, as_uint4(fma2(gate[2 * j], x[2 * j], two(__uint_as_float(r.x), __uint_as_float(r.y))),
+                                     fma2(gate[2 * j + 1], x[2 * j + 1], two(__uint_as_float(r.z), __uint_as_float(r.w)))));
         }
-        fence_generic_to_async();
-        __syncwarp();
-        const int at = col0 + 16 * h;
-        if (at < E.N && lane == 0)
-            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&A.out_map),
-                         "r"(at * (E.out_bf16 ? 2 : 4)), "r"(row0), "r"(smem_addr(buf) + 2048 * next)
-                         : "memory");
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        next ^= 1;
     }
 }
 
@@ -458,9 +502,10 @@ __device__ __forceinline__ void finish_elements(const LinearEpilogue& E, int row
     put_column(E.resid_out, row0 * E.resid_out_stride + col, E.resid_out_stride, E.resid_bf16, rows, v);
 }
 
-template <int CG, bool FP8, bool PASSES>
+template <int CG, bool FP8, bool PASSES, Results RESULTS>
 __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_constant__ LinearArgs A) {
     constexpr int EPI = kEpiWarps;
+    constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden;
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
         after_previous();
@@ -486,6 +531,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
             mbar_init(acc_empty + 8 * i, EPI * CG);
             mbar_init(smem_addr(T.cols_full) + 8 * i, EPI);
         }
+        for (int i = 0; i < EPI * kMaxRing; ++i) mbar_init(smem_addr(T.resid_full) + 8 * i, 1);
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_generic_to_async();
@@ -513,7 +559,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
         const LinearEpilogue E = A.e;
         float* const turn = T.turn[warp];
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
-        int n_done = 0, pass = 0, next_buf = 0;  // tiles, and accumulators, taken
+        int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken
         auto first_row = [&](const Tile& tile) { return (tile.m * CG + (int)rank) * kRows + quarter * 32; };
         // The operands of a tile that do not depend on its sums are loaded a tile ahead: the scale of this lane's row, and
         // where the output leaves by TMA a column's scale and bias by each thread, which the warps then share.
@@ -523,24 +569,68 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
             const Tile tile = tile_at(A, t);
             const int row = first_row(tile) + lane, col = tile.n * A.tile_n + (int)threadIdx.x;
             if (E.x_scale && row < E.M) xs = __uint_as_float(lin_ld1(E.x_scale, row, 0));
-            if (!A.tma_out || (int)threadIdx.x >= A.tile_n || col >= E.N) return;
+            if (DIRECT || (int)threadIdx.x >= A.tile_n || col >= E.N) return;
             if (E.w_scale) scale = __uint_as_float(lin_ld1(E.w_scale, col, 0));
             if (E.bias) bias = __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16));
         };
+        // The hidden state's rows of a tile are on their way to L2 a tile ahead.
+        auto to_l2 = [&](int t) {
+            if (RESULTS == Results::kOut || !E.resid_out || t >= total) return;
+            const Tile tile = tile_at(A, t);
+            const int row = first_row(tile) + lane, col0 = tile.n * A.tile_n, es = E.resid_bf16 ? 2 : 4;
+            if (row >= E.M) return;
+            const char* const q = reinterpret_cast<const char*>(E.resid) + (row * E.resid_stride + col0) * es;
+            const int bytes = min(A.tile_n, E.N - col0) * es;
+            for (int b = 128 * half; b < bytes; b += 128 * (EPI / 4)) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + b));
+        };
+        // Boxes of 2 KB of this warp: the output's, then the ring's, the first two in `turn`.
+        const uint32_t turn_at = smem_addr(turn), more_at = smem_addr(base + stages * stage_bytes) + kTailBytes + warp * A.more_boxes * kBox;
+        auto box_at = [&](int i) { return i < 2 ? turn_at + i * kBox : more_at + (i - 2) * kBox; };
+        const int out_boxes = E.out ? (E.out_bf16 ? 1 : 2) : 0, resid_boxes = E.resid_bf16 ? 1 : 2;
+        auto ring_box = [&](int slot, int i = 0) { return box_at(out_boxes + slot * resid_boxes + i); };
+        // Hidden states are fetched A.ring - 1 of this warp's chunks ahead; `n_chunks` of them are done.
+        int n_chunks = 0, n_fetched = 0;
+        Place held, fetched;
+        int f_tile = first - step, f_chunk = 0, f_chunks = 0, f_row = 0, f_col = 0;
+        auto fetch = [&](int upto) {
+            for (; n_fetched <= upto; ++n_fetched) {
+                f_chunk += EPI / 4;
+                while (f_chunk >= f_chunks) {
+                    if ((f_tile += step) >= total) return;
+                    const Tile tile = tile_at(A, f_tile);
+                    f_row = first_row(tile), f_col = tile.n * A.tile_n;
+                    f_chunks = f_row < E.M ? (min(A.tile_n, E.N - f_col) + 31) / 32 : 0;
+                    f_chunk = half;
+                }
+                const int slot = fetched.s;
+                const uint32_t bar = smem_addr(T.resid_full[warp]) + 8 * slot;
+                fetched.next(A.ring);
+                if (elected()) {
+                    const int x = (f_col + f_chunk * 32) * (E.resid_bf16 ? 2 : 4);
+                    mbar_expect_tx(bar, resid_boxes * kBox);
+                    tma_2d<1>(ring_box(slot), &A.resid_map, x, f_row, bar);
+                    if (!E.resid_bf16) tma_2d<1>(ring_box(slot, 1), &A.resid_map, x + 64, f_row, bar);
+                }
+                __syncwarp();
+            }
+        };
         look_tile(first);
+        to_l2(first);
+        if (HIDDEN) fetch(A.ring - 2);
         for (int t = first; t < total; t += step, ++n_done) {
             const Tile tile = tile_at(A, t);
             const int row0 = first_row(tile), col0 = tile.n * A.tile_n;
             const Two xs2 = two(xs, xs);
             const int chunks = row0 < E.M ? (min(A.tile_n, E.N - col0) + 31) / 32 : 0;
             const float* const cols = T.cols[n_done & 1];
-            if (A.tma_out) {
+            if (!DIRECT) {
                 T.cols[n_done & 1][threadIdx.x] = scale, T.cols[n_done & 1][kAccStride + threadIdx.x] = bias;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(T.cols_full) + 8 * (n_done & 1));
             }
             look_tile(t + step);
-            if (A.tma_out && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT)))
+            to_l2(t + step);
+            if (!DIRECT && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT)))
                 break;
             // the others' operands of a chunk are loaded while the one before it is worked on
             Ahead ahead;
@@ -550,10 +640,17 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
                 if (rows_full) look_ahead<true>(E, spot, c * 32, ahead);
                 else look_ahead<false>(E, spot, c * 32, ahead);
             };
-            if (!A.tma_out && E.wide) spot = spot_of(E, row0, col0, lane);
-            if (half < chunks && !A.tma_out) {
+            if (DIRECT && E.wide) spot = spot_of(E, row0, col0, lane);
+            if (DIRECT && half < chunks) {
                 if (E.wide) look(half);
                 else look_ahead_elements(E, row0, col0 + half * 32 + lane, ahead);
+            }
+            const char* gate_row = nullptr;  // of this lane's row's sample
+            uint4 gate_raw[8];
+            if (HIDDEN && half < chunks) {
+                gate_row = reinterpret_cast<const char*>(E.gate) +
+                           (unsigned)min(row0 + lane, E.M - 1) / E.tokens * E.gate_stride * (E.gate_bf16 ? 2 : 4);
+                look_gate(E, gate_row, col0 + half * 32, gate_raw);
             }
             const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), total_at = lanes + 256;
             constexpr int stride = PASSES ? kAccStride / 2 : kAccStride;
@@ -584,16 +681,63 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
             const uint32_t acc_at = lanes + (pass & 1) * stride;
             if (half >= chunks) release();
             for (int c = half; c < chunks; c += EPI / 4) {
+                Two gate[16];
+                if (HIDDEN) {
+                    gate_pairs(E, gate_raw, gate);
+                    if (c + EPI / 4 < chunks) look_gate(E, gate_row, col0 + (c + EPI / 4) * 32, gate_raw);
+                }
                 float v[32];
                 tmem_load(acc_at + c * 32, v);
                 if (PASSES) tmem_add(total_at + c * 32, v);
                 if (c + EPI / 4 >= chunks) release();
-                if (A.tma_out) {
-                    uint8_t* const buf = reinterpret_cast<uint8_t*>(turn);
+                if constexpr (!DIRECT) {
+                    Two x[16];
+                    if (E.act == CB_ACT_NONE) values<CB_ACT_NONE>(E, cols + c * 32, xs2, v, x);
+                    else if (E.act == CB_ACT_GELU) values<CB_ACT_GELU>(E, cols + c * 32, xs2, v, x);
+                    else values<CB_ACT_SILU>(E, cols + c * 32, xs2, v, x);
                     const int col = col0 + c * 32;
-                    if (E.act == CB_ACT_NONE) finish_tma<CB_ACT_NONE>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
-                    else if (E.act == CB_ACT_GELU) finish_tma<CB_ACT_GELU>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
-                    else finish_tma<CB_ACT_SILU>(A, E, cols + c * 32, xs2, v, buf, next_buf, row0, col, lane);
+                    if constexpr (!HIDDEN) {
+                        for (int h = 0; h < out_boxes; ++h) {
+                            // the box before the last has left
+                            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                            __syncwarp();
+                            const uint32_t box = box_at(n_boxes++ & 1);
+                            if (E.out_bf16) put_box<true>(box, lane, x);
+                            else if (h == 0) put_box<false>(box, lane, x);
+                            else put_box<false>(box, lane, x + 8);
+                            fence_generic_to_async();
+                            __syncwarp();
+                            if (lane == 0 && col + 16 * h < E.N) store_box(&A.out_map, (col + 16 * h) * (E.out_bf16 ? 2 : 4), row0, box);
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    } else {
+                        ok = all(wait(smem_addr(T.resid_full[warp]) + 8 * held.s, held.phase, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
+                        if (!ok) break;
+                        const uint32_t box = ring_box(held.s), box2 = ring_box(held.s, 1);
+                        if (E.resid_bf16) add_box<true>(box, lane, gate, x);
+                        else add_box<false>(box, lane, gate, x), add_box<false>(box2, lane, gate + 8, x + 8);
+                        // the chunk before has left its boxes
+                        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        __syncwarp();
+                        fetch(n_chunks + A.ring - 1);
+                        if (E.out) {
+                            if (E.out_bf16) put_box<true>(box_at(0), lane, x);
+                            else put_box<false>(box_at(0), lane, x), put_box<false>(box_at(1), lane, x + 8);
+                        }
+                        ++n_chunks, held.next(A.ring);
+                        fence_generic_to_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const bool more = col + 16 < E.N;
+                            if (E.out) {
+                                store_box(&A.out_map, col * (E.out_bf16 ? 2 : 4), row0, box_at(0));
+                                if (!E.out_bf16 && more) store_box(&A.out_map, col * 4 + 64, row0, box_at(1));
+                            }
+                            store_box(&A.resid_out_map, col * (E.resid_bf16 ? 2 : 4), row0, box);
+                            if (!E.resid_bf16 && more) store_box(&A.resid_out_map, col * 4 + 64, row0, box2);
+                        }
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
                     continue;
                 }
                 // a row per lane to rows of 32 columns: 16-byte pieces, swizzled against bank conflicts
@@ -614,12 +758,20 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
                     if (rows_full) finish<true>(E, spot, c * 32, now, u);
                     else finish<false>(E, spot, c * 32, now, u);
                 } else {
-                    finish_elements(E, row0, col0 + c * 32 + lane, lane, ahead, turn);
+                    const Ahead now = ahead;
                     if (c + EPI / 4 < chunks) look_ahead_elements(E, row0, col0 + (c + EPI / 4) * 32 + lane, ahead);
+                    finish_elements(E, row0, col0 + c * 32 + lane, lane, now, turn);
                 }
                 __syncwarp();
             }
+            if (!ok) break;
         }
+        for (; n_chunks < n_fetched; ++n_chunks, held.next(A.ring))  // given up: hidden states under way land first
+            if (!all(wait(smem_addr(T.resid_full[warp]) + 8 * held.s, held.phase, abort, A.status, CB_DEV_DRAIN_TIMEOUT))) {
+                const unsigned long long t0 = now_ns();
+                while (now_ns() - t0 < kMinDrainNs) {}
+                break;
+            }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp == EPI) {  // ---- products
         if (rank == 0) {
@@ -698,11 +850,10 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
     }
 }
 
-using LinearKernel = void (*)(LinearArgs);
-template <bool PASSES>
+template <Results RESULTS, bool PASSES>
 LinearKernel kernel_of(int cg, bool fp8) {
-    if (cg == 2) return fp8 ? linear_kernel<2, true, PASSES> : linear_kernel<2, false, PASSES>;
-    return fp8 ? linear_kernel<1, true, PASSES> : linear_kernel<1, false, PASSES>;
+    if (cg == 2) return fp8 ? linear_kernel<2, true, PASSES, RESULTS> : linear_kernel<2, false, PASSES, RESULTS>;
+    return fp8 ? linear_kernel<1, true, PASSES, RESULTS> : linear_kernel<1, false, PASSES, RESULTS>;
 }
 
 }  // namespace
