@@ -233,17 +233,9 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     const struct {
         const void* p;
         int dtype;
-        long long stride;
-    } used[] = {{out, io->out_dtype, ep.out_stride},     {resid, io->resid_dtype, ep.resid_stride},
-                {gate, io->gate_dtype, ep.gate_stride},  {resid_out, io->resid_dtype, ep.resid_out_stride},
-                {d.bias, d.bias_dtype, 0},              {d.w_scale, CB_FP32, 0}};
-    ep.wide = N % 4 == 0;
-    for (const auto& u : used) {
-        if (!u.p) continue;
-        const size_t s = bytes_of(u.dtype);
-        if (!on_grid(u.p, s)) return CB_ERR_ALIGN;
-        ep.wide = ep.wide && on_grid(u.p, 4 * s) && u.stride % 4 == 0;
-    }
+    } used[] = {{out, io->out_dtype}, {resid, io->resid_dtype}, {gate, io->gate_dtype}, {resid_out, io->resid_dtype}};
+    for (const auto& u : used)
+        if (u.p && !on_grid(u.p, bytes_of(u.dtype))) return CB_ERR_ALIGN;
     const Device* dev = nullptr;
     int rc = device_info(&dev);
     if (rc != CB_OK) return rc;
@@ -265,7 +257,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
     rc = results_by_tma(io, &a);
     if (rc != CB_OK) return rc;
-    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.more_boxes)) / linear_stage_bytes(cg, a.tile_n));
+    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.results, a.more_boxes)) / linear_stage_bytes(cg, a.tile_n));
     const int tiles = a.tiles_m * a.tiles_n, units = cg == 2 ? dev->pairs : dev->sms;
     const int grid = cg * (tiles < units ? tiles : units);
     const cudaStream_t s = (cudaStream_t)stream;

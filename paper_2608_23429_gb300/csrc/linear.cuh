@@ -17,7 +17,6 @@ struct LinearEpilogue {
     int act;
     unsigned tokens;       // rows of one sample
     int out_bf16, resid_bf16, bias_bf16, gate_bf16;
-    int wide;              // four columns of every operand of the epilogue are one aligned vector
     long long out_stride, resid_stride, resid_out_stride, gate_stride;  // elements
     const float *x_scale, *w_scale;
     const void *bias, *resid, *gate;
@@ -70,7 +69,7 @@ cudaError_t launch_linear_pack(LinearPackArgs& a, cudaStream_t s);
 // The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows. prepare_linear raises the kernels' shared-memory
 // limit and tells how many pairs of CTAs run at once.
 size_t linear_stage_bytes(int cg, int tile_n);
-size_t linear_fixed_bytes(int more_boxes);  // shared memory besides the stages
+size_t linear_fixed_bytes(Results r, int more_boxes);  // shared memory besides the stages
 constexpr int kBox = 2048, kMaxRing = 6;
 constexpr int kMaxLinStages = 12;
 cudaError_t prepare_linear(size_t smem, int* pairs);
@@ -90,16 +89,6 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
 
 // Loads that no store of the kernel is ordered against: inputs do not overlap outputs, and a hidden state that is
 // updated in place is read by the thread that writes it.
-__device__ __forceinline__ uint4 lin_ld16(const void* p) {
-    uint4 r;
-    asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-    return r;
-}
-__device__ __forceinline__ uint2 lin_ld8(const void* p) {
-    uint2 r;
-    asm("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
-    return r;
-}
 // One element as fp32 bits, or its half of them.
 __device__ __forceinline__ uint32_t lin_ld1(const void* p, long long e, int bf16) {
     uint32_t r = 0;
@@ -113,22 +102,6 @@ __device__ __forceinline__ uint32_t lin_ld1(const void* p, long long e, int bf16
     return r;
 }
 
-// Four consecutive elements of an aligned row, as they lie in memory, and their values.
-__device__ __forceinline__ uint4 lin_raw4(const void* p, long long e, int bf16) {
-    if (!bf16) return lin_ld16(reinterpret_cast<const float*>(p) + e);
-    const uint2 r = lin_ld8(reinterpret_cast<const uint16_t*>(p) + e);
-    return make_uint4(r.x, r.y, 0, 0);
-}
-__device__ __forceinline__ float4 lin_val4(uint4 r, int bf16) {
-    if (bf16) r = make_uint4(r.x << 16, r.x & 0xFFFF0000u, r.y << 16, r.y & 0xFFFF0000u);
-    return make_float4(__uint_as_float(r.x), __uint_as_float(r.y), __uint_as_float(r.z), __uint_as_float(r.w));
-}
-__device__ __forceinline__ void lin_put4(void* p, long long e, int bf16, float4 v) {
-    if (bf16)
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p) + e) = make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
-    else
-        *reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + e) = v;
-}
 __device__ __forceinline__ void lin_put1(void* p, long long e, int bf16, float v) {
     if (bf16)
         reinterpret_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(v);

@@ -5,7 +5,7 @@ namespace cbk {
 
 size_t linear_stage_bytes(int cg, int tile_n) { return (size_t)(kRows + tile_n / cg) * kSlab; }
 
-size_t linear_fixed_bytes(int more_boxes) { return kTailBytes + (size_t)kEpiWarps * more_boxes * kBox; }
+size_t linear_fixed_bytes(Results r, int more_boxes) { return kTailBytes + (size_t)epi_warps(r) * (kTurn + more_boxes * kBox); }
 
 cudaError_t prepare_linear(size_t smem, int* pairs) {
     for (int i = 0; i < 8; ++i)
@@ -19,7 +19,7 @@ cudaError_t prepare_linear(size_t smem, int* pairs) {
     at.val.clusterDim.x = 2, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(2);
-    c.blockDim = dim3(kLinearThreads);
+    c.blockDim = dim3(linear_threads(Results::kOut));
     c.dynamicSmemBytes = smem;
     c.attrs = &at;
     c.numAttrs = 1;
@@ -34,8 +34,8 @@ cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaS
     at[1].val.clusterDim.x = (unsigned)cg, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)grid);
-    c.blockDim = dim3(kLinearThreads);
-    c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + linear_fixed_bytes(a.more_boxes);
+    c.blockDim = dim3(linear_threads(a.results));
+    c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + linear_fixed_bytes(a.results, a.more_boxes);
     c.stream = s;
     c.attrs = at;
     c.numAttrs = cg == 2 ? 2 : 1;

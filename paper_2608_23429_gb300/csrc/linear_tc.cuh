@@ -5,8 +5,7 @@
 //   one warp fills a ring of stages by TMA with slabs of 128 bytes of K: 128 rows of x and tile_n / CG rows of w, in
 //     the 128-byte swizzle that the tensor cores read,
 //   one thread issues tcgen05.mma on them, sums in TMEM (two accumulators of up to 256 columns each),
-//   eight warps take a finished accumulator out of TMEM while the next tile is summed, turn it in shared memory so
-//     that their accesses to global memory are rows, and apply the epilogue.
+//   eight or sixteen warps take a finished accumulator out of TMEM while the next tile is summed, and apply the epilogue.
 // A pair of CTAs shares one tile: each loads its 128 rows of x and half of the tile's rows of w, the first one's
 // thread issues for both, and each holds the sums of its own rows.
 //
@@ -33,15 +32,18 @@ namespace {
 constexpr int kRows = 128;        // rows of x per CTA
 constexpr int kSlab = 128;        // bytes of K per stage
 constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the other (half of it where there are passes)
-constexpr int kEpiWarps = 8;      // two for each quarter of the TMEM lanes
-constexpr int kLinearThreads = 32 * (kEpiWarps + 2);
+// Warps of the epilogue: two for each quarter of the TMEM lanes, or four where the threads load and store the results themselves
+// and wait for that (GB300, 8192 x 8191 x 512 bf16 with a gated fp32 hidden state: eight warps, 32 rows at once each, 282 us,
+// sixteen, eight rows at once, 195).
+__host__ __device__ constexpr int epi_warps(Results r) { return r == Results::kDirect ? 16 : 8; }
+__host__ __device__ constexpr int linear_threads(Results r) { return 32 * (epi_warps(r) + 2); }
+constexpr int kTurn = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
 constexpr unsigned long long kLimitNs = 1000000000ull;
 
-struct alignas(16) Tail {  // behind the stages
-    float turn[kEpiWarps][32 * 32];
+struct alignas(16) Tail {  // behind the stages and the epilogue's warps' kTurn each
     float cols[2][2 * kAccStride];  // scales and biases of a tile's columns (where the output leaves by TMA)
     uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2], cols_full[2];
-    uint64_t resid_full[kEpiWarps][kMaxRing];
+    uint64_t resid_full[epi_warps(Results::kHidden)][kMaxRing];
     uint32_t tmem;
     int abort;
 };
@@ -232,113 +234,7 @@ __device__ __forceinline__ bool drain(Place p, int fills, int stages, uint32_t e
     return true;
 }
 
-// ---- epilogue of 32 rows by 32 columns of a warp. Wide: a thread has the rows row0 + lane / 8 + 4 i and four columns.
-
-struct Ahead {
-    uint4 scale, bias, gate, resid[8];
-};
-
-// A thread's part of a tile: where its first row and column lie, and the bytes to the row after next but two.
-struct Spot {
-    int row, col;            // of its first element in the tile's first chunk
-    long long gate;          // element of the gate of the warp's first row's sample
-    unsigned next;           // rows from here on belong to other samples
-    const char* resid;
-    char *out, *resid_out;
-    long long resid_step, out_step, resid_out_step;
-};
-
-__device__ __forceinline__ Spot spot_of(const LinearEpilogue& E, int row0, int col0, int lane) {
-    Spot p;
-    p.row = row0 + lane / 8, p.col = col0 + lane % 8 * 4;
-    const int os = E.out_bf16 ? 2 : 4, rs = E.resid_bf16 ? 2 : 4;
-    p.out = reinterpret_cast<char*>(E.out) + (p.row * E.out_stride + p.col) * os;
-    p.resid = reinterpret_cast<const char*>(E.resid) + (p.row * E.resid_stride + p.col) * rs;
-    p.resid_out = reinterpret_cast<char*>(E.resid_out) + (p.row * E.resid_out_stride + p.col) * rs;
-    p.out_step = 4 * E.out_stride * os, p.resid_step = 4 * E.resid_stride * rs, p.resid_out_step = 4 * E.resid_out_stride * rs;
-    const unsigned sample = E.gate ? (unsigned)row0 / E.tokens : 0;
-    p.gate = sample * E.gate_stride + p.col;
-    p.next = (sample + 1) * E.tokens;
-    return p;
-}
-
-// The operands of the chunk that starts `at` columns into the tile. FULL: all 32 rows exist.
-template <bool FULL>
-__device__ __forceinline__ void look_ahead(const LinearEpilogue& E, const Spot& p, int at, Ahead& a) {
-    const int col = p.col + at;
-    if (col >= E.N) return;  // N is a multiple of four
-    if (E.w_scale) a.scale = lin_raw4(E.w_scale, col, 0);
-    if (E.bias) a.bias = lin_raw4(E.bias, col, E.bias_bf16);
-    if (!E.resid_out) return;
-    if (E.gate) a.gate = lin_raw4(E.gate, p.gate + at, E.gate_bf16);
-    if (E.resid_bf16) {
-        const char* q = p.resid + 2 * at;
-#pragma unroll
-        for (int i = 0; i < 8; ++i, q += p.resid_step)
-            if (FULL || p.row + 4 * i < E.M) {
-                const uint2 v = lin_ld8(q);
-                a.resid[i].x = v.x, a.resid[i].y = v.y;
-            }
-    } else {
-        const char* q = p.resid + 4 * at;
-#pragma unroll
-        for (int i = 0; i < 8; ++i, q += p.resid_step)
-            if (FULL || p.row + 4 * i < E.M) a.resid[i] = lin_ld16(q);
-    }
-}
-
-// Eight rows of four columns from q on, `step` bytes apart.
-template <bool FULL>
-__device__ __forceinline__ void put_rows(char* q, long long step, int bf16, int rows, const ulonglong2* v) {
-    if (bf16) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i, q += step) {
-            const float2 lo = both(v[i].x), hi = both(v[i].y);
-            if (FULL || 4 * i < rows) *reinterpret_cast<uint2*>(q) = make_uint2(bf16x2(lo.x, lo.y), bf16x2(hi.x, hi.y));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i, q += step)
-            if (FULL || 4 * i < rows) *reinterpret_cast<ulonglong2*>(q) = v[i];
-    }
-}
-
-template <int ACT>
-__device__ __forceinline__ void activate(const float4& s, const float4& b, ulonglong2* v) {
-    const Two s0 = two(s.x, s.y), s1 = two(s.z, s.w), b0 = two(b.x, b.y), b1 = two(b.z, b.w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i].x = fma2(v[i].x, s0, b0);
-        v[i].y = fma2(v[i].y, s1, b1);
-        lin_act4<ACT>(v[i].x, v[i].y);
-    }
-}
-
-template <bool FULL>
-__device__ __forceinline__ void finish(const LinearEpilogue& E, const Spot& p, int at, const Ahead& a, ulonglong2* v) {
-    const int col = p.col + at, rows = E.M - p.row;
-    if (col >= E.N) return;
-    const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-    const float4 s = E.w_scale ? lin_val4(a.scale, 0) : one;
-    const float4 b = E.bias ? lin_val4(a.bias, E.bias_bf16) : make_float4(0.f, 0.f, 0.f, 0.f);
-    if (E.act == CB_ACT_NONE) activate<CB_ACT_NONE>(s, b, v);
-    else if (E.act == CB_ACT_GELU) activate<CB_ACT_GELU>(s, b, v);
-    else activate<CB_ACT_SILU>(s, b, v);
-    if (E.out) put_rows<FULL>(p.out + at * (E.out_bf16 ? 2 : 4), p.out_step, E.out_bf16, rows, v);
-    if (!E.resid_out) return;
-    float4 g = E.gate ? lin_val4(a.gate, E.gate_bf16) : one;
-    const bool mixed = E.gate && (unsigned)(p.row - p.row % 4 + 31) >= p.next;  // the warp's rows are of several samples
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const unsigned row = (unsigned)(p.row + 4 * i);
-        if (mixed && row >= p.next && (FULL || row < (unsigned)E.M))
-            g = lin_val4(lin_raw4(E.gate, (long long)(row / E.tokens) * E.gate_stride + col, E.gate_bf16), E.gate_bf16);
-        const float4 r = lin_val4(a.resid[i], E.resid_bf16);
-        v[i].x = fma2(two(g.x, g.y), v[i].x, two(r.x, r.y));
-        v[i].y = fma2(two(g.z, g.w), v[i].y, two(r.z, r.w));
-    }
-    put_rows<FULL>(p.resid_out + at * (E.resid_bf16 ? 2 : 4), p.resid_out_step, E.resid_bf16, rows, v);
-}
+// ---- epilogue of 32 rows by 32 columns of a warp (a chunk)
 
 // Results by TMA: a row per lane, as the sums come from TMEM. Columns' scale and bias are read from shared memory by all lanes
 // alike; hidden states come in and results leave in boxes of 32 rows of 64 bytes (a chunk of 32 columns is one of bf16 or two of
@@ -432,79 +328,80 @@ __device__ __forceinline__ void add_box(uint32_t box, int lane, const Two* gate,
     }
 }
 
-// The same by elements, a column per lane, for rows that are not made of aligned fours.
+// Results by the threads, for rows off the 16-byte grid: a column per lane, eight rows at a time, whose hidden states are loaded
+// while the eight before are worked on.
 
-__device__ __forceinline__ void look_ahead_elements(const LinearEpilogue& E, int row0, int col, Ahead& a) {
-    if (col >= E.N) return;
-    a.scale.x = E.w_scale ? lin_ld1(E.w_scale, col, 0) : __float_as_uint(1.0f);
-    a.bias.x = E.bias ? lin_ld1(E.bias, col, E.bias_bf16) : 0;
-    if (!E.resid_out) return;
-    a.gate.x = __float_as_uint(1.0f);
-    if (E.gate) a.gate.x = lin_ld1(E.gate, ((unsigned)row0 / E.tokens) * E.gate_stride + col, E.gate_bf16);
-    const int rows = E.M - row0, step = E.resid_bf16 ? 2 : 4;
-    const char* q = reinterpret_cast<const char*>(E.resid) + (row0 * E.resid_stride + col) * step;
-#pragma unroll
-    for (int i = 0; i < 32; ++i, q += E.resid_stride * step)
-        if (i < rows) {
-            uint32_t& w = i % 4 == 0 ? a.resid[i / 4].x : i % 4 == 1 ? a.resid[i / 4].y : i % 4 == 2 ? a.resid[i / 4].z : a.resid[i / 4].w;
-            w = lin_ld1(q, 0, E.resid_bf16);
-        }
+struct Column {  // of a lane
+    float scale, bias, gate;  // gate: of the warp's first row's sample
+};
+
+__device__ __forceinline__ Column look_column(const LinearEpilogue& E, int row0, int col) {
+    Column k{1.0f, 0.0f, 1.0f};
+    if (col >= E.N) return k;
+    if (E.w_scale) k.scale = __uint_as_float(lin_ld1(E.w_scale, col, 0));
+    if (E.bias) k.bias = __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16));
+    if (E.gate) k.gate = __uint_as_float(lin_ld1(E.gate, ((unsigned)row0 / E.tokens) * E.gate_stride + col, E.gate_bf16));
+    return k;
 }
 
-__device__ __forceinline__ void put_column(void* p, long long e, long long stride, int bf16, int rows, const float* v) {
-    if (bf16) {
-        __nv_bfloat16* q = reinterpret_cast<__nv_bfloat16*>(p) + e;
+__device__ __forceinline__ void look_rows(const LinearEpilogue& E, int row, int col, uint32_t* r) {
+    if (!E.resid_out || col >= E.N) return;
+    const int es = E.resid_bf16 ? 2 : 4;
+    const char* q = reinterpret_cast<const char*>(E.resid) + (row * E.resid_stride + col) * es;
+    const long long step = E.resid_stride * es;
 #pragma unroll
-        for (int i = 0; i < 32; ++i, q += stride)
-            if (i < rows) *q = __float2bfloat16_rn(v[i]);
-    } else {
-        float* q = reinterpret_cast<float*>(p) + e;
+    for (int i = 0; i < 8; ++i, q += step)
+        if (row + i < E.M) r[i] = lin_ld1(q, 0, E.resid_bf16);
+}
+
+__device__ __forceinline__ void put_rows(const LinearEpilogue& E, void* p, long long stride, int bf16, int row, int col, const float* v) {
+    const int es = bf16 ? 2 : 4;
+    char* q = reinterpret_cast<char*>(p) + (row * stride + col) * es;
+    const long long step = stride * es;
 #pragma unroll
-        for (int i = 0; i < 32; ++i, q += stride)
-            if (i < rows) *q = v[i];
-    }
+    for (int i = 0; i < 8; ++i, q += step)
+        if (row + i < E.M) lin_put1(q, 0, bf16, v[i]);
 }
 
 template <int ACT>
-__device__ __forceinline__ void activate_column(float s, float b, float* v) {
+__device__ __forceinline__ void activate(const Column& k, float* v) {
 #pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-        Two x = fma2(two(v[i], v[i + 1]), two(s, s), two(b, b)), y = fma2(two(v[i + 2], v[i + 3]), two(s, s), two(b, b));
+    for (int i = 0; i < 8; i += 4) {
+        Two x = fma2(two(v[i], v[i + 1]), two(k.scale, k.scale), two(k.bias, k.bias));
+        Two y = fma2(two(v[i + 2], v[i + 3]), two(k.scale, k.scale), two(k.bias, k.bias));
         lin_act4<ACT>(x, y);
         const float2 f = both(x), g = both(y);
         v[i] = f.x, v[i + 1] = f.y, v[i + 2] = g.x, v[i + 3] = g.y;
     }
 }
 
-__device__ __forceinline__ void finish_elements(const LinearEpilogue& E, int row0, int col, int lane, const Ahead& a,
-                                                const float* turn) {
+// Eight rows from `row` on (row0: the warp's first).
+__device__ __forceinline__ void finish_rows(const LinearEpilogue& E, int row0, int row, int col, const Column& k, const uint32_t* r, float* v) {
     if (col >= E.N) return;
-    const int rows = E.M - row0;
-    float v[32];
-#pragma unroll
-    for (int r = 0; r < 32; ++r) v[r] = turn[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + lane % 4];
-    const float scale = __uint_as_float(a.scale.x), bias = __uint_as_float(a.bias.x);
-    if (E.act == CB_ACT_NONE) activate_column<CB_ACT_NONE>(scale, bias, v);
-    else if (E.act == CB_ACT_GELU) activate_column<CB_ACT_GELU>(scale, bias, v);
-    else activate_column<CB_ACT_SILU>(scale, bias, v);
-    if (E.out) put_column(E.out, row0 * E.out_stride + col, E.out_stride, E.out_bf16, rows, v);
+    if (E.act == CB_ACT_NONE) activate<CB_ACT_NONE>(k, v);
+    else if (E.act == CB_ACT_GELU) activate<CB_ACT_GELU>(k, v);
+    else activate<CB_ACT_SILU>(k, v);
+    if (E.out) put_rows(E, E.out, E.out_stride, E.out_bf16, row, col, v);
     if (!E.resid_out) return;
     const unsigned next = ((unsigned)row0 / E.tokens + 1) * E.tokens;  // rows from here on belong to other samples
-    float g = __uint_as_float(a.gate.x);
+    if (!E.gate || (unsigned)row + 7 < next) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const unsigned row = (unsigned)(row0 + i);
-        if (E.gate && row >= next && i < rows)
-            g = __uint_as_float(lin_ld1(E.gate, (long long)(row / E.tokens) * E.gate_stride + col, E.gate_bf16));
-        const uint4& x = a.resid[i / 4];
-        v[i] = fmaf(g, v[i], __uint_as_float(i % 4 == 0 ? x.x : i % 4 == 1 ? x.y : i % 4 == 2 ? x.z : x.w));
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(k.gate, v[i], __uint_as_float(r[i]));
+    } else {
+        for (int i = 0; i < 8; ++i) {
+            const unsigned at = (unsigned)min(row + i, E.M - 1) / E.tokens;
+            const float g = __uint_as_float(lin_ld1(E.gate, at * E.gate_stride + col, E.gate_bf16));
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i == j) v[j] = fmaf(g, v[j], __uint_as_float(r[j]));
+        }
     }
-    put_column(E.resid_out, row0 * E.resid_out_stride + col, E.resid_out_stride, E.resid_bf16, rows, v);
+    put_rows(E, E.resid_out, E.resid_out_stride, E.resid_bf16, row, col, v);
 }
 
 template <int CG, bool FP8, bool PASSES, Results RESULTS>
-__global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_constant__ LinearArgs A) {
-    constexpr int EPI = kEpiWarps;
+__global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(const __grid_constant__ LinearArgs A) {
+    constexpr int EPI = epi_warps(RESULTS);
     constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden;
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
@@ -515,7 +412,8 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int w_rows = A.tile_n / CG, stage_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
-    Tail& T = *reinterpret_cast<Tail*>(base + stages * stage_bytes);
+    uint8_t* const turns = base + stages * stage_bytes;
+    Tail& T = *reinterpret_cast<Tail*>(turns + EPI * kTurn);
     const uint32_t ring = smem_addr(base);
     const uint32_t full = smem_addr(T.full), empty = smem_addr(T.empty);
     const uint32_t acc_full = smem_addr(T.acc_full), acc_empty = smem_addr(T.acc_empty);
@@ -531,7 +429,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
             mbar_init(acc_empty + 8 * i, EPI * CG);
             mbar_init(smem_addr(T.cols_full) + 8 * i, EPI);
         }
-        for (int i = 0; i < EPI * kMaxRing; ++i) mbar_init(smem_addr(T.resid_full) + 8 * i, 1);
+        for (int i = 0; HIDDEN && i < EPI * kMaxRing; ++i) mbar_init(smem_addr(T.resid_full) + 8 * i, 1);
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_generic_to_async();
@@ -557,7 +455,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
     const int first = blockIdx.x / CG, step = gridDim.x / CG, total = A.tiles_m * A.tiles_n;
     if (warp < EPI) {  // ---- epilogue
         const LinearEpilogue E = A.e;
-        float* const turn = T.turn[warp];
+        float* const turn = reinterpret_cast<float*>(turns + warp * kTurn);
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
         int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken
         auto first_row = [&](const Tile& tile) { return (tile.m * CG + (int)rank) * kRows + quarter * 32; };
@@ -584,7 +482,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
             for (int b = 128 * half; b < bytes; b += 128 * (EPI / 4)) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + b));
         };
         // Boxes of 2 KB of this warp: the output's, then the ring's, the first two in `turn`.
-        const uint32_t turn_at = smem_addr(turn), more_at = smem_addr(base + stages * stage_bytes) + kTailBytes + warp * A.more_boxes * kBox;
+        const uint32_t turn_at = smem_addr(turn), more_at = smem_addr(&T) + kTailBytes + warp * A.more_boxes * kBox;
         auto box_at = [&](int i) { return i < 2 ? turn_at + i * kBox : more_at + (i - 2) * kBox; };
         const int out_boxes = E.out ? (E.out_bf16 ? 1 : 2) : 0, resid_boxes = E.resid_bf16 ? 1 : 2;
         auto ring_box = [&](int slot, int i = 0) { return box_at(out_boxes + slot * resid_boxes + i); };
@@ -632,18 +530,11 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
             to_l2(t + step);
             if (!DIRECT && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT)))
                 break;
-            // the others' operands of a chunk are loaded while the one before it is worked on
-            Ahead ahead;
-            Spot spot;
-            const bool rows_full = row0 + 32 <= E.M;
-            auto look = [&](int c) {
-                if (rows_full) look_ahead<true>(E, spot, c * 32, ahead);
-                else look_ahead<false>(E, spot, c * 32, ahead);
-            };
-            if (DIRECT && E.wide) spot = spot_of(E, row0, col0, lane);
+            Column column;
+            uint32_t rows_raw[8];
             if (DIRECT && half < chunks) {
-                if (E.wide) look(half);
-                else look_ahead_elements(E, row0, col0 + half * 32 + lane, ahead);
+                column = look_column(E, row0, col0 + half * 32 + lane);
+                look_rows(E, row0, col0 + half * 32 + lane, rows_raw);
             }
             const char* gate_row = nullptr;  // of this lane's row's sample
             uint4 gate_raw[8];
@@ -746,21 +637,20 @@ __global__ void __launch_bounds__(kLinearThreads, 1) linear_kernel(const __grid_
                     *reinterpret_cast<ulonglong2*>(&turn[lane * 32 + (j ^ (lane & 7)) * 4]) =
                         make_ulonglong2(mul2(two(v[4 * j], v[4 * j + 1]), xs2), mul2(two(v[4 * j + 2], v[4 * j + 3]), xs2));
                 __syncwarp();
-                if (E.wide) {
-                    ulonglong2 u[8];
+                const int col = col0 + c * 32 + lane, next_col = c + EPI / 4 < chunks ? col + EPI * 8 : E.N;
+                const Column now = column;
+                column = look_column(E, row0, next_col);
+#pragma unroll 1
+                for (int row = 0; row < 32; row += 8) {
+                    uint32_t r[8];
+                    float f[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int r = 4 * i + lane / 8;
-                        u[i] = *reinterpret_cast<const ulonglong2*>(&turn[r * 32 + ((lane & 7) ^ (r & 7)) * 4]);
+                        r[i] = rows_raw[i];
+                        f[i] = turn[(row + i) * 32 + ((lane / 4) ^ i) * 4 + lane % 4];
                     }
-                    const Ahead now = ahead;
-                    if (c + EPI / 4 < chunks) look(c + EPI / 4);
-                    if (rows_full) finish<true>(E, spot, c * 32, now, u);
-                    else finish<false>(E, spot, c * 32, now, u);
-                } else {
-                    const Ahead now = ahead;
-                    if (c + EPI / 4 < chunks) look_ahead_elements(E, row0, col0 + (c + EPI / 4) * 32 + lane, ahead);
-                    finish_elements(E, row0, col0 + c * 32 + lane, lane, now, turn);
+                    look_rows(E, row0 + (row + 8) % 32, row + 8 < 32 ? col : next_col, rows_raw);
+                    finish_rows(E, row0, row0 + row, col, now, r, f);
                 }
                 __syncwarp();
             }
