@@ -67,29 +67,19 @@ int device_info(const Device** out) {
     return CB_OK;
 }
 
-// Copies of the operands that are not on the 16-byte grid (x, w: nullptr where they are), in stream order; `pack` then tells
-// where they lie, and the caller gives `copies` back behind the kernel that reads them.
-int make_copies(const Device& dev, const void* x, long long x_row, int M, const void* w, long long w_row, int N, int bytes,
-                LinearPackArgs* pack, char** copies, cudaStream_t s) {
+// Copies of the operands that are not on the 16-byte grid (x, w: nullptr where they are) into `at`, in stream order; `pack` then
+// tells where they lie.
+size_t copies_bytes(const void* x, int M, const void* w, int N, int bytes) {
+    const size_t row = (size_t)(bytes + 31) / 32 * 32;
+    return ((x ? M * row : 0) + 255) / 256 * 256 + ((w ? N * row : 0) + 255) / 256 * 256;
+}
+cudaError_t make_copies(const void* x, long long x_row, int M, const void* w, long long w_row, int N, int bytes, char* at, bool overlap,
+                        LinearPackArgs* pack, cudaStream_t s) {
     const unsigned chunks = (unsigned)(bytes + 31) / 32;
-    const size_t x_size = x ? ((size_t)M * chunks * 32 + 255) / 256 * 256 : 0, w_size = w ? (size_t)N * chunks * 32 : 0;
-    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    void* at = nullptr;
-    cudaError_t e = cudaStreamIsCapturing(s, &capture);
-    if (e == cudaSuccess) e = cudaMallocFromPoolAsync(&at, x_size + w_size, dev.pool, s);
-    if (e != cudaSuccess) {
-        (void)cudaGetLastError();  // returned here, so not left for a check of the caller's own launches
-        return cuda_error(e, "linear workspace");
-    }
-    *copies = static_cast<char*>(at);
-    if (x) pack->o[0] = {static_cast<const char*>(x), *copies, M, x_row, bytes, chunks};
-    if (w) pack->o[1] = {static_cast<const char*>(w), *copies + x_size, N, w_row, bytes, chunks};
-    pack->overlap = capture == cudaStreamCaptureStatusNone;  // in a graph it follows the allocation, not a kernel
-    e = launch_linear_pack(*pack, s);
-    if (e == cudaSuccess) return CB_OK;
-    (void)cudaFreeAsync(at, s);
-    *copies = nullptr;
-    return cuda_error(e, "linear launch");
+    if (x) pack->o[0] = {static_cast<const char*>(x), at, M, x_row, bytes, chunks};
+    if (w) pack->o[1] = {static_cast<const char*>(w), at + copies_bytes(x, M, nullptr, 0, bytes), N, w_row, bytes, chunks};
+    pack->overlap = overlap;
+    return launch_linear_pack(*pack, s);
 }
 
 // Rows of bytes, in boxes of `box` rows by `wide` bytes (128, or 64), swizzled by as much; behind the ends zeros come in
@@ -148,18 +138,26 @@ constexpr int kFewRows = 32;
 // lose less, 7e-7 at K = 16384).
 constexpr int kPassBf16 = 8, kPassE4m3 = 64;
 
-// CTAs per tile and the tile's columns: the fewest rounds of tiles, each as long as its loads (16 KB of x and
-// 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take.
-void choose_tile(const Device& dev, int M, int N, int most, int* cg, int* tile_n) {
+// CTAs per tile, the tile's columns and the parts of K: the fewest rounds of tiles, each as long as its loads (16 KB of x and
+// 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take, in clocks. Parts cost a launch that adds them, and
+// their sums' way through L2. GB300, calls back to back, in one part and in the chosen ones: 256 x 1152 x 4608 bf16 with a gated
+// hidden state 15.3 and 12.5 us, 77 x 1152 x 4096 13.3 and 9.4, 640 x 72 x 16384 41.8 and 12.7, 1500 x 300 x 12000 32.8 and 16.6;
+// up to 16 parts of four slabs gave the same.
+constexpr double kJoinClocks = 5000, kJoinBytesPerClock = 1300;
+constexpr int kMaxParts = 8, kPartSlabs = 8;  // no part is shorter
+void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int* cg, int* tile_n, int* parts) {
     double best = 1e300;
-    for (int g = 2; g >= 1; --g)
-        for (int n = most; n >= 32; n -= 32) {
-            if (n > 32 && n - 32 >= N) continue;
-            const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n);
-            const long long units = g == 2 ? dev.pairs : dev.sms;
-            const double cost = (double)((tiles + units - 1) / units) * (256.0 + 2.0 * n / g);
-            if (cost < best * 0.999) best = cost, *cg = g, *tile_n = n;
-        }
+    for (int p = 1; p <= kMaxParts && (p == 1 || k_blocks / p >= kPartSlabs); ++p)
+        for (int g = 2; g >= 1; --g)
+            for (int n = most; n >= 32; n -= 32) {
+                if (n > 32 && n - 32 >= N) continue;
+                const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n) * p;
+                const long long units = g == 2 ? dev.pairs : dev.sms;
+                if (p > 1 && tiles > units) continue;
+                const double join = p > 1 ? kJoinClocks + 4.0 * p * M * N / kJoinBytesPerClock : 0.0;
+                const double cost = (double)((tiles + units - 1) / units) * ((k_blocks + p - 1) / p) * (256.0 + 2.0 * n / g) + join;
+                if (cost < best * 0.999) best = cost, *cg = g, *tile_n = n, *parts = p;
+            }
 }
 
 }  // namespace
@@ -251,35 +249,61 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     // fp32 results: passes over K (see linear_tc.cuh)
     const bool fp32 = (out && !ep.out_bf16) || (resid_out && !ep.resid_bf16);
     a.pass_blocks = fp32 ? (d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks;
-    a.passes = (a.k_blocks + a.pass_blocks - 1) / a.pass_blocks;
-    choose_tile(*dev, ep.M, ep.N, a.passes > 1 ? 128 : 256, &cg, &a.tile_n);
+    choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks ? 128 : 256, &cg, &a.tile_n, &a.parts);
+    a.part_blocks = (a.k_blocks + a.parts - 1) / a.parts;
+    a.parts = (a.k_blocks + a.part_blocks - 1) / a.part_blocks;
+    a.passes = (a.part_blocks + a.pass_blocks - 1) / a.pass_blocks;
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
-    rc = results_by_tma(io, &a);
-    if (rc != CB_OK) return rc;
-    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.results, a.more_boxes)) / linear_stage_bytes(cg, a.tile_n));
-    const int tiles = a.tiles_m * a.tiles_n, units = cg == 2 ? dev->pairs : dev->sms;
-    const int grid = cg * (tiles < units ? tiles : units);
+
+    // memory for copies of operands and for the sums of parts, in stream order
     const cudaStream_t s = (cudaStream_t)stream;
-    char* copies = nullptr;
+    const void *const x_off = x_on ? nullptr : x, *const w_off = w_on ? nullptr : d.w;
+    const size_t copies = copies_bytes(x_off, ep.M, w_off, ep.N, a.k_bytes);
+    const long long row = (ep.N + 31) / 32 * 32;  // floats of a row of sums
+    a.part_rows = a.tiles_m * 128 * cg;
+    const size_t sums = a.parts > 1 ? (size_t)a.parts * a.part_rows * row * 4 : 0;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    void* space = nullptr;
+    if (copies + sums) {
+        cudaError_t e = cudaStreamIsCapturing(s, &capture);
+        if (e == cudaSuccess) e = cudaMallocFromPoolAsync(&space, copies + sums, dev->pool, s);
+        if (e != cudaSuccess) {
+            (void)cudaGetLastError();  // returned here, so not left for a check of the caller's own launches
+            return cuda_error(e, "linear workspace");
+        }
+    }
+    const bool captured = capture != cudaStreamCaptureStatusNone;  // the first kernel then follows the allocation, not a kernel
     LinearPackArgs pack{};
-    rc = x_on && w_on ? CB_OK : make_copies(*dev, x_on ? nullptr : x, x_row, ep.M, w_on ? nullptr : d.w, w_row, ep.N, a.k_bytes, &pack, &copies, s);
-    if (rc != CB_OK) return rc;
+    LinearJoinArgs join{ep, 1, a.parts, (long long)a.part_rows * row, row, nullptr};
+    cudaError_t e = cudaSuccess;
+    if (copies) e = make_copies(x_off, x_row, ep.M, w_off, w_row, ep.N, a.k_bytes, static_cast<char*>(space), !captured, &pack, s);
+    a.overlap = copies || !captured;
+    if (a.parts > 1) {
+        join.sums = reinterpret_cast<const float*>(static_cast<char*>(space) + copies);
+        ep = LinearEpilogue{ep.M, ep.N, CB_ACT_NONE, (unsigned)ep.M, 0, 0, 0, 0, row, 0, 0, 0, nullptr, nullptr, nullptr, nullptr, nullptr,
+                            const_cast<float*>(join.sums), nullptr};
+        a.results = Results::kOut;
+        rc = operand_map(&a.out_map, join.sums, (long long)a.parts * a.part_rows, 4ll * ep.N, 4 * row, 32, 64);
+    } else {
+        rc = results_by_tma(io, &a);
+    }
     const PackOperand &px = pack.o[0], &pw = pack.o[1];
-    rc = px.dst ? operand_map(&a.x_map, px.dst, ep.M, 32ll * px.chunks, 32ll * px.chunks, 128)
-                : operand_map(&a.x_map, x, ep.M, a.k_bytes, x_row, 128);
+    if (rc == CB_OK)
+        rc = px.dst ? operand_map(&a.x_map, px.dst, ep.M, 32ll * px.chunks, 32ll * px.chunks, 128)
+                    : operand_map(&a.x_map, x, ep.M, a.k_bytes, x_row, 128);
     if (rc == CB_OK)
         rc = pw.dst ? operand_map(&a.w_map, pw.dst, ep.N, 32ll * pw.chunks, 32ll * pw.chunks, a.tile_n / cg)
                     : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);
-    if (rc == CB_OK) {
-        const cudaError_t e = launch_linear(a, cg, d.type == CB_E4M3, grid, s);
-        if (e != cudaSuccess) rc = cuda_error(e, "linear launch");
+    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.results, a.more_boxes)) / linear_stage_bytes(cg, a.tile_n));
+    const long long tiles = (long long)a.tiles_m * a.tiles_n * a.parts, units = cg == 2 ? dev->pairs : dev->sms;
+    if (rc == CB_OK && e == cudaSuccess) e = launch_linear(a, cg, d.type == CB_E4M3, cg * (int)std::min(tiles, units), s);
+    if (rc == CB_OK && e == cudaSuccess && a.parts > 1) e = launch_linear_join(join, s);
+    if (space) {
+        const cudaError_t f = cudaFreeAsync(space, s);
+        if (e == cudaSuccess) e = f;
     }
-    if (copies) {
-        const cudaError_t e = cudaFreeAsync(copies, s);
-        if (e != cudaSuccess && rc == CB_OK) rc = cuda_error(e, "linear workspace");
-    }
-    return rc;
+    return rc != CB_OK ? rc : e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
 }
 
 int cb_linear_device_status(int* status, void* stream) {

@@ -36,7 +36,9 @@ struct LinearArgs {
     int k_bytes;           // bytes of a row of x and of w
     int tiles_m, tiles_n, k_blocks, stages;
     int tile_n;            // output columns of a tile
-    int passes, pass_blocks;  // parts of K that are summed by themselves, and their slabs
+    int passes, pass_blocks;  // stretches of K that are summed by themselves, and their slabs
+    int parts, part_blocks;   // parts of K that are tiles of their own, and their slabs
+    int part_rows;            // rows of the output of a part
     int* status;
 };
 
@@ -65,6 +67,15 @@ struct LinearPackArgs {
     int overlap;
 };
 cudaError_t launch_linear_pack(LinearPackArgs& a, cudaStream_t s);
+
+// Sums of parts of K, `parts` times [part_rows, stride] in fp32, added and taken through the epilogue (linear_join.cu).
+struct LinearJoinArgs {
+    LinearEpilogue e;
+    int overlap, parts;
+    long long part_size, stride;  // floats from part to part, and from row to row
+    const float* sums;
+};
+cudaError_t launch_linear_join(const LinearJoinArgs& a, cudaStream_t s);
 
 // The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows. prepare_linear raises the kernels' shared-memory
 // limit and tells how many pairs of CTAs run at once.

@@ -1,4 +1,4 @@
-// Internal: the matrix product of cb_linear_run on the fifth-generation tensor cores (linear_tc.cu, linear_tc_passes.cu).
+// Internal: the matrix product of cb_linear_run on the fifth-generation tensor cores (linear_tc_*.cu).
 //
 // A persistent grid of CTAs (CG = 1) or of pairs of CTAs on two SMs (CG = 2) works through output tiles of 128 CG
 // rows by tile_n columns. In a CTA
@@ -15,6 +15,8 @@
 // K = 16384, 2.1e-6 at 2048). Results in fp32 are therefore summed in passes over parts of K, whose sums the epilogue's warps
 // add, rounded to nearest, into a third part of TMEM while the next pass is under way (A.passes > 1, tiles of up to 128
 // columns).
+//
+// Few tiles of long sums are split over K (A.parts): each part's sums leave in fp32, and linear_join.cu adds them.
 //
 // Every wait has a limit (kLimitNs); one that runs out sets the CTA's abort flag, so that all its roles leave, after
 // the copies under way have landed, and frees the TMEM.
@@ -206,13 +208,16 @@ __device__ __forceinline__ void tmem_add(uint32_t addr, float* v) {
 }
 
 struct Tile {
-    int m, n;
+    int m, n, part;
 };
-// Groups of eight rows of tiles, so that tiles worked on together share operands in L2.
+// Groups of eight rows of tiles, so that tiles worked on together share operands in L2; SPLIT: parts of K, one after the other.
+template <bool SPLIT>
 __device__ __forceinline__ Tile tile_at(const LinearArgs& A, int t) {
+    const int part = SPLIT ? t % A.parts : 0;
+    if (SPLIT) t /= A.parts;
     const int group = 8 * A.tiles_n, g = t / group, r = t - g * group;
     const int rows = min(8, A.tiles_m - 8 * g);
-    return Tile{8 * g + r % rows, r / rows};
+    return Tile{8 * g + r % rows, r / rows, part};
 }
 
 // A place in the ring of stages, and the parity of its present use.
@@ -402,7 +407,7 @@ __device__ __forceinline__ void finish_rows(const LinearEpilogue& E, int row0, i
 template <int CG, bool FP8, bool PASSES, Results RESULTS>
 __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(const __grid_constant__ LinearArgs A) {
     constexpr int EPI = epi_warps(RESULTS);
-    constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden;
+    constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden, SPLIT = RESULTS == Results::kOut;
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
         after_previous();
@@ -452,7 +457,10 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     const uint32_t tmem = T.tmem;
     after_previous();
 
-    const int first = blockIdx.x / CG, step = gridDim.x / CG, total = A.tiles_m * A.tiles_n;
+    const int first = blockIdx.x / CG, step = gridDim.x / CG, total = A.tiles_m * A.tiles_n * (SPLIT ? A.parts : 1);
+    // slabs of a part of K
+    auto slabs_from = [&](int part) { return SPLIT ? part * A.part_blocks : 0; };
+    auto slabs_to = [&](int part) { return SPLIT ? min((part + 1) * A.part_blocks, A.k_blocks) : A.k_blocks; };
     if (warp < EPI) {  // ---- epilogue
         const LinearEpilogue E = A.e;
         float* const turn = reinterpret_cast<float*>(turns + warp * kTurn);
@@ -464,7 +472,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
         float xs = 1.0f, scale = 1.0f, bias = 0.0f;
         auto look_tile = [&](int t) {
             if (t >= total) return;
-            const Tile tile = tile_at(A, t);
+            const Tile tile = tile_at<SPLIT>(A, t);
             const int row = first_row(tile) + lane, col = tile.n * A.tile_n + (int)threadIdx.x;
             if (E.x_scale && row < E.M) xs = __uint_as_float(lin_ld1(E.x_scale, row, 0));
             if (DIRECT || (int)threadIdx.x >= A.tile_n || col >= E.N) return;
@@ -474,7 +482,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
         // The hidden state's rows of a tile are on their way to L2 a tile ahead.
         auto to_l2 = [&](int t) {
             if (RESULTS == Results::kOut || !E.resid_out || t >= total) return;
-            const Tile tile = tile_at(A, t);
+            const Tile tile = tile_at<SPLIT>(A, t);
             const int row = first_row(tile) + lane, col0 = tile.n * A.tile_n, es = E.resid_bf16 ? 2 : 4;
             if (row >= E.M) return;
             const char* const q = reinterpret_cast<const char*>(E.resid) + (row * E.resid_stride + col0) * es;
@@ -495,7 +503,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 f_chunk += EPI / 4;
                 while (f_chunk >= f_chunks) {
                     if ((f_tile += step) >= total) return;
-                    const Tile tile = tile_at(A, f_tile);
+                    const Tile tile = tile_at<SPLIT>(A, f_tile);
                     f_row = first_row(tile), f_col = tile.n * A.tile_n;
                     f_chunks = f_row < E.M ? (min(A.tile_n, E.N - f_col) + 31) / 32 : 0;
                     f_chunk = half;
@@ -516,7 +524,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
         to_l2(first);
         if (HIDDEN) fetch(A.ring - 2);
         for (int t = first; t < total; t += step, ++n_done) {
-            const Tile tile = tile_at(A, t);
+            const Tile tile = tile_at<SPLIT>(A, t);
             const int row0 = first_row(tile), col0 = tile.n * A.tile_n;
             const Two xs2 = two(xs, xs);
             const int chunks = row0 < E.M ? (min(A.tile_n, E.N - col0) + 31) / 32 : 0;
@@ -555,7 +563,8 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 ++pass;
             };
             bool ok = true;
-            for (int i = 0; PASSES && i + 1 < A.passes; ++i) {  // all but the last one's sums are added up
+            const int passes = PASSES ? (slabs_to(tile.part) - slabs_from(tile.part) + A.pass_blocks - 1) / A.pass_blocks : 1;
+            for (int i = 0; PASSES && i + 1 < passes; ++i) {  // all but the last one's sums are added up
                 ok = all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
                 if (!ok) break;
                 fence_after();
@@ -579,7 +588,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 }
                 float v[32];
                 tmem_load(acc_at + c * 32, v);
-                if (PASSES) tmem_add(total_at + c * 32, v);
+                if (PASSES && passes > 1) tmem_add(total_at + c * 32, v);
                 if (c + EPI / 4 >= chunks) release();
                 if constexpr (!DIRECT) {
                     Two x[16];
@@ -598,7 +607,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                             else put_box<false>(box, lane, x + 8);
                             fence_generic_to_async();
                             __syncwarp();
-                            if (lane == 0 && col + 16 * h < E.N) store_box(&A.out_map, (col + 16 * h) * (E.out_bf16 ? 2 : 4), row0, box);
+                            if (lane == 0 && col + 16 * h < E.N) store_box(&A.out_map, (col + 16 * h) * (E.out_bf16 ? 2 : 4), row0 + tile.part * A.part_rows, box);
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
                     } else {
@@ -676,8 +685,9 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
             bool ok = true;
             // (the slabs' loop is kept short: with passes opened and closed inside it, a slab took 260 clocks longer)
             for (int t = first; t < total && ok; t += step) {
-                for (int kb0 = 0; kb0 < A.k_blocks && ok; ++pass) {
-                    const int end = PASSES ? min(kb0 + A.pass_blocks, A.k_blocks) : A.k_blocks;
+                const int part = SPLIT ? t % A.parts : 0, to = slabs_to(part);
+                for (int kb0 = slabs_from(part); kb0 < to && ok; ++pass) {
+                    const int end = PASSES ? min(kb0 + A.pass_blocks, to) : to;
                     const uint32_t sums = tmem + (pass & 1) * stride;
                     ok = all(wait<CG == 2>(acc_empty + 8 * (pass & 1), ((pass >> 1) & 1) ^ 1, abort, A.status,
                                            CB_DEV_PRODUCER_TIMEOUT));
@@ -708,9 +718,9 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
         bool ok = true;
         const uint32_t bar0 = CG == 2 ? in_first(full) : full;
         for (int t = first; t < total && ok; t += step) {
-            const Tile tile = tile_at(A, t);
+            const Tile tile = tile_at<SPLIT>(A, t);
             const int row = (tile.m * CG + (int)rank) * kRows, col = tile.n * A.tile_n + (int)rank * w_rows;
-            for (int kb = 0; kb < A.k_blocks; ++kb, ++fills) {
+            for (int kb = slabs_from(tile.part), to = slabs_to(tile.part); kb < to; ++kb, ++fills) {
                 ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
                 if (!ok) break;
                 const uint32_t dst = ring + at.s * stage_bytes;

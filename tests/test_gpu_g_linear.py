@@ -356,3 +356,28 @@ def test_off_the_grid_on_two_streams_and_in_a_graph(lib):
     for x, w, layer, io in sets:
         block.cb_linear_destroy(layer)
     assert block.cb_linear_device_status() == 0
+
+
+# few tiles of long sums: parts of K that are summed by themselves
+PARTS = [case(40, 64, 16384, "e4m3", "GELU", "fp32"), case(256, 1152, 4608, resid="bf16", gate="bf16", tokens=100, inplace=True),
+         case(77, 1150, 4096, out="fp32", resid="fp32", tokens=7, gate="fp32", pad=1, off=1), case(100, 33, 5001, act="SILU"),
+         case(1500, 300, 12000, resid="bf16", out=None), case(64, 31, 8192, "e4m3", resid="bf16", gate="fp32", tokens=64),
+         case(300, 40, 1100, bias=None), case(130, 257, 9000, out="fp32", bias="fp32", pad=3)]
+
+
+@pytest.mark.parametrize("c", PARTS, ids=lambda c: "{m}x{n}x{k}_{type}".format(**c))
+def test_few_tiles_of_long_sums(lib, c):
+    block, cb = lib
+    d, (v, e, h, eh), out, xo = run(lib, c, seed=11)
+    assert block.cb_linear_device_status() == 0
+    if out is not None:
+        close(out, v, e, c["out"])
+    if xo is not None:
+        close(xo, h, eh, c["resid"])
+    again = run(lib, c, seed=11)
+    for a, b in ((out, again[2]), (xo, again[3])):
+        assert a is None or torch.equal(a, b)
+    for t in (out, xo):  # what lies between rows stays as it was
+        if t is not None and c["pad"]:
+            whole = torch.as_strided(t, (c["m"], c["n"] + c["pad"]), (c["n"] + c["pad"], 1), t.storage_offset())
+            assert float(whole[:, c["n"]:].abs().max()) == 0.0
