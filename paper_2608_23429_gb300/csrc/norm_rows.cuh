@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(norm_threads(W), norm_ctas(CH, W)) norm_kernel
     auto fetch = [&](unsigned row) {  // the row's chunks of x and branch, in pieces of 16 bytes
         if (row < end) {
             const char* const x = reinterpret_cast<const char*>(A.x) + (row * A.x_stride + e0) * (XB ? 2 : 4);
-                        auto copy = [&](uint32_t dst, const char* p, int size) {
+            auto copy = [&](uint32_t dst, const char* p, int size) {
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(p), "r"(size) : "memory");
             };
 #pragma unroll
@@ -156,8 +156,10 @@ __global__ void __launch_bounds__(norm_threads(W), norm_ctas(CH, W)) norm_kernel
             for (int c = 0; c < CH; ++c) lines[1][c] = load8<LB>(A.shift, line + column(c));
 #pragma unroll
         for (int c = 0; c < CH; ++c)
+            if (on(c)) {  // (zeros behind the row's end, but times its first gates)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum2 = fma2(h[c][i], h[c][i], sum2);
+                for (int i = 0; i < 4; ++i) sum2 = fma2(h[c][i], h[c][i], sum2);
+            }
         if (A.x_out) {
             const long long at = row * A.x_out_stride + e0;
 #pragma unroll

@@ -194,3 +194,45 @@ def test_side_stream_and_no_rows(lib):
     block.cb_norm_residual(desc, x, out=out)
     ref = f64(x) / np.sqrt((f64(x) ** 2).mean(1, keepdims=True) + 1e-5)
     assert (np.abs(f64(out) - ref) <= 30 * U * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("hidden", [40, 1152, 1153, 3080])
+def test_an_infinite_gate_spoils_its_own_column_only(lib, hidden):
+    """The row's sum is infinite: the column itself is NaN, all others are what zeros give."""
+    block, cb = lib
+    g = torch.Generator(device="cuda").manual_seed(hidden)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    x, branch, gate, scale, shift = r(6, hidden), r(6, hidden) + 4, r(2, hidden), r(2, hidden), r(2, hidden)
+    gate[1, 3] = float("inf")
+    out = torch.empty(6, hidden, device="cuda")
+    desc = block.cb_norm_desc(rows=6, hidden=hidden, tokens=3, out_dtype=cb.CB_FP32, eps=1e-6)
+    block.cb_norm_residual(desc, x, branch, gate, None, scale, shift, None, out)
+    want = shift[1].float().expand(3, hidden)
+    assert torch.isfinite(out[:3]).all() and torch.isnan(out[3:, 3]).all()
+    others = torch.arange(hidden, device="cuda") != 3
+    assert torch.equal(out[3:, others], want[:, others])
+
+
+@pytest.mark.parametrize("hidden", [8, 9, 15, 63, 250, 577, 1151, 1267, 2041, 3001, 4097, 8187, 16370, 16383])
+@pytest.mark.parametrize("x,branch,out", [("bf16", "bf16", "e4m3"), ("fp32", "bf16", "bf16"), ("bf16", "fp32", "fp32"), ("fp32", None, "e4m3")])
+def test_rows_off_the_grid(lib, hidden, x, branch, out):
+    """Contiguous rows whose starts take every place of a vector, lines in bf16 off the grid as well, in place."""
+    c = (45, hidden, 9, x, branch, "bf16", out, branch is not None, True, True, 0, 0)
+    d = inputs(c, seed=2)
+    want = expected(c, d)
+    check(c, d, call(lib, c, d, "same"), want)
+
+
+@pytest.mark.parametrize("hidden", [250, 1151])
+def test_only_the_row_s_own_elements_count(lib, hidden):
+    """Rows of NaN among others, and gates of NaN for the other samples."""
+    block, cb = lib
+    g = torch.Generator(device="cuda").manual_seed(hidden)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    x, branch, gate, scale = r(9, hidden), r(9, hidden), r(3, hidden), r(3, hidden)
+    desc = block.cb_norm_desc(rows=9, hidden=hidden, tokens=3, out_dtype=cb.CB_FP32, eps=1e-6)
+    whole, out = torch.empty(9, hidden, device="cuda"), torch.empty(9, hidden, device="cuda")
+    block.cb_norm_residual(desc, x, branch, gate, None, scale, None, None, whole)
+    x[3], branch[5], gate[0], scale[2] = float("nan"), float("inf"), float("nan"), float("inf")
+    block.cb_norm_residual(desc, x, branch, gate, None, scale, None, None, out)
+    assert torch.equal(out[4], whole[4]) and torch.isnan(out[:4]).all() and torch.isnan(out[5]).any()
