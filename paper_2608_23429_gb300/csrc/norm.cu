@@ -63,9 +63,13 @@ __device__ __forceinline__ void store_all(void* p, long long e, int dtype, int t
     }
 }
 
+// Weight, scale and shift are loaded while the sum is, not before: half the registers, twice the CTAs (GB300: 8192 x 4097
+// bf16 to e4m3 211 -> 156 us, 16384 x 1153 78 -> 68). Short rows have room all the same.
+__host__ __device__ constexpr bool lines_late(int CH, int W) { return CH * W > 32 && CH <= 10; }
+
 // CH elements of a thread, a row of up to 32 W CH elements in registers. HELD = false: three passes over longer rows.
 template <int CH, int W, bool HELD>
-__global__ void __launch_bounds__(32 * W) norm_elements_kernel(const __grid_constant__ NormArgs args) {
+__global__ void __launch_bounds__(32 * W, lines_late(CH, W) ? 1024 / (32 * W) : 0) norm_elements_kernel(const __grid_constant__ NormArgs args) {
     __shared__ uint32_t slots[2][W];
     constexpr int T = 32 * W;
     const NormArgs A = args;  // in registers, as stores would have them read again
@@ -89,14 +93,17 @@ __global__ void __launch_bounds__(32 * W) norm_elements_kernel(const __grid_cons
     };
     float h[CH], sum = 0.0f;
     float w[CH], sc[CH], sh[CH];
+    auto load_lines = [&] {
+        if (A.weight) load_all<CH, T>(A.weight, 0, A.param_bf16, t, A.hidden, w);
+        if (A.scale) load_all<CH, T>(A.scale, line, A.param_bf16, t, A.hidden, sc);
+        if (A.shift) load_all<CH, T>(A.shift, line, A.param_bf16, t, A.hidden, sh);
+    };
     if constexpr (HELD) {
         float b[CH], g[CH];
         load_all<CH, T>(A.x, xo, A.x_bf16, t, A.hidden, h);
         if (A.branch) load_all<CH, T>(A.branch, bo, A.branch_bf16, t, A.hidden, b);
         if (A.gate) load_all<CH, T>(A.gate, line, A.param_bf16, t, A.hidden, g);
-        if (A.weight) load_all<CH, T>(A.weight, 0, A.param_bf16, t, A.hidden, w);
-        if (A.scale) load_all<CH, T>(A.scale, line, A.param_bf16, t, A.hidden, sc);
-        if (A.shift) load_all<CH, T>(A.shift, line, A.param_bf16, t, A.hidden, sh);
+        if constexpr (!lines_late(CH, W)) load_lines();
         if (A.gate) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) h[c] = fmaf(g[c], b[c], h[c]);
@@ -107,6 +114,7 @@ __global__ void __launch_bounds__(32 * W) norm_elements_kernel(const __grid_cons
 #pragma unroll
         for (int c = 0; c < CH; ++c)
             if (c * T + t < A.hidden) sum = fmaf(h[c], h[c], sum);
+        if constexpr (lines_late(CH, W)) load_lines();
         if (A.x_out) store_all<CH, T>(A.x_out, row * A.x_out_stride, A.x_bf16 ? CB_BF16 : CB_FP32, t, A.hidden, h);
     } else {
         for (int e = t; e < A.hidden; e += T) {
