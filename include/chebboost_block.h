@@ -128,9 +128,11 @@ void cb_linear_destroy(cb_linear* layer);
  * may be NULL together, gate (with resid only) may be NULL: 1; one result at least
  * is wanted. resid_out may be resid itself (same stride). The order of a sum depends
  * on the sizes alone: equal calls give equal bits.
- * Operands whose rows do not start on 16-byte boundaries are copied onto them first where
- * there are over 32 rows. The copies are allocated and freed in stream order, from a
- * pool of the library's own that keeps 1 GiB at most between calls; in a graph they belong to the graph.
+ * Over 32 rows, operands whose rows do not start on 16-byte boundaries are copied onto
+ * them first, and few tiles of long sums are split over in_features, whose parts' sums a
+ * second kernel adds in order. Memory for either is allocated and freed in stream order,
+ * from a pool of the library's own that keeps 1 GiB at most between calls; in a graph
+ * it belongs to the graph. Where there is none left: CB_ERR_CUDA, and nothing has run.
  * Every wait of the kernels on one of their barriers has a limit of a second; one that
  * runs out is noted in the status word of cb_linear_device_status and makes the
  * kernel return early, with incomplete results.

@@ -44,6 +44,8 @@ int device_info(const Device** out) {
     if (d >= kMaxStatusDevices) return CB_ERR_LIMIT;
     if ((*out = g_devices[d].load(std::memory_order_acquire))) return CB_OK;
     Device v{};
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;  // the first call may be one that is captured
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
     e = cudaDeviceGetAttribute(&v.sms, cudaDevAttrMultiProcessorCount, d);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&v.smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, d);
     if (e == cudaSuccess) e = cudaGetSymbolAddress(reinterpret_cast<void**>(&v.status), g_linear_status);
@@ -53,6 +55,7 @@ int device_info(const Device** out) {
     cudaDriverEntryPointQueryResult found{};
     if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
     if (e == cudaSuccess && (!fn || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
     if (e != cudaSuccess) return cuda_error(e, "linear set-up");
     g_encode.store(reinterpret_cast<Encode>(fn), std::memory_order_relaxed);
     const Device* mine = new (std::nothrow) Device(v);  // kept until the process ends
@@ -153,7 +156,7 @@ void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int* c
                 if (n > 32 && n - 32 >= N) continue;
                 const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n) * p;
                 const long long units = g == 2 ? dev.pairs : dev.sms;
-                if (p > 1 && tiles > units) continue;
+                if (p > 1 && tiles > units) break;  // smaller tiles are more
                 const double join = p > 1 ? kJoinClocks + 4.0 * p * M * N / kJoinBytesPerClock : 0.0;
                 const double cost = (double)((tiles + units - 1) / units) * ((k_blocks + p - 1) / p) * (256.0 + 2.0 * n / g) + join;
                 if (cost < best * 0.999) best = cost, *cg = g, *tile_n = n, *parts = p;

@@ -6,7 +6,8 @@
 // row (reductions, roots, addresses) counts as much as its elements. A row's own work is a chain of latencies, so the
 // CTAs of the vector kernels (norm_rows.cuh) stay and go through consecutive rows: the next row's x and branch are on
 // their way to shared memory meanwhile, each thread copying what it will read itself. Rows off the 16-byte grid take
-// elements, one CTA a row.
+// elements, one CTA a row. GB300, all operands: 16384 x 4096 bf16 90 us (87 % of the copy rate), 32768 x 1152 bf16 to e4m3 49 us, 8192
+// x 1152 fp32 to e4m3 25 us; by elements 8192 x 4097 152 us.
 #include <cmath>
 
 #include "norm.cuh"

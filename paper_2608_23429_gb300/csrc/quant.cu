@@ -17,7 +17,8 @@
 // states: 73.6 us with a lane's elements consecutive instead).
 //
 // Both kernels are bound by HBM: 1 1/32 bytes per element and entry against 2 of
-// bf16. Persistent grids over tiles of 4096 elements, as in push.cu.
+// bf16. Persistent grids over tiles of 4096 elements, as in push.cu. GB300: read, 38 x [1, 4608, 3072], K = 5, 546 us (7.05
+// TB/s); write, 56 x [8, 256, 1152] bf16, 68 us (5.9 TB/s); off the grid, as above, 34 us (2.7 TB/s).
 #include <cuda_bf16.h>
 
 #include <type_traits>

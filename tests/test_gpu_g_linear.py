@@ -381,3 +381,28 @@ def test_few_tiles_of_long_sums(lib, c):
         if t is not None and c["pad"]:
             whole = torch.as_strided(t, (c["m"], c["n"] + c["pad"]), (c["n"] + c["pad"], 1), t.storage_offset())
             assert float(whole[:, c["n"]:].abs().max()) == 0.0
+
+
+FIRST_IN_A_GRAPH = """
+import torch
+from paper_2608_23429_gb300 import block, chebboost as cb
+x, w = torch.ones(100, 333, device="cuda").bfloat16(), torch.ones(50, 333, device="cuda").bfloat16()
+out = torch.zeros(100, 50, device="cuda")
+layer = block.cb_linear_create(w, 50, 333, cb.CB_BF16)
+io = block.cb_linear_io(rows=100, out_dtype=cb.CB_FP32)
+s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.stream(s), torch.cuda.graph(graph, stream=s):
+    block.cb_linear_run(layer, io, x, out=out, stream=torch.cuda.current_stream())
+graph.replay()
+torch.cuda.synchronize()
+assert bool((out == 333).all())
+"""
+
+
+def test_the_first_call_of_a_process_may_be_captured(lib):
+    import subprocess
+    import sys
+    from pathlib import Path
+    r = subprocess.run([sys.executable, "-c", FIRST_IN_A_GRAPH], cwd=Path(__file__).parents[1], capture_output=True, text=True, timeout=200)
+    assert r.returncode == 0, r.stderr
