@@ -36,6 +36,15 @@ __device__ __forceinline__ uint4 ld_v4(const void* p) {
     return v;
 }
 
+// Up to the item that `tile` belongs to, first in steps of eight, as a plan may have many small ones (GB300, 148 of 34720
+// elements, K = 1: a read of 8.6 us one by one, 5.6 so).
+__device__ __forceinline__ void pass_items(const ExtrapArgs& A, int tile, int& it) {
+#pragma unroll 1
+    while (it + 8 < A.n_items && tile >= A.tile_begin[it + 8]) it += 8;
+#pragma unroll 1
+    while (tile >= A.tile_begin[it + 1]) ++it;
+}
+
 __device__ __forceinline__ float bf16_at(const void* p, long long i) {
     return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(p)[i] << 16);
 }
@@ -212,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) quant_read_kernel(const __grid_co
     after_previous();
     int it = 0;
     for (int tile = blockIdx.x; tile < A.tiles_total; tile += gridDim.x) {
-        while (tile >= A.tile_begin[it + 1]) ++it;
+        pass_items(A, tile, it);
         const long long numel = A.numel[it];
         const long long e = (long long)(tile - A.tile_begin[it]) * TE + (long long)threadIdx.x * kReadElems;
         if (e >= numel) continue;
@@ -355,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, ELEMENTS && K <= 5 ? 0 : 2) quant_re
     };
     auto seek = [&](Unit& u) {
         if (u.tile >= A.tiles_total) return;
-        while (u.tile >= A.tile_begin[u.it + 1]) ++u.it;
+        pass_items(A, u.tile, u.it);
         u.m = A.first[u.it];
     };
     auto element = [&](const Unit& u) { return (long long)(u.tile - A.tile_begin[u.it]) * TE + (long long)threadIdx.x * N; };
@@ -558,7 +567,7 @@ __global__ void __launch_bounds__(kThreads) quant_write_kernel(const __grid_cons
     after_previous();
     int it = 0;
     for (int tile = blockIdx.x; tile < A.tiles_total; tile += gridDim.x) {
-        while (tile >= A.tile_begin[it + 1]) ++it;
+        pass_items(A, tile, it);
         const long long numel = A.numel[it], scales = scales_at(numel);
         const long long tile_e = (long long)(tile - A.tile_begin[it]) * TE;
         for (int part = 0; part < kWriteParts; part += P) {
@@ -648,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, 4) quant_write_elements_kernel(const
     float* const turn = turns[threadIdx.x / 32];
     int it = 0;
     for (int tile = blockIdx.x; tile < A.tiles_total; tile += gridDim.x) {
-        while (tile >= A.tile_begin[it + 1]) ++it;
+        pass_items(A, tile, it);
         const long long numel = A.numel[it], scales = scales_at(numel);
         const long long e0 = (long long)(tile - A.tile_begin[it]) * TE + (long long)(threadIdx.x / 32) * 32 * N;
         const long long e = e0 + lane;
