@@ -18,8 +18,8 @@
 //
 // Few tiles of long sums are split over K (A.parts): each part's sums leave in fp32, and linear_join.cu adds them.
 //
-// Bound by the tensor cores where tiles fill the SMs' rounds: GB300, 4608 x 3072 x 15360 bf16 with a gated hidden state 263 us (1.65
-// PFLOP/s, 86 % of the largest library rate), 8192 x 1152 x 4608 65 us (1.34), 4096 x 4608 x 1152 e4m3 with GELU 22 us (1.96).
+// Bound by the tensor cores where tiles fill the SMs' rounds: GB300, 4608 x 3072 x 15360 bf16 with a gated hidden state 265 us (1.64
+// PFLOP/s, 85 % of the largest library rate), 8192 x 1152 x 4608 65 us (1.34), 4096 x 4608 x 1152 e4m3 with GELU 22 us (1.96).
 //
 // Every wait has a limit (kLimitNs); one that runs out sets the CTA's abort flag, so that all its roles leave, after
 // the copies under way have landed, and frees the TMEM.
