@@ -140,6 +140,11 @@ constexpr int kFewRows = 32;
 // Slabs of 128 bytes of a pass over K, with fp32 results: an error of 5e-7 of a sum (measured: linear_tc.cuh; e4m3's products
 // lose less, 7e-7 at K = 16384).
 constexpr int kPassBf16 = 8, kPassE4m3 = 64;
+// Results in bf16 alone: one pass up to kOnePass slabs, as tiles of 256 columns are worth more (4608 x 3072 x 15360 227 -> 274 us, 8192 x
+// 8192 x 8192 554 -> 648, 8192 x 1152 x 4608 60.2 -> 62.0 with passes of 16) and what the sums lose is small against the rounding that
+// follows, 2e-3 to 4e-3: 7.2e-5 of their size at most (16384 features of bf16, all terms of one sign; 1.9e-5 with signs mixed). Longer sums
+// in passes, as it grows with the length: 3.5e-4 at 65536, 6.5e-3 at 2^20.
+constexpr int kOnePass = 256, kPassLong = 32;
 
 // CTAs per tile, the tile's columns and the parts of K: the fewest rounds of tiles, each as long as its loads (16 KB of x and
 // 16 KB * tile_n / 128 / cg of w per CTA and slab) or its products take, in clocks. Parts cost a launch that adds them, and
@@ -251,7 +256,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.k_blocks = (a.k_bytes + 127) / 128;
     // fp32 results: passes over K (see linear_tc.cuh)
     const bool fp32 = (out && !ep.out_bf16) || (resid_out && !ep.resid_bf16);
-    a.pass_blocks = fp32 ? (d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks;
+    a.pass_blocks = fp32 ? (d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
     choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks ? 128 : 256, &cg, &a.tile_n, &a.parts);
     a.part_blocks = (a.k_blocks + a.parts - 1) / a.parts;
     a.parts = (a.k_blocks + a.part_blocks - 1) / a.part_blocks;

@@ -1,0 +1,45 @@
+"""What the sums and activations of cb_linear_run lose, where tolerances that follow the sums' sizes cannot see it."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2608_23429_gb300 import build
+    build.build()
+    from paper_2608_23429_gb300 import block, chebboost
+    return block, chebboost
+
+
+def product(lib, x, w, out="fp32", act="NONE", rows=None):
+    block, cb = lib
+    code = {"bf16": cb.CB_BF16, "fp32": cb.CB_FP32}
+    layer = block.cb_linear_create(w, w.shape[0], w.shape[1], cb.CB_BF16 if w.dtype == torch.bfloat16 else cb.CB_E4M3,
+                                   activation=getattr(block, "CB_ACT_" + act))
+    y = torch.empty(x.shape[0], w.shape[0], device="cuda", dtype=DT[out])
+    torch.cuda.synchronize()
+    block.cb_linear_run(layer, block.cb_linear_io(rows=x.shape[0], out_dtype=code[out]), x, out=y)
+    torch.cuda.synchronize()
+    block.cb_linear_destroy(layer)
+    assert block.cb_linear_device_status() == 0
+    return y
+
+
+@pytest.mark.parametrize("type", ["bf16", "e4m3"])
+def test_bf16_results_of_very_long_sums_are_not_cut_off(lib, type):
+    """Positive terms, so that what a sum loses has one sign. Rounding to bf16 has none: over n results of a spread of more than a
+    step its mean is off by 2^-9 / sqrt(n) at most, a tenth of the 2^-9 / 20 that the sums may lose."""
+    m, n, k = 2048, 2048, 1 << 20
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w = (torch.empty(r, k, device="cuda", dtype=DT[type]) for r in (m, n))
+    for t in (x, w):
+        for i in range(0, t.shape[0], 256):
+            t[i:i + 256] = (torch.rand(256, k, generator=g, device="cuda") * (0.5 + torch.rand(256, 1, generator=g, device="cuda"))).to(DT[type])
+    y = product(lib, x, w, "bf16")[:256, :256].double()
+    ref = sum(x[:256, i:i + 65536].float().double() @ w[:256, i:i + 65536].float().double().t() for i in range(0, k, 65536))
+    off = float(((y - ref) / ref).mean())
+    assert abs(off) < 2.0 ** -9 / 20, off
