@@ -4,8 +4,9 @@
 // rows of w are the 16-row operand of mma.sync, so that no row of the tensor cores is wasted on rows that x does not
 // have, and fragments come from global memory without a stop in shared memory: a lane's 16 consecutive bytes of a
 // row stand for other places of K than the instruction's, but for the same ones in both operands, and a sum does not
-// mind. e4m3 is widened to fp16 (exact), whose products the tensor cores sum in fp32. The partial sums of warps and
-// CTAs are added in a fixed order.
+// mind. e4m3 is widened to fp16 (exact), whose products the tensor cores sum in fp32. They cut off what a sum loses (65536 features of
+// one sign in one such sum a warp: 3e-5 of it), so each of a warp's batches of loads, 128 features of bf16 at most, is summed by itself
+// and added rounded to nearest. The partial sums of warps and CTAs are added in a fixed order.
 #include <cuda_fp16.h>
 
 #include "linear.cuh"
@@ -92,9 +93,9 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
 #pragma unroll
     for (int i = 0; i < NT; ++i) xl[i] = line(x, 8 * i + g, M, A.x_row);
 
-    float d[NT][4];
+    float sum[NT][4];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) d[i][0] = d[i][1] = d[i][2] = d[i][3] = 0.0f;
+    for (int i = 0; i < NT; ++i) sum[i][0] = sum[i][1] = sum[i][2] = sum[i][3] = 0.0f;
     const int step = kTurn * kWarps * (int)ranks;
     constexpr int DEEP = NT >= 4 ? 2 : kDeep;
     for (int k0 = kTurn * (kWarps * (int)rank + warp); k0 < k_bytes; k0 += DEEP * step) {
@@ -107,16 +108,21 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < NT; ++i) xv[j][i] = bytes16<SHIFT>(xl[i], k, left);
         }
+        float d[NT][4] = {};
 #pragma unroll
         for (int j = 0; j < DEEP; ++j)
 #pragma unroll
             for (int i = 0; i < NT; ++i) product<FP8>(d[i], lo[j], hi[j], xv[j][i]);
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[i][q] += d[i][q];
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
         float(*p)[16] = part[warp] + 8 * i;
-        p[2 * t][g] = d[i][0], p[2 * t + 1][g] = d[i][1];
-        p[2 * t][g + 8] = d[i][2], p[2 * t + 1][g + 8] = d[i][3];
+        p[2 * t][g] = sum[i][0], p[2 * t + 1][g] = sum[i][1];
+        p[2 * t][g + 8] = sum[i][2], p[2 * t + 1][g + 8] = sum[i][3];
     }
     __syncthreads();
     // this CTA's sums into part[0]

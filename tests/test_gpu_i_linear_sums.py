@@ -43,3 +43,24 @@ def test_bf16_results_of_very_long_sums_are_not_cut_off(lib, type):
     ref = sum(x[:256, i:i + 65536].float().double() @ w[:256, i:i + 65536].float().double().t() for i in range(0, k, 65536))
     off = float(((y - ref) / ref).mean())
     assert abs(off) < 2.0 ** -9 / 20, off
+
+
+@pytest.mark.parametrize("type", ["bf16", "e4m3"])
+@pytest.mark.parametrize("m,k", [(1, 4096), (8, 16384), (32, 16384), (1, 1 << 20), (32, 1 << 20)])
+def test_fp32_sums_of_few_rows(lib, type, m, k):
+    """As many output features as leave each row's sums to the warps of one CTA. A part of 512 products loses 1.3e-6 at most on the
+    tensor cores (32 additions, each of which cuts off half of 2^-23 of a running sum that averages two thirds of the part's);
+    the parts are then added rounded to nearest, which loses up to 2^-24 of the running sum each, independently: sqrt(parts) 2^-24."""
+    n, seen = 3664, 64
+    g = torch.Generator(device="cuda").manual_seed(k + m)
+    for positive in (False, True):
+        draw = lambda r: (torch.rand if positive else torch.randn)(r, k, generator=g, device="cuda").to(DT[type])  # noqa: E731
+        x = draw(m)
+        w = torch.empty(n, k, device="cuda", dtype=DT[type])
+        for i in range(0, n, 229):  # (parts: memory for all of it in fp32 is not taken)
+            w[i:i + 229] = draw(min(229, n - i))
+        y = product(lib, x, w)[:, :seen].double()
+        ref = sum(x[:, i:i + 65536].float().double() @ w[:seen, i:i + 65536].float().double().t() for i in range(0, k, 65536))
+        off = float((y - ref).norm() / ref.norm())
+        assert off < 1.3e-6 + (k / 512) ** 0.5 * U, off
+        del x, w
