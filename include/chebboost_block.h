@@ -121,7 +121,7 @@ void cb_linear_destroy(cb_linear* layer);
  *     resid_out = round(resid + gate * v)   the hidden state (gate: a line per sample)
  * with sums, epilogue and hidden state in fp32 and one rounding to each result. The
  * tensor cores cut sums off rather than round them: where a result is fp32 they sum
- * parts of 512 features (e4m3: 8192; up to 32 rows: 128 at most), which are added rounded
+ * parts of 512 features (e4m3: 4096; up to 32 rows: 128 at most), which are added rounded
  * to nearest. Measured, relative to sum_k |x w|: 5e-7 with signs mixed, 8e-7 with all terms
  * of one sign, and up to 2^-24 for every part added (of which most cancel: 2^-24 times the
  * root of their number). bf16 results: parts of 2048 (e4m3: 4096) where rows are longer

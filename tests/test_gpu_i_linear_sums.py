@@ -64,3 +64,19 @@ def test_fp32_sums_of_few_rows(lib, type, m, k):
         off = float((y - ref).norm() / ref.norm())
         assert off < 1.3e-6 + (k / 512) ** 0.5 * U, off
         del x, w
+
+
+@pytest.mark.parametrize("type", ["bf16", "e4m3"])
+@pytest.mark.parametrize("k", [4096, 16384, 1 << 17])
+def test_fp32_sums_of_terms_of_one_sign(lib, type, k):
+    """Over 32 rows, with the bound of test_fp32_sums_of_few_rows, and as many features as leave no parts of K to other tiles."""
+    m, n, seen = 384, 12000, 64
+    g = torch.Generator(device="cuda").manual_seed(k)
+    x = torch.rand(m, k, generator=g, device="cuda").to(DT[type])
+    w = torch.empty(n, k, device="cuda", dtype=DT[type])
+    for i in range(0, n, 500):
+        w[i:i + 500] = torch.rand(500, k, generator=g, device="cuda").to(DT[type])
+    y = product(lib, x, w)[:, :seen].double()
+    ref = sum(x[:, i:i + 16384].float().double() @ w[:seen, i:i + 16384].float().double().t() for i in range(0, k, 16384))
+    off = float((y - ref).norm() / ref.norm())
+    assert off < 1.3e-6 + (k / 512) ** 0.5 * U, off
