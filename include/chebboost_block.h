@@ -70,7 +70,8 @@ int cb_norm_residual(const cb_norm_desc* desc, const void* x, const void* branch
 /* Largest in_features: a sum that long takes a fraction of a wait's limit (cb_linear_run). */
 #define CB_MAX_IN_FEATURES (1LL << 22)
 
-/* Activations of a matrix product's epilogue. */
+/* Activations of a matrix product's epilogue, off by a few units in the last place of their own value however small (zero
+ * below 2^-126 |v|); NaN at -infinity, as their quotients are. */
 enum {
     CB_ACT_NONE = 0,
     CB_ACT_GELU = 1, /* v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))), the form of the blocks' MLPs */

@@ -150,35 +150,55 @@ __device__ __forceinline__ Two add2(Two a, Two b) {
 
 // v / (1 + 2^t): SiLU with t = -v log2(e), the tanh form of GELU with t = -2 log2(e) sqrt(2/pi) (v + 0.044715 v^3),
 // since (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z)). Four at a time, with one reciprocal of the product of their
-// denominators, as the unit for special functions is what an epilogue with an activation waits for. t ends at 30,
-// where the result is below 2^-30 |v|, so that the product stays finite (and a NaN stays with its own value).
-template <int ACT>
-__device__ __forceinline__ void lin_act4(Two& v, Two& w) {
+// denominators, as the unit for special functions is what an epilogue with an activation waits for. Where a product passes 2^120
+// (four values of t = 30: SiLU at -20.8, GELU at -5.7; or one of 120), or one of its values is a NaN, all N pairs are made anew with a
+// reciprocal each. At -infinity that gives NaN, as the quotient is. Asked for once for all pairs: a branch for every four
+// values keeps them from being worked on together (GB300, 4096 x 4608 x 1152 e4m3 with GELU, 10 % longer).
+template <int ACT, int N>
+__device__ __forceinline__ void lin_act(Two* x) {
     if constexpr (ACT != CB_ACT_NONE) {
-        constexpr float kSilu = -1.44269504f, kGelu1 = -2.30220820f, kGelu3 = -0.102943239f;
-        auto denominators = [](Two x) {
-            const Two t = ACT == CB_ACT_SILU ? mul2(x, two(kSilu, kSilu))
-                                             : mul2(x, fma2(two(kGelu3, kGelu3), mul2(x, x), two(kGelu1, kGelu1)));
-            float2 e = both(t);
-            e.x = fminf(e.x, 30.0f), e.y = fminf(e.y, 30.0f);
-            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
-            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
-            return add2(two(e.x, e.y), two(1.0f, 1.0f));
+        static_assert(N % 2 == 0, "two pairs at a time");
+        constexpr float kSilu = -1.44269504f, kGelu1 = -2.30220820f, kGelu3 = -0.102943239f, kMost = 1.32922800e36f;  // 2^120
+        auto denominators = [](Two v) {
+            float2 t = both(ACT == CB_ACT_SILU ? mul2(v, two(kSilu, kSilu))
+                                               : mul2(v, fma2(two(kGelu3, kGelu3), mul2(v, v), two(kGelu1, kGelu1))));
+            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.x));
+            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.y));
+            return add2(two(t.x, t.y), two(1.0f, 1.0f));
         };
-        const Two a = denominators(v), b = denominators(w);
-        const float2 p = both(mul2(a, b));
-        float r = p.x * p.y;
-        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
-        const Two q = mul2(two(r, r), two(p.y, p.x));  // 1 / (a b), pair by pair
-        v = mul2(v, mul2(q, b));
-        w = mul2(w, mul2(q, a));
+        auto reciprocal = [](float d) {
+            asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d));
+            return d;
+        };
+        Two y[N];
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const Two a = denominators(x[i]), b = denominators(x[i + 1]);
+            const float2 p = both(mul2(a, b));
+            float r = p.x * p.y;
+            asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(r));
+            r = reciprocal(r);
+            const Two q = mul2(two(r, r), two(p.y, p.x));  // 1 / (a b), pair by pair
+            y[i] = mul2(x[i], mul2(q, b));
+            y[i + 1] = mul2(x[i + 1], mul2(q, a));
+        }
+        if (!(most <= kMost)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float2 d = both(denominators(x[i]));
+                y[i] = mul2(x[i], two(reciprocal(d.x), reciprocal(d.y)));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = y[i];
     }
 }
 template <int ACT>
 __device__ __forceinline__ float lin_act1(float v) {
-    Two a = two(v, v), b = a;
-    lin_act4<ACT>(a, b);
-    return both(a).x;
+    Two a[2] = {two(v, v), two(v, v)};
+    lin_act<ACT, 2>(a);
+    return both(a[0]).x;
 }
 
 }  // namespace

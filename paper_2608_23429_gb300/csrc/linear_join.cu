@@ -11,9 +11,9 @@ constexpr int kJoinThreads = 256;
 
 template <int ACT>
 __device__ __forceinline__ void activate(float* v) {
-    Two x = two(v[0], v[1]), y = two(v[2], v[3]);
-    lin_act4<ACT>(x, y);
-    const float2 f = both(x), g = both(y);
+    Two x[2] = {two(v[0], v[1]), two(v[2], v[3])};
+    lin_act<ACT, 2>(x);
+    const float2 f = both(x[0]), g = both(x[1]);
     v[0] = f.x, v[1] = f.y, v[2] = g.x, v[3] = g.y;
 }
 

@@ -29,6 +29,49 @@ def product(lib, x, w, out="fp32", act="NONE", rows=None):
     return y
 
 
+# pre-activations on both sides of where the factor's denominator passes 2^30, and far beyond
+TAIL = [0.0, -1.0, -4.0, -5.5, -5.6, -5.75, -6.0, -6.5, -8.0, -10.0, -12.5, -14.0, -20.0, -20.75, -21.0, -25.0, -30.0, -40.0, -60.0, -80.0, -87.0,
+        -100.0, -1e3, -1e6, -1e9, -1e30, -3e38, 5.5, 20.0, 1e3, 1e9, 1e30, 3e38]
+
+
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+@pytest.mark.parametrize("act", ["SILU", "GELU"])
+@pytest.mark.parametrize("m,n,k", [(3, 33, 8), (40, 33, 8), (200, 264, 64), (40, 36, 8192)])  # few rows, off the grid, by TMA, parts of K
+def test_activations_go_to_zero(lib, m, n, k, act, out):
+    """One product of 1 with the value itself, so that sums are exact. With t the exponent (SiLU: -v, GELU: -2 sqrt(2/pi) (v +
+    0.044715 v^3)), rounding t moves exp(t) by 3 u |t|, the remaining steps by 8 u: of the activation, not of the value. Below
+    2^-126 the special function unit gives zero: 2^-126 |v|, taken up to where t passes 126 (v down to -88)."""
+    v = torch.tensor(TAIL, dtype=torch.float32).bfloat16()
+    x, w = torch.zeros(m, k, device="cuda").bfloat16(), torch.zeros(n, k, device="cuda").bfloat16()
+    x[:, k - 3] = 1.0
+    w[:, k - 3] = v.repeat(-(-n // len(TAIL)))[:n].cuda()
+    y = product(lib, x, w, out, act).double()
+    s = w[:, k - 3].double()
+    t = -s if act == "SILU" else -2.0 * (2.0 / torch.pi) ** 0.5 * (s + 0.044715 * s ** 3)
+    ref = s / (1.0 + torch.exp(t))
+    slack = (16 + 4 * t.abs().clamp_max(200)) * U * ref.abs() + 2.0 ** -126 * 90
+    step = ref.abs() * (2.0 ** -8 if out == "bf16" else 2.0 ** -24) + 2.0 ** -134  # half a step of the result, bf16's smallest included
+    assert bool(((y - ref).abs() <= slack + step).all()), (s[((y - ref).abs() > slack + step).any(0)], y[0], ref)
+
+
+@pytest.mark.parametrize("act", ["SILU", "GELU"])
+@pytest.mark.parametrize("m,n", [(3, 40), (200, 40), (200, 33)])
+def test_activations_of_values_that_are_not_finite(lib, m, n, act):
+    """v / (1 + exp(-v)) and its like at the ends: NaN at -infinity (which it would divide by infinity), infinity at infinity; the
+    values around them, which share a reciprocal with them, keep theirs but for its rounding (16 u, as above)."""
+    x, w = torch.zeros(m, 64, device="cuda").bfloat16(), torch.zeros(n, 64, device="cuda").bfloat16()
+    x[:, 0] = 1.0
+    w[:, 0] = 1.5
+    plain = product(lib, x, w, "fp32", act)[0, 0]
+    for at, value in ((5, float("-inf")), (10, float("inf")), (15, float("nan"))):
+        w[at, 0] = value
+    y = product(lib, x, w, "fp32", act)
+    assert bool(torch.isnan(y[:, 5]).all()) and bool((y[:, 10] == float("inf")).all()) and bool(torch.isnan(y[:, 15]).all())
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[[5, 10, 15]] = False
+    assert bool(((y[:, rest] - plain).abs() <= 16 * U * plain).all())
+
+
 @pytest.mark.parametrize("type", ["bf16", "e4m3"])
 def test_bf16_results_of_very_long_sums_are_not_cut_off(lib, type):
     """Positive terms, so that what a sum loses has one sign. Rounding to bf16 has none: over n results of a spread of more than a
