@@ -8,7 +8,7 @@
 namespace cbk {
 namespace {
 
-__device__ int g_linear_status;  // CB_DEV_* codes of this device's launches
+__device__ int g_linear_status[1];  // CB_DEV_* codes of this device's launches
 
 bool wide_type(cb_dtype t) { return t == CB_BF16 || t == CB_FP32; }
 size_t bytes_of(int t) { return t == CB_BF16 ? 2 : t == CB_FP32 ? 4 : 1; }
@@ -102,6 +102,9 @@ int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes
 // with a bf16 output and hidden state 178 -> 150 us, fp32 hidden state alone 212 -> 192; 4096 x 1152 x 4608 64.1 -> 66.2 ({2, 5}).
 constexpr int kShortBlocks = 16, kMoreBoxes[2][2] = {{1, 4}, {4, 7}};
 
+// Bytes of a row up to which a box's place in it (and a gate's piece's), and that of the box behind, is a positive int.
+constexpr long long kMaxRowBytes = (1LL << 31) - 1024;
+
 // Results and hidden states whose rows lie on the 16-byte grid go by TMA, in boxes of 32 rows by 64 bytes.
 int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
     const LinearEpilogue& e = a->e;
@@ -114,10 +117,10 @@ int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
                 {e.resid, e.resid_stride, (long long)bytes_of(io->resid_dtype), &a->resid_map},
                 {e.resid_out, e.resid_out_stride, (long long)bytes_of(io->resid_dtype), &a->resid_out_map}};
     for (const auto& u : used)
-        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40)) return CB_OK;
+        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40 || e.N * u.es > kMaxRowBytes)) return CB_OK;
     // a gate's pieces of 16 bytes are read whole
     const long long gs = (long long)bytes_of(io->gate_dtype);
-    if (e.gate && (!on_grid(e.gate, 16) || e.gate_stride * gs % 16 != 0 || e.N * gs % 16 != 0)) return CB_OK;
+    if (e.gate && (!on_grid(e.gate, 16) || e.gate_stride * gs % 16 != 0 || e.N * gs % 16 != 0 || e.N * gs > kMaxRowBytes)) return CB_OK;
     for (const auto& u : used) {
         if (!u.p) continue;
         const int rc = operand_map(u.map, u.p, e.M, e.N * u.es, u.row * u.es, 32, 64);

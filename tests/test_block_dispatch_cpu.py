@@ -1,0 +1,81 @@
+"""Which kernel a matrix product runs, with what: the host side of cb_linear_* over stand-ins for the CUDA runtime and the launchers
+(linear_stub.cpp), on the CPU."""
+import ctypes
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OUT, HIDDEN, DIRECT = 0, 1, 2  # ways in which results leave
+
+
+@pytest.fixture(scope="module")
+def library(tmp_path_factory):
+    from paper_2608_23429_gb300 import build
+    build.build()
+    so = str(tmp_path_factory.mktemp("stub") / "liblinear_stub.so")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(build._nvcc()))), "include")
+    subprocess.run([shutil.which("g++"), "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-Bsymbolic", f"-I{cuda}", "-o", so,
+                    os.path.join(ROOT, "tests", "linear_stub.cpp"), "-x", "c++", os.path.join(build.CSRC, "linear.cu")], check=True)
+    return so
+
+
+def _load(path):
+    from paper_2608_23429_gb300 import block, chebboost as cb
+    lib = ctypes.CDLL(path)
+    lib.stub_log.restype = ctypes.c_char_p
+    for name in ("cb_linear_create", "cb_linear_run", "cb_linear_destroy", "cb_linear_device_status"):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = block._sig[name]
+    return lib, block, cb
+
+
+@pytest.fixture()
+def stub(library):
+    s = _load(library)
+    s[0].stub_reset()
+    return s
+
+
+def _log(lib):
+    """(name, {field: value}) of every call noted since the last reset."""
+    return [(line.split()[0], {k: int(v) for k, v in re.findall(r"(\w+)=(-?\d+)", line)}) for line in lib.stub_log().decode().splitlines()]
+
+
+def run(stub, rows, n, k, type=0, out=None, resid=None, gate=None, off=0, **io):
+    """One call on addresses that nothing reads; `out`, `resid`, `gate`: their types."""
+    lib, block, cb = stub
+    d = block.cb_linear_desc(in_features=k, out_features=n, type=type, w=(1 << 40) + off)
+    layer = ctypes.c_void_p()
+    assert lib.cb_linear_create(ctypes.addressof(d), ctypes.byref(layer)) == 0
+    desc = block.cb_linear_io(rows=rows, out_dtype=out or 0, resid_dtype=resid or 0, gate_dtype=gate or 0, **io)
+    at = lambda i, t: None if t is None else i << 42  # noqa: E731
+    rc = lib.cb_linear_run(layer, ctypes.addressof(desc), (1 << 41) + off, None, at(1, resid), at(2, gate), at(3, out), at(4, resid), None)
+    lib.cb_linear_destroy(layer)
+    return rc, [c for c in _log(lib) if c[0] != "trim"]
+
+
+BF16, FP32 = 0, 1
+
+
+@pytest.mark.parametrize("n,kw,results", [
+    ((1 << 29) - 1024, dict(out=FP32), OUT), ((1 << 29) + 64, dict(out=FP32), DIRECT), ((1 << 30) - 1024, dict(out=BF16), OUT),
+    ((1 << 30) + 64, dict(out=BF16), DIRECT), ((1 << 29) + 64, dict(resid=FP32), DIRECT), ((1 << 29) + 64, dict(resid=BF16), HIDDEN),
+    ((1 << 29) + 64, dict(resid=BF16, gate=FP32), DIRECT), ((1 << 29) + 64, dict(resid=BF16, out=FP32), DIRECT),
+    ((1 << 31) - 1024, dict(out=BF16, resid=FP32), DIRECT)])
+def test_very_wide_results_leave_by_64_bit_addresses(stub, n, kw, results):
+    """The places in a row that copies by TMA are given are signed 32-bit bytes: rows that pass them are stored by the threads."""
+    rc, log = run(stub, 33, n, 8, **kw)
+    assert rc == 0 and [c[0] for c in log][-1] == "tc"
+    assert log[-1][1]["results"] == results
+    assert all(c[1]["wide"] < 1 << 31 for c in log if c[0] == "map"), log
+
+
+def test_parts_of_k_and_operands_off_the_grid(stub):
+    assert [c[0] for c in run(stub, 256, 1152, 4608, out=BF16)[1]] == ["malloc", "map", "map", "map", "tc", "join", "free"]
+    stub[0].stub_reset()
+    assert [c[0] for c in run(stub, 4096, 1152, 1152, off=2, out=BF16)[1]] == ["malloc", "pack", "map", "map", "map", "tc", "free"]
+    stub[0].stub_reset()
+    assert [c[0] for c in run(stub, 32, 1152, 4608, out=BF16)[1]] == ["few"]

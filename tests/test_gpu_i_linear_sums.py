@@ -1,4 +1,4 @@
-"""What the sums and activations of cb_linear_run lose, where tolerances that follow the sums' sizes cannot see it."""
+"""What the sums and activations of cb_linear_run lose, where tolerances that follow the sums' sizes cannot see it, and its largest sizes."""
 import pytest
 import torch
 
@@ -123,3 +123,18 @@ def test_fp32_sums_of_terms_of_one_sign(lib, type, k):
     ref = sum(x[:, i:i + 16384].float().double() @ w[:seen, i:i + 16384].float().double().t() for i in range(0, k, 16384))
     off = float((y - ref).norm() / ref.norm())
     assert off < 1.3e-6 + (k / 512) ** 0.5 * U, off
+
+
+def test_results_wider_than_2_31_bytes(lib):
+    """Rows of fp32 results of 2^31 bytes and more, 76 GB in all."""
+    m, n, k = 33, (1 << 29) + 1184, 8
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 120e9:
+        pytest.skip("needs 120 GB")
+    x = torch.randint(-4, 5, (m, k), device="cuda").bfloat16()
+    w = torch.randint(-4, 5, (n, k), device="cuda", dtype=torch.int8).bfloat16()
+    y = product(lib, x, w)
+    for at in (0, (1 << 28) - 512, (1 << 29) - 512, n - 1024):  # small whole numbers: exact
+        assert torch.equal(y[:, at:at + 1024].double(), x.double() @ w[at:at + 1024].double().t())
+    del y, w
+    torch.cuda.empty_cache()
