@@ -165,6 +165,7 @@ void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int* c
                 if (n > 32 && n - 32 >= N) continue;
                 const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n) * p;
                 const long long units = g == 2 ? dev.pairs : dev.sms;
+                if (units < 1) break;  // no room for pairs
                 if (p > 1 && tiles > units) break;  // smaller tiles are more
                 const double join = p > 1 ? kJoinClocks + 4.0 * p * M * N / kJoinBytesPerClock : 0.0;
                 const double cost = (double)((tiles + units - 1) / units) * ((k_blocks + p - 1) / p) * (256.0 + 2.0 * n / g) + join;

@@ -5,6 +5,7 @@ import os
 import re
 import shutil
 import subprocess
+import sys
 
 import pytest
 
@@ -79,3 +80,24 @@ def test_parts_of_k_and_operands_off_the_grid(stub):
     assert [c[0] for c in run(stub, 4096, 1152, 1152, off=2, out=BF16)[1]] == ["malloc", "pack", "map", "map", "map", "tc", "free"]
     stub[0].stub_reset()
     assert [c[0] for c in run(stub, 32, 1152, 4608, out=BF16)[1]] == ["few"]
+
+
+NO_PAIRS = """
+import sys
+sys.path.insert(0, {tests!r})
+import test_block_dispatch_cpu as t
+stub = t._load({so!r})
+stub[0].stub_pairs(0)
+for m, n, k in ((33, 64, 64), (4096, 1152, 1152), (256, 1152, 4608)):
+    stub[0].stub_reset()
+    rc, log = t.run(stub, m, n, k, out=0)
+    tc = [f for name, f in log if name == "tc"]
+    assert rc == 0 and [f["cg"] for f in tc] == [1] and tc[0]["grid"] > 0, log
+"""
+
+
+def test_no_room_for_pairs_of_ctas(library):
+    """A device (or its share of one) on which no two CTAs can run as a pair: single ones, and no division by their number."""
+    r = subprocess.run([sys.executable, "-c", NO_PAIRS.format(tests=os.path.join(ROOT, "tests"), so=library)], cwd=ROOT,
+                       capture_output=True, text=True, timeout=200)
+    assert r.returncode == 0, (r.returncode, r.stderr)
