@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(32 * W, lines_late(CH, W) ? 1024 / (32 * W) : 
     const int t = threadIdx.x;
     const long long line = (long long)(row / A.tokens) * A.line_stride;
     const long long xo = row * A.x_stride, bo = row * A.branch_stride;
-    auto hidden = [&](int e) {
+    auto hidden = [&](unsigned e) {
         float v = value_at(A.x, xo + e, A.x_bf16);
         if (A.branch) {
             const float b = value_at(A.branch, bo + e, A.branch_bf16);
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(32 * W, lines_late(CH, W) ? 1024 / (32 * W) : 
         }
         return v;
     };
-    auto normed = [&](float v, int e) {
+    auto normed = [&](float v, unsigned e) {
         if (A.weight) v *= value_at(A.weight, e, A.param_bf16);
         if (A.scale) v = fmaf(v, value_at(A.scale, line + e, A.param_bf16), v);
         return A.shift ? v + value_at(A.shift, line + e, A.param_bf16) : v;
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(32 * W, lines_late(CH, W) ? 1024 / (32 * W) : 
         if constexpr (lines_late(CH, W)) load_lines();
         if (A.x_out) store_all<CH, T>(A.x_out, row * A.x_out_stride, A.x_bf16 ? CB_BF16 : CB_FP32, t, A.hidden, h);
     } else {
-        for (int e = t; e < A.hidden; e += T) {
+        for (unsigned e = t; e < (unsigned)A.hidden; e += T) {  // (an int would pass its end on the way out of the longest rows)
             const float v = hidden(e);
             sum = fmaf(v, v, sum);
         }
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(32 * W, lines_late(CH, W) ? 1024 / (32 * W) : 
             if (c * T + t < A.hidden) amax = max_abs(amax, n);
         }
     } else if (A.out_dtype == CB_E4M3) {
-        for (int e = t; e < A.hidden; e += T) amax = max_abs(amax, normed(hidden(e) * rstd, e));
+        for (unsigned e = t; e < (unsigned)A.hidden; e += T) amax = max_abs(amax, normed(hidden(e) * rstd, e));
     }
     if (A.out_dtype == CB_E4M3) {
         const float s = norm_scale_of(row_reduce<W, true>(__float_as_uint(amax) & 0x7FFFFFFFu, slots[1]));
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(32 * W, lines_late(CH, W) ? 1024 / (32 * W) : 
         for (int c = 0; c < CH; ++c) h[c] *= inv;
         store_all<CH, T>(A.out, row * A.out_stride, A.out_dtype, t, A.hidden, h);
     } else {
-        for (int e = t; e < A.hidden; e += T) {
+        for (unsigned e = t; e < (unsigned)A.hidden; e += T) {
             const float v = hidden(e);
             if (A.x_out) put(A.x_out, row * A.x_out_stride + e, A.x_bf16 ? CB_BF16 : CB_FP32, v);
             put(A.out, row * A.out_stride + e, A.out_dtype, normed(v * rstd, e) * inv);
