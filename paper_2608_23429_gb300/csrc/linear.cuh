@@ -105,10 +105,10 @@ __device__ __forceinline__ uint32_t lin_ld1(const void* p, long long e, int bf16
     uint32_t r = 0;
     if (bf16) {
         uint16_t h;
-        asm("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(reinterpret_cast<const uint16_t*>(p) + e));
+        asm volatile("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(reinterpret_cast<const uint16_t*>(p) + e));
         r = (uint32_t)h << 16;
     } else {
-        asm("ld.global.u32 %0, [%1];" : "=r"(r) : "l"(reinterpret_cast<const uint32_t*>(p) + e));
+        asm volatile("ld.global.u32 %0, [%1];" : "=r"(r) : "l"(reinterpret_cast<const uint32_t*>(p) + e));
     }
     return r;
 }

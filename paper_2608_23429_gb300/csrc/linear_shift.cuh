@@ -11,7 +11,7 @@ namespace {
 // The aligned 16 bytes at p where `on`, else zeros; predicated, so that loads are in flight together.
 __device__ __forceinline__ uint4 ld16_if(const char* p, bool on) {
     uint4 v;
-    asm("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\t"
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\t"
         "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
         "@p ld.global.v4.u32 {%0,%1,%2,%3}, [%4];\n\t}"
         : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)

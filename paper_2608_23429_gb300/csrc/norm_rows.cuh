@@ -36,7 +36,7 @@ __device__ __forceinline__ Raw8<BF16> load8(const void* p, long long e) {
     const char* a = reinterpret_cast<const char*>(p) + (BF16 ? 2 : 4) * e;
 #pragma unroll
     for (int i = 0; i < (BF16 ? 1 : 2); ++i)
-        asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w) : "l"(a + 16 * i));
+        asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w) : "l"(a + 16 * i));
     return r;
 }
 // fp32 in one store of 32 bytes where it lies on such a boundary: two of 16 leave half a sector for each other.

@@ -17,7 +17,7 @@ namespace {
 // GB300 (663 against 635 us for 2 x 2.15 GB at 4 CTAs per SM).
 __device__ __forceinline__ uint4 ld_v4(const void* p) {
     uint4 v;
-    asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 

@@ -32,7 +32,7 @@ constexpr float kTiny = 1.17549435e-38f;  // 2^-126, the smallest scale: its rec
 
 __device__ __forceinline__ uint4 ld_v4(const void* p) {
     uint4 v;
-    asm("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 
