@@ -149,56 +149,57 @@ __device__ __forceinline__ Two add2(Two a, Two b) {
 }
 
 // v / (1 + 2^t): SiLU with t = -v log2(e), the tanh form of GELU with t = -2 log2(e) sqrt(2/pi) (v + 0.044715 v^3),
-// since (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z)). Four at a time, with one reciprocal of the product of their
-// denominators, as the unit for special functions is what an epilogue with an activation waits for. Where a product passes 2^120
-// (four values of t = 30: SiLU at -20.8, GELU at -5.7; or one of 120), or one of its values is a NaN, all N pairs are made anew with a
-// reciprocal each. At -infinity that gives NaN, as the quotient is. Asked for once for all pairs: a branch for every four
-// values keeps them from being worked on together (GB300, 4096 x 4608 x 1152 e4m3 with GELU, 10 % longer).
+// since (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z)). At -infinity it is NaN, as the quotients are.
+template <int ACT>
+__device__ __forceinline__ Two lin_denominators(Two v) {
+    constexpr float kSilu = -1.44269504f, kGelu1 = -2.30220820f, kGelu3 = -0.102943239f;
+    float2 t = both(ACT == CB_ACT_SILU ? mul2(v, two(kSilu, kSilu))
+                                       : mul2(v, fma2(two(kGelu3, kGelu3), mul2(v, v), two(kGelu1, kGelu1))));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.y));
+    return add2(two(t.x, t.y), two(1.0f, 1.0f));
+}
+__device__ __forceinline__ float lin_reciprocal(float d) {
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d));
+    return d;
+}
+template <int ACT>
+__device__ __forceinline__ Two lin_act(Two v) {
+    if constexpr (ACT == CB_ACT_NONE) return v;
+    const float2 d = both(lin_denominators<ACT>(v));
+    return mul2(v, two(lin_reciprocal(d.x), lin_reciprocal(d.y)));
+}
+
+// The same for N pairs, with one reciprocal of four denominators' product, for epilogues that wait for the unit for special
+// functions. Where a product passes 2^120 (four values of t = 30: SiLU at -20.8, GELU at -5.7; or one of 120), or one of its values is a NaN,
+// all pairs are made anew with a reciprocal each. Asked for once for all of them: a branch for every four values keeps them from
+// being worked on together (GB300, 4096 x 4608 x 1152 e4m3 with GELU, 10 % longer), and where results leave by the threads,
+// which wait for loads, a branch costs more than the reciprocals (999 x 1155 x 577 SiLU, fp32 hidden state: 12.4 us as above, 12.6 so).
 template <int ACT, int N>
-__device__ __forceinline__ void lin_act(Two* x) {
+__device__ __forceinline__ void lin_act_all(Two* x) {
     if constexpr (ACT != CB_ACT_NONE) {
         static_assert(N % 2 == 0, "two pairs at a time");
-        constexpr float kSilu = -1.44269504f, kGelu1 = -2.30220820f, kGelu3 = -0.102943239f, kMost = 1.32922800e36f;  // 2^120
-        auto denominators = [](Two v) {
-            float2 t = both(ACT == CB_ACT_SILU ? mul2(v, two(kSilu, kSilu))
-                                               : mul2(v, fma2(two(kGelu3, kGelu3), mul2(v, v), two(kGelu1, kGelu1))));
-            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.x));
-            asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.y));
-            return add2(two(t.x, t.y), two(1.0f, 1.0f));
-        };
-        auto reciprocal = [](float d) {
-            asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d));
-            return d;
-        };
+        constexpr float kMost = 1.32922800e36f;  // 2^120
         Two y[N];
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-            const Two a = denominators(x[i]), b = denominators(x[i + 1]);
+            const Two a = lin_denominators<ACT>(x[i]), b = lin_denominators<ACT>(x[i + 1]);
             const float2 p = both(mul2(a, b));
             float r = p.x * p.y;
             asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(r));
-            r = reciprocal(r);
+            r = lin_reciprocal(r);
             const Two q = mul2(two(r, r), two(p.y, p.x));  // 1 / (a b), pair by pair
             y[i] = mul2(x[i], mul2(q, b));
             y[i + 1] = mul2(x[i + 1], mul2(q, a));
         }
         if (!(most <= kMost)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float2 d = both(denominators(x[i]));
-                y[i] = mul2(x[i], two(reciprocal(d.x), reciprocal(d.y)));
-            }
+            for (int i = 0; i < N; ++i) y[i] = lin_act<ACT>(x[i]);
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = y[i];
     }
-}
-template <int ACT>
-__device__ __forceinline__ float lin_act1(float v) {
-    Two a[2] = {two(v, v), two(v, v)};
-    lin_act<ACT, 2>(a);
-    return both(a[0]).x;
 }
 
 }  // namespace

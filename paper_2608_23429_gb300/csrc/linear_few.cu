@@ -155,8 +155,8 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
         if (E.x_scale) v *= E.x_scale[row];
         const float s = E.w_scale ? E.w_scale[col] : 1.0f;
         v = fmaf(v, s, E.bias ? __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16)) : 0.0f);
-        if (E.act == CB_ACT_GELU) v = lin_act1<CB_ACT_GELU>(v);
-        if (E.act == CB_ACT_SILU) v = lin_act1<CB_ACT_SILU>(v);
+        if (E.act == CB_ACT_GELU) v = both(lin_act<CB_ACT_GELU>(two(v, v))).x;
+        if (E.act == CB_ACT_SILU) v = both(lin_act<CB_ACT_SILU>(two(v, v))).x;
         if (E.out) lin_put1(E.out, row * E.out_stride + col, E.out_bf16, v);
         if (E.resid_out) {
             const float r = __uint_as_float(lin_ld1(E.resid, row * E.resid_stride + col, E.resid_bf16));

@@ -11,9 +11,7 @@ constexpr int kJoinThreads = 256;
 
 template <int ACT>
 __device__ __forceinline__ void activate(float* v) {
-    Two x[2] = {two(v[0], v[1]), two(v[2], v[3])};
-    lin_act<ACT, 2>(x);
-    const float2 f = both(x[0]), g = both(x[1]);
+    const float2 f = both(lin_act<ACT>(two(v[0], v[1]))), g = both(lin_act<ACT>(two(v[2], v[3])));
     v[0] = f.x, v[1] = f.y, v[2] = g.x, v[3] = g.y;
 }
 

@@ -283,7 +283,7 @@ __device__ __forceinline__ void values(const LinearEpilogue& E, const float* col
         if (E.x_scale) p = mul2(p, xs2), q = mul2(q, xs2);
         x[2 * j] = fma2(p, s.x, b.x);
         x[2 * j + 1] = fma2(q, s.y, b.y);
-        if (j % 4 == 3) lin_act<ACT, 8>(x + 2 * j - 6);
+        if (j % 4 == 3) lin_act_all<ACT, 8>(x + 2 * j - 6);
     }
 }
 
@@ -373,14 +373,10 @@ __device__ __forceinline__ void put_rows(const LinearEpilogue& E, void* p, long 
 
 template <int ACT>
 __device__ __forceinline__ void activate(const Column& k, float* v) {
-    Two x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = fma2(two(v[2 * i], v[2 * i + 1]), two(k.scale, k.scale), two(k.bias, k.bias));
-    lin_act<ACT, 4>(x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = both(x[i]);
-        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    for (int i = 0; i < 8; i += 2) {
+        const float2 f = both(lin_act<ACT>(fma2(two(v[i], v[i + 1]), two(k.scale, k.scale), two(k.bias, k.bias))));
+        v[i] = f.x, v[i + 1] = f.y;
     }
 }
 
