@@ -58,23 +58,31 @@ struct Line {
     bool on;
 };
 
-// Its 16 bytes `k` bytes on, of which `left` belong to the row; zeros behind them.
-template <bool SHIFT>
+// How rows lie: on 16-byte boundaries and made of whole pieces, on them with a last piece that is not whole, or off them. The kernel for
+// the second is one of its own, as the last pieces' bytes take registers from the loads in flight.
+enum FewRows { kWhole, kTail, kShift };
+
+// Its 16 bytes `k` bytes on, of which `left` belong to the row; zeros behind them. kTail: zeros for a piece that is not whole, which
+// last_bytes reads, so that nothing behind the operand is.
+template <FewRows ROWS>
 __device__ __forceinline__ uint4 bytes16(const Line& l, int k, int left) {
-    if constexpr (!SHIFT) {
-        uint4 v = ld16_if(l.at + k, l.on && left > 0);
+    const char* const p = l.at + k;
+    if constexpr (ROWS != kShift) {
+        uint4 v = ld16_if(p, l.on && left >= (ROWS == kWhole ? 1 : 16));
+        // (zeros already, but without it fewer loads are in flight: GB300, 1 x 12288 x 4096 18.3 -> 23.6 us)
         if (left < 16) v = first_bytes(v, left);
         return v;
     } else {
-        const char* const p = l.at + k;
         const int m = (int)((uintptr_t)p & 15);
         const bool lo = l.on && left > 0, hi = lo && m && left > 16 - m;
         if (lo && (p - m < l.from || p - m + (hi ? 32 : 16) > l.to)) return bytes_at(p, left);  // at the operand's ends
         return first_bytes(shifted(ld16_if(p - m, lo), ld16_if(p - m + 16, hi), m), left);
     }
 }
+// A row's last bytes, fewer than 16, in the lane that has them.
+__device__ __forceinline__ uint4 last_bytes(const Line& l, int k, int left) { return bytes_at(l.at + k, l.on && left < 16 ? left : 0); }
 
-template <int NT, bool FP8, bool SHIFT>
+template <int NT, bool FP8, FewRows ROWS>
 __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_constant__ LinearFewArgs A) {
     __shared__ float part[kWarps][8 * NT][16];
     after_previous();
@@ -103,10 +111,10 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
 #pragma unroll
         for (int j = 0; j < DEEP; ++j) {
             const int k = k0 + j * step, left = k_bytes - k - 16 * t;
-            lo[j] = bytes16<SHIFT>(w_lo, k, left);
-            hi[j] = bytes16<SHIFT>(w_hi, k, left);
+            lo[j] = bytes16<ROWS>(w_lo, k, left);
+            hi[j] = bytes16<ROWS>(w_hi, k, left);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) xv[j][i] = bytes16<SHIFT>(xl[i], k, left);
+            for (int i = 0; i < NT; ++i) xv[j][i] = bytes16<ROWS>(xl[i], k, left);
         }
         float d[NT][4] = {};
 #pragma unroll
@@ -117,6 +125,18 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
         for (int i = 0; i < NT; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) sum[i][q] += d[i][q];
+    }
+    const int last = k_bytes / kTurn * kTurn;  // the last turn, which has the rows' last bytes
+    if (ROWS == kTail && last / kTurn % (kWarps * (int)ranks) == kWarps * (int)rank + warp) {
+        const int left = k_bytes - last - 16 * t;
+        const uint4 lo = last_bytes(w_lo, last, left), hi = last_bytes(w_hi, last, left);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            float d[4] = {};
+            product<FP8>(d, lo, hi, last_bytes(xl[i], last, left));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[i][q] += d[q];
+        }
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -171,17 +191,19 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
 }
 
 using Kernel = void (*)(LinearFewArgs);
-template <int NT>
-Kernel pick(bool fp8, bool shift) {
-    if (shift) return fp8 ? linear_few_kernel<NT, true, true> : linear_few_kernel<NT, false, true>;
-    return fp8 ? linear_few_kernel<NT, true, false> : linear_few_kernel<NT, false, false>;
+template <int NT, bool FP8>
+Kernel pick(FewRows rows) {
+    return rows == kShift ? linear_few_kernel<NT, FP8, kShift> : rows == kTail ? linear_few_kernel<NT, FP8, kTail> : linear_few_kernel<NT, FP8, kWhole>;
 }
+template <int NT>
+Kernel pick(bool fp8, FewRows rows) { return fp8 ? pick<NT, true>(rows) : pick<NT, false>(rows); }
 
 }  // namespace
 
 cudaError_t launch_linear_few(const LinearFewArgs& a, bool fp8, bool shift, int sms, cudaStream_t s) {
     const int nt = a.e.M <= 8 ? 1 : a.e.M <= 16 ? 2 : 4;
-    const Kernel k = nt == 1 ? pick<1>(fp8, shift) : nt == 2 ? pick<2>(fp8, shift) : pick<4>(fp8, shift);
+    const FewRows rows = shift ? kShift : a.k_bytes % 16 != 0 ? kTail : kWhole;
+    const Kernel k = nt == 1 ? pick<1>(fp8, rows) : nt == 2 ? pick<2>(fp8, rows) : pick<4>(fp8, rows);
     const unsigned cols = (unsigned)((a.e.N + 15) / 16);
     // CTAs along K while there are fewer than three per SM and every warp keeps two turns
     unsigned cluster = 1;
