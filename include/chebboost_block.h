@@ -146,7 +146,8 @@ int cb_linear_run(const cb_linear* layer, const cb_linear_io* io, const void* x,
                   const void* resid, const void* gate, void* out, void* resid_out, void* stream);
 
 /* The status word of this device's matrix products (CB_DEV_* codes, 0: nothing noted since the last
- * read) into *status, and clear it. Synchronises `stream`. Errors: CB_ERR_ARG, CB_ERR_CUDA. */
+ * read) into *status, and clear it, in one step: a code noted meanwhile by another stream's product is
+ * left for the next read. Synchronises `stream`. Errors: CB_ERR_ARG, CB_ERR_CUDA. */
 int cb_linear_device_status(int* status, void* stream);
 
 #ifdef __cplusplus

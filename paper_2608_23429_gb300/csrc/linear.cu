@@ -320,15 +320,27 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
 }
 
 int cb_linear_device_status(int* status, void* stream) {
+    using namespace cbk;
     if (!status) return CB_ERR_ARG;
+    const Device* dev = nullptr;
+    const int rc = device_info(&dev);
+    if (rc != CB_OK) return rc;
+    // one kernel takes the word and clears it: between a copy and a memset another stream's product might note a code
     const cudaStream_t s = (cudaStream_t)stream;
-    int* word = nullptr;
+    void* taken = nullptr;
     int v = 0;
-    cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&word), cbk::g_linear_status);
-    if (e == cudaSuccess) e = cudaMemcpyAsync(&v, word, sizeof v, cudaMemcpyDeviceToHost, s);
-    if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof v, s);
+    cudaError_t e = cudaMallocFromPoolAsync(&taken, sizeof v, dev->pool, s);
+    if (e == cudaSuccess) {
+        e = take_status(dev->status, static_cast<int*>(taken), s);
+        if (e == cudaSuccess) e = cudaMemcpyAsync(&v, taken, sizeof v, cudaMemcpyDeviceToHost, s);
+        const cudaError_t f = cudaFreeAsync(taken, s);
+        if (e == cudaSuccess) e = f;
+    }
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    if (e != cudaSuccess) return cbk::cuda_error(e, "linear status");
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();  // returned here
+        return cuda_error(e, "linear status");
+    }
     *status = v;
     return CB_OK;
 }

@@ -82,6 +82,21 @@ def test_parts_of_k_and_operands_off_the_grid(stub):
     assert [c[0] for c in run(stub, 32, 1152, 4608, out=BF16)[1]] == ["few"]
 
 
+def test_the_status_is_taken_and_cleared_in_one_step(stub):
+    """A code that another stream's product notes between a read and a clearing would be lost: one kernel exchanges the word."""
+    lib = stub[0]
+    status = ctypes.c_int(-1)
+    assert lib.cb_linear_device_status(ctypes.addressof(status), None) == 0 and status.value == 0
+    assert [c[0] for c in _log(lib)] == ["malloc", "take_status", "memcpy", "free", "synchronize"]
+    for fails in ("malloc", "take_status", "memcpy", "free", "synchronize"):
+        lib.stub_reset()
+        lib.stub_fail(fails.encode())
+        status.value = -1
+        assert lib.cb_linear_device_status(ctypes.addressof(status), None) == -7 and status.value == -1
+        names = [c[0] for c in _log(lib)]
+        assert fails == "malloc" or "free" in names  # the word that it was taken to is given back
+
+
 NO_PAIRS = """
 import sys
 sys.path.insert(0, {tests!r})
