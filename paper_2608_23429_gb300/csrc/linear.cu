@@ -76,12 +76,12 @@ size_t copies_bytes(const void* x, int M, const void* w, int N, int bytes) {
     const size_t row = (size_t)(bytes + 31) / 32 * 32;
     return ((x ? M * row : 0) + 255) / 256 * 256 + ((w ? N * row : 0) + 255) / 256 * 256;
 }
-cudaError_t make_copies(const void* x, long long x_row, int M, const void* w, long long w_row, int N, int bytes, char* at, bool overlap,
+cudaError_t make_copies(const void* x, long long x_row, int M, const void* w, long long w_row, int N, int bytes, char* at,
                         LinearPackArgs* pack, cudaStream_t s) {
     const unsigned chunks = (unsigned)(bytes + 31) / 32;
     if (x) pack->o[0] = {static_cast<const char*>(x), at, M, x_row, bytes, chunks};
     if (w) pack->o[1] = {static_cast<const char*>(w), at + copies_bytes(x, M, nullptr, 0, bytes), N, w_row, bytes, chunks};
-    pack->overlap = overlap;
+    pack->overlap = 1;
     return launch_linear_pack(*pack, s);
 }
 
@@ -276,22 +276,18 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     const long long row = (ep.N + 31) / 32 * 32;  // floats of a row of sums
     a.part_rows = a.tiles_m * 128 * cg;
     const size_t sums = a.parts > 1 ? (size_t)a.parts * a.part_rows * row * 4 : 0;
-    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     void* space = nullptr;
     if (copies + sums) {
-        cudaError_t e = cudaStreamIsCapturing(s, &capture);
-        if (e == cudaSuccess) e = cudaMallocFromPoolAsync(&space, copies + sums, dev->pool, s);
+        const cudaError_t e = cudaMallocFromPoolAsync(&space, copies + sums, dev->pool, s);
         if (e != cudaSuccess) {
             (void)cudaGetLastError();  // returned here, so not left for a check of the caller's own launches
             return cuda_error(e, "linear workspace");
         }
     }
-    const bool captured = capture != cudaStreamCaptureStatusNone;  // the first kernel then follows the allocation, not a kernel
     LinearPackArgs pack{};
     LinearJoinArgs join{ep, 1, a.parts, (long long)a.part_rows * row, row, nullptr};
     cudaError_t e = cudaSuccess;
-    if (copies) e = make_copies(x_off, x_row, ep.M, w_off, w_row, ep.N, a.k_bytes, static_cast<char*>(space), !captured, &pack, s);
-    a.overlap = copies || !captured;
+    if (copies) e = make_copies(x_off, x_row, ep.M, w_off, w_row, ep.N, a.k_bytes, static_cast<char*>(space), &pack, s);
     if (a.parts > 1) {
         join.sums = reinterpret_cast<const float*>(static_cast<char*>(space) + copies);
         ep = LinearEpilogue{ep.M, ep.N, CB_ACT_NONE, (unsigned)ep.M, 0, 0, 0, 0, row, 0, 0, 0, nullptr, nullptr, nullptr, nullptr, nullptr,
