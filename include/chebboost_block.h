@@ -8,7 +8,8 @@
  * Conventions are those of chebboost.h: the caller owns every device buffer and
  * stream, work is enqueued on `stream` asynchronously, all arguments are
  * checked before anything is enqueued, and a negative status is an error
- * (cb_status_string, cb_last_error_message). No call allocates device memory.
+ * (cb_status_string, cb_last_error_message). No call but cb_linear_run, where it says so,
+ * and cb_linear_device_status (4 bytes) allocates device memory.
  * Buffers given for output must not overlap inputs, but for the one pair that
  * each call names.
  *
@@ -114,6 +115,8 @@ typedef struct cb_linear cb_linear; /* opaque, host-owned; holds no device memor
  * beyond 2^31 - 1024, in_features beyond CB_MAX_IN_FEATURES, or a row stride of w or x
  * beyond 2^31 - 256 bytes). The layer keeps the pointers: its buffers must outlive it. */
 int cb_linear_create(const cb_linear_desc* desc, cb_linear** out);
+/* The process's last layer gives back the device memory that cb_linear_run keeps (what work under way still
+ * uses stays until the next last one). NULL does nothing. */
 void cb_linear_destroy(cb_linear* layer);
 
 /* Matrix product with its epilogue. For every row m and output feature n
@@ -135,8 +138,8 @@ void cb_linear_destroy(cb_linear* layer);
  * Over 32 rows, operands whose rows do not start on 16-byte boundaries are copied onto
  * them first, and few tiles of long sums are split over in_features, whose parts' sums a
  * second kernel adds in order. Memory for either is allocated and freed in stream order,
- * from a pool of the library's own that keeps 1 GiB at most between calls; in a graph
- * it belongs to the graph. Where there is none left: CB_ERR_CUDA, and nothing has run.
+ * from a pool of the library's own that keeps 1 GiB at most between calls, until the last layer
+ * is destroyed; in a graph it belongs to the graph. Where there is none left: CB_ERR_CUDA, and nothing has run.
  * Every wait of the kernels on one of their barriers has a limit of a second; one that
  * runs out is noted in the status word of cb_linear_device_status and makes the
  * kernel return early, with incomplete results.

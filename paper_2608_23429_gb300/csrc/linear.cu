@@ -37,6 +37,18 @@ cudaError_t make_pool(int device, cudaMemPool_t* pool) {
     return e;
 }
 
+// Layers that exist; the last one gives back what the pools keep.
+std::atomic<long long> g_layers;
+
+void give_back() {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;  // another stream may be captured
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
+    for (auto& d : g_devices)
+        if (const Device* v = d.load(std::memory_order_acquire))
+            if (cudaMemPoolTrimTo(v->pool, 0) != cudaSuccess) (void)cudaGetLastError();  // (the process may be ending)
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
+}
+
 int device_info(const Device** out) {
     int d = 0;
     cudaError_t e = cudaGetDevice(&d);
@@ -200,11 +212,16 @@ int cb_linear_create(const cb_linear_desc* d, cb_linear** out) {
     if (!l) return CB_ERR_LIMIT;
     l->d = *d;
     if (l->d.w_stride == 0) l->d.w_stride = d->in_features;
+    cbk::g_layers.fetch_add(1, std::memory_order_relaxed);
     *out = l;
     return CB_OK;
 }
 
-void cb_linear_destroy(cb_linear* l) { delete l; }
+void cb_linear_destroy(cb_linear* l) {
+    if (!l) return;
+    delete l;
+    if (cbk::g_layers.fetch_sub(1, std::memory_order_acq_rel) == 1) cbk::give_back();
+}
 
 int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, const float* x_scale, const void* resid,
                   const void* gate, void* out, void* resid_out, void* stream) {

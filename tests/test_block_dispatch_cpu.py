@@ -82,6 +82,22 @@ def test_parts_of_k_and_operands_off_the_grid(stub):
     assert [c[0] for c in run(stub, 32, 1152, 4608, out=BF16)[1]] == ["few"]
 
 
+def test_the_last_layer_gives_the_workspace_back(stub):
+    lib, block, cb = stub
+    run(stub, 4096, 1152, 1152, off=2, out=BF16)  # the pool exists from here on
+    layers = [ctypes.c_void_p() for _ in range(3)]
+    d = block.cb_linear_desc(in_features=64, out_features=64, w=1 << 40)
+    for l in layers:
+        assert lib.cb_linear_create(ctypes.addressof(d), ctypes.byref(l)) == 0
+    lib.stub_reset()
+    lib.cb_linear_destroy(None)
+    lib.cb_linear_destroy(layers[1])
+    lib.cb_linear_destroy(layers[0])
+    assert _log(lib) == []
+    lib.cb_linear_destroy(layers[2])
+    assert [c[0] for c in _log(lib)] == ["trim"]
+
+
 def test_the_status_is_taken_and_cleared_in_one_step(stub):
     """A code that another stream's product notes between a read and a clearing would be lost: one kernel exchanges the word."""
     lib = stub[0]
