@@ -119,6 +119,12 @@ int cb_linear_create(const cb_linear_desc* desc, cb_linear** out);
  * uses stays until the next last one). NULL does nothing. */
 void cb_linear_destroy(cb_linear* layer);
 
+/* CB_OPT_WAIT_NS: limit of every wait of the layer's kernels on one of their barriers, ns (default 1e9, at most
+ * 6e10). CB_OPT_TEST_WITHHOLD: 1: (tests of the failure path only) over 32 rows the kernels announce more
+ * bytes of operands than they copy, so that the waits for them run out; results are then
+ * invalid. Errors: CB_ERR_ARG. */
+int cb_linear_set_option(cb_linear* layer, int option, int64_t value);
+
 /* Matrix product with its epilogue. For every row m and output feature n
  *     v = act(x_scale[m] * w_scale[n] * sum_k x[m, k] w[n, k] + bias[n])
  *     out = round(v)                        the branch output, as cb_cache_push takes it
@@ -140,7 +146,7 @@ void cb_linear_destroy(cb_linear* layer);
  * second kernel adds in order. Memory for either is allocated and freed in stream order,
  * from a pool of the library's own that keeps 1 GiB at most between calls, until the last layer
  * is destroyed; in a graph it belongs to the graph. Where there is none left: CB_ERR_CUDA, and nothing has run.
- * Every wait of the kernels on one of their barriers has a limit of a second; one that
+ * Every wait of the kernels on one of their barriers has a limit (cb_linear_set_option); one that
  * runs out is noted in the status word of cb_linear_device_status and makes the
  * kernel return early, with incomplete results.
  * Errors: CB_ERR_ARG, CB_ERR_ALIGN, CB_ERR_LIMIT (rows beyond 2^31 - 1024, or over 2^28

@@ -48,6 +48,7 @@ _sig = {
     "cb_norm_residual": ([_P] * 11, _I),
     "cb_linear_create": ([_P, ctypes.POINTER(_P)], _I),
     "cb_linear_destroy": ([_P], None),
+    "cb_linear_set_option": ([_P, _I, _L], _I),
     "cb_linear_run": ([_P] * 9, _I),
     "cb_linear_device_status": ([_P, _P], _I),
 }
@@ -82,6 +83,12 @@ def cb_linear_create(w, out_features: int, in_features: int, type: int, w_scale=
 
 def cb_linear_destroy(layer) -> None:
     _lib.cb_linear_destroy(layer)
+
+
+def cb_linear_set_option(layer, option: int, value: int) -> None:
+    rc = _lib.cb_linear_set_option(layer, option, int(value))
+    if rc < 0:
+        _raise(rc, "cb_linear_set_option")
 
 
 def cb_linear_run(layer, io: cb_linear_io, x, x_scale=None, resid=None, gate=None, out=None, resid_out=None,

@@ -190,6 +190,8 @@ void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int* c
 
 struct cb_linear {
     cb_linear_desc d;
+    unsigned long long wait_ns = 1000000000ull;
+    unsigned withheld = 0;
 };
 
 extern "C" {
@@ -221,6 +223,21 @@ void cb_linear_destroy(cb_linear* l) {
     if (!l) return;
     delete l;
     if (cbk::g_layers.fetch_sub(1, std::memory_order_acq_rel) == 1) cbk::give_back();
+}
+
+int cb_linear_set_option(cb_linear* l, int option, int64_t value) {
+    if (!l) return CB_ERR_ARG;
+    switch (option) {
+    case CB_OPT_WAIT_NS:
+        if (value < 0 || value > 60000000000LL) return CB_ERR_ARG;
+        l->wait_ns = (unsigned long long)value;
+        return CB_OK;
+    case CB_OPT_TEST_WITHHOLD:
+        if (value != 0 && value != 1) return CB_ERR_ARG;
+        l->withheld = 16 * (unsigned)value;
+        return CB_OK;
+    default: return CB_ERR_ARG;
+    }
 }
 
 int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, const float* x_scale, const void* resid,
@@ -267,7 +284,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     const Device* dev = nullptr;
     int rc = device_info(&dev);
     if (rc != CB_OK) return rc;
-    a.status = dev->status;
+    a.status = dev->status, a.wait_ns = l->wait_ns, a.withheld = l->withheld;
     const bool x_on = on_grid(x, 16) && x_row % 16 == 0, w_on = on_grid(d.w, 16) && w_row % 16 == 0;
     if (ep.M <= kFewRows) {
         const LinearFewArgs f{ep, 1, a.k_bytes, x_row, w_row, x, d.w};

@@ -39,6 +39,8 @@ struct LinearArgs {
     int passes, pass_blocks;  // stretches of K that are summed by themselves, and their slabs
     int parts, part_blocks;   // parts of K that are tiles of their own, and their slabs
     int part_rows;            // rows of the output of a part
+    unsigned withheld;        // tests only: bytes of every slab that are announced but never copied
+    unsigned long long wait_ns;  // limit of every wait on a barrier
     int* status;
 };
 

@@ -21,7 +21,7 @@
 // Bound by the tensor cores where tiles fill the SMs' rounds: GB300, 4608 x 3072 x 15360 bf16 with a gated hidden state 265 us (1.64
 // PFLOP/s, 85 % of the largest library rate), 8192 x 1152 x 4608 65 us (1.34), 4096 x 4608 x 1152 e4m3 with GELU 22 us (1.96).
 //
-// Every wait has a limit (kLimitNs); one that runs out sets the CTA's abort flag, so that all its roles leave, after
+// Every wait has a limit (A.wait_ns); one that runs out sets the CTA's abort flag, so that all its roles leave, after
 // the copies under way have landed, and frees the TMEM.
 #pragma once
 
@@ -43,7 +43,6 @@ constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the ot
 __host__ __device__ constexpr int epi_warps(Results r) { return r == Results::kDirect ? 16 : 8; }
 __host__ __device__ constexpr int linear_threads(Results r) { return 32 * (epi_warps(r) + 2); }
 constexpr int kTurn = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
-constexpr unsigned long long kLimitNs = 1000000000ull;
 
 struct alignas(16) Tail {  // behind the stages and the epilogue's warps' kTurn each
     float cols[2][2 * kAccStride];  // scales and biases of a tile's columns (where the output leaves by TMA)
@@ -84,19 +83,26 @@ __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) 
     return ok != 0;
 }
 
+// What ends a wait: the CTA's abort flag, or the limit, which sets it and notes a code.
+struct Limit {
+    volatile int* abort;
+    int* status;
+    unsigned long long ns;
+};
+
 // Wait for a phase of a barrier, until the limit or the CTA's abort flag.
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort, int* status, int code) {
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, const Limit& limit, int code) {
     unsigned long long t0 = 0;
     while (true) {
         for (int i = 0; i < 64; ++i)
             if (CLUSTER ? try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
-        if (*abort) return false;
+        if (*limit.abort) return false;
         const unsigned long long t = now_ns();
         if (t0 == 0) t0 = t;
-        if (t - t0 > kLimitNs) {
-            *abort = 1;
-            record(status, code);
+        if (t - t0 > limit.ns) {
+            *limit.abort = 1;
+            record(limit.status, code);
             return false;
         }
     }
@@ -234,10 +240,10 @@ struct Place {
 
 // Waits until the stages' last fills have been read: no copy and no arrival is under way then. `p`: the place behind
 // them, `fills`: how many there were.
-__device__ __forceinline__ bool drain(Place p, int fills, int stages, uint32_t empty, volatile int* abort, int* status) {
+__device__ __forceinline__ bool drain(Place p, int fills, int stages, uint32_t empty, const Limit& limit) {
     for (int i = 0; i < min(fills, stages); ++i) {
         p.s = p.s == 0 ? (p.phase ^= 1, stages - 1) : p.s - 1;
-        if (!wait(empty + 8 * p.s, p.phase, abort, status, CB_DEV_DRAIN_TIMEOUT)) return false;
+        if (!wait(empty + 8 * p.s, p.phase, limit, CB_DEV_DRAIN_TIMEOUT)) return false;
     }
     return true;
 }
@@ -422,7 +428,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     const uint32_t ring = smem_addr(base);
     const uint32_t full = smem_addr(T.full), empty = smem_addr(T.empty);
     const uint32_t acc_full = smem_addr(T.acc_full), acc_empty = smem_addr(T.acc_empty);
-    volatile int* const abort = &T.abort;
+    const Limit limit{&T.abort, A.status, A.wait_ns};
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
@@ -435,7 +441,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
             mbar_init(smem_addr(T.cols_full) + 8 * i, EPI);
         }
         for (int i = 0; HIDDEN && i < EPI * kMaxRing; ++i) mbar_init(smem_addr(T.resid_full) + 8 * i, 1);
-        *abort = 0;
+        *limit.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_generic_to_async();
     }
@@ -536,7 +542,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
             }
             look_tile(t + step);
             to_l2(t + step);
-            if (!DIRECT && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT)))
+            if (!DIRECT && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT)))
                 break;
             Column column;
             uint32_t rows_raw[8];
@@ -565,7 +571,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
             bool ok = true;
             const int passes = PASSES ? (slabs_to(tile.part) - slabs_from(tile.part) + A.pass_blocks - 1) / A.pass_blocks : 1;
             for (int i = 0; PASSES && i + 1 < passes; ++i) {  // all but the last one's sums are added up
-                ok = all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
+                ok = all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT));
                 if (!ok) break;
                 fence_after();
                 for (int c = half; c < chunks; c += EPI / 4) {
@@ -576,7 +582,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 }
                 release();
             }
-            if (!ok || !all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, abort, A.status, CB_DEV_CONSUMER_TIMEOUT))) break;
+            if (!ok || !all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT))) break;
             fence_after();
             const uint32_t acc_at = lanes + (pass & 1) * stride;
             if (half >= chunks) release();
@@ -611,7 +617,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
                     } else {
-                        ok = all(wait(smem_addr(T.resid_full[warp]) + 8 * held.s, held.phase, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
+                        ok = all(wait(smem_addr(T.resid_full[warp]) + 8 * held.s, held.phase, limit, CB_DEV_CONSUMER_TIMEOUT));
                         if (!ok) break;
                         const uint32_t box = ring_box(held.s), box2 = ring_box(held.s, 1);
                         if (E.resid_bf16) add_box<true>(box, lane, gate, x);
@@ -666,7 +672,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
             if (!ok) break;
         }
         for (; n_chunks < n_fetched; ++n_chunks, held.next(A.ring))  // given up: hidden states under way land first
-            if (!all(wait(smem_addr(T.resid_full[warp]) + 8 * held.s, held.phase, abort, A.status, CB_DEV_DRAIN_TIMEOUT))) {
+            if (!all(wait(smem_addr(T.resid_full[warp]) + 8 * held.s, held.phase, limit, CB_DEV_DRAIN_TIMEOUT))) {
                 const unsigned long long t0 = now_ns();
                 while (now_ns() - t0 < kMinDrainNs) {}
                 break;
@@ -689,12 +695,12 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 for (int kb0 = slabs_from(part); kb0 < to && ok; ++pass) {
                     const int end = PASSES ? min(kb0 + A.pass_blocks, to) : to;
                     const uint32_t sums = tmem + (pass & 1) * stride;
-                    ok = all(wait<CG == 2>(acc_empty + 8 * (pass & 1), ((pass >> 1) & 1) ^ 1, abort, A.status,
+                    ok = all(wait<CG == 2>(acc_empty + 8 * (pass & 1), ((pass >> 1) & 1) ^ 1, limit,
                                            CB_DEV_PRODUCER_TIMEOUT));
                     fence_after();
                     for (int kb = kb0; kb < end && ok; ++kb) {
                         const uint64_t a = desc0 + (uint32_t)(at.s * stage_bytes) / 16, b = a + kRows * kSlab / 16;
-                        ok = all(wait(full + 8 * at.s, at.phase, abort, A.status, CB_DEV_CONSUMER_TIMEOUT));
+                        ok = all(wait(full + 8 * at.s, at.phase, limit, CB_DEV_CONSUMER_TIMEOUT));
                         if (!ok) break;
                         fence_after();
                         const int steps = kb + 1 < A.k_blocks ? 4 : last_steps;
@@ -717,22 +723,23 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
         int fills = 0;
         bool ok = true;
         const uint32_t bar0 = CG == 2 ? in_first(full) : full;
+        const uint32_t announced = CG * stage_bytes + A.withheld;
         for (int t = first; t < total && ok; t += step) {
             const Tile tile = tile_at<SPLIT>(A, t);
             const int row = (tile.m * CG + (int)rank) * kRows, col = tile.n * A.tile_n + (int)rank * w_rows;
             for (int kb = slabs_from(tile.part), to = slabs_to(tile.part); kb < to; ++kb, ++fills) {
-                ok = all(wait(empty + 8 * at.s, at.phase ^ 1, abort, A.status, CB_DEV_PRODUCER_TIMEOUT));
+                ok = all(wait(empty + 8 * at.s, at.phase ^ 1, limit, CB_DEV_PRODUCER_TIMEOUT));
                 if (!ok) break;
                 const uint32_t dst = ring + at.s * stage_bytes;
                 if (elected()) {
-                    if (rank == 0) mbar_expect_tx(full + 8 * at.s, CG * stage_bytes);
+                    if (rank == 0) mbar_expect_tx(full + 8 * at.s, announced);
                     tma_2d<CG>(dst, &A.x_map, kb * kSlab, row, bar0 + 8 * at.s);
                     tma_2d<CG>(dst + kRows * kSlab, &A.w_map, kb * kSlab, col, bar0 + 8 * at.s);
                 }
                 at.next(stages);
             }
         }
-        if (!drain(at, fills, stages, empty, abort, A.status)) {
+        if (!drain(at, fills, stages, empty, limit)) {
             const unsigned long long t0 = now_ns();  // given up: copies under way land in microseconds
             while (now_ns() - t0 < kMinDrainNs) {}
         }
