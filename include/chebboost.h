@@ -111,7 +111,8 @@ enum { CB_KERNEL_AUTO = 0, CB_KERNEL_DIRECT = 1, CB_KERNEL_BULK = 2 };
 enum {
     CB_DEV_CONSUMER_TIMEOUT = 1, /* a consumer's wait for a filled stage ran out */
     CB_DEV_PRODUCER_TIMEOUT = 2, /* the producer's wait for a released stage ran out */
-    CB_DEV_DRAIN_TIMEOUT = 4     /* the producer's final wait for its own copies ran out */
+    CB_DEV_DRAIN_TIMEOUT = 4,    /* the producer's final wait for its own copies ran out */
+    CB_DEV_PLACEMENT = 8         /* a block's shared memory was off the boundary that its copies need: nothing was done */
 };
 
 /* Full-computation schedule (Sec. 3.3, Eq. for F; Alg. 1 offline stage):

@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
         after_previous();
-        if (threadIdx.x == 0) record(A.status, CB_DEV_PRODUCER_TIMEOUT);
+        if (threadIdx.x == 0) record(A.status, CB_DEV_PLACEMENT);
         return;
     }
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;

@@ -132,3 +132,14 @@ def test_no_room_for_pairs_of_ctas(library):
     r = subprocess.run([sys.executable, "-c", NO_PAIRS.format(tests=os.path.join(ROOT, "tests"), so=library)], cwd=ROOT,
                        capture_output=True, text=True, timeout=200)
     assert r.returncode == 0, (r.returncode, r.stderr)
+
+
+def test_each_device_status_is_a_bit_of_its_own():
+    """...and every code that a kernel notes without having waited says so."""
+    from paper_2608_23429_gb300 import build, chebboost as cb
+    header = open(os.path.join(ROOT, "include", "chebboost.h")).read()
+    codes = {name: int(v) for name, v in re.findall(r"\b(CB_DEV_\w+) = (\d+)", header)}
+    assert len(codes) >= 4 and sorted(codes.values()) == [1 << i for i in range(len(codes))]
+    assert all(getattr(cb, name) == v for name, v in codes.items())
+    kernel = open(os.path.join(build.CSRC, "linear_tc.cuh")).read()
+    assert re.findall(r"record\(A\.status, (\w+)\)", kernel) == ["CB_DEV_PLACEMENT"]
