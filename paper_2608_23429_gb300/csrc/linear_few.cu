@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const __grid_co
         part[0][i / 16][i % 16] = v;
     }
     if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-    const LinearEpilogue E = A.e;
+    const LinearEpilogue E = from_here(A.e);
     // the cluster's CTAs share the rest; the loops above and below deal the same elements to a thread
     for (int i = threadIdx.x; i < 8 * NT * 16; i += 32 * kWarps) {
         if (ranks > 1 && (i / (32 * kWarps)) % ranks != rank) continue;

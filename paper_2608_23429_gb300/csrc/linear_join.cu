@@ -17,7 +17,7 @@ __device__ __forceinline__ void activate(float* v) {
 
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ LinearJoinArgs A) {
     after_previous();
-    const LinearEpilogue& E = A.e;
+    const LinearEpilogue E = from_here(A.e);
     const unsigned quads = (unsigned)(E.N + 3) / 4;
     const unsigned long long at = (unsigned long long)blockIdx.x * kJoinThreads + threadIdx.x;
     if (at >= (unsigned long long)quads * E.M) return;

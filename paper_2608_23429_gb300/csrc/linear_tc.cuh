@@ -11,15 +11,15 @@
 //
 // Operands whose rows do not start on 16-byte boundaries cannot come by TMA; linear_pack.cu copies them onto the grid first.
 //
-// The tensor cores cut off what a sum loses where it is added to, which adds up over K: 1.1e-9 K of a result (bf16; 1.9e-5 at
-// K = 16384, 2.1e-6 at 2048). Results in fp32 are therefore summed in passes over parts of K, whose sums the epilogue's warps
-// add, rounded to nearest, into a third part of TMEM while the next pass is under way (A.passes > 1, tiles of up to 128
-// columns).
+// The tensor cores cut off what a sum loses where it is added to, which adds up over K: 1.1e-9 K of a result (bf16, signs mixed; 1.9e-5
+// at K = 16384, 2.1e-6 at 2048), up to 6e-9 K where all terms have one sign. Results in fp32, and all of very long sums, are
+// therefore summed in passes over parts of K, whose sums the epilogue's warps add, rounded to nearest, into a third part of TMEM
+// while the next pass is under way (A.passes > 1, tiles of up to 128 columns).
 //
 // Few tiles of long sums are split over K (A.parts): each part's sums leave in fp32, and linear_join.cu adds them.
 //
-// Bound by the tensor cores where tiles fill the SMs' rounds: GB300, 4608 x 3072 x 15360 bf16 with a gated hidden state 265 us (1.64
-// PFLOP/s, 85 % of the largest library rate), 8192 x 1152 x 4608 65 us (1.34), 4096 x 4608 x 1152 e4m3 with GELU 22 us (1.96).
+// Bound by the tensor cores where tiles fill the SMs' rounds: GB300, 4608 x 3072 x 15360 bf16 with a gated hidden state 264 us (1.65
+// PFLOP/s, 85 % of the largest library rate), 8192 x 1152 x 4608 65 us (1.34), 4096 x 4608 x 1152 e4m3 with GELU 22.5 us (1.93).
 //
 // Every wait has a limit (A.wait_ns); one that runs out sets the CTA's abort flag, so that all its roles leave, after
 // the copies under way have landed, and frees the TMEM.
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     auto slabs_from = [&](int part) { return SPLIT ? part * A.part_blocks : 0; };
     auto slabs_to = [&](int part) { return SPLIT ? min((part + 1) * A.part_blocks, A.k_blocks) : A.k_blocks; };
     if (warp < EPI) {  // ---- epilogue
-        const LinearEpilogue E = A.e;
+        const LinearEpilogue E = from_here(A.e);
         float* const turn = reinterpret_cast<float*>(turns + warp * kTurn);
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
         int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken

@@ -29,4 +29,17 @@ def test_loads_of_memory_stay_behind_the_wait_for_the_previous_kernel():
     assert len(every) > 50
     loads = [s for s in every if re.search(r"\bld\.(global|shared)|cp\.async|tcgen05\.ld\b", s[2])]
     assert len(loads) > 15
-    assert not [s[:2] for s in loads if not re.match(r"asm\s+volatile", s[2])]
+    free = [s for s in loads if not re.match(r"asm\s+volatile", s[2])]
+    assert {s[0] for s in free} <= {"linear.cuh"} and len(free) == 2, [s[:2] for s in free]  # lin_ld1's
+
+
+def test_epilogues_take_their_pointers_behind_the_wait():
+    """lin_ld1 is not volatile: each kernel that uses it has the epilogue's pointers from from_here(), volatile asm behind the wait."""
+    users = [n for n in sorted(os.listdir(CSRC)) if n.endswith((".cu", ".cuh")) and n != "linear.cuh" and "lin_ld1(" in open(os.path.join(CSRC, n)).read()]
+    assert users == ["linear_few.cu", "linear_join.cu", "linear_tc.cuh"]
+    for name in users:
+        text = open(os.path.join(CSRC, name)).read()
+        kernel = text[text.index("__global__"):]
+        assert kernel.index("after_previous();") < kernel.index("const LinearEpilogue E = from_here(A.e);")
+        assert not re.search(r"LinearEpilogue&? E = A\.e|A\.e\.(x_scale|w_scale|bias|resid|gate)\b", kernel)
+    assert 'asm volatile("" : "+l"(e.x_scale)' in open(os.path.join(CSRC, "linear.cuh")).read()
