@@ -45,7 +45,8 @@ typedef struct {
     int32_t reserved;      /* must be 0 */
 } cb_norm_desc;
 
-/* Root-mean-square norm with the residual's addition. For every row
+/* Root-mean-square norm with the residual's addition: the norm of blocks that subtract no
+ * mean (DiT-XL/2, PixArt-Sigma and FLUX.1-dev do: theirs is another). For every row
  *     h = x + gate * branch
  *     x_out = round(h)
  *     n = h / sqrt(mean(h^2) + eps) * weight
@@ -60,7 +61,8 @@ typedef struct {
  * stored. x_out may be x itself (same stride). With eps > 0 a row of zeros gives
  * zeros (with shift: its values). A row that holds a NaN gives NaN; one that holds an
  * infinity gives NaN in e4m3, otherwise NaN there and what zeros give elsewhere. No
- * other row is touched by either.
+ * other row is touched by either. Squares are summed in fp32: of a row with elements beyond
+ * 2^63 the sum is infinite and n is zero.
  * Rows and hidden sizes on the 16-byte grid take vector loads, others elements.
  * Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size), CB_ERR_LIMIT
  * (rows or hidden beyond 2^31 - 1), CB_ERR_CUDA. */
@@ -131,12 +133,12 @@ int cb_linear_set_option(cb_linear* layer, int option, int64_t value);
  *     resid_out = round(resid + gate * v)   the hidden state (gate: a line per sample)
  * with sums, epilogue and hidden state in fp32 and one rounding to each result. The
  * tensor cores cut sums off rather than round them: where a result is fp32 they sum
- * parts of 512 features (e4m3: 4096; up to 32 rows: 128 at most), which are added rounded
- * to nearest. Measured, relative to sum_k |x w|: 5e-7 with signs mixed, 8e-7 with all terms
- * of one sign, and up to 2^-24 for every part added (of which most cancel: 2^-24 times the
- * root of their number). bf16 results: parts of 2048 (e4m3: 4096) where rows are longer
- * than 32 KB, else one part, which is off by up to 7.2e-5 of the sums' size (16384 features
- * of one sign) before the rounding to bf16.
+ * parts of 512 features (e4m3: 4096; up to 32 rows: 128 and 256 at most), which are added
+ * rounded to nearest. Measured, in the root mean square relative to the sums': 5e-7 with signs
+ * mixed, 8e-7 with all terms of one sign, and up to 2^-24 for every part added (of which most
+ * cancel: 2^-24 times the root of their number). bf16 results: parts of 2048 (e4m3: 4096) where rows are longer
+ * than 32 KB, else one part, which is off by up to 7.2e-5 (16384 features of one sign) before
+ * the rounding to bf16.
  * x_scale: one float a row (CB_E4M3 only, NULL: 1). out may be NULL, resid and resid_out
  * may be NULL together, gate (with resid only) may be NULL: 1; one result at least
  * is wanted. resid_out may be resid itself (same stride). The order of a sum depends

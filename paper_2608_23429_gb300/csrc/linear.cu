@@ -111,7 +111,7 @@ int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes
 
 // Boxes of shared memory of a warp, besides two, for hidden states in bf16 and fp32: [1] where sums are short, as the results are
 // what takes the time then, [0] where they are long and stages are worth more. GB300, {1, 4} -> {4, 7}: 16384 x 8192 x 512 e4m3
-// with a bf16 output and hidden state 178 -> 150 us, fp32 hidden state alone 212 -> 192; 4096 x 1152 x 4608 64.1 -> 66.2 ({2, 5}).
+// with a bf16 output and hidden state 178 -> 150 us, fp32 hidden state alone 212 -> 192; 8192 x 1152 x 4608 64.1 -> 66.2 ({2, 5}).
 constexpr int kShortBlocks = 16, kMoreBoxes[2][2] = {{1, 4}, {4, 7}};
 
 // Bytes of a row up to which a box's place in it (and a gate's piece's), and that of the box behind, is a positive int.

@@ -185,7 +185,7 @@ __device__ __forceinline__ Two lin_act(Two v) {
 // functions. Where a product passes 2^120 (four values of t = 30: SiLU at -20.8, GELU at -5.7; or one of 120), or one of its values is a NaN,
 // all pairs are made anew with a reciprocal each. Asked for once for all of them: a branch for every four values keeps them from
 // being worked on together (GB300, 4096 x 4608 x 1152 e4m3 with GELU, 10 % longer), and where results leave by the threads,
-// which wait for loads, a branch costs more than the reciprocals (999 x 1155 x 577 SiLU, fp32 hidden state: 12.4 us as above, 12.6 so).
+// which wait for loads, a branch costs more than the reciprocals (999 x 1155 x 577 SiLU, fp32 hidden state: 11.9 us as above, 12.7 so).
 template <int ACT, int N>
 __device__ __forceinline__ void lin_act_all(Two* x) {
     if constexpr (ACT != CB_ACT_NONE) {

@@ -1,6 +1,8 @@
 """The MLP branches of a few blocks over a run with skipped steps, in 8 bits: an example of the block operators
 (``chebboost_block.h``) with the int8 history.
 
+The blocks are made up around the operators: RMS norms with a modulation, at a diffusion transformer's sizes.
+
 Full step: each block's norm adds the previous branch to the hidden state and gives e4m3 rows; the first matrix product reads
 them and applies GELU; the second gives the un-gated branch output, which the int8 history keeps; the last one also makes
 the gated hidden state. Skipped step: one call predicts all branches from the history and adds them, gated.
