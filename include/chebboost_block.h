@@ -158,7 +158,8 @@ int cb_linear_run(const cb_linear* layer, const cb_linear_io* io, const void* x,
 
 /* The status word of this device's matrix products (CB_DEV_* codes, 0: nothing noted since the last
  * read) into *status, and clear it, in one step: a code noted meanwhile by another stream's product is
- * left for the next read. Synchronises `stream`. Errors: CB_ERR_ARG, CB_ERR_CUDA. */
+ * left for the next read. Synchronises `stream`. Errors: CB_ERR_ARG, CB_ERR_LIMIT (a device beyond the
+ * 64th), CB_ERR_CUDA. */
 int cb_linear_device_status(int* status, void* stream);
 
 #ifdef __cplusplus
