@@ -63,7 +63,8 @@ typedef enum {
     CB_BF16 = 0,
     CB_FP32 = 1,
     CB_INT8 = 2, /* of the history buffer only: 8-bit codes with block scales (cb_plan_create) */
-    CB_E4M3 = 3  /* of the full step's operators only */
+    CB_E4M3 = 3, /* of the full step's operators only */
+    CB_MXFP4 = 4 /* of the full step's operators only: 4-bit codes, 32 of which share a power of two (chebboost_block.h) */
 } cb_dtype;
 
 /* One cached branch tensor (Sec. 3.1: the self-attention, cross-attention

@@ -70,6 +70,48 @@ int cb_norm_residual(const cb_norm_desc* desc, const void* x, const void* branch
                      const void* weight, const void* scale, const void* shift, void* x_out, void* out,
                      float* out_scale, void* stream);
 
+/* ---- rows in 4 bits (CB_MXFP4)
+ *
+ * A matrix [rows, features] is held as codes and scales. An element is an e2m1 code c (sign, two
+ * bits of exponent, one of mantissa: 0, 1/2, 1, 3/2, 2, 3, 4, 6) times 2^(e - 127), where the byte e is
+ * shared by CB_MX_BLOCK consecutive elements of a row (e = 255: all of them are NaN).
+ *   codes: two a byte, the even element's in the low half. A row is CB_MX_BLOCK / 2 bytes for every
+ *     block begun; codes behind its last feature are 0. Rows start on 16-byte boundaries.
+ *   scales: cb_mx_scale_bytes(rows, features) bytes on a 16-byte boundary, in tiles of 128 rows by 4
+ *     blocks. Block b of row r is at byte
+ *       ((r / 128) * ceil(blocks / 4) + b / 4) * 512 + (r % 32) * 16 + (r / 32 % 4) * 4 + b % 4,
+ *     blocks = ceil(features / CB_MX_BLOCK). Bytes of a row's blocks behind the last one are 0; those
+ *     of rows behind the last are neither read for a result nor written.
+ * The calls below write matrices so; one that comes from elsewhere has to have these zeros too. */
+#define CB_MX_BLOCK 32
+
+/* Bytes of the scales of a matrix into *bytes. Errors: CB_ERR_ARG, CB_ERR_LIMIT (as below). */
+int cb_mx_scale_bytes(int64_t rows, int64_t features, size_t* bytes);
+
+/* Sizes and types of cb_mx_quantize and cb_mx_dequantize. Strides are in elements from one row to
+ * the next; 0 means contiguous. */
+typedef struct {
+    int64_t rows;         /* >= 0; 0 does nothing */
+    int64_t features;     /* >= 1 */
+    int64_t stride;       /* of the rows in dtype */
+    int64_t codes_stride; /* a multiple of CB_MX_BLOCK */
+    cb_dtype dtype;       /* CB_BF16 or CB_FP32 */
+    int32_t reserved;     /* must be 0 */
+} cb_mx_desc;
+
+/* Rows into CB_MXFP4. Every block's e is that of its largest magnitude, which is taken to two
+ * significant bits first: 2^(e - 127) is the power of two that brings it to 3.5 at least and below 7,
+ * where 6 to 7 become 6 (root mean square error of normal values 0.112 of theirs; below 6, and nothing cut off,
+ * 0.115; below 8 0.115); at least 2^-127. Codes are rounded to nearest, ties to even. A block with a NaN or
+ * an infinity has e = 255 and codes of 0.
+ * Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size, codes or scales off 16
+ * bytes), CB_ERR_LIMIT (rows beyond 2^31 - 1, features beyond 2^31 - 256, or 2^31 pieces of 32 rows by
+ * 256 features), CB_ERR_CUDA. */
+int cb_mx_quantize(const cb_mx_desc* desc, const void* x, void* codes, void* scales, void* stream);
+
+/* Rows from CB_MXFP4, exact (beyond fp32's range: infinite). Errors: as above. */
+int cb_mx_dequantize(const cb_mx_desc* desc, const void* codes, const void* scales, void* x, void* stream);
+
 /* Largest in_features: a sum that long takes a fraction of a wait's limit (cb_linear_run). */
 #define CB_MAX_IN_FEATURES (1LL << 22)
 

@@ -28,6 +28,12 @@ class cb_norm_desc(ctypes.Structure):
                 ("param_dtype", _I), ("out_dtype", _I), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
+class cb_mx_desc(ctypes.Structure):
+    """Sizes and types of :func:`cb_mx_quantize` and :func:`cb_mx_dequantize`; strides of 0 mean contiguous."""
+    _fields_ = [("rows", _L), ("features", _L), ("stride", _L), ("codes_stride", _L), ("dtype", _I),
+                ("reserved", ctypes.c_int32)]
+
+
 class cb_linear_desc(ctypes.Structure):
     """A layer, as :func:`cb_linear_create` fills it in."""
     _fields_ = [("in_features", _L), ("out_features", _L), ("w_stride", _L), ("type", _I), ("bias_dtype", _I),
@@ -43,9 +49,13 @@ class cb_linear_io(ctypes.Structure):
 
 CB_ACT_NONE, CB_ACT_GELU, CB_ACT_SILU = 0, 1, 2
 CB_MAX_IN_FEATURES = 1 << 22
+CB_MX_BLOCK = 32
 
 _sig = {
     "cb_norm_residual": ([_P] * 11, _I),
+    "cb_mx_scale_bytes": ([_L, _L, _P], _I),
+    "cb_mx_quantize": ([_P] * 5, _I),
+    "cb_mx_dequantize": ([_P] * 5, _I),
     "cb_linear_create": ([_P, ctypes.POINTER(_P)], _I),
     "cb_linear_destroy": ([_P], None),
     "cb_linear_set_option": ([_P, _I, _L], _I),
@@ -58,6 +68,7 @@ for _name, (_args, _res) in _sig.items():
 
 EXPORTED = tuple(_sig)
 _norm_residual, _linear_run = _lib.cb_norm_residual, _lib.cb_linear_run
+_mx_quantize, _mx_dequantize = _lib.cb_mx_quantize, _lib.cb_mx_dequantize
 
 
 def cb_norm_residual(desc: cb_norm_desc, x, branch=None, gate=None, weight=None, scale=None, shift=None, x_out=None,
@@ -67,6 +78,29 @@ def cb_norm_residual(desc: cb_norm_desc, x, branch=None, gate=None, weight=None,
                         _addr(x_out), _addr(out), _addr(out_scale), None if stream is None else _stream(stream))
     if rc < 0:
         _raise(rc, "cb_norm_residual")
+
+
+def cb_mx_scale_bytes(rows: int, features: int) -> int:
+    """Bytes of the scales of ``rows`` rows of ``features`` elements in CB_MXFP4."""
+    n = ctypes.c_size_t(0)
+    rc = _lib.cb_mx_scale_bytes(rows, features, ctypes.addressof(n))
+    if rc < 0:
+        _raise(rc, "cb_mx_scale_bytes")
+    return n.value
+
+
+def cb_mx_quantize(desc: cb_mx_desc, x, codes, scales, stream=None) -> None:
+    """Rows ``x`` into CB_MXFP4: ``codes`` and ``scales``."""
+    rc = _mx_quantize(ctypes.addressof(desc), _addr(x), _addr(codes), _addr(scales), None if stream is None else _stream(stream))
+    if rc < 0:
+        _raise(rc, "cb_mx_quantize")
+
+
+def cb_mx_dequantize(desc: cb_mx_desc, codes, scales, x, stream=None) -> None:
+    """Rows ``x`` from CB_MXFP4."""
+    rc = _mx_dequantize(ctypes.addressof(desc), _addr(codes), _addr(scales), _addr(x), None if stream is None else _stream(stream))
+    if rc < 0:
+        _raise(rc, "cb_mx_dequantize")
 
 
 def cb_linear_create(w, out_features: int, in_features: int, type: int, w_scale=None, bias=None,

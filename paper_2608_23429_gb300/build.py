@@ -34,7 +34,7 @@ SOURCES = ["extrapolate.cu", "extrapolate_gated.cu", "extrapolate_precise.cu", "
            "extrapolate_bulk_precise.cu", "extrapolate_bulk_precise_fp32.cu", "extrapolate_bulk_strided.cu",
            "extrapolate_bulk_strided_fp32.cu", "push.cu", "epilogue.cu", "quant.cu", "norm.cu", "norm_lines_bf16.cu",
            "norm_lines_fp32.cu", "linear.cu", "linear_tc.cu", "linear_tc_out.cu", "linear_tc_hidden.cu", "linear_tc_direct.cu",
-           "linear_few.cu", "linear_pack.cu", "linear_join.cu", "static_status.cu", "plan.cpp"]
+           "linear_few.cu", "linear_pack.cu", "linear_join.cu", "mx.cu", "static_status.cu", "plan.cpp"]
 
 
 def _nvcc() -> str:

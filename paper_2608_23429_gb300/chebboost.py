@@ -24,7 +24,7 @@ if not os.path.exists(LIB_PATH):
 
 _lib = ctypes.CDLL(LIB_PATH)
 
-CB_BF16, CB_FP32, CB_INT8, CB_E4M3 = 0, 1, 2, 3
+CB_BF16, CB_FP32, CB_INT8, CB_E4M3, CB_MXFP4 = 0, 1, 2, 3, 4
 CB_MAX_K, CB_MAX_TENSORS, CB_MAX_BRANCHES, CB_CACHE_ALIGN, CB_STATUS_BYTES = 8, 256, 4, 256, 256
 CB_MAX_NUMEL = 1 << 48
 CB_INT8_BLOCK = 64

@@ -1,0 +1,89 @@
+"""Rows in 4 bits on the CPU: the tests' reference by itself, sizes, and every refusal that comes before a launch."""
+import ctypes
+import os
+import sys
+
+import numpy as np
+import pytest
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import mx_reference as R  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2608_23429_gb300 import build
+    build.build()
+    from paper_2608_23429_gb300 import block, chebboost
+    return block, chebboost
+
+
+def test_reference_by_hand():
+    v = np.zeros((2, 33))
+    v[0, :10] = [6, -5, 5.01, 2.5, 1.75, 0.25, 0.26, -0.74, 3.5, -0.0]  # power 1
+    v[0, 32] = 7.0  # power 2: 3.5, a tie
+    v[1, 0] = np.inf
+    e = R.scale_bytes(v)
+    assert e.tolist() == [[127, 128], [255, 0]]
+    c = R.codes(v, e)
+    assert R.values(c, e, 33)[0, :10].tolist() == [6, -4, 6, 2, 2, 0, 0.5, -0.5, 4, 0]
+    assert R.values(c, e, 33)[0, 32] == 8.0 and c[0, 32] == 6 and np.isnan(R.values(c, e, 33)[1, :32]).all()
+    assert R.packed(c)[0, :2].tolist() == [7 | 14 << 4, 7 | 4 << 4]
+    assert np.array_equal(R.unpacked(R.packed(c)), c)
+    assert R.scale_bytes(np.array([[6.99]]))[0, 0] == 127 and R.scale_bytes(np.array([[3.49]]))[0, 0] == 126
+    assert R.scale_bytes(np.array([[2.0 ** -149]]))[0, 0] == 0 and R.scale_bytes(np.array([[3.4e38]]))[0, 0] == 253
+
+
+def test_tiles_by_hand():
+    assert [R.place(r, b, 9) for r, b in ((0, 0), (1, 0), (32, 0), (127, 3), (0, 4), (0, 8), (128, 0), (161, 5))] == [
+        0, 16, 4, 511, 512, 1024, 1536, 1536 + 512 + 16 + 4 + 1]
+    e = np.random.default_rng(0).integers(0, 255, (300, 9)).astype(np.uint8)
+    t = R.tiled(e)
+    assert t.size == 3 * 3 * 512 and np.array_equal(R.from_tiles(t, 300, 9), e)
+
+
+def test_scale_bytes(lib):
+    block, cb = lib
+    for r, k in ((0, 1), (1, 1), (128, 128), (129, 129), (1000, 577)):
+        assert block.cb_mx_scale_bytes(r, k) == -(-r // 128) * -(-(-(-k // 32)) // 4) * 512
+    for r, k in ((-1, 4), (4, 0), (4, -1)):
+        with pytest.raises(cb.CbError) as e:
+            block.cb_mx_scale_bytes(r, k)
+        assert e.value.status == cb.CB_ERR_ARG
+    for r, k in ((1 << 31, 4), (4, 1 << 31)):
+        with pytest.raises(cb.CbError) as e:
+            block.cb_mx_scale_bytes(r, k)
+        assert e.value.status == cb.CB_ERR_LIMIT
+    assert cb._lib.cb_mx_scale_bytes(4, 4, None) == cb.CB_ERR_ARG
+
+
+def test_refusals(lib):
+    block, cb = lib
+    X, C, S = 0x10000, 0x20000, 0x30000  # never dereferenced
+    A, L, M = cb.CB_ERR_ARG, cb.CB_ERR_ALIGN, cb.CB_ERR_LIMIT
+
+    def both(x=X, c=C, s=S, **kw):
+        d = dict(rows=4, features=100, dtype=cb.CB_BF16)
+        d.update(kw)
+        d = block.cb_mx_desc(**d)
+        got = set()
+        for f, a in ((block.cb_mx_quantize, (x, c, s)), (block.cb_mx_dequantize, (c, s, x))):
+            with pytest.raises(cb.CbError) as e:
+                f(d, *a)
+            got.add(e.value.status)
+        assert len(got) == 1
+        return got.pop()
+
+    assert both(x=None) == A and both(c=None) == A and both(s=None) == A and both(rows=-1) == A and both(features=0) == A
+    assert both(reserved=1) == A and both(dtype=cb.CB_E4M3) == A and both(dtype=cb.CB_MXFP4) == A and both(dtype=-1) == A
+    assert both(stride=99) == A and both(stride=-100) == A and both(codes_stride=100) == A and both(codes_stride=96) == A
+    assert both(codes_stride=-128) == A and both(codes_stride=130) == A
+    assert both(stride=cb.CB_MAX_NUMEL + 1) == M and both(codes_stride=cb.CB_MAX_NUMEL + 32) == M
+    assert both(rows=1 << 31) == M and both(features=1 << 31) == M and both(rows=(1 << 31) - 1, features=0x7FFFFF00) == M
+    assert both(x=X + 1) == L and both(x=X + 2, dtype=cb.CB_FP32) == L and both(c=C + 8) == L and both(s=S + 8) == L
+    for f in (cb._lib.cb_mx_quantize, cb._lib.cb_mx_dequantize):
+        assert f(None, X, C, S, None) == A
+    nothing = block.cb_mx_desc(rows=0, features=4)
+    block.cb_mx_quantize(nothing, None, None, None)
+    block.cb_mx_dequantize(nothing, None, None, None)
+    assert ctypes.sizeof(block.cb_mx_desc) == 40
