@@ -129,12 +129,12 @@ typedef struct {
     int64_t in_features;   /* >= 1 */
     int64_t out_features;  /* >= 1 */
     int64_t w_stride;
-    cb_dtype type;         /* of w and of the rows x: CB_BF16 or CB_E4M3 */
+    cb_dtype type;         /* of w and of the rows x: CB_BF16, CB_E4M3 or CB_MXFP4 (w_stride: a multiple of CB_MX_BLOCK) */
     cb_dtype bias_dtype;   /* CB_BF16 or CB_FP32 */
     int32_t activation;    /* CB_ACT_* */
     int32_t reserved;      /* must be 0 */
     const void* w;
-    const float* w_scale;  /* CB_E4M3 only: [out_features] (NULL: 1) */
+    const void* w_scale;   /* CB_E4M3: fp32 [out_features] (NULL: 1); CB_MXFP4: w's scales */
     const void* bias;      /* [out_features] (NULL: 0) */
 } cb_linear_desc;
 
@@ -147,15 +147,16 @@ typedef struct {
     int64_t resid_stride;
     int64_t resid_out_stride;
     int64_t gate_stride;      /* from one sample's gate to the next's */
-    cb_dtype out_dtype;       /* CB_BF16 or CB_FP32 */
+    cb_dtype out_dtype;       /* CB_BF16, CB_FP32, or of a CB_MXFP4 layer CB_MXFP4 (out_stride: a multiple of CB_MX_BLOCK) */
     cb_dtype resid_dtype;     /* of resid and resid_out: CB_BF16 or CB_FP32 */
     cb_dtype gate_dtype;      /* CB_BF16 or CB_FP32 */
     int32_t reserved;         /* must be 0 */
+    void* out_scale;          /* read for an output in CB_MXFP4 only: its scales */
 } cb_linear_io;
 
 typedef struct cb_linear cb_linear; /* opaque, host-owned; holds no device memory */
 
-/* Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size), CB_ERR_LIMIT (out_features
+/* Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size; codes or scales in 4 bits off 16 bytes), CB_ERR_LIMIT (out_features
  * beyond 2^31 - 1024, in_features beyond CB_MAX_IN_FEATURES, or a row stride of w or x
  * beyond 2^31 - 256 bytes). The layer keeps the pointers: its buffers must outlive it. */
 int cb_linear_create(const cb_linear_desc* desc, cb_linear** out);
@@ -181,7 +182,10 @@ int cb_linear_set_option(cb_linear* layer, int option, int64_t value);
  * cancel: 2^-24 times the root of their number). bf16 results: parts of 2048 (e4m3: 4096) where rows are longer
  * than 32 KB, else one part, which is off by up to 7.2e-5 (16384 features of one sign) before
  * the rounding to bf16.
- * x_scale: one float a row (CB_E4M3 only, NULL: 1). out may be NULL, resid and resid_out
+ * CB_MXFP4 layers: x_scale are x's scales, and their factors 2^(e - 127) stand in place of x_scale[m] w_scale[n] within the
+ * sum, whose products are exact. out in CB_MXFP4 (no hidden state then): v as cb_mx_quantize makes
+ * it of fp32 rows, with io->out_scale.
+ * x_scale: one float a row (CB_E4M3, NULL: 1; not for CB_BF16). out may be NULL, resid and resid_out
  * may be NULL together, gate (with resid only) may be NULL: 1; one result at least
  * is wanted. resid_out may be resid itself (same stride). The order of a sum depends
  * on the sizes alone: equal calls give equal bits.
@@ -195,7 +199,7 @@ int cb_linear_set_option(cb_linear* layer, int option, int64_t value);
  * kernel return early, with incomplete results.
  * Errors: CB_ERR_ARG, CB_ERR_ALIGN, CB_ERR_LIMIT (rows beyond 2^31 - 1024, or over 2^28
  * tiles of 128 rows and 32 to 256 columns), CB_ERR_CUDA. */
-int cb_linear_run(const cb_linear* layer, const cb_linear_io* io, const void* x, const float* x_scale,
+int cb_linear_run(const cb_linear* layer, const cb_linear_io* io, const void* x, const void* x_scale,
                   const void* resid, const void* gate, void* out, void* resid_out, void* stream);
 
 /* The status word of this device's matrix products (CB_DEV_* codes, 0: nothing noted since the last

@@ -44,7 +44,7 @@ class cb_linear_io(ctypes.Structure):
     """Sizes and types of one :func:`cb_linear_run`; strides of 0 mean contiguous."""
     _fields_ = [("rows", _L), ("tokens", _L), ("x_stride", _L), ("out_stride", _L), ("resid_stride", _L),
                 ("resid_out_stride", _L), ("gate_stride", _L), ("out_dtype", _I), ("resid_dtype", _I), ("gate_dtype", _I),
-                ("reserved", ctypes.c_int32)]
+                ("reserved", ctypes.c_int32), ("out_scale", _P)]
 
 
 CB_ACT_NONE, CB_ACT_GELU, CB_ACT_SILU = 0, 1, 2

@@ -4,6 +4,7 @@
 #include <new>
 
 #include "linear.cuh"
+#include "mx.cuh"
 
 namespace cbk {
 namespace {
@@ -13,6 +14,11 @@ __device__ int g_linear_status[1];  // CB_DEV_* codes of this device's launches
 bool wide_type(cb_dtype t) { return t == CB_BF16 || t == CB_FP32; }
 size_t bytes_of(int t) { return t == CB_BF16 ? 2 : t == CB_FP32 ? 4 : 1; }
 bool on_grid(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
+
+// Rows of operands: their bytes, and the longest strides, in elements. Rows in 4 bits are whole blocks.
+long long row_bytes(int type, long long elements) { return type == CB_MXFP4 ? mx_row_bytes(elements) : elements * (long long)bytes_of(type); }
+long long most_stride(int type) { return type == CB_MXFP4 ? 0x7FFFFF00LL * 2 : 0x7FFFFF00LL / (long long)bytes_of(type); }
+bool bad_mx_stride(long long stride, long long features) { return stride < mx_blocks(features) * kMxBlock || stride % kMxBlock != 0; }
 
 // What the calls need to know of a device, found out by the first one there.
 struct Device {
@@ -109,6 +115,18 @@ int operand_map(CUtensorMap* map, const void* p, long long rows, long long bytes
     return r == CUDA_SUCCESS ? CB_OK : cuda_error(cudaErrorInvalidValue, "tensor map");
 }
 
+// Tiles of scales of rows in 4 bits, in boxes of two (256 features of 128 rows); zeros come in behind the ends.
+int scales_map(CUtensorMap* map, const void* p, long long rows, long long features) {
+    const long long tiles = mx_tiles_k(features);
+    const cuuint64_t dims[2] = {(cuuint64_t)tiles * kMxTileBytes / 4, (cuuint64_t)((rows + kMxTileRows - 1) / kMxTileRows)};
+    const cuuint64_t strides[1] = {(cuuint64_t)tiles * kMxTileBytes};
+    const cuuint32_t boxes[2] = {kMxScales / 4, 1}, steps[2] = {1, 1};
+    const CUresult r = g_encode.load(std::memory_order_relaxed)(
+        map, CU_TENSOR_MAP_DATA_TYPE_INT32, 2, const_cast<void*>(p), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CB_OK : cuda_error(cudaErrorInvalidValue, "tensor map");
+}
+
 // Boxes of shared memory of a warp, besides two, for hidden states in bf16 and fp32: [1] where sums are short, as the results are
 // what takes the time then, [0] where they are long and stages are worth more. GB300, {1, 4} -> {4, 7}: 16384 x 8192 x 512 e4m3
 // with a bf16 output and hidden state 178 -> 150 us, fp32 hidden state alone 212 -> 192; 8192 x 1152 x 4608 64.1 -> 66.2 ({2, 5}).
@@ -155,7 +173,7 @@ constexpr int kFewRows = 32;
 // Slabs of 128 bytes of a pass over K, with fp32 results: an error of 5e-7 of a sum, 7e-7 where all terms have one sign (measured:
 // linear_tc.cuh; e4m3's products lose less, 1.4e-7 in 2048 features of one sign and 1.8e-6 in 8192; 4096 x 4608 x 8192 takes 104 us in two passes of
 // narrower tiles and 89 in one).
-constexpr int kPassBf16 = 8, kPassE4m3 = 32;
+constexpr int kPassBf16 = 8, kPassE4m3 = 32, kPassMx = 16;
 // Results in bf16 alone: one pass up to kOnePass slabs, as tiles of 256 columns are worth more (4608 x 3072 x 15360 227 -> 274 us, 8192 x
 // 8192 x 8192 554 -> 648, 8192 x 1152 x 4608 60.2 -> 62.0 with passes of 16) and what the sums lose is small against the rounding that
 // follows, 2e-3 to 4e-3: 7.2e-5 of their size at most (16384 features of bf16, all terms of one sign; 1.9e-5 with signs mixed). Longer sums
@@ -169,12 +187,12 @@ constexpr int kOnePass = 256, kPassLong = 32;
 // up to 16 parts of four slabs gave the same.
 constexpr double kJoinClocks = 5000, kJoinBytesPerClock = 1300;
 constexpr int kMaxParts = 8, kPartSlabs = 8;  // no part is shorter
-void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int* cg, int* tile_n, int* parts) {
+void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int step, int max_parts, int* cg, int* tile_n, int* parts) {
     double best = 1e300;
-    for (int p = 1; p <= kMaxParts && (p == 1 || k_blocks / p >= kPartSlabs); ++p)
+    for (int p = 1; p <= max_parts && (p == 1 || k_blocks / p >= kPartSlabs); ++p)
         for (int g = 2; g >= 1; --g)
-            for (int n = most; n >= 32; n -= 32) {
-                if (n > 32 && n - 32 >= N) continue;
+            for (int n = most; n >= step; n -= step) {
+                if (n > step && n - step >= N) continue;
                 const long long tiles = (long long)((M + 128 * g - 1) / (128 * g)) * ((N + n - 1) / n) * p;
                 const long long units = g == 2 ? dev.pairs : dev.sms;
                 if (units < 1) break;  // no room for pairs
@@ -201,19 +219,19 @@ int cb_linear_create(const cb_linear_desc* d, cb_linear** out) {
     if (!out) return CB_ERR_ARG;
     *out = nullptr;
     if (!d || d->reserved != 0 || d->in_features < 1 || d->out_features < 1 || !d->w) return CB_ERR_ARG;
-    if (d->type != CB_BF16 && d->type != CB_E4M3) return CB_ERR_ARG;
+    const bool mx = d->type == CB_MXFP4;
+    if (d->type != CB_BF16 && d->type != CB_E4M3 && !mx) return CB_ERR_ARG;
     if (d->bias && !wide_type(d->bias_dtype)) return CB_ERR_ARG;
     if (d->activation < CB_ACT_NONE || d->activation > CB_ACT_SILU) return CB_ERR_ARG;
-    if (d->w_scale && d->type != CB_E4M3) return CB_ERR_ARG;
-    if (d->w_stride != 0 && d->w_stride < d->in_features) return CB_ERR_ARG;
-    const long long row = 0x7FFFFF00LL / (long long)bytes_of(d->type);
-    if (d->out_features > 0x7FFFFC00LL || d->in_features > CB_MAX_IN_FEATURES || d->w_stride > row) return CB_ERR_LIMIT;
-    if (!on_grid(d->w, bytes_of(d->type)) || !on_grid(d->w_scale, 4)) return CB_ERR_ALIGN;
+    if (mx ? !d->w_scale : d->w_scale && d->type != CB_E4M3) return CB_ERR_ARG;
+    if (d->w_stride != 0 && (d->w_stride < d->in_features || (mx && bad_mx_stride(d->w_stride, d->in_features)))) return CB_ERR_ARG;
+    if (d->out_features > 0x7FFFFC00LL || d->in_features > CB_MAX_IN_FEATURES || d->w_stride > most_stride(d->type)) return CB_ERR_LIMIT;
+    if (!on_grid(d->w, mx ? 16 : bytes_of(d->type)) || !on_grid(d->w_scale, mx ? 16 : 4)) return CB_ERR_ALIGN;
     if (d->bias && !on_grid(d->bias, bytes_of(d->bias_dtype))) return CB_ERR_ALIGN;
     cb_linear* l = new (std::nothrow) cb_linear;
     if (!l) return CB_ERR_LIMIT;
     l->d = *d;
-    if (l->d.w_stride == 0) l->d.w_stride = d->in_features;
+    if (l->d.w_stride == 0) l->d.w_stride = mx ? mx_blocks(d->in_features) * kMxBlock : d->in_features;
     cbk::g_layers.fetch_add(1, std::memory_order_relaxed);
     *out = l;
     return CB_OK;
@@ -240,41 +258,47 @@ int cb_linear_set_option(cb_linear* l, int option, int64_t value) {
     }
 }
 
-int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, const float* x_scale, const void* resid,
+int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, const void* x_scale, const void* resid,
                   const void* gate, void* out, void* resid_out, void* stream) {
     using namespace cbk;
     if (!l || !io || io->reserved != 0 || io->rows < 0 || io->tokens < 0) return CB_ERR_ARG;
     const cb_linear_desc& d = l->d;
-    if (!wide_type(io->out_dtype) || !wide_type(io->resid_dtype) || !wide_type(io->gate_dtype)) return CB_ERR_ARG;
-    const long long es = (long long)bytes_of(d.type), K = d.in_features, N = d.out_features;
+    const bool mx = d.type == CB_MXFP4, out_mx = mx && io->out_dtype == CB_MXFP4;
+    if (!(wide_type(io->out_dtype) || out_mx) || !wide_type(io->resid_dtype) || !wide_type(io->gate_dtype)) return CB_ERR_ARG;
+    const long long K = d.in_features, N = d.out_features;
     if (io->rows > 0x7FFFFC00LL) return CB_ERR_LIMIT;
-    if (io->x_stride != 0 && io->x_stride < K) return CB_ERR_ARG;
-    if (io->x_stride > 0x7FFFFF00LL / es) return CB_ERR_LIMIT;
+    if (io->x_stride != 0 && (io->x_stride < K || (mx && bad_mx_stride(io->x_stride, K)))) return CB_ERR_ARG;
+    if (io->x_stride > most_stride(d.type)) return CB_ERR_LIMIT;
     const int64_t strides[] = {io->out_stride, io->resid_stride, io->resid_out_stride, io->gate_stride};
     for (int64_t s : strides)
         if (s != 0 && (s < N || s > CB_MAX_NUMEL)) return s < N ? CB_ERR_ARG : CB_ERR_LIMIT;
-    if (x_scale && d.type != CB_E4M3) return CB_ERR_ARG;
+    if (x_scale && d.type != CB_E4M3 && !mx) return CB_ERR_ARG;
+    if (out_mx && (resid || (io->out_stride != 0 && bad_mx_stride(io->out_stride, N)))) return CB_ERR_ARG;
     if ((resid != nullptr) != (resid_out != nullptr) || (gate && !resid)) return CB_ERR_ARG;
     if (io->rows == 0) return CB_OK;
     if (!x || (!out && !resid_out)) return CB_ERR_ARG;
+    if ((mx && !x_scale) || (out_mx && !io->out_scale)) return CB_ERR_ARG;
 
     LinearArgs a{};
     a.overlap = 1;
-    a.k_bytes = (int)(K * es);
-    const long long x_row = (io->x_stride ? io->x_stride : K) * es, w_row = d.w_stride * es;
+    a.operands = mx ? Operands::kMx : d.type == CB_E4M3 ? Operands::kE4m3 : Operands::kBf16;
+    a.k_bytes = (int)row_bytes(d.type, K);
+    const long long x_row = io->x_stride ? row_bytes(d.type, io->x_stride) : a.k_bytes, w_row = row_bytes(d.type, d.w_stride);
     LinearEpilogue& ep = a.e;
     ep.M = (int)io->rows, ep.N = (int)N;
     ep.act = d.activation;
     ep.tokens = io->tokens == 0 || io->tokens > io->rows ? (unsigned)io->rows : (unsigned)io->tokens;
     ep.out_bf16 = io->out_dtype == CB_BF16, ep.resid_bf16 = io->resid_dtype == CB_BF16;
     ep.bias_bf16 = d.bias_dtype == CB_BF16, ep.gate_bf16 = io->gate_dtype == CB_BF16;
-    ep.out_stride = io->out_stride ? io->out_stride : N;
+    ep.out_stride = io->out_stride ? io->out_stride : out_mx ? mx_blocks(N) * kMxBlock : N;
     ep.resid_stride = io->resid_stride ? io->resid_stride : N;
     ep.resid_out_stride = io->resid_out_stride ? io->resid_out_stride : N;
     ep.gate_stride = io->gate_stride ? io->gate_stride : N;
-    ep.x_scale = x_scale, ep.w_scale = d.w_scale, ep.bias = d.bias;
+    ep.bias = d.bias;
+    if (!mx) ep.x_scale = static_cast<const float*>(x_scale), ep.w_scale = static_cast<const float*>(d.w_scale);
     ep.resid = resid, ep.gate = gate, ep.out = out, ep.resid_out = resid_out;
-    if (!on_grid(x, es) || !on_grid(x_scale, 4)) return CB_ERR_ALIGN;
+    if (!on_grid(x, mx ? 16 : bytes_of(d.type)) || !on_grid(x_scale, mx ? 16 : 4)) return CB_ERR_ALIGN;
+    if (out_mx && (!on_grid(out, 16) || !on_grid(io->out_scale, 16))) return CB_ERR_ALIGN;
     const struct {
         const void* p;
         int dtype;
@@ -286,7 +310,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     if (rc != CB_OK) return rc;
     a.status = dev->status, a.wait_ns = l->wait_ns, a.withheld = l->withheld;
     const bool x_on = on_grid(x, 16) && x_row % 16 == 0, w_on = on_grid(d.w, 16) && w_row % 16 == 0;
-    if (ep.M <= kFewRows) {
+    if (ep.M <= kFewRows && !mx) {
         const LinearFewArgs f{ep, 1, a.k_bytes, x_row, w_row, x, d.w};
         const cudaError_t e = launch_linear_few(f, d.type == CB_E4M3, !x_on || !w_on, dev->sms, (cudaStream_t)stream);
         return e == cudaSuccess ? CB_OK : cuda_error(e, "linear launch");
@@ -295,8 +319,9 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.k_blocks = (a.k_bytes + 127) / 128;
     // fp32 results: passes over K (see linear_tc.cuh)
     const bool fp32 = (out && !ep.out_bf16) || (resid_out && !ep.resid_bf16);
-    a.pass_blocks = fp32 ? (d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
-    choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks ? 128 : 256, &cg, &a.tile_n, &a.parts);
+    a.pass_blocks = fp32 ? (mx ? kPassMx : d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
+    choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks ? 128 : mx ? kMxMostN : 256, mx ? kMxStepN : 32,
+                out_mx ? 1 : kMaxParts, &cg, &a.tile_n, &a.parts);
     a.part_blocks = (a.k_blocks + a.parts - 1) / a.parts;
     a.parts = (a.k_blocks + a.part_blocks - 1) / a.part_blocks;
     a.passes = (a.part_blocks + a.pass_blocks - 1) / a.pass_blocks;
@@ -328,9 +353,14 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
                             const_cast<float*>(join.sums), nullptr};
         a.results = Results::kOut;
         rc = operand_map(&a.out_map, join.sums, (long long)a.parts * a.part_rows, 4ll * ep.N, 4 * row, 32, 64);
+    } else if (out_mx) {
+        a.results = Results::kQuant;
+        a.out_scales = static_cast<uint8_t*>(io->out_scale), a.out_tiles = (unsigned)mx_tiles_k(N);
     } else {
         rc = results_by_tma(io, &a);
     }
+    if (rc == CB_OK && mx) rc = scales_map(&a.x_scale_map, x_scale, ep.M, K);
+    if (rc == CB_OK && mx) rc = scales_map(&a.w_scale_map, d.w_scale, N, K);
     const PackOperand &px = pack.o[0], &pw = pack.o[1];
     if (rc == CB_OK)
         rc = px.dst ? operand_map(&a.x_map, px.dst, ep.M, 32ll * px.chunks, 32ll * px.chunks, 128)
@@ -338,7 +368,8 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     if (rc == CB_OK)
         rc = pw.dst ? operand_map(&a.w_map, pw.dst, ep.N, 32ll * pw.chunks, 32ll * pw.chunks, a.tile_n / cg)
                     : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);
-    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.results, a.more_boxes)) / linear_stage_bytes(cg, a.tile_n));
+    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.results, a.more_boxes)) /
+                                                          (linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0)));
     const long long tiles = (long long)a.tiles_m * a.tiles_n * a.parts, units = cg == 2 ? dev->pairs : dev->sms;
     if (rc == CB_OK && e == cudaSuccess) e = launch_linear(a, cg, d.type == CB_E4M3, cg * (int)std::min(tiles, units), s);
     if (rc == CB_OK && e == cudaSuccess && a.parts > 1) e = launch_linear_join(join, s);

@@ -23,11 +23,26 @@ struct LinearEpilogue {
     void *out, *resid_out;
 };
 
-// How results leave: an output alone by TMA, a hidden state with or without an output by TMA, or either by the threads.
-enum class Results { kOut, kHidden, kDirect };
+// How results leave: an output alone by TMA, a hidden state with or without an output by TMA, either by the threads, or an output in
+// 4 bits by the threads.
+enum class Results { kOut, kHidden, kDirect, kQuant };
+
+// Types of the operands.
+enum class Operands { kBf16, kE4m3, kMx };
+
+// Operands in 4 bits: a stage holds scales behind its codes, two tiles of 4 blocks (256 features) of 128 rows of x and of as many of
+// w as the tile's columns touch (a multiple of 64 from a multiple of 64 on).
+constexpr int kMxScales = 1024;  // bytes for 128 rows
+__host__ __device__ constexpr int mx_w_tiles(int tile_n) { return (tile_n + 127) / 128; }
+__host__ __device__ constexpr int mx_scale_bytes(int tile_n) { return kMxScales * (1 + mx_w_tiles(tile_n)); }
+constexpr int kMxMostN = 192, kMxStepN = 64;  // columns of a tile: TMEM holds two accumulators and scales
 
 struct LinearArgs {
     Results results;
+    Operands operands;
+    CUtensorMap x_scale_map, w_scale_map;  // kMx
+    uint8_t* out_scales;                   // kQuant
+    unsigned out_tiles;                    // kQuant: tiles of scales of a row of the output
     CUtensorMap x_map, w_map;
     CUtensorMap out_map, resid_map, resid_out_map;
     int ring, more_boxes;  // hidden states of chunks that a warp holds; boxes of shared memory that it needs for them besides two
@@ -90,6 +105,7 @@ using LinearKernel = void (*)(LinearArgs);
 LinearKernel linear_out_kernel(int cg, bool fp8, bool passes);     // linear_tc_out.cu
 LinearKernel linear_hidden_kernel(int cg, bool fp8, bool passes);  // linear_tc_hidden.cu
 LinearKernel linear_direct_kernel(int cg, bool fp8, bool passes);  // linear_tc_direct.cu
+LinearKernel linear_mx_kernel(Results r, int cg, bool passes);     // linear_tc_mx.cu
 cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaStream_t s);
 
 #ifdef __CUDACC__

@@ -13,6 +13,11 @@ cudaError_t prepare_linear(size_t smem, int* pairs) {
             const cudaError_t e = cudaFuncSetAttribute(of(1 + i % 2, i & 2, i & 4), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e != cudaSuccess) return e;
         }
+    for (int i = 0; i < 4; ++i)
+        for (Results r : {Results::kOut, Results::kHidden, Results::kDirect, Results::kQuant}) {
+            const cudaError_t e = cudaFuncSetAttribute(linear_mx_kernel(r, 1 + i % 2, i & 2), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+        }
     // pairs of CTAs that run at once
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
@@ -35,12 +40,14 @@ cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaS
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)grid);
     c.blockDim = dim3(linear_threads(a.results));
-    c.dynamicSmemBytes = (size_t)a.stages * linear_stage_bytes(cg, a.tile_n) + linear_fixed_bytes(a.results, a.more_boxes);
+    const bool mx = a.operands == Operands::kMx;
+    const size_t stage = linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0);
+    c.dynamicSmemBytes = (size_t)a.stages * stage + linear_fixed_bytes(a.results, a.more_boxes);
     c.stream = s;
     c.attrs = at;
     c.numAttrs = cg == 2 ? 2 : 1;
     const auto of = a.results == Results::kOut ? linear_out_kernel : a.results == Results::kHidden ? linear_hidden_kernel : linear_direct_kernel;
-    const LinearKernel k = of(cg, fp8, a.passes > 1);
+    const LinearKernel k = mx ? linear_mx_kernel(a.results, cg, a.passes > 1) : of(cg, fp8, a.passes > 1);
     void* args[] = {const_cast<void*>(static_cast<const void*>(&a))};
     const cudaError_t e = cudaLaunchKernelExC(&c, reinterpret_cast<const void*>(k), args);
     if (e != cudaSuccess) (void)cudaGetLastError();

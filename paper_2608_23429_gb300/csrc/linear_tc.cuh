@@ -30,6 +30,7 @@
 #include "cb_async.cuh"
 #include "linear.cuh"
 #include "linear_shift.cuh"
+#include "mx.cuh"
 
 namespace cbk {
 namespace {
@@ -42,6 +43,7 @@ constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the ot
 // sixteen, eight rows at once, 195).
 __host__ __device__ constexpr int epi_warps(Results r) { return r == Results::kDirect ? 16 : 8; }
 __host__ __device__ constexpr int linear_threads(Results r) { return 32 * (epi_warps(r) + 2); }
+constexpr int kMxTmem = 448;      // TMEM column of the scales of two slabs (4 bits; accumulators have 192 columns at most)
 constexpr int kTurn = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
 
 struct alignas(16) Tail {  // behind the stages and the epilogue's warps' kTurn each
@@ -129,6 +131,31 @@ __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int
 // Operand in shared memory: rows of 128 bytes, K innermost, 128-byte swizzle in groups of eight rows (1024 bytes).
 __device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
     return (uint64_t)((addr & 0x3FFFF) >> 4) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+// Scales in shared memory: 32 rows of 16 bytes, one behind the other (eight rows: 128 bytes).
+__device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | 1ull << 16 | (uint64_t)(128 >> 4) << 32 | 1ull << 46;
+}
+// Copies a tile of scales to four columns of TMEM (a lane: those of rows 32 apart, four bytes each), for all four quarters of the
+// lanes. In order with the products issued before and behind it. A pair of CTAs: in both, from the same place of each.
+template <int CG>
+__device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
+    if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory");
+}
+// 64 features in 4 bits under two scales a row, at a_scale and b_scale in TMEM.
+template <int CG>
+__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t a_scale, uint32_t b_scale, bool add) {
+    const uint32_t on = add;
+#define CB_MMA(GROUP)                                                                                              \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"                                                 \
+                 "tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::"r"(d), \
+                 "l"(a), "l"(b), "r"(idesc), "r"(on), "r"(a_scale), "r"(b_scale)                                     \
+                 : "memory")
+    if constexpr (CG == 1) CB_MMA("1");
+    else CB_MMA("2");
+#undef CB_MMA
 }
 
 template <int CG, bool FP8>
@@ -342,6 +369,37 @@ __device__ __forceinline__ void add_box(uint32_t box, int lane, const Two* gate,
     }
 }
 
+// A lane's row of 32 columns as a block in 4 bits: 16 bytes of codes and a byte of scale (and zeros for the blocks that fill up the
+// row's last tile of scales).
+__device__ __forceinline__ void put_quantised(const LinearEpilogue& E, uint8_t* scales, unsigned tiles, int row, int col, const Two* x) {
+    float v[32];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float2 f = both(x[i]);
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    }
+    if (col + 32 > E.N) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (col + i >= E.N) v[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    const uint32_t e = mx_scale_of(most);
+    const float inverse = mx_inverse(e);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= inverse;
+    if (row >= E.M) return;
+    const uint4 codes = e == 255 ? make_uint4(0, 0, 0, 0) : make_uint4(mx_codes8(v), mx_codes8(v + 8), mx_codes8(v + 16), mx_codes8(v + 24));
+    *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(E.out) + (row * E.out_stride + col) / 2) = codes;
+    const int block = col / kMxBlock;
+    uint8_t* const to = scales + mx_word_at((unsigned)row, (unsigned)block / kMxTileBlocks, tiles);
+    to[block % kMxTileBlocks] = (uint8_t)e;
+    if (col + kMxBlock >= E.N)
+        for (int b = block % kMxTileBlocks + 1; b < kMxTileBlocks; ++b) to[b] = 0;
+}
+
 // Results by the threads, for rows off the 16-byte grid: a column per lane, eight rows at a time, whose hidden states are loaded
 // while the eight before are worked on.
 
@@ -410,9 +468,10 @@ __device__ __forceinline__ void finish_rows(const LinearEpilogue& E, int row0, i
     put_rows(E, E.resid_out, E.resid_out_stride, E.resid_bf16, row, col, v);
 }
 
-template <int CG, bool FP8, bool PASSES, Results RESULTS>
+template <int CG, Operands OPERANDS, bool PASSES, Results RESULTS>
 __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(const __grid_constant__ LinearArgs A) {
     constexpr int EPI = epi_warps(RESULTS);
+    constexpr bool FP8 = OPERANDS == Operands::kE4m3, MX = OPERANDS == Operands::kMx, QUANT = RESULTS == Results::kQuant;
     constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden, SPLIT = RESULTS == Results::kOut;
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
@@ -422,7 +481,8 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     }
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const int w_rows = A.tile_n / CG, stage_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
+    const int w_rows = A.tile_n / CG, codes_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
+    const int stage_bytes = codes_bytes + (MX ? mx_scale_bytes(A.tile_n) : 0);
     uint8_t* const turns = base + stages * stage_bytes;
     Tail& T = *reinterpret_cast<Tail*>(turns + EPI * kTurn);
     const uint32_t ring = smem_addr(base);
@@ -487,7 +547,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
         };
         // The hidden state's rows of a tile are on their way to L2 a tile ahead.
         auto to_l2 = [&](int t) {
-            if (RESULTS == Results::kOut || !E.resid_out || t >= total) return;
+            if (RESULTS == Results::kOut || QUANT || !E.resid_out || t >= total) return;
             const Tile tile = tile_at<SPLIT>(A, t);
             const int row = first_row(tile) + lane, col0 = tile.n * A.tile_n, es = E.resid_bf16 ? 2 : 4;
             if (row >= E.M) return;
@@ -602,7 +662,9 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                     else if (E.act == CB_ACT_GELU) values<CB_ACT_GELU>(E, cols + c * 32, xs2, v, x);
                     else values<CB_ACT_SILU>(E, cols + c * 32, xs2, v, x);
                     const int col = col0 + c * 32;
-                    if constexpr (!HIDDEN) {
+                    if constexpr (QUANT) {
+                        put_quantised(E, A.out_scales, A.out_tiles, row0 + lane, col, x);
+                    } else if constexpr (!HIDDEN) {
                         for (int h = 0; h < out_boxes; ++h) {
                             // the box before the last has left
                             asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
@@ -681,17 +743,21 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     } else if (warp == EPI) {  // ---- products
         if (rank == 0) {
             // fp32 sums; A and B bf16 (kind f16) or e4m3 (kind f8f6f4), both with K innermost; N / 8, M / 16
-            const uint32_t idesc =
-                1u << 4 | (FP8 ? 0u : 1u << 7 | 1u << 10) | (uint32_t)(A.tile_n / 8) << 17 | (uint32_t)(kRows * CG / 16) << 24;
+            // (4 bits, kind mxf4: e2m1 operands and e8m0 scales; which scales of a word in TMEM goes in with each product)
+            const uint32_t idesc = (MX ? 1u << 7 | 1u << 10 | 1u << 23 : 1u << 4 | (FP8 ? 0u : 1u << 7 | 1u << 10)) |
+                                   (uint32_t)(A.tile_n / 8) << 17 | (uint32_t)(kRows * CG / 16) << 24;
+            constexpr uint32_t upper_scales = 2u << 29 | 2u << 4;
             const uint64_t desc0 = operand_desc(ring);
             const int last_steps = (A.k_bytes - (A.k_blocks - 1) * kSlab + 31) / 32;  // of 32 bytes of K
             Place at;
             constexpr int stride = PASSES ? kAccStride / 2 : kAccStride;
-            int pass = 0;
+            int pass = 0, n_slabs = 0;
             bool ok = true;
             // (the slabs' loop is kept short: with passes opened and closed inside it, a slab took 260 clocks longer)
             for (int t = first; t < total && ok; t += step) {
                 const int part = SPLIT ? t % A.parts : 0, to = slabs_to(part);
+                // (4 bits) the word of w's tile of scales that the results' tile begins with
+                const uint32_t w_word = MX ? tile_at<SPLIT>(A, t).n * A.tile_n % kMxTileRows / 32 : 0;
                 for (int kb0 = slabs_from(part); kb0 < to && ok; ++pass) {
                     const int end = PASSES ? min(kb0 + A.pass_blocks, to) : to;
                     const uint32_t sums = tmem + (pass & 1) * stride;
@@ -704,7 +770,26 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                         if (!ok) break;
                         fence_after();
                         const int steps = kb + 1 < A.k_blocks ? 4 : last_steps;
-                        if (elected()) {
+                        if constexpr (MX) {
+                            // scales of x (two tiles of four blocks), then of w (two, with the columns' 128s next to each other)
+                            const uint32_t xs = tmem + kMxTmem + 32 * (n_slabs++ & 1), ws = xs + 8;
+                            const uint64_t scales = scales_desc(ring + at.s * stage_bytes + codes_bytes);
+                            const uint32_t w_at = ws + w_word;
+                            if (elected()) {
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    scales_to_tmem<CG>(xs + 4 * j, scales + kMxTileBytes / 16 * j);
+                                    scales_to_tmem<CG>(ws + 8 * j, scales + (kMxScales + kMxTileBytes * j) / 16);
+                                    if (A.tile_n > 128) scales_to_tmem<CG>(ws + 8 * j + 4, scales + (2 * kMxScales + kMxTileBytes * j) / 16);
+                                }
+                                mma_mx<CG>(sums, a, b, idesc, xs, w_at, kb > kb0);
+                                if (steps > 1) mma_mx<CG>(sums, a + 2, b + 2, idesc | upper_scales, xs, w_at, true);
+                                if (steps > 2) mma_mx<CG>(sums, a + 4, b + 4, idesc, xs + 4, w_at + 8, true);
+                                if (steps > 3) mma_mx<CG>(sums, a + 6, b + 6, idesc | upper_scales, xs + 4, w_at + 8, true);
+                                commit<CG>(empty + 8 * at.s);
+                                if (kb + 1 == end) commit<CG>(acc_full + 8 * (pass & 1));
+                            }
+                        } else if (elected()) {
                             mma<CG, FP8>(sums, a, b, idesc, kb > kb0);
                             if (steps > 1) mma<CG, FP8>(sums, a + 2, b + 2, idesc, true);
                             if (steps > 2) mma<CG, FP8>(sums, a + 4, b + 4, idesc, true);
@@ -735,6 +820,13 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                     if (rank == 0) mbar_expect_tx(full + 8 * at.s, announced);
                     tma_2d<CG>(dst, &A.x_map, kb * kSlab, row, bar0 + 8 * at.s);
                     tma_2d<CG>(dst + kRows * kSlab, &A.w_map, kb * kSlab, col, bar0 + 8 * at.s);
+                    if constexpr (MX) {  // (in words; both CTAs of a pair take the scales of all columns)
+                        const int w_tile = tile.n * A.tile_n / kMxTileRows;
+                        const uint32_t scales = dst + codes_bytes;
+                        tma_2d<CG>(scales, &A.x_scale_map, kb * (kMxScales / 4), row / kMxTileRows, bar0 + 8 * at.s);
+                        for (int i = 0; i < mx_w_tiles(A.tile_n); ++i)
+                            tma_2d<CG>(scales + kMxScales * (1 + i), &A.w_scale_map, kb * (kMxScales / 4), w_tile + i, bar0 + 8 * at.s);
+                    }
                 }
                 at.next(stages);
             }
@@ -759,8 +851,9 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
 
 template <Results RESULTS, bool PASSES>
 LinearKernel kernel_of(int cg, bool fp8) {
-    if (cg == 2) return fp8 ? linear_kernel<2, true, PASSES, RESULTS> : linear_kernel<2, false, PASSES, RESULTS>;
-    return fp8 ? linear_kernel<1, true, PASSES, RESULTS> : linear_kernel<1, false, PASSES, RESULTS>;
+    constexpr Operands B = Operands::kBf16, F = Operands::kE4m3;
+    if (cg == 2) return fp8 ? linear_kernel<2, F, PASSES, RESULTS> : linear_kernel<2, B, PASSES, RESULTS>;
+    return fp8 ? linear_kernel<1, F, PASSES, RESULTS> : linear_kernel<1, B, PASSES, RESULTS>;
 }
 
 }  // namespace

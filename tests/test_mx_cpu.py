@@ -87,3 +87,37 @@ def test_refusals(lib):
     block.cb_mx_quantize(nothing, None, None, None)
     block.cb_mx_dequantize(nothing, None, None, None)
     assert ctypes.sizeof(block.cb_mx_desc) == 40
+
+
+def test_linear_refusals(lib):
+    block, cb = lib
+    A, L, M = cb.CB_ERR_ARG, cb.CB_ERR_ALIGN, cb.CB_ERR_LIMIT
+    W, X, O, R_, S, T = 0x10000, 0x20000, 0x30000, 0x40000, 0x50000, 0x60000  # never dereferenced
+
+    def status(f, *a, **kw):
+        with pytest.raises(cb.CbError) as e:
+            f(*a, **kw)
+        return e.value.status
+
+    def create(w=W, n=64, k=100, w_scale=S, **kw):
+        return status(block.cb_linear_create, w, n, k, cb.CB_MXFP4, w_scale=w_scale, **kw)
+
+    assert create(w_scale=None) == A and create(w_stride=96) == A and create(w_stride=100) == A and create(w_stride=144) == A
+    assert create(w=W + 8) == L and create(w_scale=S + 8) == L and create(w_stride=1 << 33) == M and create(k=(1 << 22) + 1) == M
+    layer, wide = block.cb_linear_create(W, 100, 100, cb.CB_MXFP4, w_scale=S), block.cb_linear_create(W, 100, 100, cb.CB_BF16)
+
+    def run(x=X, x_scale=S, resid=None, gate=None, out=O, resid_out=None, layer=layer, **kw):
+        d = dict(rows=4, out_dtype=cb.CB_BF16, resid_dtype=cb.CB_BF16, gate_dtype=cb.CB_BF16)
+        d.update(kw)
+        return status(block.cb_linear_run, layer, block.cb_linear_io(**d), x, x_scale, resid, gate, out, resid_out)
+
+    mx = dict(out_dtype=cb.CB_MXFP4, out_scale=T)
+    assert run(x_scale=None) == A and run(x=X + 8) == L and run(x_scale=S + 4) == L and run(x_stride=100) == A and run(x_stride=96) == A
+    assert run(x_stride=1 << 33) == M and run(out_dtype=cb.CB_MXFP4) == A and run(out=None, **mx) == A
+    assert run(resid=R_, resid_out=R_, **mx) == A and run(out=None, resid=R_, resid_out=R_, **mx) == A
+    assert run(out_stride=100, **mx) == A and run(out_stride=96, **mx) == A and run(out=O + 8, **mx) == L
+    assert run(out_dtype=cb.CB_MXFP4, out_scale=T + 8) == L and run(out_dtype=cb.CB_E4M3) == A and run(resid_dtype=cb.CB_MXFP4) == A
+    assert run(layer=wide, x_scale=None, **mx) == A and run(layer=wide) == A
+    block.cb_linear_run(layer, block.cb_linear_io(rows=0), None)
+    block.cb_linear_destroy(layer)
+    block.cb_linear_destroy(wide)
