@@ -70,6 +70,64 @@ int cb_norm_residual(const cb_norm_desc* desc, const void* x, const void* branch
                      const void* weight, const void* scale, const void* shift, void* x_out, void* out,
                      float* out_scale, void* stream);
 
+/* Kinds of norm of cb_norm_around: none, root mean square, layer norm (less the mean first). */
+enum {
+    CB_NORM_NONE = 0,
+    CB_NORM_RMS = 1,
+    CB_NORM_LAYER = 2
+};
+
+/* Sizes and types of cb_norm_around. Strides are in elements from one row (or sample) to the next; 0 means
+ * contiguous. */
+typedef struct {
+    int64_t rows;          /* >= 0; 0 does nothing */
+    int64_t hidden;        /* >= 1 */
+    int64_t tokens;        /* rows of one sample; 0: all rows are one sample */
+    int64_t x_stride;
+    int64_t branch_stride;
+    int64_t x_out_stride;
+    int64_t out_stride;    /* of an output in CB_MXFP4: a multiple of CB_MX_BLOCK */
+    int64_t line_stride;   /* from one sample's gate, scale and shift to the next's */
+    cb_dtype x_dtype;      /* of x and x_out: CB_BF16 or CB_FP32 */
+    cb_dtype branch_dtype; /* CB_BF16 or CB_FP32 */
+    cb_dtype param_dtype;  /* of all lines: CB_BF16 or CB_FP32 */
+    cb_dtype out_dtype;    /* CB_BF16, CB_FP32, CB_E4M3 or CB_MXFP4 */
+    int32_t after;         /* CB_NORM_* of the branch, after its block */
+    int32_t before;        /* CB_NORM_* of the hidden state, before the next block */
+    float after_eps;       /* >= 0, finite */
+    float before_eps;      /* >= 0, finite */
+    float x_factor;        /* finite; 1 where the residual is not scaled */
+    float branch_factor;   /* finite; 1 where the branch is not scaled */
+    int32_t reserved;      /* must be 0 */
+} cb_norm_around_desc;
+
+/* The norms around a block: the branch is normalised and added to the hidden state, and that is normalised
+ * for the next branch, row by row:
+ *     N(v) = v                                                  CB_NORM_NONE
+ *            v / sqrt(mean(v^2) + eps)                          CB_NORM_RMS
+ *            (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps)  CB_NORM_LAYER
+ *     r = N_after(branch) * after_weight + after_bias
+ *     h = x_factor * x + branch_factor * gate * r
+ *     x_out = round(h)
+ *     y = (N_before(h) * weight + bias) * (1 + scale) + shift
+ * in fp32 (h enters its norm un-rounded; mean and squares in two passes), and out = y in bf16 or fp32, in e4m3
+ * with a scale a row as cb_norm_residual makes it (out_scale: fp32 [rows]), or in 4 bits as cb_mx_quantize
+ * makes it of fp32 rows (out_scale: its scales). It takes layer norms with a modulation (the adaptive ones
+ * of diffusion transformers: before = CB_NORM_LAYER, scale, shift, gate) and blocks that are normed on
+ * both sides. With CB_NORM_NONE after, no branch or eps = 0 the formulas hold as they stand.
+ * x, branch, x_out, out: rows of `hidden` elements; gate, scale, shift: a line per sample; after_weight,
+ * after_bias, weight, bias: one line. May be NULL: branch (then without gate, after_weight and after_bias, with
+ * after = CB_NORM_NONE), each line (factors 1, terms 0), and x_out or out (with its scale). after_weight
+ * and after_bias go with a norm after, weight and bias with one before, and scale and shift with an out. x_out may be
+ * x itself (same stride). Rows that are not finite touch no others; in 4 bits a block with a NaN or an
+ * infinity is NaN.
+ * Rows and hidden sizes up to 16384 on the 16-byte grid take vector loads, others elements.
+ * Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size; an output in 4 bits or its scales off 16
+ * bytes), CB_ERR_LIMIT (rows beyond 2^31 - 1 or hidden beyond 2^31 - 256), CB_ERR_CUDA. */
+int cb_norm_around(const cb_norm_around_desc* desc, const void* x, const void* branch, const void* gate,
+                   const void* after_weight, const void* after_bias, const void* weight, const void* bias,
+                   const void* scale, const void* shift, void* x_out, void* out, void* out_scale, void* stream);
+
 /* ---- rows in 4 bits (CB_MXFP4)
  *
  * A matrix [rows, features] is held as codes and scales. An element is an e2m1 code c (sign, two

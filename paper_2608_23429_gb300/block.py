@@ -28,6 +28,20 @@ class cb_norm_desc(ctypes.Structure):
                 ("param_dtype", _I), ("out_dtype", _I), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
+class cb_norm_around_desc(ctypes.Structure):
+    """Sizes and types of :func:`cb_norm_around`; strides of 0 mean contiguous. Made by name, its factors are 1."""
+    _fields_ = [("rows", _L), ("hidden", _L), ("tokens", _L), ("x_stride", _L), ("branch_stride", _L),
+                ("x_out_stride", _L), ("out_stride", _L), ("line_stride", _L), ("x_dtype", _I), ("branch_dtype", _I),
+                ("param_dtype", _I), ("out_dtype", _I), ("after", ctypes.c_int32), ("before", ctypes.c_int32),
+                ("after_eps", ctypes.c_float), ("before_eps", ctypes.c_float), ("x_factor", ctypes.c_float),
+                ("branch_factor", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+    def __init__(self, *args, **kw):
+        if not args:
+            kw = {"x_factor": 1.0, "branch_factor": 1.0, **kw}
+        super().__init__(*args, **kw)
+
+
 class cb_mx_desc(ctypes.Structure):
     """Sizes and types of :func:`cb_mx_quantize` and :func:`cb_mx_dequantize`; strides of 0 mean contiguous."""
     _fields_ = [("rows", _L), ("features", _L), ("stride", _L), ("codes_stride", _L), ("dtype", _I),
@@ -48,11 +62,13 @@ class cb_linear_io(ctypes.Structure):
 
 
 CB_ACT_NONE, CB_ACT_GELU, CB_ACT_SILU = 0, 1, 2
+CB_NORM_NONE, CB_NORM_RMS, CB_NORM_LAYER = 0, 1, 2
 CB_MAX_IN_FEATURES = 1 << 22
 CB_MX_BLOCK = 32
 
 _sig = {
     "cb_norm_residual": ([_P] * 11, _I),
+    "cb_norm_around": ([_P] * 14, _I),
     "cb_mx_scale_bytes": ([_L, _L, _P], _I),
     "cb_mx_quantize": ([_P] * 5, _I),
     "cb_mx_dequantize": ([_P] * 5, _I),
@@ -68,6 +84,7 @@ for _name, (_args, _res) in _sig.items():
 
 EXPORTED = tuple(_sig)
 _norm_residual, _linear_run = _lib.cb_norm_residual, _lib.cb_linear_run
+_norm_around = _lib.cb_norm_around
 _mx_quantize, _mx_dequantize = _lib.cb_mx_quantize, _lib.cb_mx_dequantize
 
 
@@ -78,6 +95,16 @@ def cb_norm_residual(desc: cb_norm_desc, x, branch=None, gate=None, weight=None,
                         _addr(x_out), _addr(out), _addr(out_scale), None if stream is None else _stream(stream))
     if rc < 0:
         _raise(rc, "cb_norm_residual")
+
+
+def cb_norm_around(desc: cb_norm_around_desc, x, branch=None, gate=None, after_weight=None, after_bias=None, weight=None,
+                   bias=None, scale=None, shift=None, x_out=None, out=None, out_scale=None, stream=None) -> None:
+    """The branch, normed after its block, added to ``x`` (into ``x_out``), and the sum normed before the next (into ``out``)."""
+    rc = _norm_around(ctypes.addressof(desc), _addr(x), _addr(branch), _addr(gate), _addr(after_weight), _addr(after_bias),
+                      _addr(weight), _addr(bias), _addr(scale), _addr(shift), _addr(x_out), _addr(out), _addr(out_scale),
+                      None if stream is None else _stream(stream))
+    if rc < 0:
+        _raise(rc, "cb_norm_around")
 
 
 def cb_mx_scale_bytes(rows: int, features: int) -> int:

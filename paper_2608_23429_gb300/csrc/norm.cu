@@ -15,18 +15,6 @@
 namespace cbk {
 namespace {
 
-__device__ __forceinline__ float value_at(const void* p, long long e, int bf16) {
-    return bf16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(p)[e] << 16) : reinterpret_cast<const float*>(p)[e];
-}
-__device__ __forceinline__ void put(void* p, long long e, int dtype, float v) {
-    if (dtype == CB_BF16)
-        reinterpret_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(v);
-    else if (dtype == CB_FP32)
-        reinterpret_cast<float*>(p)[e] = v;
-    else
-        reinterpret_cast<uint8_t*>(p)[e] = (uint8_t)norm_e4m3x2(v, 0.0f);
-}
-
 // Elements t, t + T, ... of a row from or to p (threads behind its end read its start and write nothing). The type is
 // asked for once, so that all loads are in flight together.
 template <int CH, int T>

@@ -92,6 +92,18 @@ __device__ __forceinline__ uint32_t row_reduce(uint32_t v, uint32_t* slots) {
     return v;
 }
 
+__device__ __forceinline__ float value_at(const void* p, long long e, int bf16) {
+    return bf16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(p)[e] << 16) : reinterpret_cast<const float*>(p)[e];
+}
+__device__ __forceinline__ void put(void* p, long long e, int dtype, float v) {
+    if (dtype == CB_BF16)
+        reinterpret_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(v);
+    else if (dtype == CB_FP32)
+        reinterpret_cast<float*>(p)[e] = v;
+    else
+        reinterpret_cast<uint8_t*>(p)[e] = (uint8_t)norm_e4m3x2(v, 0.0f);
+}
+
 // The larger magnitude; a NaN wins.
 __device__ __forceinline__ float max_abs(float a, float b) {
     float r;

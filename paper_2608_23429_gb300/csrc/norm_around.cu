@@ -1,0 +1,219 @@
+// cb_norm_around: the norm after a branch, its addition to the hidden state, and the norm before the next branch.
+//
+// Bound by HBM: a row is read once and written once, and stays on the SM between its reductions: in registers where it is reached by
+// vectors (norm_around_rows.cuh), in shared memory where it is not (below). A layer norm takes two of them, one after the other:
+// the squares of what is left when the mean is off lose nothing where the mean is far larger than the deviation, as sums of squares
+// less the mean's square do.
+#include <cmath>
+
+#include "norm_around.cuh"
+
+namespace cbk {
+namespace {
+
+constexpr int kAroundHeld = 49152;  // elements of a row in shared memory
+
+// A row by elements; HELD: in shared memory, else read again for each reduction.
+template <int W, bool HELD>
+__global__ void __launch_bounds__(32 * W) around_elements_kernel(const __grid_constant__ AroundArgs args) {
+    __shared__ uint32_t slots[5][W];
+    extern __shared__ float held[];
+    constexpr unsigned T = 32 * W;
+    const AroundArgs A = args;  // in registers, as stores would have them read again
+    after_previous();
+    const unsigned row = blockIdx.x, n = (unsigned)A.hidden, t = threadIdx.x;
+    const long long line = (long long)(row / A.tokens) * A.line_stride;
+    const long long xo = row * A.x_stride, bo = row * A.branch_stride;
+    auto at_line = [&](const void* p, long long e, float none) { return p ? value_at(p, e, A.param_bf16) : none; };
+    auto sum_of = [&](uint32_t* s, auto f) {  // over the row; each thread has the same elements in all of them
+        float sum = 0.0f;
+#pragma unroll 4
+        for (unsigned e = t; e < n; e += T) sum += f(e);
+        return __uint_as_float(row_reduce<W, false>(__float_as_uint(sum), s));
+    };
+    // (v - mean) rstd of the values f(e)
+    auto moments = [&](int kind, float eps, uint32_t (*s)[W], auto f, float* mean, float* rstd) {
+        *mean = kind == CB_NORM_LAYER ? sum_of(s[0], f) * A.inv_hidden : 0.0f;
+        const float off = *mean;
+        const float squares = sum_of(s[1], [&](unsigned e) {
+            const float v = f(e) - off;
+            return v * v;
+        });
+        *rstd = 1.0f / sqrtf(fmaf(squares, A.inv_hidden, eps));
+    };
+    float after_mean = 0.0f, after_rstd = 1.0f, mean = 0.0f, rstd = 1.0f;
+    auto branch_at = [&](unsigned e) { return value_at(A.branch, bo + e, A.branch_bf16); };
+    auto hidden_of = [&](float b, unsigned e) {
+        const float x = value_at(A.x, xo + e, A.x_bf16) * A.x_factor;
+        if (!A.branch) return x;
+        if (A.after != CB_NORM_NONE)
+            b = (b - after_mean) * after_rstd * at_line(A.after_weight, e, 1.0f) + at_line(A.after_bias, e, 0.0f);
+        return fmaf(b * at_line(A.gate, line + e, 1.0f), A.branch_factor, x);
+    };
+    if (A.after != CB_NORM_NONE) {
+        if constexpr (HELD) {
+#pragma unroll 4
+            for (unsigned e = t; e < n; e += T) held[e] = branch_at(e);
+            moments(A.after, A.after_eps, slots, [&](unsigned e) { return held[e]; }, &after_mean, &after_rstd);
+        } else {
+            moments(A.after, A.after_eps, slots, branch_at, &after_mean, &after_rstd);
+        }
+    }
+    auto made = [&](unsigned e) {
+        return hidden_of(HELD && A.after != CB_NORM_NONE ? held[e] : A.branch ? branch_at(e) : 0.0f, e);
+    };
+    auto put_x = [&](unsigned e, float h) {
+        if (A.x_out) put(A.x_out, row * A.x_out_stride + e, A.x_bf16 ? CB_BF16 : CB_FP32, h);
+    };
+    if constexpr (HELD) {
+#pragma unroll 4
+        for (unsigned e = t; e < n; e += T) {
+            const float h = made(e);
+            held[e] = h;
+            put_x(e, h);
+        }
+    }
+    auto hidden = [&](unsigned e) { return HELD ? held[e] : made(e); };
+    if (A.out && A.before != CB_NORM_NONE) moments(A.before, A.before_eps, slots + 2, hidden, &mean, &rstd);
+    auto normed = [&](float h, unsigned e) {
+        float y = h;
+        if (A.before != CB_NORM_NONE) y = (h - mean) * rstd * at_line(A.weight, e, 1.0f) + at_line(A.bias, e, 0.0f);
+        if (A.scale) y = fmaf(y, value_at(A.scale, line + e, A.param_bf16), y);
+        return A.shift ? y + value_at(A.shift, line + e, A.param_bf16) : y;
+    };
+    float inv = 1.0f;
+    if (A.out && A.out_dtype == CB_E4M3) {
+        float amax = 0.0f;
+#pragma unroll 4
+        for (unsigned e = t; e < n; e += T) amax = max_abs(amax, normed(hidden(e), e));
+        const float s = norm_scale_of(row_reduce<W, true>(__float_as_uint(amax) & 0x7FFFFFFFu, slots[4]));
+        if (t == 0) reinterpret_cast<float*>(A.out_scale)[row] = s;
+        inv = __frcp_rn(s);
+    }
+    if (A.out && A.out_dtype == CB_MXFP4) {
+        // a block is a warp; those that fill up the last tile of scales are zeros
+        uint8_t* const out = reinterpret_cast<uint8_t*>(A.out) + row * A.out_stride;
+        const unsigned ends = A.out_tiles * kMxTileBlocks * kMxBlock, codes_end = (n + kMxBlock - 1) / kMxBlock * kMxBlock;
+        for (unsigned e = t; e < ends; e += T) {
+            float y = 0.0f;
+            if (e < n) {
+                const float h = hidden(e);
+                if (!HELD) put_x(e, h);
+                y = normed(h, e);
+            }
+            const uint32_t scale = mx_scale_of(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
+            y *= mx_inverse(scale);
+            const float v[8] = {y, __shfl_down_sync(0xFFFFFFFFu, y, 1)};
+            if (t % 2 == 0 && e < codes_end) out[e / 2] = scale == 255 ? 0 : (uint8_t)mx_codes8(v);
+            const unsigned block = e / kMxBlock;
+            if (t % 32 == 0)
+                reinterpret_cast<uint8_t*>(A.out_scale)[mx_word_at(row, block / kMxTileBlocks, A.out_tiles) + block % kMxTileBlocks] = (uint8_t)scale;
+        }
+        return;
+    }
+    if (HELD && !A.out) return;
+    for (unsigned e = t; e < n; e += T) {
+        const float h = hidden(e);
+        if (!HELD) put_x(e, h);
+        if (A.out) put(A.out, row * A.out_stride + e, A.out_dtype, normed(h, e) * inv);
+    }
+}
+
+template <int W, bool HELD>
+cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
+    const auto k = around_elements_kernel<W, HELD>;
+    const size_t smem = HELD ? (size_t)a.hidden * 4 : 0;
+    if (smem > 47 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_overlapped(k, (int)a.rows, 32 * W, smem, s, a);
+}
+
+cudaError_t launch_row(AroundArgs& a, bool vec, int sms, cudaStream_t s) {
+    const int n = a.hidden;
+    if (vec && n <= 16384) return a.param_bf16 ? launch_around_bf16_lines(a, sms, s) : launch_around_fp32_lines(a, sms, s);
+    if (n <= 512) return launch_elements<4, true>(a, s);
+    if (n <= 2048) return launch_elements<8, true>(a, s);
+    if (n <= kAroundHeld) return launch_elements<16, true>(a, s);
+    return launch_elements<16, false>(a, s);
+}
+
+size_t bytes_of(int dtype) { return dtype == CB_BF16 ? 2 : dtype == CB_FP32 ? 4 : 1; }
+bool on_grid(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
+
+}  // namespace
+}  // namespace cbk
+
+extern "C" int cb_norm_around(const cb_norm_around_desc* d, const void* x, const void* branch, const void* gate,
+                              const void* after_weight, const void* after_bias, const void* weight, const void* bias,
+                              const void* scale, const void* shift, void* x_out, void* out, void* out_scale, void* stream) {
+    using namespace cbk;
+    auto wide = [](cb_dtype t) { return t == CB_BF16 || t == CB_FP32; };
+    auto kind = [](int32_t k) { return k >= CB_NORM_NONE && k <= CB_NORM_LAYER; };
+    auto eps = [](float e) { return e >= 0.0f && std::isfinite(e); };
+    if (!d || d->reserved != 0 || d->rows < 0 || d->hidden < 1 || d->tokens < 0) return CB_ERR_ARG;
+    if (!wide(d->x_dtype) || !wide(d->branch_dtype) || !wide(d->param_dtype)) return CB_ERR_ARG;
+    const bool mx = d->out_dtype == CB_MXFP4, scaled = mx || d->out_dtype == CB_E4M3;
+    if (!wide(d->out_dtype) && !scaled) return CB_ERR_ARG;
+    if (!kind(d->after) || !kind(d->before) || !eps(d->after_eps) || !eps(d->before_eps)) return CB_ERR_ARG;
+    if (!std::isfinite(d->x_factor) || !std::isfinite(d->branch_factor)) return CB_ERR_ARG;
+    if (d->rows > 0x7FFFFFFFLL || d->hidden > 0x7FFFFF00LL) return CB_ERR_LIMIT;
+    const int64_t strides[] = {d->x_stride, d->branch_stride, d->x_out_stride, d->out_stride, d->line_stride};
+    for (int64_t s : strides)
+        if (s != 0 && (s < d->hidden || s > CB_MAX_NUMEL)) return s < d->hidden ? CB_ERR_ARG : CB_ERR_LIMIT;
+    const long long blocks = mx_blocks(d->hidden);
+    if (mx && d->out_stride != 0 && (d->out_stride < blocks * kMxBlock || d->out_stride % kMxBlock != 0)) return CB_ERR_ARG;
+    if (d->rows == 0) return CB_OK;
+    if (!x || (!out && !x_out) || (scaled && out) != (out_scale != nullptr)) return CB_ERR_ARG;
+    if (!branch && (gate || d->after != CB_NORM_NONE)) return CB_ERR_ARG;
+    if (d->after == CB_NORM_NONE && (after_weight || after_bias)) return CB_ERR_ARG;
+    if (d->before == CB_NORM_NONE && (weight || bias)) return CB_ERR_ARG;
+    if (!out && (weight || bias || scale || shift)) return CB_ERR_ARG;
+    AroundArgs a{};
+    a.overlap = 1;
+    a.rows = (unsigned)d->rows;
+    a.hidden = (int)d->hidden;
+    a.tokens = d->tokens == 0 || d->tokens > d->rows ? a.rows : (unsigned)d->tokens;
+    a.x_stride = d->x_stride ? d->x_stride : d->hidden;
+    a.branch_stride = d->branch_stride ? d->branch_stride : d->hidden;
+    a.x_out_stride = d->x_out_stride ? d->x_out_stride : d->hidden;
+    a.out_stride = mx ? (d->out_stride ? d->out_stride : blocks * kMxBlock) / 2 : d->out_stride ? d->out_stride : d->hidden;
+    a.line_stride = d->line_stride ? d->line_stride : d->hidden;
+    a.x = x, a.branch = branch, a.gate = gate, a.after_weight = after_weight, a.after_bias = after_bias;
+    a.weight = weight, a.bias = bias, a.scale = scale, a.shift = shift;
+    a.x_out = x_out, a.out = out, a.out_scale = out_scale;
+    a.after = d->after, a.before = d->before, a.after_eps = d->after_eps, a.before_eps = d->before_eps;
+    a.x_factor = d->x_factor, a.branch_factor = d->branch_factor;
+    a.inv_hidden = (float)(1.0 / (double)d->hidden);
+    a.x_bf16 = d->x_dtype == CB_BF16;
+    a.branch_bf16 = d->branch_dtype == CB_BF16;
+    a.param_bf16 = d->param_dtype == CB_BF16;
+    a.out_dtype = d->out_dtype;
+    a.out_tiles = (unsigned)mx_tiles_k(d->hidden);
+    // a pointer, its element size and the stride behind it (rows start on the grid too)
+    const struct {
+        const void* p;
+        int dtype;
+        long long stride;
+    } used[] = {{x, d->x_dtype, a.x_stride},            {branch, d->branch_dtype, a.branch_stride},
+                {gate, d->param_dtype, a.line_stride},  {after_weight, d->param_dtype, 0},
+                {after_bias, d->param_dtype, 0},        {weight, d->param_dtype, 0},
+                {bias, d->param_dtype, 0},              {scale, d->param_dtype, a.line_stride},
+                {shift, d->param_dtype, a.line_stride}, {x_out, d->x_dtype, a.x_out_stride},
+                {mx ? nullptr : out, d->out_dtype, a.out_stride}};
+    bool vec = d->hidden % 8 == 0;
+    for (const auto& u : used) {
+        const size_t es = bytes_of(u.dtype), grid = es == 1 ? 8 : 16;
+        if (!u.p) continue;
+        if (!on_grid(u.p, es)) return CB_ERR_ALIGN;
+        vec = vec && on_grid(u.p, grid) && (size_t)u.stride * es % grid == 0;
+    }
+    if (mx && (!on_grid(out, 16) || !on_grid(out_scale, 16))) return CB_ERR_ALIGN;
+    if (!on_grid(out_scale, 4)) return CB_ERR_ALIGN;
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = launch_row(a, vec, sms, (cudaStream_t)stream);
+    return e == cudaSuccess ? CB_OK : cuda_error(e, "norm launch");
+}

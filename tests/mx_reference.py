@@ -73,3 +73,22 @@ def quantised(v):
     e = scale_bytes(v)
     c = codes(v, e)
     return values(c, e, v.shape[1]), packed(c), tiled(e)
+
+
+def check_quantised(v, e, out, t, fill=0xA5):
+    """Rows in 4 bits (packed, with what lies between rows, and scales) hold what the format makes of some values within e of v: the
+    scale lies between those of the block's largest magnitude less and more the bound, and each code between those of the
+    value less and more the bound, under that scale. Zeros behind the last feature and block, all else as it was."""
+    m, n = v.shape
+    blocks = -(-n // 32)
+    got = from_tiles(t, m, blocks)
+    low, high = np.maximum(np.abs(v) - e, 0.0), np.abs(v) + e
+    assert (got >= scale_bytes(low)).all() and (got <= scale_bytes(high)).all()
+    assert np.array_equal(t, tiled(got, fill))
+    assert (out[:, 16 * blocks:] == fill).all()
+    c = unpacked(out[:, :16 * blocks])
+    assert (c[:, n:] == 0).all()
+    q = values(c, got, n)
+    least, most = (values(codes(v + s * e, got), got, n) for s in (-1, 1))
+    bad = ~((q >= least) & (q <= most))
+    assert not bad.any(), (bad.sum(), np.argwhere(bad)[:3], q[bad][:3], v[bad][:3])

@@ -107,30 +107,11 @@ def run(lib, c, seed=0, stream=None, spread=0.5):
     return (v, e, h, eh), out, xo, out_scale
 
 
-def check_quantised(c, v, e, out, scales):
-    m, n = c["m"], c["n"]
-    blocks = -(-n // 32)
-    v, e = v.cpu().numpy(), e.cpu().numpy()
-    t = scales.cpu().numpy()
-    got = R.from_tiles(t, m, blocks)
-    low, high = np.maximum(np.abs(v) - e, 0.0), np.abs(v) + e
-    assert (got >= R.scale_bytes(low)).all() and (got <= R.scale_bytes(high)).all()
-    assert np.array_equal(t, R.tiled(got, 0xA5))  # zeros behind the last block, rows behind the last as they were
-    b = out.cpu().numpy()
-    assert (b[:, 16 * blocks:] == 0xA5).all()
-    codes = R.unpacked(b[:, :16 * blocks])
-    assert (codes[:, n:] == 0).all()
-    q = R.values(codes, got, n)
-    least, most = (R.values(R.codes(v + s * e, got), got, n) for s in (-1, 1))
-    bad = ~((q >= least) & (q <= most))
-    assert not bad.any(), (bad.sum(), np.argwhere(bad)[:3], q[bad][:3], v[bad][:3])
-
-
 def check(lib, c, seed=0, **kw):
     (v, e, h, eh), out, xo, scales = run(lib, c, seed, **kw)
     assert lib[0].cb_linear_device_status() == 0
     if c["out"] == "mx":
-        check_quantised(c, v, e, out, scales)
+        R.check_quantised(v.cpu().numpy(), e.cpu().numpy(), out.cpu().numpy(), scales.cpu().numpy())
     elif out is not None:
         close(out, v, e, c["out"])
     if xo is not None:

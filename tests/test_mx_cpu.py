@@ -121,3 +121,49 @@ def test_linear_refusals(lib):
     block.cb_linear_run(layer, block.cb_linear_io(rows=0), None)
     block.cb_linear_destroy(layer)
     block.cb_linear_destroy(wide)
+
+
+def test_norm_around_refusals(lib):
+    block, cb = lib
+    A, L, M = cb.CB_ERR_ARG, cb.CB_ERR_ALIGN, cb.CB_ERR_LIMIT
+    P = {n: 0x10000 * (i + 1) for i, n in enumerate(("x", "branch", "gate", "after_weight", "after_bias", "weight", "bias", "scale", "shift",
+                                                    "x_out", "out", "out_scale"))}  # never dereferenced
+    order = list(P)
+
+    def norm(given=("x", "x_out", "out"), at=None, **kw):
+        d = dict(rows=4, hidden=100, tokens=2, x_dtype=cb.CB_BF16, branch_dtype=cb.CB_BF16, param_dtype=cb.CB_BF16, out_dtype=cb.CB_BF16,
+                 before=block.CB_NORM_LAYER, before_eps=1e-6)
+        d.update(kw)
+        a = {**{n: P[n] for n in given}, **(at or {})}
+        with pytest.raises(cb.CbError) as e:
+            block.cb_norm_around(block.cb_norm_around_desc(**d), *[a.get(n) for n in order])
+        return e.value.status
+
+    rms, every = dict(after=block.CB_NORM_RMS), tuple(order[:-1])
+    assert norm(("out",)) == A and norm(("x",)) == A and norm(("x", "out", "gate")) == A and norm(("x", "out"), **rms) == A
+    assert norm(("x", "branch", "out", "after_weight")) == A and norm(("x", "branch", "out", "after_bias")) == A
+    for n in ("weight", "bias"):
+        assert norm(("x", "out", n), before=block.CB_NORM_NONE) == A
+    for n in ("weight", "bias", "scale", "shift", "out_scale"):
+        assert norm(("x", "x_out", n)) == A
+    assert norm(("x", "out", "out_scale")) == A and norm(out_dtype=cb.CB_E4M3) == A and norm(out_dtype=cb.CB_MXFP4) == A
+    assert norm(("x", "x_out", "out_scale"), out_dtype=cb.CB_MXFP4) == A
+    assert norm(rows=-1) == A and norm(hidden=0) == A and norm(tokens=-1) == A and norm(reserved=1) == A
+    for n in ("x_dtype", "branch_dtype", "param_dtype"):
+        assert norm(**{n: cb.CB_E4M3}) == A and norm(**{n: cb.CB_MXFP4}) == A and norm(**{n: 9}) == A
+    assert norm(out_dtype=cb.CB_INT8) == A and norm(after=3) == A and norm(before=-1) == A
+    for n in ("after_eps", "before_eps"):
+        assert norm(**{n: -1.0}) == A and norm(**{n: float("nan")}) == A and norm(**{n: float("inf")}) == A
+    for n in ("x_factor", "branch_factor"):
+        assert norm(**{n: float("nan")}) == A and norm(**{n: float("inf")}) == A
+    for s in ("x_stride", "branch_stride", "x_out_stride", "out_stride", "line_stride"):
+        assert norm(**{s: 99}) == A and norm(**{s: -100}) == A and norm(**{s: cb.CB_MAX_NUMEL + 1}) == M
+    mx = dict(given=("x", "out", "out_scale"), out_dtype=cb.CB_MXFP4)
+    assert norm(out_stride=100, **mx) == A and norm(out_stride=130, **mx) == A
+    assert norm(rows=1 << 31) == M and norm(hidden=1 << 31) == M
+    for n in every:
+        assert norm(every, {n: P[n] + 1}, **rms) == L
+    assert norm(at={"out": P["out"] + 8}, **mx) == L and norm(at={"out_scale": P["out_scale"] + 8}, **mx) == L
+    assert norm(("x", "out", "out_scale"), {"out_scale": P["out_scale"] + 2}, out_dtype=cb.CB_E4M3) == L
+    assert cb._lib.cb_norm_around(None, *[P["x"]] * 12, None) == A
+    block.cb_norm_around(block.cb_norm_around_desc(rows=0, hidden=4), None)
