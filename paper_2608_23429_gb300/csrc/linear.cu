@@ -327,6 +327,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.passes = (a.part_blocks + a.pass_blocks - 1) / a.pass_blocks;
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
+    a.group_magic = ~0ull / (8ull * (unsigned)a.tiles_n) + 1;
 
     // memory for copies of operands and for the sums of parts, in stream order
     const cudaStream_t s = (cudaStream_t)stream;
@@ -368,8 +369,9 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     if (rc == CB_OK)
         rc = pw.dst ? operand_map(&a.w_map, pw.dst, ep.N, 32ll * pw.chunks, 32ll * pw.chunks, a.tile_n / cg)
                     : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);
-    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - linear_fixed_bytes(a.results, a.more_boxes)) /
-                                                          (linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0)));
+    const size_t fixed = linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes) : 0);
+    const size_t stage = linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0);
+    a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - fixed) / stage);
     const long long tiles = (long long)a.tiles_m * a.tiles_n * a.parts, units = cg == 2 ? dev->pairs : dev->sms;
     if (rc == CB_OK && e == cudaSuccess) e = launch_linear(a, cg, d.type == CB_E4M3, cg * (int)std::min(tiles, units), s);
     if (rc == CB_OK && e == cudaSuccess && a.parts > 1) e = launch_linear_join(join, s);

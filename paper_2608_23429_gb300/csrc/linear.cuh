@@ -37,6 +37,15 @@ __host__ __device__ constexpr int mx_w_tiles(int tile_n) { return (tile_n + 127)
 __host__ __device__ constexpr int mx_scale_bytes(int tile_n) { return kMxScales * (1 + mx_w_tiles(tile_n)); }
 constexpr int kMxMostN = 192, kMxStepN = 64;  // columns of a tile: TMEM holds two accumulators and scales
 
+// Warps of the epilogue: two for each quarter of the TMEM lanes, or four where the threads load and store the results themselves
+// and wait for that (GB300, 8192 x 8191 x 512 bf16 with a gated fp32 hidden state: eight warps, 32 rows at once each, 282 us,
+// sixteen, eight rows at once, 195).
+__host__ __device__ constexpr int epi_warps(Results r, bool mx = false) {
+    if (mx) return r == Results::kDirect ? 16 : r == Results::kHidden ? 8 : 12;
+    return r == Results::kDirect ? 16 : 8;
+}
+constexpr int kTurnBytes = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
+
 struct LinearArgs {
     Results results;
     Operands operands;
@@ -50,6 +59,7 @@ struct LinearArgs {
     int overlap;
     int k_bytes;           // bytes of a row of x and of w
     int tiles_m, tiles_n, k_blocks, stages;
+    unsigned long long group_magic;  // ceil(2^64 / (8 tiles_n)): t group_magic / 2^64 is t / (8 tiles_n) for every 32-bit t
     int tile_n;            // output columns of a tile
     int passes, pass_blocks;  // stretches of K that are summed by themselves, and their slabs
     int parts, part_blocks;   // parts of K that are tiles of their own, and their slabs
@@ -99,6 +109,8 @@ cudaError_t launch_linear_join(const LinearJoinArgs& a, cudaStream_t s);
 size_t linear_stage_bytes(int cg, int tile_n);
 size_t linear_fixed_bytes(Results r, int more_boxes);  // shared memory besides the stages
 constexpr int kBox = 2048, kMaxRing = 6;
+// ...and more of it, of the kernels for operands in 4 bits
+constexpr size_t mx_more_bytes(Results r, int more_boxes) { return (size_t)(epi_warps(r, true) - epi_warps(r)) * (kTurnBytes + more_boxes * kBox); }
 constexpr int kMaxLinStages = 12;
 cudaError_t prepare_linear(size_t smem, int* pairs);
 using LinearKernel = void (*)(LinearArgs);

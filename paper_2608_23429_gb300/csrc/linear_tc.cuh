@@ -38,18 +38,13 @@ namespace {
 constexpr int kRows = 128;        // rows of x per CTA
 constexpr int kSlab = 128;        // bytes of K per stage
 constexpr int kAccStride = 256;   // TMEM columns from one accumulator to the other (half of it where there are passes)
-// Warps of the epilogue: two for each quarter of the TMEM lanes, or four where the threads load and store the results themselves
-// and wait for that (GB300, 8192 x 8191 x 512 bf16 with a gated fp32 hidden state: eight warps, 32 rows at once each, 282 us,
-// sixteen, eight rows at once, 195).
-__host__ __device__ constexpr int epi_warps(Results r) { return r == Results::kDirect ? 16 : 8; }
-__host__ __device__ constexpr int linear_threads(Results r) { return 32 * (epi_warps(r) + 2); }
+__host__ __device__ constexpr int linear_threads(Results r, bool mx = false) { return 32 * (epi_warps(r, mx) + 2); }
 constexpr int kMxTmem = 448;      // TMEM column of the scales of two slabs (4 bits; accumulators have 192 columns at most)
-constexpr int kTurn = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
 
-struct alignas(16) Tail {  // behind the stages and the epilogue's warps' kTurn each
+struct alignas(16) Tail {  // behind the stages and the epilogue's warps' kTurnBytes each
     float cols[2][2 * kAccStride];  // scales and biases of a tile's columns (where the output leaves by TMA)
     uint64_t full[kMaxLinStages], empty[kMaxLinStages], acc_full[2], acc_empty[2], cols_full[2];
-    uint64_t resid_full[epi_warps(Results::kHidden)][kMaxRing];
+    uint64_t resid_full[16][kMaxRing];
     uint32_t tmem;
     int abort;
 };
@@ -246,13 +241,18 @@ __device__ __forceinline__ void tmem_add(uint32_t addr, float* v) {
 struct Tile {
     int m, n, part;
 };
-// Groups of eight rows of tiles, so that tiles worked on together share operands in L2; SPLIT: parts of K, one after the other.
+// Groups of eight rows of tiles, so that tiles worked on together share operands in L2; SPLIT: parts of K, one after the other. Without
+// divisions, but for a last group of other than eight rows: three tiles are sought for each one that is worked on, in front of everything
+// else of its epilogue.
 template <bool SPLIT>
 __device__ __forceinline__ Tile tile_at(const LinearArgs& A, int t) {
-    const int part = SPLIT ? t % A.parts : 0;
-    if (SPLIT) t /= A.parts;
-    const int group = 8 * A.tiles_n, g = t / group, r = t - g * group;
-    const int rows = min(8, A.tiles_m - 8 * g);
+    int part = 0;
+    if (SPLIT && A.parts > 1) {
+        part = t % A.parts;
+        t /= A.parts;
+    }
+    const int g = (int)__umul64hi((unsigned long long)t, A.group_magic), r = t - g * 8 * A.tiles_n, rows = A.tiles_m - 8 * g;
+    if (rows >= 8) return Tile{8 * g + r % 8, r / 8, part};
     return Tile{8 * g + r % rows, r / rows, part};
 }
 
@@ -320,6 +320,18 @@ __device__ __forceinline__ void values(const LinearEpilogue& E, const float* col
     }
 }
 
+// The same without scales (operands in 4 bits: theirs are in the sums).
+template <int ACT>
+__device__ __forceinline__ void values_mx(const float* bias, const float* v, Two* x) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(bias + 4 * j);
+        x[2 * j] = add2(two(v[4 * j], v[4 * j + 1]), b.x);
+        x[2 * j + 1] = add2(two(v[4 * j + 2], v[4 * j + 3]), b.y);
+        if (j % 4 == 3) lin_act_all<ACT, 8>(x + 2 * j - 6);
+    }
+}
+
 // A box's worth of values (16 of fp32, 32 of bf16) into shared memory.
 template <bool BF16>
 __device__ __forceinline__ void put_box(uint32_t box, int lane, const Two* x) {
@@ -369,35 +381,60 @@ __device__ __forceinline__ void add_box(uint32_t box, int lane, const Two* gate,
     }
 }
 
-// A lane's row of 32 columns as a block in 4 bits: 16 bytes of codes and a byte of scale (and zeros for the blocks that fill up the
-// row's last tile of scales).
-__device__ __forceinline__ void put_quantised(const LinearEpilogue& E, uint8_t* scales, unsigned tiles, int row, int col, const Two* x) {
-    float v[32];
-    uint32_t most = 0;
+// A lane's row of 32 columns from `col` on as a block in 4 bits: its codes, and the scale byte.
+__device__ __forceinline__ uint32_t quantised(const LinearEpilogue& E, int col, Two* x, uint32_t* codes) {
+    if (col + kMxBlock > E.N) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 f = both(x[i]);
+            x[i] = two(col + 2 * i < E.N ? f.x : 0.0f, col + 2 * i + 1 < E.N ? f.y : 0.0f);
+        }
+    }
+    float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const float2 f = both(x[i]);
-        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        most = mx_max_abs(most, f.x, f.y);
     }
-    if (col + 32 > E.N) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (col + i >= E.N) v[i] = 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < 32; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    const uint32_t e = mx_scale_of(most);
+    const uint32_t e = mx_scale_of(__float_as_uint(most));
     const float inverse = mx_inverse(e);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] *= inverse;
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = both(mul2(x[4 * i + j], two(inverse, inverse)));
+            v[2 * j] = f.x, v[2 * j + 1] = f.y;
+        }
+        codes[i] = mx_codes8(v);
+        if (e == 255) codes[i] = 0;
+    }
+    return e;
+}
+// One or two neighbouring blocks of a lane's row (the first one's place in the row is even) and their scale bytes; behind the row's
+// last block zeros fill up its tile of scales. `whole`: two blocks lie on 32-byte boundaries, a sector of L2.
+__device__ __forceinline__ void put_blocks(const LinearEpilogue& E, uint8_t* scales, unsigned tiles, bool whole, int row, int col, int blocks,
+                                           const uint32_t* codes, uint32_t e) {
     if (row >= E.M) return;
-    const uint4 codes = e == 255 ? make_uint4(0, 0, 0, 0) : make_uint4(mx_codes8(v), mx_codes8(v + 8), mx_codes8(v + 16), mx_codes8(v + 24));
-    *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(E.out) + (row * E.out_stride + col) / 2) = codes;
-    const int block = col / kMxBlock;
-    uint8_t* const to = scales + mx_word_at((unsigned)row, (unsigned)block / kMxTileBlocks, tiles);
-    to[block % kMxTileBlocks] = (uint8_t)e;
-    if (col + kMxBlock >= E.N)
-        for (int b = block % kMxTileBlocks + 1; b < kMxTileBlocks; ++b) to[b] = 0;
+    char* const p = reinterpret_cast<char*>(E.out) + (row * E.out_stride + col) / 2;
+    uint8_t* const to = scales + mx_word_at((unsigned)row, (unsigned)col / (kMxBlock * kMxTileBlocks), tiles);
+    const int first = col / kMxBlock % kMxTileBlocks;
+    if (blocks == 2) {
+        if (whole) {
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(codes[0]), "r"(codes[1]), "r"(codes[2]), "r"(codes[3]),
+                         "r"(codes[4]), "r"(codes[5]), "r"(codes[6]), "r"(codes[7])
+                         : "memory");
+        } else {
+            *reinterpret_cast<uint4*>(p) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+            *reinterpret_cast<uint4*>(p + 16) = make_uint4(codes[4], codes[5], codes[6], codes[7]);
+        }
+        *reinterpret_cast<uint16_t*>(to + first) = (uint16_t)e;
+    } else {
+        *reinterpret_cast<uint4*>(p) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+        to[first] = (uint8_t)e;
+    }
+    if (col + kMxBlock * blocks >= E.N)
+        for (int b = first + blocks; b < kMxTileBlocks; ++b) to[b] = 0;
 }
 
 // Results by the threads, for rows off the 16-byte grid: a column per lane, eight rows at a time, whose hidden states are loaded
@@ -469,10 +506,11 @@ __device__ __forceinline__ void finish_rows(const LinearEpilogue& E, int row0, i
 }
 
 template <int CG, Operands OPERANDS, bool PASSES, Results RESULTS>
-__global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(const __grid_constant__ LinearArgs A) {
-    constexpr int EPI = epi_warps(RESULTS);
+__global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::kMx), 1) linear_kernel(const __grid_constant__ LinearArgs A) {
+    constexpr int EPI = epi_warps(RESULTS, OPERANDS == Operands::kMx);
     constexpr bool FP8 = OPERANDS == Operands::kE4m3, MX = OPERANDS == Operands::kMx, QUANT = RESULTS == Results::kQuant;
     constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden, SPLIT = RESULTS == Results::kOut;
+    constexpr bool BIAS = MX && !DIRECT, COLS = !MX && !DIRECT;  // how columns' operands come
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
         after_previous();
@@ -484,7 +522,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     const int w_rows = A.tile_n / CG, codes_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
     const int stage_bytes = codes_bytes + (MX ? mx_scale_bytes(A.tile_n) : 0);
     uint8_t* const turns = base + stages * stage_bytes;
-    Tail& T = *reinterpret_cast<Tail*>(turns + EPI * kTurn);
+    Tail& T = *reinterpret_cast<Tail*>(turns + EPI * kTurnBytes);
     const uint32_t ring = smem_addr(base);
     const uint32_t full = smem_addr(T.full), empty = smem_addr(T.empty);
     const uint32_t acc_full = smem_addr(T.acc_full), acc_empty = smem_addr(T.acc_empty);
@@ -529,8 +567,11 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
     auto slabs_to = [&](int part) { return SPLIT ? min((part + 1) * A.part_blocks, A.k_blocks) : A.k_blocks; };
     if (warp < EPI) {  // ---- epilogue
         const LinearEpilogue E = from_here(A.e);
-        float* const turn = reinterpret_cast<float*>(turns + warp * kTurn);
+        float* const turn = reinterpret_cast<float*>(turns + warp * kTurnBytes);
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
+        const int begin = QUANT ? 2 * half : half;      // its first one
+        auto behind = [](int c) { return !QUANT ? c + EPI / 4 : c % 2 == 0 ? c + 1 : c + EPI / 2 - 1; };
+        const bool whole = QUANT && ((uintptr_t)E.out | (uintptr_t)E.out_stride / 2) % 32 == 0;
         int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken
         auto first_row = [&](const Tile& tile) { return (tile.m * CG + (int)rank) * kRows + quarter * 32; };
         // The operands of a tile that do not depend on its sums are loaded a tile ahead: the scale of this lane's row, and
@@ -586,23 +627,30 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 __syncwarp();
             }
         };
-        look_tile(first);
+        // (4 bits) The bias of a chunk's columns, one by each lane, is loaded a chunk ahead, and shared by the warp through T.cols.
+        float next_bias = 0.0f;
+        int n_shared = 0;
+        auto look_bias = [&](int col) { next_bias = E.bias && col < E.N ? __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16)) : 0.0f; };
+        Tile tile = tile_at<SPLIT>(A, first), next = tile;
+        if (!BIAS) look_tile(first);
+        if (BIAS) look_bias(tile.n * A.tile_n + begin * 32 + lane);
         to_l2(first);
         if (HIDDEN) fetch(A.ring - 2);
         for (int t = first; t < total; t += step, ++n_done) {
-            const Tile tile = tile_at<SPLIT>(A, t);
+            if (BIAS) tile = next, next = t + step < total ? tile_at<SPLIT>(A, t + step) : tile;
+            else tile = tile_at<SPLIT>(A, t);
             const int row0 = first_row(tile), col0 = tile.n * A.tile_n;
             const Two xs2 = two(xs, xs);
             const int chunks = row0 < E.M ? (min(A.tile_n, E.N - col0) + 31) / 32 : 0;
             const float* const cols = T.cols[n_done & 1];
-            if (!DIRECT) {
+            if (COLS) {
                 T.cols[n_done & 1][threadIdx.x] = scale, T.cols[n_done & 1][kAccStride + threadIdx.x] = bias;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(T.cols_full) + 8 * (n_done & 1));
             }
-            look_tile(t + step);
+            if (!BIAS) look_tile(t + step);
             to_l2(t + step);
-            if (!DIRECT && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT)))
+            if (COLS && !all(wait(smem_addr(T.cols_full) + 8 * (n_done & 1), (n_done >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT)))
                 break;
             Column column;
             uint32_t rows_raw[8];
@@ -634,7 +682,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 ok = all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT));
                 if (!ok) break;
                 fence_after();
-                for (int c = half; c < chunks; c += EPI / 4) {
+                for (int c = begin; c < chunks; c = behind(c)) {
                     float v[32];
                     tmem_load(lanes + (pass & 1) * stride + c * 32, v);
                     if (i > 0) tmem_add(total_at + c * 32, v);
@@ -645,8 +693,13 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
             if (!ok || !all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT))) break;
             fence_after();
             const uint32_t acc_at = lanes + (pass & 1) * stride;
-            if (half >= chunks) release();
-            for (int c = half; c < chunks; c += EPI / 4) {
+            const int next_col = next.n * A.tile_n + begin * 32 + lane;
+            if (begin >= chunks) {
+                if (BIAS) look_bias(next_col);
+                release();
+            }
+            uint32_t codes[8], scales = 0;  // of a pair of blocks
+            for (int c = begin; c < chunks; c = behind(c)) {
                 Two gate[16];
                 if (HIDDEN) {
                     gate_pairs(E, gate_raw, gate);
@@ -655,15 +708,27 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
                 float v[32];
                 tmem_load(acc_at + c * 32, v);
                 if (PASSES && passes > 1) tmem_add(total_at + c * 32, v);
-                if (c + EPI / 4 >= chunks) release();
+                if (behind(c) >= chunks) release();
                 if constexpr (!DIRECT) {
                     Two x[16];
-                    if (E.act == CB_ACT_NONE) values<CB_ACT_NONE>(E, cols + c * 32, xs2, v, x);
+                    if constexpr (BIAS) {
+                        float* const shared = &T.cols[n_shared++ & 1][warp * 32];
+                        shared[lane] = next_bias;
+                        __syncwarp();
+                        look_bias(behind(c) < chunks ? col0 + behind(c) * 32 + lane : next_col);
+                        if (E.act == CB_ACT_NONE) values_mx<CB_ACT_NONE>(shared, v, x);
+                        else if (E.act == CB_ACT_GELU) values_mx<CB_ACT_GELU>(shared, v, x);
+                        else values_mx<CB_ACT_SILU>(shared, v, x);
+                    } else if (E.act == CB_ACT_NONE) values<CB_ACT_NONE>(E, cols + c * 32, xs2, v, x);
                     else if (E.act == CB_ACT_GELU) values<CB_ACT_GELU>(E, cols + c * 32, xs2, v, x);
                     else values<CB_ACT_SILU>(E, cols + c * 32, xs2, v, x);
                     const int col = col0 + c * 32;
                     if constexpr (QUANT) {
-                        put_quantised(E, A.out_scales, A.out_tiles, row0 + lane, col, x);
+                        // two neighbouring blocks leave together
+                        if (c % 2 == 0) scales = quantised(E, col, x, codes);
+                        else scales |= quantised(E, col, x, codes + 4) << 8;
+                        if (c % 2 == 1 || c + 1 == chunks)
+                            put_blocks(E, A.out_scales, A.out_tiles, whole, row0 + lane, col - c % 2 * 32, c % 2 + 1, codes, scales);
                     } else if constexpr (!HIDDEN) {
                         for (int h = 0; h < out_boxes; ++h) {
                             // the box before the last has left
@@ -755,7 +820,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS), 1) linear_kernel(cons
             bool ok = true;
             // (the slabs' loop is kept short: with passes opened and closed inside it, a slab took 260 clocks longer)
             for (int t = first; t < total && ok; t += step) {
-                const int part = SPLIT ? t % A.parts : 0, to = slabs_to(part);
+                const int part = SPLIT && A.parts > 1 ? t % A.parts : 0, to = slabs_to(part);
                 // (4 bits) the word of w's tile of scales that the results' tile begins with
                 const uint32_t w_word = MX ? tile_at<SPLIT>(A, t).n * A.tile_n % kMxTileRows / 32 : 0;
                 for (int kb0 = slabs_from(part); kb0 < to && ok; ++pass) {

@@ -37,6 +37,13 @@ __device__ __forceinline__ float mx_inverse(uint32_t e) { return __uint_as_float
 // 2^(e - 127): a subnormal for e = 0, NaN for e = 255.
 __device__ __forceinline__ float mx_power(uint32_t e) { return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7FC00000u : e << 23); }
 
+// The largest magnitude of three; a NaN wins.
+__device__ __forceinline__ float mx_max_abs(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // Codes of eight scaled values, the first in the lowest bits, to nearest even and 6 at most.
 __device__ __forceinline__ uint32_t mx_codes8(const float* v) {
     uint32_t r;
