@@ -131,6 +131,9 @@ int scales_map(CUtensorMap* map, const void* p, long long rows, long long featur
 // what takes the time then, [0] where they are long and stages are worth more. GB300, {1, 4} -> {4, 7}: 16384 x 8192 x 512 e4m3
 // with a bf16 output and hidden state 178 -> 150 us, fp32 hidden state alone 212 -> 192; 8192 x 1152 x 4608 64.1 -> 66.2 ({2, 5}).
 constexpr int kShortBlocks = 16, kMoreBoxes[2][2] = {{1, 4}, {4, 7}};
+// Operands in 4 bits, 8 warps for long sums and 12 for short ones. GB300, 8192 x 1152 x 4608 and 4608 x 4096 x 15360, bf16 gated with and without an
+// output: 8 warps 25.9 and 98.8 us, 12 (and so two stages fewer) 28.2 and 118; 8192 x 1152 x 1152 with an output 22.5 and 18.1.
+constexpr int kMxMoreBoxes[2][2] = {{1, 4}, {2, 4}};
 
 // Bytes of a row up to which a box's place in it (and a gate's piece's), and that of the box behind, is a positive int.
 constexpr long long kMaxRowBytes = (1LL << 31) - 1024;
@@ -139,6 +142,7 @@ constexpr long long kMaxRowBytes = (1LL << 31) - 1024;
 int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
     const LinearEpilogue& e = a->e;
     a->results = Results::kDirect;
+    const bool mx = a->operands == Operands::kMx;
     const struct {
         const void* p;
         long long row, es;
@@ -159,7 +163,9 @@ int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
     a->results = e.resid_out ? Results::kHidden : Results::kOut;
     if (e.resid_out) {
         const int out = !e.out ? 0 : e.out_bf16 ? 1 : 2, resid = e.resid_bf16 ? 1 : 2;
-        a->more_boxes = std::max(kMoreBoxes[a->k_blocks <= kShortBlocks][resid - 1], out + 2 * resid - 2);
+        const bool is_short = a->k_blocks <= kShortBlocks;
+        if (mx && !is_short) a->results = Results::kHiddenLong;
+        a->more_boxes = std::max((mx ? kMxMoreBoxes : kMoreBoxes)[is_short][resid - 1], out + 2 * resid - 2);
         a->ring = (2 + a->more_boxes - out) / resid;
     }
     return CB_OK;
@@ -328,6 +334,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.tiles_m = (ep.M + 128 * cg - 1) / (128 * cg), a.tiles_n = (ep.N + a.tile_n - 1) / a.tile_n;
     if ((long long)a.tiles_m * a.tiles_n > 0x7FFFFFFFLL / 8) return CB_ERR_LIMIT;
     a.group_magic = ~0ull / (8ull * (unsigned)a.tiles_n) + 1;
+    a.tokens_magic = ~0ull / ep.tokens + 1;
 
     // memory for copies of operands and for the sums of parts, in stream order
     const cudaStream_t s = (cudaStream_t)stream;
@@ -369,8 +376,11 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     if (rc == CB_OK)
         rc = pw.dst ? operand_map(&a.w_map, pw.dst, ep.N, 32ll * pw.chunks, 32ll * pw.chunks, a.tile_n / cg)
                     : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);
-    const size_t fixed = linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes) : 0);
+    // one box instead of two for each of the 12 warps makes room for a stage more (8192^3 to bf16 159 -> 152 us)
+    a.out_boxes = mx && a.results == Results::kOut && a.k_blocks > kShortBlocks ? 1 : 2;
+    const size_t fixed = linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes, a.out_boxes) : 0);
     const size_t stage = linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0);
+    if (fixed + 2 * stage > (size_t)dev->smem) rc = CB_ERR_LIMIT;  // (no device that the library is built for)
     a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - fixed) / stage);
     const long long tiles = (long long)a.tiles_m * a.tiles_n * a.parts, units = cg == 2 ? dev->pairs : dev->sms;
     if (rc == CB_OK && e == cudaSuccess) e = launch_linear(a, cg, d.type == CB_E4M3, cg * (int)std::min(tiles, units), s);

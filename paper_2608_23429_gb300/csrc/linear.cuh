@@ -24,8 +24,8 @@ struct LinearEpilogue {
 };
 
 // How results leave: an output alone by TMA, a hidden state with or without an output by TMA, either by the threads, or an output in
-// 4 bits by the threads.
-enum class Results { kOut, kHidden, kDirect, kQuant };
+// 4 bits by the threads; kHiddenLong: kHidden for long sums of operands in 4 bits, whose warps are fewer for the sake of stages.
+enum class Results { kOut, kHidden, kDirect, kQuant, kHiddenLong };
 
 // Types of the operands.
 enum class Operands { kBf16, kE4m3, kMx };
@@ -41,7 +41,7 @@ constexpr int kMxMostN = 192, kMxStepN = 64;  // columns of a tile: TMEM holds t
 // and wait for that (GB300, 8192 x 8191 x 512 bf16 with a gated fp32 hidden state: eight warps, 32 rows at once each, 282 us,
 // sixteen, eight rows at once, 195).
 __host__ __device__ constexpr int epi_warps(Results r, bool mx = false) {
-    if (mx) return r == Results::kDirect ? 16 : r == Results::kHidden ? 8 : 12;
+    if (mx) return r == Results::kDirect ? 16 : r == Results::kHiddenLong ? 8 : 12;
     return r == Results::kDirect ? 16 : 8;
 }
 constexpr int kTurnBytes = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
@@ -54,11 +54,13 @@ struct LinearArgs {
     unsigned out_tiles;                    // kQuant: tiles of scales of a row of the output
     CUtensorMap x_map, w_map;
     CUtensorMap out_map, resid_map, resid_out_map;
+    int out_boxes;         // operands in 4 bits: boxes of an output alone, of a warp
     int ring, more_boxes;  // hidden states of chunks that a warp holds; boxes of shared memory that it needs for them besides two
     LinearEpilogue e;
     int overlap;
     int k_bytes;           // bytes of a row of x and of w
     int tiles_m, tiles_n, k_blocks, stages;
+    unsigned long long tokens_magic; // the same of tokens; 0 for 1
     unsigned long long group_magic;  // ceil(2^64 / (8 tiles_n)): t group_magic / 2^64 is t / (8 tiles_n) for every 32-bit t
     int tile_n;            // output columns of a tile
     int passes, pass_blocks;  // stretches of K that are summed by themselves, and their slabs
@@ -109,9 +111,13 @@ cudaError_t launch_linear_join(const LinearJoinArgs& a, cudaStream_t s);
 size_t linear_stage_bytes(int cg, int tile_n);
 size_t linear_fixed_bytes(Results r, int more_boxes);  // shared memory besides the stages
 constexpr int kBox = 2048, kMaxRing = 6;
-// ...and more of it, of the kernels for operands in 4 bits
-constexpr size_t mx_more_bytes(Results r, int more_boxes) { return (size_t)(epi_warps(r, true) - epi_warps(r)) * (kTurnBytes + more_boxes * kBox); }
 constexpr int kMaxLinStages = 12;
+// ...and more of it, of the kernels for operands in 4 bits
+constexpr int kMxLines = 128;  // floats of a warp: twice, biases and gates of 32 columns
+constexpr size_t mx_more_bytes(Results r, int more_boxes, int out_boxes) {
+    return (size_t)epi_warps(r, true) * (out_boxes * kBox + more_boxes * kBox + kMxLines * 4) -
+           (size_t)epi_warps(r) * (kTurnBytes + more_boxes * kBox);
+}
 cudaError_t prepare_linear(size_t smem, int* pairs);
 using LinearKernel = void (*)(LinearArgs);
 LinearKernel linear_out_kernel(int cg, bool fp8, bool passes);     // linear_tc_out.cu

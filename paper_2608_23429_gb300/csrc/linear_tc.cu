@@ -14,7 +14,7 @@ cudaError_t prepare_linear(size_t smem, int* pairs) {
             if (e != cudaSuccess) return e;
         }
     for (int i = 0; i < 4; ++i)
-        for (Results r : {Results::kOut, Results::kHidden, Results::kDirect, Results::kQuant}) {
+        for (Results r : {Results::kOut, Results::kHidden, Results::kDirect, Results::kQuant, Results::kHiddenLong}) {
             const cudaError_t e = cudaFuncSetAttribute(linear_mx_kernel(r, 1 + i % 2, i & 2), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e != cudaSuccess) return e;
         }
@@ -42,7 +42,7 @@ cudaError_t launch_linear(const LinearArgs& a, int cg, bool fp8, int grid, cudaS
     c.blockDim = dim3(linear_threads(a.results, a.operands == Operands::kMx));
     const bool mx = a.operands == Operands::kMx;
     const size_t stage = linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0);
-    c.dynamicSmemBytes = (size_t)a.stages * stage + linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes) : 0);
+    c.dynamicSmemBytes = (size_t)a.stages * stage + linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes, a.out_boxes) : 0);
     c.stream = s;
     c.attrs = at;
     c.numAttrs = cg == 2 ? 2 : 1;

@@ -437,6 +437,43 @@ __device__ __forceinline__ void put_blocks(const LinearEpilogue& E, uint8_t* sca
         for (int b = first + blocks; b < kMxTileBlocks; ++b) to[b] = 0;
 }
 
+// (4 bits) The same with gates in shared memory, where all lanes read alike (`line`), or, where the warp's rows are of more than one
+// sample, each lane's in its own sample's row (`row`, with `columns` from there on): a register for a column's instead of 64.
+template <bool BF16>
+__device__ __forceinline__ void add_box_shared(const LinearEpilogue& E, uint32_t box, int lane, const float* line, const char* row, int columns,
+                                               const Two* x) {
+    constexpr int PAIRS = BF16 ? 4 : 2;  // of values, of a piece
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t at = piece_at(box, lane, j);
+        Two g[PAIRS];
+        if (!row) {
+#pragma unroll
+            for (int i = 0; i < PAIRS; i += 2) {
+                const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(line + 2 * (PAIRS * j + i));
+                g[i] = q.x, g[i + 1] = q.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                const int c = 2 * (PAIRS * j + i);
+                const float f0 = c < columns ? __uint_as_float(lin_ld1(row, c, E.gate_bf16)) : 0.0f;
+                const float f1 = c + 1 < columns ? __uint_as_float(lin_ld1(row, c + 1, E.gate_bf16)) : 0.0f;
+                g[i] = two(f0, f1);
+            }
+        }
+        const uint4 r = ld_shared16(at);
+        if constexpr (BF16) {
+            const Two h[4] = {fma2(g[0], x[4 * j], widened(r.x)), fma2(g[1], x[4 * j + 1], widened(r.y)),
+                              fma2(g[2], x[4 * j + 2], widened(r.z)), fma2(g[3], x[4 * j + 3], widened(r.w))};
+            st_shared16(at, packed8(h));
+        } else {
+            st_shared16(at, as_uint4(fma2(g[0], x[2 * j], two(__uint_as_float(r.x), __uint_as_float(r.y))),
+                                     fma2(g[1], x[2 * j + 1], two(__uint_as_float(r.z), __uint_as_float(r.w)))));
+        }
+    }
+}
+
 // Results by the threads, for rows off the 16-byte grid: a column per lane, eight rows at a time, whose hidden states are loaded
 // while the eight before are worked on.
 
@@ -509,7 +546,7 @@ template <int CG, Operands OPERANDS, bool PASSES, Results RESULTS>
 __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::kMx), 1) linear_kernel(const __grid_constant__ LinearArgs A) {
     constexpr int EPI = epi_warps(RESULTS, OPERANDS == Operands::kMx);
     constexpr bool FP8 = OPERANDS == Operands::kE4m3, MX = OPERANDS == Operands::kMx, QUANT = RESULTS == Results::kQuant;
-    constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden, SPLIT = RESULTS == Results::kOut;
+    constexpr bool DIRECT = RESULTS == Results::kDirect, HIDDEN = RESULTS == Results::kHidden || RESULTS == Results::kHiddenLong, SPLIT = RESULTS == Results::kOut;
     constexpr bool BIAS = MX && !DIRECT, COLS = !MX && !DIRECT;  // how columns' operands come
     extern __shared__ __align__(1024) uint8_t base[];
     if (smem_addr(base) & 1023) {  // the swizzle goes by addresses
@@ -522,7 +559,8 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
     const int w_rows = A.tile_n / CG, codes_bytes = (kRows + w_rows) * kSlab, stages = A.stages;
     const int stage_bytes = codes_bytes + (MX ? mx_scale_bytes(A.tile_n) : 0);
     uint8_t* const turns = base + stages * stage_bytes;
-    Tail& T = *reinterpret_cast<Tail*>(turns + EPI * kTurnBytes);
+    const int turn_bytes = MX ? A.out_boxes * kBox : kTurnBytes;
+    Tail& T = *reinterpret_cast<Tail*>(turns + EPI * turn_bytes);
     const uint32_t ring = smem_addr(base);
     const uint32_t full = smem_addr(T.full), empty = smem_addr(T.empty);
     const uint32_t acc_full = smem_addr(T.acc_full), acc_empty = smem_addr(T.acc_empty);
@@ -567,9 +605,9 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
     auto slabs_to = [&](int part) { return SPLIT ? min((part + 1) * A.part_blocks, A.k_blocks) : A.k_blocks; };
     if (warp < EPI) {  // ---- epilogue
         const LinearEpilogue E = from_here(A.e);
-        float* const turn = reinterpret_cast<float*>(turns + warp * kTurnBytes);
+        float* const turn = reinterpret_cast<float*>(turns + warp * turn_bytes);
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
-        const int begin = QUANT ? 2 * half : half;      // its first one
+        const int begin = QUANT ? 2 * half : half;      // its first one; outputs in 4 bits go by pairs of neighbours
         auto behind = [](int c) { return !QUANT ? c + EPI / 4 : c % 2 == 0 ? c + 1 : c + EPI / 2 - 1; };
         const bool whole = QUANT && ((uintptr_t)E.out | (uintptr_t)E.out_stride / 2) % 32 == 0;
         int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken
@@ -588,7 +626,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
         };
         // The hidden state's rows of a tile are on their way to L2 a tile ahead.
         auto to_l2 = [&](int t) {
-            if (RESULTS == Results::kOut || QUANT || !E.resid_out || t >= total) return;
+            if (RESULTS == Results::kOut || BIAS || !E.resid_out || t >= total) return;  // (BIAS: the ring has more of it)
             const Tile tile = tile_at<SPLIT>(A, t);
             const int row = first_row(tile) + lane, col0 = tile.n * A.tile_n, es = E.resid_bf16 ? 2 : 4;
             if (row >= E.M) return;
@@ -628,17 +666,29 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
             }
         };
         // (4 bits) The bias of a chunk's columns, one by each lane, is loaded a chunk ahead, and shared by the warp through T.cols.
-        float next_bias = 0.0f;
+        float next_bias = 0.0f, next_gate = 1.0f;
         int n_shared = 0;
-        auto look_bias = [&](int col) { next_bias = E.bias && col < E.N ? __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16)) : 0.0f; };
+        float* const lines = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(&T) + kTailBytes + EPI * A.more_boxes * kBox) + warp * kMxLines;
+        auto sample_at = [&](int row) {
+            const unsigned r = (unsigned)min(row, E.M - 1);
+            return A.tokens_magic ? (unsigned)__umul64hi(r, A.tokens_magic) : r;
+        };
+        auto sample_of = [&](const Tile& tile) { return E.gate ? sample_at(first_row(tile)) : 0u; };
+        auto look_bias = [&](int col, unsigned sample) {
+            next_bias = E.bias && col < E.N ? __uint_as_float(lin_ld1(E.bias, col, E.bias_bf16)) : 0.0f;
+            if (HIDDEN && E.gate && col < E.N) next_gate = __uint_as_float(lin_ld1(E.gate, sample * E.gate_stride + col, E.gate_bf16));
+        };
         Tile tile = tile_at<SPLIT>(A, first), next = tile;
         if (!BIAS) look_tile(first);
-        if (BIAS) look_bias(tile.n * A.tile_n + begin * 32 + lane);
+        unsigned sample = BIAS && HIDDEN ? sample_of(tile) : 0, next_sample = sample;
+        if (BIAS) look_bias(tile.n * A.tile_n + begin * 32 + lane, sample);
         to_l2(first);
         if (HIDDEN) fetch(A.ring - 2);
         for (int t = first; t < total; t += step, ++n_done) {
-            if (BIAS) tile = next, next = t + step < total ? tile_at<SPLIT>(A, t + step) : tile;
-            else tile = tile_at<SPLIT>(A, t);
+            if (BIAS) {
+                tile = next, next = t + step < total ? tile_at<SPLIT>(A, t + step) : tile;
+                if (HIDDEN) sample = next_sample, next_sample = sample_of(next);
+            } else tile = tile_at<SPLIT>(A, t);
             const int row0 = first_row(tile), col0 = tile.n * A.tile_n;
             const Two xs2 = two(xs, xs);
             const int chunks = row0 < E.M ? (min(A.tile_n, E.N - col0) + 31) / 32 : 0;
@@ -658,12 +708,14 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                 column = look_column(E, row0, col0 + half * 32 + lane);
                 look_rows(E, row0, col0 + half * 32 + lane, rows_raw);
             }
+            // (4 bits) the warp's rows are of more than one sample
+            const bool mixed = BIAS && HIDDEN && E.gate && sample_at(row0 + 31) != sample;
             const char* gate_row = nullptr;  // of this lane's row's sample
             uint4 gate_raw[8];
-            if (HIDDEN && half < chunks) {
+            if (HIDDEN && half < chunks && (!BIAS || mixed)) {
                 gate_row = reinterpret_cast<const char*>(E.gate) +
                            (unsigned)min(row0 + lane, E.M - 1) / E.tokens * E.gate_stride * (E.gate_bf16 ? 2 : 4);
-                look_gate(E, gate_row, col0 + half * 32, gate_raw);
+                if (!BIAS) look_gate(E, gate_row, col0 + half * 32, gate_raw);
             }
             const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), total_at = lanes + 256;
             constexpr int stride = PASSES ? kAccStride / 2 : kAccStride;
@@ -695,13 +747,13 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
             const uint32_t acc_at = lanes + (pass & 1) * stride;
             const int next_col = next.n * A.tile_n + begin * 32 + lane;
             if (begin >= chunks) {
-                if (BIAS) look_bias(next_col);
+                if (BIAS) look_bias(next_col, next_sample);
                 release();
             }
             uint32_t codes[8], scales = 0;  // of a pair of blocks
             for (int c = begin; c < chunks; c = behind(c)) {
                 Two gate[16];
-                if (HIDDEN) {
+                if (HIDDEN && !BIAS) {
                     gate_pairs(E, gate_raw, gate);
                     if (c + EPI / 4 < chunks) look_gate(E, gate_row, col0 + (c + EPI / 4) * 32, gate_raw);
                 }
@@ -711,14 +763,17 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                 if (behind(c) >= chunks) release();
                 if constexpr (!DIRECT) {
                     Two x[16];
+                    float* line = nullptr;
                     if constexpr (BIAS) {
-                        float* const shared = &T.cols[n_shared++ & 1][warp * 32];
-                        shared[lane] = next_bias;
+                        line = lines + (n_shared++ & 1) * (kMxLines / 2);
+                        line[lane] = next_bias;
+                        if (HIDDEN) line[32 + lane] = next_gate;
                         __syncwarp();
-                        look_bias(behind(c) < chunks ? col0 + behind(c) * 32 + lane : next_col);
-                        if (E.act == CB_ACT_NONE) values_mx<CB_ACT_NONE>(shared, v, x);
-                        else if (E.act == CB_ACT_GELU) values_mx<CB_ACT_GELU>(shared, v, x);
-                        else values_mx<CB_ACT_SILU>(shared, v, x);
+                        if (behind(c) < chunks) look_bias(col0 + behind(c) * 32 + lane, sample);
+                        else look_bias(next_col, next_sample);
+                        if (E.act == CB_ACT_NONE) values_mx<CB_ACT_NONE>(line, v, x);
+                        else if (E.act == CB_ACT_GELU) values_mx<CB_ACT_GELU>(line, v, x);
+                        else values_mx<CB_ACT_SILU>(line, v, x);
                     } else if (E.act == CB_ACT_NONE) values<CB_ACT_NONE>(E, cols + c * 32, xs2, v, x);
                     else if (E.act == CB_ACT_GELU) values<CB_ACT_GELU>(E, cols + c * 32, xs2, v, x);
                     else values<CB_ACT_SILU>(E, cols + c * 32, xs2, v, x);
@@ -731,10 +786,11 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                             put_blocks(E, A.out_scales, A.out_tiles, whole, row0 + lane, col - c % 2 * 32, c % 2 + 1, codes, scales);
                     } else if constexpr (!HIDDEN) {
                         for (int h = 0; h < out_boxes; ++h) {
-                            // the box before the last has left
-                            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                            // the box before the last has left, or the last one where there is one
+                            if (MX && A.out_boxes == 1) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                            else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                             __syncwarp();
-                            const uint32_t box = box_at(n_boxes++ & 1);
+                            const uint32_t box = box_at(MX && A.out_boxes == 1 ? 0 : n_boxes++ & 1);
                             if (E.out_bf16) put_box<true>(box, lane, x);
                             else if (h == 0) put_box<false>(box, lane, x);
                             else put_box<false>(box, lane, x + 8);
@@ -747,7 +803,15 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                         ok = all(wait(smem_addr(T.resid_full[warp]) + 8 * held.s, held.phase, limit, CB_DEV_CONSUMER_TIMEOUT));
                         if (!ok) break;
                         const uint32_t box = ring_box(held.s), box2 = ring_box(held.s, 1);
-                        if (E.resid_bf16) add_box<true>(box, lane, gate, x);
+                        if constexpr (BIAS) {
+                            const char* const row = gate_row ? gate_row + (long long)col * (E.gate_bf16 ? 2 : 4) : nullptr;
+                            if (E.resid_bf16) {
+                                add_box_shared<true>(E, box, lane, line + 32, row, E.N - col, x);
+                            } else {
+                                add_box_shared<false>(E, box, lane, line + 32, row, E.N - col, x);
+                                add_box_shared<false>(E, box2, lane, line + 48, row ? row + 16 * (E.gate_bf16 ? 2 : 4) : nullptr, E.N - col - 16, x + 8);
+                            }
+                        } else if (E.resid_bf16) add_box<true>(box, lane, gate, x);
                         else add_box<false>(box, lane, gate, x), add_box<false>(box2, lane, gate + 8, x + 8);
                         // the chunk before has left its boxes
                         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");

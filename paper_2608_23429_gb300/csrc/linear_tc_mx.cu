@@ -16,6 +16,7 @@ LinearKernel of(int cg, bool passes) {
 LinearKernel linear_mx_kernel(Results r, int cg, bool passes) {
     return r == Results::kOut      ? of<Results::kOut>(cg, passes)
            : r == Results::kHidden ? of<Results::kHidden>(cg, passes)
+           : r == Results::kHiddenLong ? of<Results::kHiddenLong>(cg, passes)
            : r == Results::kDirect ? of<Results::kDirect>(cg, passes)
                                    : of<Results::kQuant>(cg, passes);
 }
