@@ -178,8 +178,9 @@ constexpr int kFewRows = 32;
 
 // Slabs of 128 bytes of a pass over K, with fp32 results: an error of 5e-7 of a sum, 7e-7 where all terms have one sign (measured:
 // linear_tc.cuh; e4m3's products lose less, 1.4e-7 in 2048 features of one sign and 1.8e-6 in 8192; 4096 x 4608 x 8192 takes 104 us in two passes of
-// narrower tiles and 89 in one).
-constexpr int kPassBf16 = 8, kPassE4m3 = 32, kPassMx = 16;
+// narrower tiles and 89 in one; 4 bits under scales that differ, 16384 features 1.9e-7 and 6.2e-7, 65536 3.2e-6 and 6.4e-6; 8192^3 in
+// passes of 4096 features 210 us, in one 170).
+constexpr int kPassBf16 = 8, kPassE4m3 = 32, kPassMx = 64;
 // Results in bf16 alone: one pass up to kOnePass slabs, as tiles of 256 columns are worth more (4608 x 3072 x 15360 227 -> 274 us, 8192 x
 // 8192 x 8192 554 -> 648, 8192 x 1152 x 4608 60.2 -> 62.0 with passes of 16) and what the sums lose is small against the rounding that
 // follows, 2e-3 to 4e-3: 7.2e-5 of their size at most (16384 features of bf16, all terms of one sign; 1.9e-5 with signs mixed). Longer sums

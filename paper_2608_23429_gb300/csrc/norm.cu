@@ -15,43 +15,6 @@
 namespace cbk {
 namespace {
 
-// Elements t, t + T, ... of a row from or to p (threads behind its end read its start and write nothing). The type is
-// asked for once, so that all loads are in flight together.
-template <int CH, int T>
-__device__ __forceinline__ void load_all(const void* p, long long e, int bf16, int t, int hidden, float* v) {
-    if (bf16) {
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + e;
-        uint16_t w[CH];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) w[c] = q[c * T + t < hidden ? c * T + t : 0];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = __uint_as_float((uint32_t)w[c] << 16);
-    } else {
-        const float* q = reinterpret_cast<const float*>(p) + e;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = q[c * T + t < hidden ? c * T + t : 0];
-    }
-}
-template <int CH, int T>
-__device__ __forceinline__ void store_all(void* p, long long e, int dtype, int t, int hidden, const float* v) {
-    if (dtype == CB_BF16) {
-        __nv_bfloat16* q = reinterpret_cast<__nv_bfloat16*>(p) + e + t;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-            if (c * T + t < hidden) q[c * T] = __float2bfloat16_rn(v[c]);
-    } else if (dtype == CB_FP32) {
-        float* q = reinterpret_cast<float*>(p) + e + t;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-            if (c * T + t < hidden) q[c * T] = v[c];
-    } else {
-        uint8_t* q = reinterpret_cast<uint8_t*>(p) + e + t;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-            if (c * T + t < hidden) q[c * T] = (uint8_t)norm_e4m3x2(v[c], 0.0f);
-    }
-}
-
 // Weight, scale and shift are loaded while the sum is, not before: half the registers, twice the CTAs (GB300: 8192 x 4097
 // bf16 to e4m3 211 -> 156 us, 16384 x 1153 78 -> 68). Short rows have room all the same.
 __host__ __device__ constexpr bool lines_late(int CH, int W) { return CH * W > 32 && CH <= 10; }

@@ -13,7 +13,120 @@ namespace {
 
 constexpr int kAroundHeld = 49152;  // elements of a row in shared memory
 
-// A row by elements; HELD: in shared memory, else read again for each reduction.
+// A row by elements, in registers: CH of them in each thread of its W warps. The lines are loaded with the row where there is room for
+// them, each when it is wanted where there is not.
+__host__ __device__ constexpr bool around_early(int CH, int W) { return CH * W <= 40; }
+
+template <int CH, int W>
+__global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 * W)) around_held_kernel(const __grid_constant__ AroundArgs args) {
+    __shared__ uint32_t slots[5][W];
+    constexpr int T = 32 * W;
+    constexpr bool EARLY = around_early(CH, W);
+    const AroundArgs A = args;  // in registers, as stores would have them read again
+    after_previous();
+    const unsigned row = blockIdx.x;
+    const int t = threadIdx.x;
+    auto on = [&](int c) { return c * T + t < A.hidden; };
+    const long long line = (long long)(row / A.tokens) * A.line_stride;
+    float early[7][CH];
+    auto look = [&](int i, const void* p, long long at) {
+        if (EARLY && p) load_all<CH, T>(p, at, A.param_bf16, t, A.hidden, early[i]);
+    };
+    // v = f(v, line), of line i at p
+    auto with_line = [&](int i, const void* p, long long at, float (&v)[CH], auto f) {
+        if (!p) return;
+        float late[CH];
+        if (!EARLY) load_all<CH, T>(p, at, A.param_bf16, t, A.hidden, late);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = f(v[c], EARLY ? early[i][c] : late[c]);
+    };
+    auto normalise = [&](float (&v)[CH], int kind, float eps, uint32_t (*s)[W]) {
+        if (kind == CB_NORM_LAYER) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (on(c)) sum += v[c];
+            const float mean = __uint_as_float(row_reduce<W, false>(__float_as_uint(sum), s[0])) * A.inv_hidden;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) v[c] -= mean;
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (on(c)) sum = fmaf(v[c], v[c], sum);
+        sum = __uint_as_float(row_reduce<W, false>(__float_as_uint(sum), s[1]));
+        const float rstd = 1.0f / sqrtf(fmaf(sum, A.inv_hidden, eps));
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] *= rstd;
+    };
+    const auto times = [](float v, float w) { return v * w; };
+    const auto plus = [](float v, float w) { return v + w; };
+    float h[CH], r[CH];
+    load_all<CH, T>(A.x, row * A.x_stride, A.x_bf16, t, A.hidden, h);
+    if (A.branch) load_all<CH, T>(A.branch, row * A.branch_stride, A.branch_bf16, t, A.hidden, r);
+    look(0, A.after_weight, 0);
+    look(1, A.after_bias, 0);
+    look(2, A.gate, line);
+    look(3, A.weight, 0);
+    look(4, A.bias, 0);
+    look(5, A.scale, line);
+    look(6, A.shift, line);
+    if (A.x_factor != 1.0f) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) h[c] *= A.x_factor;
+    }
+    if (A.branch) {
+        if (A.after != CB_NORM_NONE) {
+            normalise(r, A.after, A.after_eps, slots);
+            with_line(0, A.after_weight, 0, r, times);
+            with_line(1, A.after_bias, 0, r, plus);
+        }
+        with_line(2, A.gate, line, r, times);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) h[c] = fmaf(r[c], A.branch_factor, h[c]);
+    }
+    if (A.x_out) store_all<CH, T>(A.x_out, row * A.x_out_stride, A.x_bf16 ? CB_BF16 : CB_FP32, t, A.hidden, h);
+    if (!A.out) return;
+    if (A.before != CB_NORM_NONE) {
+        normalise(h, A.before, A.before_eps, slots + 2);
+        with_line(3, A.weight, 0, h, times);
+        with_line(4, A.bias, 0, h, plus);
+    }
+    with_line(5, A.scale, line, h, [](float v, float w) { return fmaf(v, w, v); });
+    with_line(6, A.shift, line, h, plus);
+    if (A.out_dtype == CB_MXFP4) {
+        // a block is a warp; those that fill up the last tile of scales are zeros
+        uint8_t* const out = reinterpret_cast<uint8_t*>(A.out) + row * A.out_stride;
+        const unsigned ends = A.out_tiles * kMxTileBlocks * kMxBlock, codes_end = ((unsigned)A.hidden + kMxBlock - 1) / kMxBlock * kMxBlock;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const unsigned e = c * T + t;
+            const float y = on(c) ? h[c] : 0.0f;
+            const uint32_t scale = mx_scale_of(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
+            const float q = y * mx_inverse(scale);
+            const float v[8] = {q, __shfl_down_sync(0xFFFFFFFFu, q, 1)};
+            if (t % 2 == 0 && e < codes_end) out[e / 2] = scale == 255 ? 0 : (uint8_t)mx_codes8(v);
+            const unsigned block = e / kMxBlock;
+            if (t % 32 == 0 && e < ends)
+                reinterpret_cast<uint8_t*>(A.out_scale)[mx_word_at(row, block / kMxTileBlocks, A.out_tiles) + block % kMxTileBlocks] = (uint8_t)scale;
+        }
+        return;
+    }
+    if (A.out_dtype == CB_E4M3) {
+        float amax = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (on(c)) amax = max_abs(amax, h[c]);
+        const float s = norm_scale_of(row_reduce<W, true>(__float_as_uint(amax) & 0x7FFFFFFFu, slots[4]));
+        if (t == 0) reinterpret_cast<float*>(A.out_scale)[row] = s;
+        const float inv = __frcp_rn(s);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) h[c] *= inv;
+    }
+    store_all<CH, T>(A.out, row * A.out_stride, A.out_dtype, t, A.hidden, h);
+}
+
+// Longer rows by elements; HELD: in shared memory, else read again for each reduction.
 template <int W, bool HELD>
 __global__ void __launch_bounds__(32 * W) around_elements_kernel(const __grid_constant__ AroundArgs args) {
     __shared__ uint32_t slots[5][W];
@@ -119,6 +232,10 @@ __global__ void __launch_bounds__(32 * W) around_elements_kernel(const __grid_co
     }
 }
 
+template <int CH, int W>
+cudaError_t launch_held(const AroundArgs& a, cudaStream_t s) {
+    return launch_overlapped(around_held_kernel<CH, W>, (int)a.rows, 32 * W, 0, s, a);
+}
 template <int W, bool HELD>
 cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
     const auto k = around_elements_kernel<W, HELD>;
@@ -133,8 +250,16 @@ cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
 cudaError_t launch_row(AroundArgs& a, bool vec, int sms, cudaStream_t s) {
     const int n = a.hidden;
     if (vec && n <= 16384) return a.param_bf16 ? launch_around_bf16_lines(a, sms, s) : launch_around_fp32_lines(a, sms, s);
-    if (n <= 512) return launch_elements<4, true>(a, s);
-    if (n <= 2048) return launch_elements<8, true>(a, s);
+    if (n <= 256) return launch_held<2, 4>(a, s);
+    if (n <= 384) return launch_held<3, 4>(a, s);
+    if (n <= 640) return launch_held<5, 4>(a, s);
+    if (n <= 1024) return launch_held<8, 4>(a, s);
+    if (n <= 1280) return launch_held<10, 4>(a, s);
+    if (n <= 2048) return launch_held<8, 8>(a, s);
+    if (n <= 2560) return launch_held<10, 8>(a, s);
+    if (n <= 4096) return launch_held<8, 16>(a, s);
+    if (n <= 5120) return launch_held<10, 16>(a, s);
+    if (n <= 8192) return launch_held<16, 16>(a, s);
     if (n <= kAroundHeld) return launch_elements<16, true>(a, s);
     return launch_elements<16, false>(a, s);
 }

@@ -46,6 +46,11 @@ __device__ __forceinline__ void normalise(Two (&v)[CH][4], int kind, float eps, 
         for (int i = 0; i < 4; ++i) v[c][i] = mul2(v[c][i], two(rstd, rstd));
 }
 
+template <bool BF16>
+struct RowType {
+    static constexpr bool bf16 = BF16;
+};
+
 template <int CH, int W, bool XB, bool BB, bool LB>
 __global__ void __launch_bounds__(norm_threads(W), norm_ctas(CH, W)) around_kernel(const __grid_constant__ AroundArgs args) {
     __shared__ uint32_t slots[2][kAroundReductions][W];
@@ -56,38 +61,47 @@ __global__ void __launch_bounds__(norm_threads(W), norm_ctas(CH, W)) around_kern
     const unsigned team = W == 1 ? blockIdx.x * kWarpRows + threadIdx.x / 32 : blockIdx.x;
     const unsigned first = (unsigned)min((unsigned long long)team * A.team_rows, (unsigned long long)A.rows);
     const unsigned end = first + min(A.team_rows, A.rows - first);
-    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
     const int e0 = t * 8;  // its first element; the others follow in steps of 8 * threads
-    auto on = [&](int c) { return e0 + c * threads * 8 < A.hidden; };
+    auto on = [&](int c) { return c + 1 < CH || e0 + c * threads * 8 < A.hidden; };  // (the launch has as few chunks as the row needs)
     auto column = [&](int c) { return on(c) ? c * threads * 8 : -e0; };  // of chunk c behind e0, or the row's start
-    auto fetch = [&](unsigned row) {  // the row's chunks of x and branch, in pieces of 16 bytes
-        if (row < end) {
-            const char* const x = reinterpret_cast<const char*>(A.x) + (row * A.x_stride + e0) * (XB ? 2 : 4);
-            auto copy = [&](uint32_t dst, const char* p, int size) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(p), "r"(size) : "memory");
-            };
+    // A row comes to shared memory in pieces of 16 bytes. Each lane copies its own of bf16; of fp32, where a lane's eight elements are two,
+    // the warp copies 512 bytes at a time (two halves of every sector took the copies twice as long) and reads across lanes.
+    const int lane = threadIdx.x % 32;
+    const uint32_t own = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    const uint32_t across = (uint32_t)__cvta_generic_to_shared(ring) + (threadIdx.x - lane) * 16 + lane / 16 * step + lane % 16 * 32;
+    auto copy = [&](uint32_t dst, const char* p, bool in) {
+        const int size = in ? 16 : 0;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(p), "r"(size) : "memory");
+    };
+    auto fetch_rows = [&](const char* p, auto type, int piece) {  // p: the row's start
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (decltype(type)::bf16) {
+                copy(own + (c * P + piece) * step, p + (e0 + column(c)) * 2, on(c));
+            } else {
 #pragma unroll
-                for (int i = 0; i < (XB ? 1 : 2); ++i)
-                    copy(mine + (c * P + i) * step, x + column(c) * (XB ? 2 : 4) + 16 * i, on(c) ? 16 : 0);
-            if (A.branch) {
-                const char* const b = reinterpret_cast<const char*>(A.branch) + (row * A.branch_stride + e0) * (BB ? 2 : 4);
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-#pragma unroll
-                    for (int i = 0; i < (BB ? 1 : 2); ++i)
-                        copy(mine + (c * P + (XB ? 1 : 2) + i) * step, b + column(c) * (BB ? 2 : 4) + 16 * i, on(c) ? 16 : 0);
+                for (int i = 0; i < 2; ++i) {
+                    const int e = c * threads * 8 + (t - lane) * 8 + i * 128 + lane * 4;
+                    const bool in = c + 1 < CH || e < A.hidden;
+                    copy(own + (c * P + piece + i) * step, p + (in ? e : 0) * 4, in);
+                }
             }
+        }
+    };
+    auto fetch = [&](unsigned row) {  // the row's chunks of x and branch
+        if (row < end) {
+            fetch_rows(reinterpret_cast<const char*>(A.x) + row * A.x_stride * (XB ? 2 : 4), RowType<XB>{}, 0);
+            if (A.branch) fetch_rows(reinterpret_cast<const char*>(A.branch) + row * A.branch_stride * (BB ? 2 : 4), RowType<BB>{}, XB ? 1 : 2);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto landed = [&](uint32_t from, auto& r) {
+    auto landed = [&](int c, int piece, auto& r) {
+        constexpr bool bf16 = sizeof(r) == 16;
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(r) / 16); ++i)
+        for (int i = 0; i < (bf16 ? 1 : 2); ++i)
             asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
                          : "=r"(r.w[i].x), "=r"(r.w[i].y), "=r"(r.w[i].z), "=r"(r.w[i].w)
-                         : "r"(from + i * step));
+                         : "r"((bf16 ? own : across) + (c * P + piece) * step + i * 16));
     };
     // v = f(v, line) with a line's values, which all chunks load together.
     auto with_line = [&](const void* p, long long at, auto& v, auto f) {
@@ -105,7 +119,6 @@ __global__ void __launch_bounds__(norm_threads(W), norm_ctas(CH, W)) around_kern
     };
     const auto times = [](Two v, Two w) { return mul2(v, w); };
     const auto plus = [](Two v, Two w) { return add2(v, w); };
-    const Two keep = two(A.x_factor, A.x_factor), add = two(A.branch_factor, A.branch_factor);
     after_previous();
     unsigned sample = 0, next_sample = 0;  // the next sample's first row
     if (first < end) sample = first / A.tokens, next_sample = sample * A.tokens;
@@ -117,37 +130,56 @@ __global__ void __launch_bounds__(norm_threads(W), norm_ctas(CH, W)) around_kern
             ++sample, next_sample += min(A.tokens, 0xFFFFFFFFu - next_sample);
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (!XB || !BB) __syncwarp();
         uint32_t(*const words)[W] = slots[row % 2];
         Two h[CH][4], r[CH][4];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             Raw8<XB> x;
-            landed(mine + c * P * step, x);
+            landed(c, 0, x);
             pairs_of(x, h[c]);
         }
         if (A.branch)
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 Raw8<BB> b;
-                landed(mine + (c * P + (XB ? 1 : 2)) * step, b);
+                landed(c, XB ? 1 : 2, b);
                 pairs_of(b, r[c]);
             }
+        if (!XB || !BB) __syncwarp();
         fetch(row + 1);  // into the places just read
+        auto scaled = [](auto& v, float by) {
+            if (by == 1.0f) return;
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[c][i] = mul2(h[c][i], keep);
+                for (int i = 0; i < 4; ++i) v[c][i] = mul2(v[c][i], two(by, by));
+        };
+        scaled(h, A.x_factor);
         if (A.branch) {
             if (A.after != CB_NORM_NONE) {
                 normalise<CH, W>(r, A.after, A.after_eps, A.inv_hidden, on, words);
                 with_line(A.after_weight, e0, r, times);
                 with_line(A.after_bias, e0, r, plus);
             }
-            with_line(A.gate, line, r, times);
+            scaled(r, A.branch_factor);
+            if (A.gate) {
+                Raw8<LB> raw[CH];
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+                for (int c = 0; c < CH; ++c) raw[c] = load8<LB>(A.gate, line + column(c));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) h[c][i] = fma2(r[c][i], add, h[c][i]);
+                for (int c = 0; c < CH; ++c) {
+                    Two g[4];
+                    pairs_of(raw[c], g);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[c][i] = fma2(g[i], r[c][i], h[c][i]);
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[c][i] = add2(h[c][i], r[c][i]);
+            }
         }
         if (A.x_out) {
             const long long at = row * A.x_out_stride + e0;
@@ -199,21 +231,24 @@ __global__ void __launch_bounds__(norm_threads(W), norm_ctas(CH, W)) around_kern
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int e = e0 + c * threads * 8;
-                float v[8];
-                uint32_t most = 0;
+                float v[8], top = 0.0f;
+                if (!on(c)) h[c][0] = h[c][1] = h[c][2] = h[c][3] = two(0.0f, 0.0f);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 f = both(h[c][i]);
-                    v[2 * i] = on(c) ? f.x : 0.0f, v[2 * i + 1] = on(c) ? f.y : 0.0f;
-                    most = max(most, max(__float_as_uint(v[2 * i]) & 0x7FFFFFFFu, __float_as_uint(v[2 * i + 1]) & 0x7FFFFFFFu));
+                    top = mx_max_abs(top, f.x, f.y);
                 }
+                uint32_t most = __float_as_uint(top);
                 most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
                 most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
                 const uint32_t scale = mx_scale_of(most);
                 const float inverse = mx_inverse(scale);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= inverse;
-                if (e < (A.hidden + kMxBlock - 1) / kMxBlock * kMxBlock)
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = both(mul2(h[c][i], two(inverse, inverse)));
+                    v[2 * i] = f.x, v[2 * i + 1] = f.y;
+                }
+                if (c + 1 < CH || e < (A.hidden + kMxBlock - 1) / kMxBlock * kMxBlock)
                     *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(A.out) + row * A.out_stride + e / 2) = scale == 255 ? 0u : mx_codes8(v);
                 uint32_t w = scale << 8 * (t / 4 % 4);
                 w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
@@ -250,18 +285,22 @@ cudaError_t launch_around(AroundArgs& a, int sms, cudaStream_t s) {
     return launch_overlapped(k, (int)((used + teams - 1) / teams), threads, smem, s, a);
 }
 
-// The row's warps and chunks, as in cb_norm_residual.
+// The row's warps and chunks: one warp up to 1280 elements, then four, eight or sixteen with up to four chunks a thread, of which all but
+// the last lie in the row.
 template <bool XB, bool BB, bool LB>
 cudaError_t launch_around_types(AroundArgs& a, int sms, cudaStream_t s) {
     const int n = a.hidden / 8;
     if (n <= 32) return launch_around<1, 1, XB, BB, LB>(a, sms, s);
     if (n <= 64) return launch_around<2, 1, XB, BB, LB>(a, sms, s);
     if (n <= 96) return launch_around<3, 1, XB, BB, LB>(a, sms, s);
+    if (n <= 128) return launch_around<4, 1, XB, BB, LB>(a, sms, s);
     if (n <= 160) return launch_around<5, 1, XB, BB, LB>(a, sms, s);
     if (n <= 256) return launch_around<2, 4, XB, BB, LB>(a, sms, s);
     if (n <= 384) return launch_around<3, 4, XB, BB, LB>(a, sms, s);
     if (n <= 512) return launch_around<4, 4, XB, BB, LB>(a, sms, s);
+    if (n <= 768) return launch_around<3, 8, XB, BB, LB>(a, sms, s);
     if (n <= 1024) return launch_around<4, 8, XB, BB, LB>(a, sms, s);
+    if (n <= 1536) return launch_around<3, 16, XB, BB, LB>(a, sms, s);
     return launch_around<4, 16, XB, BB, LB>(a, sms, s);
 }
 
