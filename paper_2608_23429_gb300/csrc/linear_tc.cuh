@@ -123,6 +123,8 @@ __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int
             : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
 // Operand in shared memory: rows of 128 bytes, K innermost, 128-byte swizzle in groups of eight rows (1024 bytes).
 __device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
     return (uint64_t)((addr & 0x3FFFF) >> 4) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
@@ -566,6 +568,13 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
     const uint32_t acc_full = smem_addr(T.acc_full), acc_empty = smem_addr(T.acc_empty);
     const Limit limit{&T.abort, A.status, A.wait_ns};
 
+    if (warp == EPI + 1 && elected()) {  // the maps, which are arguments, are on their way while the previous kernel ends
+        prefetch_map(&A.x_map), prefetch_map(&A.w_map);
+        if constexpr (MX) prefetch_map(&A.x_scale_map), prefetch_map(&A.w_scale_map);
+        if constexpr (!DIRECT && !QUANT)
+            if (A.e.out) prefetch_map(&A.out_map);
+        if constexpr (HIDDEN) prefetch_map(&A.resid_map), prefetch_map(&A.resid_out_map);
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
             mbar_init(full + 8 * s, 1);

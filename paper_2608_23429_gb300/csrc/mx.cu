@@ -54,9 +54,15 @@ __device__ __forceinline__ void store8(void* p, long long e, int n, const float*
             for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
             *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p) + e) = *reinterpret_cast<const uint4*>(h);
         } else {
-            float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + e);
-            q[0] = make_float4(v[0], v[1], v[2], v[3]);
-            q[1] = make_float4(v[4], v[5], v[6], v[7]);
+            float* const q = reinterpret_cast<float*>(p) + e;
+            if ((uintptr_t)q % 32 == 0) {  // a sector in one store
+                asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(q), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+                             "f"(v[5]), "f"(v[6]), "f"(v[7])
+                             : "memory");
+            } else {
+                reinterpret_cast<float4*>(q)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                reinterpret_cast<float4*>(q)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
         }
         return;
     }
@@ -123,29 +129,49 @@ __global__ void __launch_bounds__(32 * kMxWarps) mx_dequantize_kernel(const __gr
     after_previous();
     const auto [row0, col] = mx_place(A);
     const int n = (int)min(A.features - min(col, A.features), 8u), lane = threadIdx.x % 32;
-    if (n <= 0 || row0 >= A.rows) return;
-    const uint4 q = *reinterpret_cast<const uint4*>(A.scales + mx_word_at(row0, col / (kMxBlock * kMxTileBlocks), A.tiles_k));
-    const uint32_t words[kMxRows] = {q.x, q.y, q.z, q.w};
-    uint32_t codes[kMxRows];
+    if ((VEC && n <= 0) || row0 >= A.rows) return;
+    uint32_t words[kMxRows] = {}, codes[kMxRows];
+    const unsigned k = col / (kMxBlock * kMxTileBlocks);
+    if (k < A.tiles_k) {
+        const uint4 q = *reinterpret_cast<const uint4*>(A.scales + mx_word_at(row0, k, A.tiles_k));
+        words[0] = q.x, words[1] = q.y, words[2] = q.z, words[3] = q.w;
+    }
 #pragma unroll
     for (int j = 0; j < kMxRows; ++j) {
         const unsigned row = row0 + 32 * j;
-        codes[j] = row < A.rows ? *reinterpret_cast<const uint32_t*>(A.codes + row * A.codes_row + col / 2) : 0u;
+        codes[j] = row < A.rows && n > 0 ? *reinterpret_cast<const uint32_t*>(A.codes + row * A.codes_row + col / 2) : 0u;
     }
 #pragma unroll
     for (int j = 0; j < kMxRows; ++j) {
         const unsigned row = row0 + 32 * j;
         if (row >= A.rows) break;
-        const float power = mx_power(words[j] >> 8 * (lane / 4 % 4) & 255u);
-        uint32_t h[4];
-        float v[8];
-        mx_widen8(codes[j], h);
+        if constexpr (VEC) {
+            const float power = mx_power(words[j] >> 8 * (lane / 4 % 4) & 255u);
+            uint32_t h[4];
+            float v[8];
+            mx_widen8(codes[j], h);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-            v[2 * i] = f.x * power, v[2 * i + 1] = f.y * power;
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+                v[2 * i] = f.x * power, v[2 * i + 1] = f.y * power;
+            }
+            store8<BF16, VEC>(A.x, row * A.stride + col, n, v);
+        } else {
+            // a block of the warp's eight at a time, an element a lane: neighbours' stores share sectors
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t power = __shfl_sync(0xFFFFFFFFu, words[j], 16 * (i / 4)) >> 8 * (i % 4) & 255u;
+                const uint32_t eight = __shfl_sync(0xFFFFFFFFu, codes[j], 4 * i + lane / 8);
+                uint32_t h[4];
+                mx_widen8(eight >> 4 * (lane % 8) & 15u, h);
+                const float v = __half22float2(*reinterpret_cast<const __half2*>(&h[0])).x * mx_power(power);
+                const unsigned e = col - lane * 8 + 32 * i + lane;
+                if (e < A.features) {
+                    if constexpr (BF16) reinterpret_cast<__nv_bfloat16*>(A.x)[row * A.stride + e] = __float2bfloat16_rn(v);
+                    else reinterpret_cast<float*>(A.x)[row * A.stride + e] = v;
+                }
+            }
         }
-        store8<BF16, VEC>(A.x, row * A.stride + col, n, v);
     }
 }
 
