@@ -23,10 +23,10 @@ struct MxArgs {
     uint8_t *codes, *scales;
 };
 
-// Eight elements of a row, zeros behind its end.
+// Eight elements of a row by vectors, or n by elements and zeros behind them.
 template <bool BF16, bool VEC>
 __device__ __forceinline__ void load8(const void* p, long long e, int n, float* v) {
-    if (VEC && n >= 8) {
+    if constexpr (VEC) {
         if constexpr (BF16) {
             const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + e);
             const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -89,15 +89,21 @@ __global__ void __launch_bounds__(32 * kMxWarps) mx_quantize_kernel(const __grid
     const auto [row0, col] = mx_place(A);
     const int n = (int)min(A.features - min(col, A.features), 8u), lane = threadIdx.x % 32;
     float v[kMxRows][8];
+    if (VEC && n == 8) {  // all rows' loads together (rows behind the last: that one's)
 #pragma unroll
-    for (int j = 0; j < kMxRows; ++j)
-        load8<BF16, VEC>(A.x, (long long)(row0 + 32 * j) * A.stride + col, row0 + 32 * j < A.rows ? n : 0, v[j]);
+        for (int j = 0; j < kMxRows; ++j) load8<BF16, true>(A.x, (long long)min(row0 + 32 * j, A.rows - 1) * A.stride + col, 8, v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kMxRows; ++j)
+            load8<BF16, false>(A.x, (long long)(row0 + 32 * j) * A.stride + col, row0 + 32 * j < A.rows ? n : 0, v[j]);
+    }
     uint32_t words[kMxRows];
 #pragma unroll
     for (int j = 0; j < kMxRows; ++j) {
-        uint32_t most = 0;
+        float top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[j][i]) & 0x7FFFFFFFu);
+        for (int i = 0; i < 8; i += 2) top = mx_max_abs(top, v[j][i], v[j][i + 1]);
+        uint32_t most = __float_as_uint(top);
         most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
         most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
         const uint32_t e = mx_scale_of(most);
