@@ -378,7 +378,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
         rc = pw.dst ? operand_map(&a.w_map, pw.dst, ep.N, 32ll * pw.chunks, 32ll * pw.chunks, a.tile_n / cg)
                     : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);
     // one box instead of two for each of the 12 warps makes room for a stage more (8192^3 to bf16 159 -> 152 us)
-    a.out_boxes = mx && a.results == Results::kOut && a.k_blocks > kShortBlocks ? 1 : 2;
+    a.out_boxes = a.results == Results::kQuant ? 0 : mx && a.results == Results::kOut && a.k_blocks > kShortBlocks ? 1 : 2;
     const size_t fixed = linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes, a.out_boxes) : 0);
     const size_t stage = linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0);
     if (fixed + 2 * stage > (size_t)dev->smem) rc = CB_ERR_LIMIT;  // (no device that the library is built for)

@@ -40,8 +40,10 @@ constexpr int kMxMostN = 192, kMxStepN = 64;  // columns of a tile: TMEM holds t
 // Warps of the epilogue: two for each quarter of the TMEM lanes, or four where the threads load and store the results themselves
 // and wait for that (GB300, 8192 x 8191 x 512 bf16 with a gated fp32 hidden state: eight warps, 32 rows at once each, 282 us,
 // sixteen, eight rows at once, 195).
+// Operands in 4 bits, whose sums are made four times as fast: 12 and 16 (GB300, 8192 x 4608 x 1152 with GELU to bf16 with 8 warps 35.4 us,
+// 12 27.3, 16 27.0; to 4 bits 12 33.3, 16 28.7).
 __host__ __device__ constexpr int epi_warps(Results r, bool mx = false) {
-    if (mx) return r == Results::kDirect ? 16 : r == Results::kHiddenLong ? 8 : 12;
+    if (mx) return r == Results::kDirect ? 16 : r == Results::kHiddenLong ? 8 : r == Results::kQuant ? 16 : 12;
     return r == Results::kDirect ? 16 : 8;
 }
 constexpr int kTurnBytes = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
