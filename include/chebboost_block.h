@@ -223,7 +223,7 @@ int cb_linear_create(const cb_linear_desc* desc, cb_linear** out);
 void cb_linear_destroy(cb_linear* layer);
 
 /* CB_OPT_WAIT_NS: limit of every wait of the layer's kernels on one of their barriers, ns (default 1e9, at most
- * 6e10). CB_OPT_TEST_WITHHOLD: 1: (tests of the failure path only) over 32 rows the kernels announce more
+ * 6e10). CB_OPT_TEST_WITHHOLD: 1: (tests of the failure path only) over 32 rows (CB_MXFP4: always) the kernels announce more
  * bytes of operands than they copy, so that the waits for them run out; results are then
  * invalid. Errors: CB_ERR_ARG. */
 int cb_linear_set_option(cb_linear* layer, int option, int64_t value);
