@@ -183,6 +183,28 @@ def test_every_scale_stands_at_its_own_rows_and_blocks(lib):
         assert np.array_equal(out.cpu().numpy().astype(np.float64), want[:rows])
 
 
+def test_the_smallest_and_largest_scales(lib):
+    """Scales of 2^-127 against such of 2^127, and both in one sum: terms far apart do not disturb each other."""
+    block, cb = lib
+    m, n, k = 160, 72, 128
+    ex, ew = np.full((m, 4), 127, np.uint8), np.full((n, 4), 127, np.uint8)
+    ex[:, 0], ew[:, 0] = 0, 254
+    ex[:, 1], ew[:, 1] = 254, 0
+    ex[:, 2], ew[:, 2] = 0, 0  # 2^-254: nothing
+    ex[5] = 0
+    rng = np.random.default_rng(0)
+    cx, cw = rng.integers(0, 16, (m, k)).astype(np.uint8), rng.integers(0, 16, (n, k)).astype(np.uint8)
+    x, w, xs, ws = (torch.from_numpy(t).cuda() for t in (R.packed(cx), R.packed(cw), R.tiled(ex), R.tiled(ew)))
+    out = torch.zeros(m, n, device="cuda")
+    layer = block.cb_linear_create(w, n, k, cb.CB_MXFP4, ws)
+    block.cb_linear_run(layer, block.cb_linear_io(rows=m, out_dtype=cb.CB_FP32), x, xs, out=out)
+    torch.cuda.synchronize()
+    block.cb_linear_destroy(layer)
+    xv, wv = R.values(cx, ex, k), R.values(cw, ew, k)
+    want, size = torch.from_numpy(xv @ wv.T), torch.from_numpy(np.abs(xv) @ np.abs(wv).T)
+    close(out.cpu(), want, (k + 4) * U * size + 2.0 ** -126, "fp32")
+
+
 def test_blocks_that_are_not_finite_stay_apart(lib):
     block, cb = lib
     for m, n, k in ((300, 264, 192), (9, 264, 192), (130, 99, 101)):
