@@ -194,7 +194,10 @@ constexpr int kOnePass = 256, kPassLong = 32;
 // up to 16 parts of four slabs gave the same.
 constexpr double kJoinClocks = 5000, kJoinBytesPerClock = 1300;
 constexpr int kMaxParts = 8, kPartSlabs = 8;  // no part is shorter
-void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int step, int max_parts, int* cg, int* tile_n, int* parts) {
+// A slab in 4 bits takes as much (its scales' way to TMEM, and the products behind it) however few its rows and columns are; of tiles that
+// take as long the smaller ones, on more SMs. GB300, 42 x 280 x 9752 12.3 us where slabs count by their bytes, 9.4 so.
+constexpr double kMxSlabClocks = 320;
+void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int step, int max_parts, int x_rows, double least, int* cg, int* tile_n, int* parts) {
     double best = 1e300;
     for (int p = 1; p <= max_parts && (p == 1 || k_blocks / p >= kPartSlabs); ++p)
         for (int g = 2; g >= 1; --g)
@@ -205,8 +208,8 @@ void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int st
                 if (units < 1) break;  // no room for pairs
                 if (p > 1 && tiles > units) break;  // smaller tiles are more
                 const double join = p > 1 ? kJoinClocks + 4.0 * p * M * N / kJoinBytesPerClock : 0.0;
-                const double cost = (double)((tiles + units - 1) / units) * ((k_blocks + p - 1) / p) * (256.0 + 2.0 * n / g) + join;
-                if (cost < best * 0.999) best = cost, *cg = g, *tile_n = n, *parts = p;
+                const double cost = (double)((tiles + units - 1) / units) * ((k_blocks + p - 1) / p) * std::max(least, 2.0 * x_rows + 2.0 * n / g) + join;
+                if (cost < best * (least > 0.0 ? 1.001 : 0.999)) best = cost, *cg = g, *tile_n = n, *parts = p;
             }
 }
 
@@ -327,8 +330,10 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     // fp32 results: passes over K (see linear_tc.cuh)
     const bool fp32 = (out && !ep.out_bf16) || (resid_out && !ep.resid_bf16);
     a.pass_blocks = fp32 ? (mx ? kPassMx : d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
+    // (4 bits) rows that x does not have are not loaded: what the tensor cores read in their place makes sums that nobody takes
+    a.x_rows = mx ? std::min(128, (ep.M + 7) / 8 * 8) : 128;
     choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks ? 128 : mx ? kMxMostN : 256, mx ? kMxStepN : 32,
-                out_mx ? 1 : kMaxParts, &cg, &a.tile_n, &a.parts);
+                out_mx ? 1 : kMaxParts, a.x_rows, mx ? kMxSlabClocks : 0.0, &cg, &a.tile_n, &a.parts);
     a.part_blocks = (a.k_blocks + a.parts - 1) / a.parts;
     a.parts = (a.k_blocks + a.part_blocks - 1) / a.part_blocks;
     a.passes = (a.part_blocks + a.pass_blocks - 1) / a.pass_blocks;
@@ -373,7 +378,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     const PackOperand &px = pack.o[0], &pw = pack.o[1];
     if (rc == CB_OK)
         rc = px.dst ? operand_map(&a.x_map, px.dst, ep.M, 32ll * px.chunks, 32ll * px.chunks, 128)
-                    : operand_map(&a.x_map, x, ep.M, a.k_bytes, x_row, 128);
+                    : operand_map(&a.x_map, x, ep.M, a.k_bytes, x_row, a.x_rows);
     if (rc == CB_OK)
         rc = pw.dst ? operand_map(&a.w_map, pw.dst, ep.N, 32ll * pw.chunks, 32ll * pw.chunks, a.tile_n / cg)
                     : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);

@@ -61,6 +61,7 @@ struct LinearArgs {
     LinearEpilogue e;
     int overlap;
     int k_bytes;           // bytes of a row of x and of w
+    int x_rows;            // rows of x of a slab that are loaded
     int tiles_m, tiles_n, k_blocks, stages;
     unsigned long long tokens_magic; // the same of tokens; 0 for 1
     unsigned long long group_magic;  // ceil(2^64 / (8 tiles_n)): t group_magic / 2^64 is t / (8 tiles_n) for every 32-bit t

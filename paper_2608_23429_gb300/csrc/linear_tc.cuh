@@ -949,7 +949,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
         int fills = 0;
         bool ok = true;
         const uint32_t bar0 = CG == 2 ? in_first(full) : full;
-        const uint32_t announced = CG * stage_bytes + A.withheld;
+        const uint32_t announced = CG * (MX ? stage_bytes - (kRows - A.x_rows) * kSlab : stage_bytes) + A.withheld;
         for (int t = first; t < total && ok; t += step) {
             const Tile tile = tile_at<SPLIT>(A, t);
             const int row = (tile.m * CG + (int)rank) * kRows, col = tile.n * A.tile_n + (int)rank * w_rows;

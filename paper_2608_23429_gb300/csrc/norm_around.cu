@@ -13,11 +13,30 @@ namespace {
 
 constexpr int kAroundHeld = 49152;  // elements of a row in shared memory
 
+// Elements t, t + T, ... of a row from p on. The first FULL lie in every row that the kernel is launched for, at places that the compiler knows:
+// a select and an address for each of them took a third of the kernel's instructions. Threads behind the row's end read its start.
+template <int CH, int T, int FULL>
+__device__ __forceinline__ void load_row(const void* p, long long e, int bf16, int t, int hidden, float* v) {
+    auto at = [&](int c) { return c < FULL || c * T + t < hidden ? c * T : -t; };
+    if (bf16) {
+        const uint16_t* const q = reinterpret_cast<const uint16_t*>(p) + e + t;
+        uint16_t w[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) w[c] = q[at(c)];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = __uint_as_float((uint32_t)w[c] << 16);
+    } else {
+        const float* const q = reinterpret_cast<const float*>(p) + e + t;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = q[at(c)];
+    }
+}
+
 // A row by elements, in registers: CH of them in each thread of its W warps. The lines are loaded with the row where there is room for
 // them, each when it is wanted where there is not.
 __host__ __device__ constexpr bool around_early(int CH, int W) { return CH * W <= 40; }
 
-template <int CH, int W>
+template <int CH, int W, int FULL>
 __global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 * W)) around_held_kernel(const __grid_constant__ AroundArgs args) {
     __shared__ uint32_t slots[5][W];
     constexpr int T = 32 * W;
@@ -26,17 +45,17 @@ __global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 *
     after_previous();
     const unsigned row = blockIdx.x;
     const int t = threadIdx.x;
-    auto on = [&](int c) { return c * T + t < A.hidden; };
+    auto on = [&](int c) { return c < FULL || c * T + t < A.hidden; };
     const long long line = (long long)(row / A.tokens) * A.line_stride;
     float early[7][CH];
     auto look = [&](int i, const void* p, long long at) {
-        if (EARLY && p) load_all<CH, T>(p, at, A.param_bf16, t, A.hidden, early[i]);
+        if (EARLY && p) load_row<CH, T, FULL>(p, at, A.param_bf16, t, A.hidden, early[i]);
     };
     // v = f(v, line), of line i at p
     auto with_line = [&](int i, const void* p, long long at, float (&v)[CH], auto f) {
         if (!p) return;
         float late[CH];
-        if (!EARLY) load_all<CH, T>(p, at, A.param_bf16, t, A.hidden, late);
+        if (!EARLY) load_row<CH, T, FULL>(p, at, A.param_bf16, t, A.hidden, late);
 #pragma unroll
         for (int c = 0; c < CH; ++c) v[c] = f(v[c], EARLY ? early[i][c] : late[c]);
     };
@@ -62,8 +81,8 @@ __global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 *
     const auto times = [](float v, float w) { return v * w; };
     const auto plus = [](float v, float w) { return v + w; };
     float h[CH], r[CH];
-    load_all<CH, T>(A.x, row * A.x_stride, A.x_bf16, t, A.hidden, h);
-    if (A.branch) load_all<CH, T>(A.branch, row * A.branch_stride, A.branch_bf16, t, A.hidden, r);
+    load_row<CH, T, FULL>(A.x, row * A.x_stride, A.x_bf16, t, A.hidden, h);
+    if (A.branch) load_row<CH, T, FULL>(A.branch, row * A.branch_stride, A.branch_bf16, t, A.hidden, r);
     look(0, A.after_weight, 0);
     look(1, A.after_bias, 0);
     look(2, A.gate, line);
@@ -95,20 +114,37 @@ __global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 *
     with_line(5, A.scale, line, h, [](float v, float w) { return fmaf(v, w, v); });
     with_line(6, A.shift, line, h, plus);
     if (A.out_dtype == CB_MXFP4) {
-        // a block is a warp; those that fill up the last tile of scales are zeros
-        uint8_t* const out = reinterpret_cast<uint8_t*>(A.out) + row * A.out_stride;
-        const unsigned ends = A.out_tiles * kMxTileBlocks * kMxBlock, codes_end = ((unsigned)A.hidden + kMxBlock - 1) / kMxBlock * kMxBlock;
+        // Through shared memory to eight consecutive elements of a thread, so that a block is four lanes and a word of scales sixteen
+        // (a block as a warp, a code by every other lane, took four times the instructions). Zeros fill up the last tile of scales.
+        extern __shared__ __align__(16) float turned[];
+        const int ends = (int)A.out_tiles * kMxTileBlocks * kMxBlock;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const unsigned e = c * T + t;
-            const float y = on(c) ? h[c] : 0.0f;
-            const uint32_t scale = mx_scale_of(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
-            const float q = y * mx_inverse(scale);
-            const float v[8] = {q, __shfl_down_sync(0xFFFFFFFFu, q, 1)};
-            if (t % 2 == 0 && e < codes_end) out[e / 2] = scale == 255 ? 0 : (uint8_t)mx_codes8(v);
-            const unsigned block = e / kMxBlock;
-            if (t % 32 == 0 && e < ends)
-                reinterpret_cast<uint8_t*>(A.out_scale)[mx_word_at(row, block / kMxTileBlocks, A.out_tiles) + block % kMxTileBlocks] = (uint8_t)scale;
+        for (int c = 0; c < CH; ++c)
+            if (c * T + t < ends) turned[c * T + t] = on(c) ? h[c] : 0.0f;
+        for (int e = CH * T + t; e < ends; e += T) turned[e] = 0.0f;
+        __syncthreads();
+        for (int e = t * 8; e < ends; e += T * 8) {  // (whole words of scales: sixteen lanes are in or out together)
+            const unsigned mask = __activemask();
+            float v[8];
+            *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(turned + e);
+            *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(turned + e + 4);
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) top = mx_max_abs(top, v[i], v[i + 1]);
+            uint32_t most = __float_as_uint(top);
+            most = max(most, __shfl_xor_sync(mask, most, 1));
+            most = max(most, __shfl_xor_sync(mask, most, 2));
+            const uint32_t scale = mx_scale_of(most);
+            const float inverse = mx_inverse(scale);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= inverse;
+            if (e < (A.hidden + kMxBlock - 1) / kMxBlock * kMxBlock)
+                *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(A.out) + row * A.out_stride + e / 2) = scale == 255 ? 0u : mx_codes8(v);
+            uint32_t w = scale << 8 * (t / 4 % 4);
+            w |= __shfl_xor_sync(mask, w, 4);
+            w |= __shfl_xor_sync(mask, w, 8);
+            if (t % 16 == 0)
+                *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(A.out_scale) + mx_word_at(row, e / (kMxBlock * kMxTileBlocks), A.out_tiles)) = w;
         }
         return;
     }
@@ -232,9 +268,11 @@ __global__ void __launch_bounds__(32 * W) around_elements_kernel(const __grid_co
     }
 }
 
-template <int CH, int W>
+template <int CH, int W, int FULL>
 cudaError_t launch_held(const AroundArgs& a, cudaStream_t s) {
-    return launch_overlapped(around_held_kernel<CH, W>, (int)a.rows, 32 * W, 0, s, a);
+    // (33 KB at most)
+    const size_t smem = a.out && a.out_dtype == CB_MXFP4 ? (size_t)a.out_tiles * kMxTileBlocks * kMxBlock * 4 : 0;
+    return launch_overlapped(around_held_kernel<CH, W, FULL>, (int)a.rows, 32 * W, smem, s, a);
 }
 template <int W, bool HELD>
 cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
@@ -250,16 +288,16 @@ cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
 cudaError_t launch_row(AroundArgs& a, bool vec, int sms, cudaStream_t s) {
     const int n = a.hidden;
     if (vec && n <= 16384) return a.param_bf16 ? launch_around_bf16_lines(a, sms, s) : launch_around_fp32_lines(a, sms, s);
-    if (n <= 256) return launch_held<2, 4>(a, s);
-    if (n <= 384) return launch_held<3, 4>(a, s);
-    if (n <= 640) return launch_held<5, 4>(a, s);
-    if (n <= 1024) return launch_held<8, 4>(a, s);
-    if (n <= 1280) return launch_held<10, 4>(a, s);
-    if (n <= 2048) return launch_held<8, 8>(a, s);
-    if (n <= 2560) return launch_held<10, 8>(a, s);
-    if (n <= 4096) return launch_held<8, 16>(a, s);
-    if (n <= 5120) return launch_held<10, 16>(a, s);
-    if (n <= 8192) return launch_held<16, 16>(a, s);
+    if (n <= 256) return launch_held<2, 4, 0>(a, s);
+    if (n <= 384) return launch_held<3, 4, 2>(a, s);
+    if (n <= 640) return launch_held<5, 4, 3>(a, s);
+    if (n <= 1024) return launch_held<8, 4, 5>(a, s);
+    if (n <= 1280) return launch_held<10, 4, 8>(a, s);
+    if (n <= 2048) return launch_held<8, 8, 5>(a, s);
+    if (n <= 2560) return launch_held<10, 8, 8>(a, s);
+    if (n <= 4096) return launch_held<8, 16, 5>(a, s);
+    if (n <= 5120) return launch_held<10, 16, 8>(a, s);
+    if (n <= 8192) return launch_held<16, 16, 10>(a, s);
     if (n <= kAroundHeld) return launch_elements<16, true>(a, s);
     return launch_elements<16, false>(a, s);
 }
