@@ -195,9 +195,11 @@ constexpr int kOnePass = 256, kPassLong = 32;
 constexpr double kJoinClocks = 5000, kJoinBytesPerClock = 1300;
 constexpr int kMaxParts = 8, kPartSlabs = 8;  // no part is shorter
 // A slab in 4 bits takes as much (its scales' way to TMEM, and the products behind it) however few its rows and columns are; of tiles that
-// take as long the smaller ones, on more SMs. GB300, 42 x 280 x 9752 12.3 us where slabs count by their bytes, 9.4 so.
-constexpr double kMxSlabClocks = 320;
-void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int step, int max_parts, int x_rows, double least, int* cg, int* tile_n, int* parts) {
+// take as long the smaller ones, on more SMs. A launch of pairs starts later than one of single CTAs, which counts where products are this
+// fast. GB300: 42 x 280 x 9752 12.3 us where slabs count by their bytes, 8.5 so; 256 x 4608 x 1152 with GELU 5.5 us in pairs,
+// 4.7 in single CTAs, 4096^3 29.0 and 26.8.
+constexpr double kMxSlabClocks = 320, kMxPairClocks = 3000;
+void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int step, int max_parts, int x_rows, double least, double pair, int* cg, int* tile_n, int* parts) {
     double best = 1e300;
     for (int p = 1; p <= max_parts && (p == 1 || k_blocks / p >= kPartSlabs); ++p)
         for (int g = 2; g >= 1; --g)
@@ -208,7 +210,7 @@ void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int st
                 if (units < 1) break;  // no room for pairs
                 if (p > 1 && tiles > units) break;  // smaller tiles are more
                 const double join = p > 1 ? kJoinClocks + 4.0 * p * M * N / kJoinBytesPerClock : 0.0;
-                const double cost = (double)((tiles + units - 1) / units) * ((k_blocks + p - 1) / p) * std::max(least, 2.0 * x_rows + 2.0 * n / g) + join;
+                const double cost = (double)((tiles + units - 1) / units) * ((k_blocks + p - 1) / p) * std::max(least, 2.0 * x_rows + 2.0 * n / g) + join + (g - 1) * pair;
                 if (cost < best * (least > 0.0 ? 1.001 : 0.999)) best = cost, *cg = g, *tile_n = n, *parts = p;
             }
 }
@@ -333,7 +335,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     // (4 bits) rows that x does not have are not loaded: what the tensor cores read in their place makes sums that nobody takes
     a.x_rows = mx ? std::min(128, (ep.M + 7) / 8 * 8) : 128;
     choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks ? 128 : mx ? kMxMostN : 256, mx ? kMxStepN : 32,
-                out_mx ? 1 : kMaxParts, a.x_rows, mx ? kMxSlabClocks : 0.0, &cg, &a.tile_n, &a.parts);
+                out_mx ? 1 : kMaxParts, a.x_rows, mx ? kMxSlabClocks : 0.0, mx ? kMxPairClocks : 0.0, &cg, &a.tile_n, &a.parts);
     a.part_blocks = (a.k_blocks + a.parts - 1) / a.parts;
     a.parts = (a.k_blocks + a.part_blocks - 1) / a.part_blocks;
     a.passes = (a.part_blocks + a.pass_blocks - 1) / a.pass_blocks;
