@@ -1,8 +1,8 @@
 /*
  * chebboost_block.h — the full step's operators around the history, in the same
- * library: the norm that takes a block's hidden state with the last branch added,
- * and the matrix product whose epilogue makes a branch output and the new hidden
- * state (paper Sec. 3.1: B(x) = x + S(x) + C(x) + M(x), each branch a norm and
+ * library: the norms that take a block's hidden state with the last branch added,
+ * the matrix product whose epilogue makes a branch output and the new hidden
+ * state, and rows in 4 bits that go between them (paper Sec. 3.1: B(x) = x + S(x) + C(x) + M(x), each branch a norm and
  * matrix products). Their results are what cb_cache_push stores.
  *
  * Conventions are those of chebboost.h: the caller owns every device buffer and

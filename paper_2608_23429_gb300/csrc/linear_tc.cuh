@@ -18,6 +18,13 @@
 //
 // Few tiles of long sums are split over K (A.parts): each part's sums leave in fp32, and linear_join.cu adds them.
 //
+// Operands in 4 bits (OPERANDS = kMx; slabs of 256 features) come with their scales, two tiles of 128 rows by 4 blocks of x and of each 128
+// columns, which one thread copies to TMEM ahead of the products that take them: they leave room for tiles of 192 columns. The
+// products are four times as fast, so the epilogue counts four times as much: each warp brings its own columns' biases and gates (no wait for
+// other warps), tiles are sought without divisions, and there are 12 or 16 warps where the sums are short. GB300: 8192^3 to bf16 149 to 153 us (7.3
+// PFLOP/s, the tensor cores busy 83 % of the time), 8192 x 4608 x 1152 with GELU to 4 bits 29 us, 8192 x 1152 x 4608 with output and gated hidden
+// state 26.
+//
 // Bound by the tensor cores where tiles fill the SMs' rounds: GB300, 4608 x 3072 x 15360 bf16 with a gated hidden state 264 us (1.65
 // PFLOP/s, 85 % of the largest library rate), 8192 x 1152 x 4608 65 us (1.34), 4096 x 4608 x 1152 e4m3 with GELU 22.5 us (1.93).
 //

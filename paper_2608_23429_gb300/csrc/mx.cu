@@ -2,7 +2,9 @@
 //
 // Bound by HBM: an element is read and written once. A lane has eight consecutive elements, so a block is four lanes and two shuffles
 // find its largest magnitude; a warp has 256 elements of four rows, 32 apart, whose scales are 16 consecutive bytes of a
-// tile of them, and the CTA's eight warps have neighbouring rows, whose are 128.
+// tile of them, and the CTA's eight warps have neighbouring rows, whose are 128. GB300: 129024 x 1152 fp32 written in 93 us (106 % of the copy
+// rate) and read back in 100 (99 %); 65536 x 4608 bf16 122 and 111 (93 and 102 %; with each row's loads behind a branch of its own 192);
+// rows off the 16-byte grid 16384 x 1153 bf16 16 and 16 (a copy of their bytes: 7).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
