@@ -151,7 +151,9 @@ int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
                 {e.resid, e.resid_stride, (long long)bytes_of(io->resid_dtype), &a->resid_map},
                 {e.resid_out, e.resid_out_stride, (long long)bytes_of(io->resid_dtype), &a->resid_out_map}};
     for (const auto& u : used)
-        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40 || e.N * u.es > kMaxRowBytes)) return CB_OK;
+        // (a store writes whole pieces of 16 bytes, past the end of a row that is not made of them)
+        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40 || e.N * u.es > kMaxRowBytes || e.N * u.es % 16 != 0))
+            return CB_OK;
     // a gate's pieces of 16 bytes are read whole
     const long long gs = (long long)bytes_of(io->gate_dtype);
     if (e.gate && (!on_grid(e.gate, 16) || e.gate_stride * gs % 16 != 0 || e.N * gs % 16 != 0 || e.N * gs > kMaxRowBytes)) return CB_OK;

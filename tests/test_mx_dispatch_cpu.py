@@ -70,3 +70,12 @@ def test_failures_leave_nothing_behind(stub):
         lib.stub_fail(fails.encode())
         rc, log = run(stub, 256, 128, 32768, out=BF16)
         assert rc == -7 and (fails == "malloc") == ("free" not in [c[0] for c in log])
+
+
+def test_rows_that_end_inside_16_bytes_are_stored_by_the_threads(stub):
+    """A copy by TMA would write the rest of the piece, too."""
+    for kw, results in ((dict(out=BF16), OUT), (dict(resid=BF16), HIDDEN), (dict(resid=FP32, out=BF16), HIDDEN)):
+        for n, off in ((264, False), (260, True), (262, True)):
+            stub[0].stub_reset()
+            rc, log = run(stub, 300, n, 320, out_stride=264, resid_stride=264, resid_out_stride=264, gate_stride=264, **kw)
+            assert rc == 0 and log[-1][1]["results"] == (DIRECT if off else results), (n, kw)
