@@ -55,7 +55,7 @@ class cb_linear_desc(ctypes.Structure):
 
 
 class cb_linear_io(ctypes.Structure):
-    """Sizes and types of one :func:`cb_linear_run`; strides of 0 mean contiguous."""
+    """Sizes and types of one :func:`cb_linear_run`; strides of 0 mean contiguous. ``out_scale`` is an address."""
     _fields_ = [("rows", _L), ("tokens", _L), ("x_stride", _L), ("out_stride", _L), ("resid_stride", _L),
                 ("resid_out_stride", _L), ("gate_stride", _L), ("out_dtype", _I), ("resid_dtype", _I), ("gate_dtype", _I),
                 ("reserved", ctypes.c_int32), ("out_scale", _P)]

@@ -124,17 +124,18 @@ __global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 *
             if (c * T + t < ends) turned[c * T + t] = on(c) ? h[c] : 0.0f;
         for (int e = CH * T + t; e < ends; e += T) turned[e] = 0.0f;
         __syncthreads();
-        for (int e = t * 8; e < ends; e += T * 8) {  // (whole words of scales: sixteen lanes are in or out together)
-            const unsigned mask = __activemask();
-            float v[8];
-            *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(turned + e);
-            *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(turned + e + 4);
-            float top = 0.0f;
+        for (int first = t / 32 * 256; first < ends; first += T * 8) {  // (of the warp; it ends with a word of scales, sixteen lanes)
+            const int e = first + t % 32 * 8;
+            float v[8] = {}, top = 0.0f;
+            if (e < ends) {
+                *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(turned + e);
+                *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(turned + e + 4);
+            }
 #pragma unroll
             for (int i = 0; i < 8; i += 2) top = mx_max_abs(top, v[i], v[i + 1]);
             uint32_t most = __float_as_uint(top);
-            most = max(most, __shfl_xor_sync(mask, most, 1));
-            most = max(most, __shfl_xor_sync(mask, most, 2));
+            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
             const uint32_t scale = mx_scale_of(most);
             const float inverse = mx_inverse(scale);
 #pragma unroll
@@ -142,9 +143,9 @@ __global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 *
             if (e < (A.hidden + kMxBlock - 1) / kMxBlock * kMxBlock)
                 *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(A.out) + row * A.out_stride + e / 2) = scale == 255 ? 0u : mx_codes8(v);
             uint32_t w = scale << 8 * (t / 4 % 4);
-            w |= __shfl_xor_sync(mask, w, 4);
-            w |= __shfl_xor_sync(mask, w, 8);
-            if (t % 16 == 0)
+            w |= __shfl_xor_sync(0xFFFFFFFFu, w, 4);
+            w |= __shfl_xor_sync(0xFFFFFFFFu, w, 8);
+            if (t % 16 == 0 && e < ends)
                 *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(A.out_scale) + mx_word_at(row, e / (kMxBlock * kMxTileBlocks), A.out_tiles)) = w;
         }
         return;
