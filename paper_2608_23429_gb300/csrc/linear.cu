@@ -131,9 +131,11 @@ int scales_map(CUtensorMap* map, const void* p, long long rows, long long featur
 // what takes the time then, [0] where they are long and stages are worth more. GB300, {1, 4} -> {4, 7}: 16384 x 8192 x 512 e4m3
 // with a bf16 output and hidden state 178 -> 150 us, fp32 hidden state alone 212 -> 192; 8192 x 1152 x 4608 64.1 -> 66.2 ({2, 5}).
 constexpr int kShortBlocks = 16, kMoreBoxes[2][2] = {{1, 4}, {4, 7}};
-// Operands in 4 bits, 8 warps for long sums and 12 for short ones. GB300, 8192 x 1152 x 4608 and 4608 x 4096 x 15360, bf16 gated with and without an
-// output: 8 warps 25.9 and 98.8 us, 12 (and so two stages fewer) 28.2 and 118; 8192 x 1152 x 1152 with an output 22.5 and 18.1.
-constexpr int kMxMoreBoxes[2][2] = {{1, 4}, {2, 4}};
+// Operands in 4 bits: 12 warps and hidden states of three chunks ahead where sums are short; where they are long two, as stages are worth more, and
+// 8 warps unless there is a bf16 hidden state alone. GB300, gated, 8192 x 1152 x 4608: bf16 with an output 8 warps 26.0 us, 12 (and so two stages
+// fewer) 28.2, bf16 alone 24.8 and 23.1, fp32 alone 29.2 and 32.1 (33 with four chunks ahead); 8192 x 1152 x 1152 with an output 22.5 and 18.1. An output stored
+// by the threads instead of its boxes: 18.1 -> 19.5, 32768 rows 47 -> 55.
+constexpr int kMxShortBoxes[2] = {1, 4};
 
 // Bytes of a row up to which a box's place in it (and a gate's piece's), and that of the box behind, is a positive int.
 constexpr long long kMaxRowBytes = (1LL << 31) - 1024;
@@ -166,9 +168,14 @@ int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
     if (e.resid_out) {
         const int out = !e.out ? 0 : e.out_bf16 ? 1 : 2, resid = e.resid_bf16 ? 1 : 2;
         const bool is_short = a->k_blocks <= kShortBlocks;
-        if (mx && !is_short) a->results = Results::kHiddenLong;
-        a->more_boxes = std::max((mx ? kMxMoreBoxes : kMoreBoxes)[is_short][resid - 1], out + 2 * resid - 2);
-        a->ring = (2 + a->more_boxes - out) / resid;
+        if (mx) {
+            a->results = is_short || (out == 0 && resid == 1) ? Results::kHidden : Results::kHiddenLong;
+            a->more_boxes = std::max(is_short ? kMxShortBoxes[resid - 1] + (resid == 1 ? out : 0) : 0, out + 2 * resid - 2);
+            a->ring = (2 + a->more_boxes - out) / resid;
+        } else {
+            a->more_boxes = std::max(kMoreBoxes[is_short][resid - 1], out + 2 * resid - 2);
+            a->ring = (2 + a->more_boxes - out) / resid;
+        }
     }
     return CB_OK;
 }
@@ -388,8 +395,12 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
                     : operand_map(&a.w_map, d.w, ep.N, a.k_bytes, w_row, a.tile_n / cg);
     // one box instead of two for each of the 12 warps makes room for a stage more (8192^3 to bf16 159 -> 152 us)
     a.out_boxes = a.results == Results::kQuant ? 0 : mx && a.results == Results::kOut && a.k_blocks > kShortBlocks ? 1 : 2;
-    const size_t fixed = linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes, a.out_boxes) : 0);
     const size_t stage = linear_stage_bytes(cg, a.tile_n) + (mx ? mx_scale_bytes(a.tile_n) : 0);
+    auto fixed_bytes = [&] { return linear_fixed_bytes(a.results, a.more_boxes) + (mx ? mx_more_bytes(a.results, a.more_boxes, a.out_boxes) : 0); };
+    // (4 bits) of hidden states two at least, and more where three stages are left
+    while (mx && resid && a.ring > 2 && fixed_bytes() + 3 * stage > (size_t)dev->smem) a.more_boxes -= ep.resid_bf16 ? 1 : 2, --a.ring;
+    if (a.results == Results::kHidden && mx && fixed_bytes() + 2 * stage > (size_t)dev->smem) a.results = Results::kHiddenLong;
+    const size_t fixed = fixed_bytes();
     if (fixed + 2 * stage > (size_t)dev->smem) rc = CB_ERR_LIMIT;  // (no device that the library is built for)
     a.stages = (int)std::min<size_t>(kMaxLinStages, (dev->smem - fixed) / stage);
     const long long tiles = (long long)a.tiles_m * a.tiles_n * a.parts, units = cg == 2 ? dev->pairs : dev->sms;

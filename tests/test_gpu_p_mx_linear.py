@@ -141,6 +141,8 @@ CASES = [
     case(300, 256, 320, resid="fp32", gate="bf16", tokens=1), case(300, 260, 320, resid="bf16", gate="fp32", tokens=31, pad=4),
     case(300, 264, 320, resid="fp32", gate="fp32", tokens=13, out=None), case(200, 264, 8192, resid="bf16", gate="bf16", tokens=7, out=None),
     case(5000, 264, 8192, resid="bf16", gate="bf16", tokens=33), case(2500, 1160, 5000, resid="fp32", gate="bf16", tokens=100, out="fp32"),
+    # hidden states in fp32 beside outputs in fp32: the most shared memory for boxes, over short and long sums
+    case(4000, 1152, 1152, resid="fp32", gate="bf16", tokens=500, out="fp32"), case(2000, 1152, 5000, resid="fp32", gate="fp32", tokens=500, out="bf16"),
     # outputs in 4 bits
     case(128, 64, 64, out="mx"), case(128, 192, 256, out="mx"), case(999, 1155, 577, "GELU", "mx"), case(256, 4608, 1152, "GELU", "mx"),
     case(1000, 1152, 4608, "SILU", "mx", xpad=2), case(300, 33, 100, out="mx"), case(400, 200, 8192, out="mx"), case(77, 31, 40, out="mx", bias="fp32"),

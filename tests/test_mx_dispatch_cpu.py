@@ -34,7 +34,7 @@ def run(stub, rows, n, k, out=None, resid=None, gate=None, **io):
 
 @pytest.mark.parametrize("rows,n,k,kw,results", [
     (1, 6912, 1152, dict(out=BF16), OUT), (4096, 4608, 1152, dict(out=FP32), OUT), (4096, 4608, 1152, dict(out=MX), QUANT), (8, 33, 40, dict(out=MX), QUANT),
-    (4096, 1152, 4096, dict(resid=BF16, gate=BF16), HIDDEN), (4096, 1152, 4097, dict(resid=BF16, out=BF16), HIDDEN_LONG),
+    (4096, 1152, 4096, dict(resid=BF16, gate=BF16), HIDDEN), (4096, 1152, 4097, dict(resid=FP32, out=BF16), HIDDEN_LONG),
     (999, 1155, 577, dict(resid=FP32, out=BF16), DIRECT), (999, 1155, 577, dict(out=BF16), DIRECT)])
 def test_how_results_leave(stub, rows, n, k, kw, results):
     rc, log = run(stub, rows, n, k, **kw)
@@ -79,3 +79,18 @@ def test_rows_that_end_inside_16_bytes_are_stored_by_the_threads(stub):
             stub[0].stub_reset()
             rc, log = run(stub, 300, n, 320, out_stride=264, resid_stride=264, resid_out_stride=264, gate_stride=264, **kw)
             assert rc == 0 and log[-1][1]["results"] == (DIRECT if off else results), (n, kw)
+
+
+@pytest.mark.parametrize("out", [None, BF16, FP32, MX])
+@pytest.mark.parametrize("resid", [None, BF16, FP32])
+def test_every_size_is_served(stub, out, resid):
+    """No choice of tiles leaves a kernel without shared memory for its stages."""
+    if (out is None and resid is None) or (out == MX and resid is not None):
+        return
+    lib = stub[0]
+    for rows in (1, 8, 40, 129, 300, 1000, 4096, 8192, 30000):
+        for n in (8, 64, 200, 1152, 4608, 12288):
+            for k in (32, 1152, 4096, 4608, 16384, 40000):
+                lib.stub_reset()
+                rc, log = run(stub, rows, n, k, out=out, resid=resid, gate=resid)
+                assert rc == 0 and "tc" in [c[0] for c in log], (rows, n, k)
