@@ -4,7 +4,7 @@
 // vectors (norm_around_rows.cuh), in shared memory where it is not (below). A layer norm takes two of them, one after the other:
 // the squares of what is left when the mean is off lose nothing where the mean is far larger than the deviation, as sums of squares
 // less the mean's square do. GB300, gate and modulation: 16384 x 4096 bf16 97 us (82 % of the copy rate), 8192 x 1152 to 4 bits 16.5, to bf16 16.1; fp32
-// stream, branch normed too, to e4m3 25 us; by elements 8192 x 4097 112 us, 16384 x 1153 to bf16 46, to 4 bits 51.
+// stream, branch normed too, to e4m3 25 us; by elements 8192 x 4097 86 us, 16384 x 1153 to bf16 44, to 4 bits 50, x 250 13.
 #include <cmath>
 
 #include "norm_around.cuh"
@@ -33,19 +33,32 @@ __device__ __forceinline__ void load_row(const void* p, long long e, int bf16, i
     }
 }
 
-// A row by elements, in registers: CH of them in each thread of its W warps. The lines are loaded with the row where there is room for
-// them, each when it is wanted where there is not (all of them early up to 1280 elements: 16384 x 1153 to 4 bits 93 us instead of 51).
-__host__ __device__ constexpr bool around_early(int CH, int W) { return CH * W <= 20; }
+// A row by elements, in registers: CH of them in each thread of its W warps. Short rows have a warp each, four to a CTA: there is nothing to wait
+// for but the row's own loads, and a CTA is launched for four rows (17300 x 220, layer norms, to fp32: 11.7 us, with four warps a row 25.9).
+// Their lines, and those of rows above 640 elements, are loaded when they are wanted, which leaves registers for more warps (220 elements 18.3 us
+// with the lines loaded early, 16384 x 1153 to 4 bits 93 instead of 51); four warps and up to 640 elements load them with the row, as few such
+// rows are bound by their loads' time (999 x 577 4.8 us; a warp each, late, 6.9).
+constexpr int kHeldRows = 4;  // warps of a CTA whose rows have a warp each
+__host__ __device__ constexpr int held_rows(int W) { return W == 1 ? kHeldRows : 1; }
+__host__ __device__ constexpr bool around_early(int CH, int W) { return W > 1 && CH * W <= 20; }
+// CTAs of an SM, by the registers that this leaves a thread: 40 for ten elements, 64 for sixteen, 80 for twenty.
+__host__ __device__ constexpr int around_ctas(int CH, int W) {
+    if (around_early(CH, W)) return 0;
+    if (W == 1) return CH <= 4 ? 12 : CH <= 8 ? 8 : 6;
+    if (W == 4) return 8;
+    return (CH <= 10 ? 1536 : CH <= 16 ? 1024 : 768) / (32 * W);
+}
 
 template <int CH, int W, int FULL>
-__global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 * W)) around_held_kernel(const __grid_constant__ AroundArgs args) {
+__global__ void __launch_bounds__(32 * W * held_rows(W), around_ctas(CH, W)) around_held_kernel(const __grid_constant__ AroundArgs args) {
     __shared__ uint32_t slots[5][W];
     constexpr int T = 32 * W;
     constexpr bool EARLY = around_early(CH, W);
     const AroundArgs A = args;  // in registers, as stores would have them read again
     after_previous();
-    const unsigned row = blockIdx.x;
-    const int t = threadIdx.x;
+    const unsigned row = W == 1 ? blockIdx.x * kHeldRows + threadIdx.x / T : blockIdx.x;
+    const int t = threadIdx.x % T;
+    if (W == 1 && row >= A.rows) return;
     auto on = [&](int c) { return c < FULL || c * T + t < A.hidden; };
     const long long line = (long long)(row / A.tokens) * A.line_stride;
     float early[7][CH];
@@ -117,13 +130,15 @@ __global__ void __launch_bounds__(32 * W, around_early(CH, W) ? 0 : 1024 / (32 *
     if (A.out_dtype == CB_MXFP4) {
         // Through shared memory to eight consecutive elements of a thread, so that a block is four lanes and a word of scales sixteen
         // (a block as a warp, a code by every other lane, took four times the instructions). Zeros fill up the last tile of scales.
-        extern __shared__ __align__(16) float turned[];
+        extern __shared__ __align__(16) float turned_rows[];
         const int ends = (int)A.out_tiles * kMxTileBlocks * kMxBlock;
+        float* const turned = turned_rows + (W == 1 ? threadIdx.x / T * ends : 0);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
             if (c * T + t < ends) turned[c * T + t] = on(c) ? h[c] : 0.0f;
         for (int e = CH * T + t; e < ends; e += T) turned[e] = 0.0f;
-        __syncthreads();
+        if (W == 1) __syncwarp();
+        else __syncthreads();
         for (int first = t / 32 * 256; first < ends; first += T * 8) {  // (of the warp; it ends with a word of scales, sixteen lanes)
             const int e = first + t % 32 * 8;
             float v[8] = {}, top = 0.0f;
@@ -272,9 +287,10 @@ __global__ void __launch_bounds__(32 * W) around_elements_kernel(const __grid_co
 
 template <int CH, int W, int FULL>
 cudaError_t launch_held(const AroundArgs& a, cudaStream_t s) {
+    constexpr int rows = held_rows(W);
     // (33 KB at most)
-    const size_t smem = a.out && a.out_dtype == CB_MXFP4 ? (size_t)a.out_tiles * kMxTileBlocks * kMxBlock * 4 : 0;
-    return launch_overlapped(around_held_kernel<CH, W, FULL>, (int)a.rows, 32 * W, smem, s, a);
+    const size_t smem = a.out && a.out_dtype == CB_MXFP4 ? (size_t)a.out_tiles * kMxTileBlocks * kMxBlock * 4 * rows : 0;
+    return launch_overlapped(around_held_kernel<CH, W, FULL>, (int)((a.rows + rows - 1) / rows), 32 * W * rows, smem, s, a);
 }
 template <int W, bool HELD>
 cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
@@ -290,15 +306,30 @@ cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
 cudaError_t launch_row(AroundArgs& a, bool vec, int sms, cudaStream_t s) {
     const int n = a.hidden;
     if (vec && n <= 16384) return a.param_bf16 ? launch_around_bf16_lines(a, sms, s) : launch_around_fp32_lines(a, sms, s);
-    if (n <= 256) return launch_held<2, 4, 0>(a, s);
+    // A warp a row up to 256 elements (250: 1000 rows 4.4 us, four warps 5.7; 16384 rows 12.9 and 28.8), and up to 768 where the rows are more
+    // than CTAs of four warps fit on the SMs, 12 on each (577: 1000 rows 6.9, four warps 4.8; 1500 rows 7.1 and 7.2; 3000 rows 7.4 and 10.3;
+    // 16384 rows 29 and 49; 16384 x 700 34 and 47, x 801 44 and 47, x 1153 59 and 54).
+    if (n <= 256 || (n <= 768 && a.rows > 12u * sms)) {
+        if (n <= 64) return launch_held<2, 1, 0>(a, s);
+        if (n <= 128) return launch_held<4, 1, 2>(a, s);
+        if (n <= 192) return launch_held<6, 1, 4>(a, s);
+        if (n <= 256) return launch_held<8, 1, 6>(a, s);
+        if (n <= 384) return launch_held<12, 1, 8>(a, s);
+        if (n <= 512) return launch_held<16, 1, 12>(a, s);
+        if (n <= 640) return launch_held<20, 1, 16>(a, s);
+        return launch_held<24, 1, 20>(a, s);
+    }
     if (n <= 384) return launch_held<3, 4, 2>(a, s);
     if (n <= 640) return launch_held<5, 4, 3>(a, s);
+    // as few warps as hold the row: twice as many with half the elements each took 8192 x 2047 from 45 to 52 us, x 3383 from 88 to 106, x 5001
+    // from 114 to 121; half as many with twice the elements 8192 x 2047 to 49, x 4095 from 92 to 94, x 7001 from 193 to 199
     if (n <= 1024) return launch_held<8, 4, 5>(a, s);
     if (n <= 1280) return launch_held<10, 4, 8>(a, s);
-    if (n <= 2048) return launch_held<8, 8, 5>(a, s);
+    if (n <= 2048) return launch_held<16, 4, 10>(a, s);
     if (n <= 2560) return launch_held<10, 8, 8>(a, s);
-    if (n <= 4096) return launch_held<8, 16, 5>(a, s);
-    if (n <= 5120) return launch_held<10, 16, 8>(a, s);
+    if (n <= 4096) return launch_held<16, 8, 10>(a, s);
+    if (n <= 5120) return launch_held<20, 8, 16>(a, s);
+    if (n <= 6144) return launch_held<12, 16, 10>(a, s);
     if (n <= 8192) return launch_held<16, 16, 10>(a, s);
     if (n <= kAroundHeld) return launch_elements<16, true>(a, s);
     return launch_elements<16, false>(a, s);

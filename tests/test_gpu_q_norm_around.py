@@ -179,6 +179,14 @@ def test_sizes(lib, hidden):
             check(lib, case(rows, hidden, after, before, x, out=out, tokens=50))
 
 
+@pytest.mark.parametrize("hidden", [255, 257, 383, 385, 511, 577, 640, 641, 767, 768, 769])
+def test_many_short_rows_by_elements(lib, hidden):
+    """More rows than have four warps each at once, in a number that fills no CTA."""
+    pad = 1 if hidden % 8 == 0 else 0
+    for after, before, out, x in (("rms", "layer", "mx", "bf16"), ("layer", "rms", "bf16", "fp32"), ("none", "layer", "e4m3", "bf16"), ("layer", "layer", "fp32", "fp32")):
+        check(lib, case(2051, hidden, after, before, x, out=out, tokens=700, pad=0 if out == "mx" else pad, off=0 if out == "mx" else pad))
+
+
 @pytest.mark.parametrize("c", [
     case(200, 256, pad=8, off=8), case(200, 256, pad=1, off=1), case(200, 250, pad=6, off=3), case(129, 1152, pad=1152, off=1152, out="mx"),
     case(129, 1152, pad=4, out="mx"), case(130, 130, pad=3, out="mx", x="fp32"), case(64, 640, pad=4, x="fp32", branch="fp32", param="fp32", out="fp32"),
