@@ -141,25 +141,36 @@ constexpr int kMxShortBoxes[2] = {1, 4};
 constexpr long long kMaxRowBytes = (1LL << 31) - 1024;
 
 // Results and hidden states whose rows lie on the 16-byte grid go by TMA, in boxes of 32 rows by 64 bytes.
+struct TmaRows {
+    const void* p;
+    long long row, es;
+    CUtensorMap* map;
+};
+struct TmaResults {
+    TmaRows used[3];
+};
+TmaResults tma_results(const cb_linear_io* io, LinearArgs* a) {
+    const LinearEpilogue& e = a->e;
+    return {{{e.out, e.out_stride, (long long)bytes_of(io->out_dtype), &a->out_map},
+             {e.resid, e.resid_stride, (long long)bytes_of(io->resid_dtype), &a->resid_map},
+             {e.resid_out, e.resid_out_stride, (long long)bytes_of(io->resid_dtype), &a->resid_out_map}}};
+}
+bool goes_by_tma(const cb_linear_io* io, LinearArgs* a) {
+    const LinearEpilogue& e = a->e;
+    for (const auto& u : tma_results(io, a).used)
+        // (a store writes whole pieces of 16 bytes, past the end of a row that is not made of them)
+        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40 || e.N * u.es > kMaxRowBytes || e.N * u.es % 16 != 0))
+            return false;
+    // a gate's pieces of 16 bytes are read whole
+    const long long gs = (long long)bytes_of(io->gate_dtype);
+    return !e.gate || (on_grid(e.gate, 16) && e.gate_stride * gs % 16 == 0 && e.N * gs % 16 == 0 && e.N * gs <= kMaxRowBytes);
+}
 int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
     const LinearEpilogue& e = a->e;
     a->results = Results::kDirect;
     const bool mx = a->operands == Operands::kMx;
-    const struct {
-        const void* p;
-        long long row, es;
-        CUtensorMap* map;
-    } used[] = {{e.out, e.out_stride, (long long)bytes_of(io->out_dtype), &a->out_map},
-                {e.resid, e.resid_stride, (long long)bytes_of(io->resid_dtype), &a->resid_map},
-                {e.resid_out, e.resid_out_stride, (long long)bytes_of(io->resid_dtype), &a->resid_out_map}};
-    for (const auto& u : used)
-        // (a store writes whole pieces of 16 bytes, past the end of a row that is not made of them)
-        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40 || e.N * u.es > kMaxRowBytes || e.N * u.es % 16 != 0))
-            return CB_OK;
-    // a gate's pieces of 16 bytes are read whole
-    const long long gs = (long long)bytes_of(io->gate_dtype);
-    if (e.gate && (!on_grid(e.gate, 16) || e.gate_stride * gs % 16 != 0 || e.N * gs % 16 != 0 || e.N * gs > kMaxRowBytes)) return CB_OK;
-    for (const auto& u : used) {
+    if (!goes_by_tma(io, a)) return CB_OK;
+    for (const auto& u : tma_results(io, a).used) {
         if (!u.p) continue;
         const int rc = operand_map(u.map, u.p, e.M, e.N * u.es, u.row * u.es, 32, 64);
         if (rc != CB_OK) return rc;
@@ -207,6 +218,9 @@ constexpr int kMaxParts = 8, kPartSlabs = 8;  // no part is shorter
 // take as long the smaller ones, on more SMs. A launch of pairs starts later than one of single CTAs, which counts where products are this
 // fast. GB300: 42 x 280 x 9752 12.3 us where slabs count by their bytes, 8.5 so; 256 x 4608 x 1152 with GELU 5.5 us in pairs,
 // 4.7 in single CTAs, 4096^3 29.0 and 26.8.
+// Results by the threads over short sums in tiles of 128 columns at most, a chunk of 32 for each warp of four, where 192 give two of them a second one:
+// 6036 rows, gated fp32 hidden state and output, K = 1152, 4097 columns 92 -> 76 us, 1153 34 -> 25, K = 4608 98 -> 85 and 39 -> 31; in bf16 K = 1152
+// 64 -> 59 and 28 -> 22, K = 4608 67 and 70, 32 and 27; an output with GELU alone, K = 2304 37 -> 36 and 18 -> 15, K = 4608 46 and 55, 22 and 22.
 constexpr double kMxSlabClocks = 320, kMxPairClocks = 3000;
 void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int step, int max_parts, int x_rows, double least, double pair, int* cg, int* tile_n, int* parts) {
     double best = 1e300;
@@ -343,7 +357,8 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.pass_blocks = fp32 ? (mx ? kPassMx : d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
     // (4 bits) rows that x does not have are not loaded: what the tensor cores read in their place makes sums that nobody takes
     a.x_rows = mx ? std::min(128, (ep.M + 7) / 8 * 8) : 128;
-    choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks ? 128 : mx ? kMxMostN : 256, mx ? kMxStepN : 32,
+    const bool narrow = mx && !out_mx && a.k_blocks <= (!resid ? kShortBlocks / 2 : ep.resid_bf16 ? kShortBlocks : 2 * kShortBlocks) && !goes_by_tma(io, &a);
+    choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks || narrow ? 128 : mx ? kMxMostN : 256, mx ? kMxStepN : 32,
                 out_mx ? 1 : kMaxParts, a.x_rows, mx ? kMxSlabClocks : 0.0, mx ? kMxPairClocks : 0.0, &cg, &a.tile_n, &a.parts);
     a.part_blocks = (a.k_blocks + a.parts - 1) / a.parts;
     a.parts = (a.k_blocks + a.part_blocks - 1) / a.part_blocks;
