@@ -219,7 +219,7 @@ constexpr int kMaxParts = 8, kPartSlabs = 8;  // no part is shorter
 // fast. GB300: 42 x 280 x 9752 12.3 us where slabs count by their bytes, 8.5 so; 256 x 4608 x 1152 with GELU 5.5 us in pairs,
 // 4.7 in single CTAs, 4096^3 29.0 and 26.8.
 // Results by the threads over short sums in tiles of 128 columns at most, a chunk of 32 for each warp of four, where 192 give two of them a second one:
-// 6036 rows, gated fp32 hidden state and output, K = 1152, 4097 columns 92 -> 76 us, 1153 34 -> 25, K = 4608 98 -> 85 and 39 -> 31; in bf16 K = 1152
+// 6036 rows, gated fp32 hidden state and output, K = 1152, 4097 columns 92 -> 76 us, 1153 34 -> 25, K = 4608 98 -> 85 and 39 -> 31, K = 8192 112 and 121, 46 and 44; in bf16 K = 1152
 // 64 -> 59 and 28 -> 22, K = 4608 67 and 70, 32 and 27; an output with GELU alone, K = 2304 37 -> 36 and 18 -> 15, K = 4608 46 and 55, 22 and 22.
 constexpr double kMxSlabClocks = 320, kMxPairClocks = 3000;
 void choose_tile(const Device& dev, int M, int N, int k_blocks, int most, int step, int max_parts, int x_rows, double least, double pair, int* cg, int* tile_n, int* parts) {
@@ -357,7 +357,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     a.pass_blocks = fp32 ? (mx ? kPassMx : d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
     // (4 bits) rows that x does not have are not loaded: what the tensor cores read in their place makes sums that nobody takes
     a.x_rows = mx ? std::min(128, (ep.M + 7) / 8 * 8) : 128;
-    const bool narrow = mx && !out_mx && a.k_blocks <= (!resid ? kShortBlocks / 2 : ep.resid_bf16 ? kShortBlocks : 2 * kShortBlocks) && !goes_by_tma(io, &a);
+    const bool narrow = mx && !out_mx && a.k_blocks <= (!resid ? kShortBlocks / 2 : ep.resid_bf16 ? kShortBlocks : kShortBlocks * 3 / 2) && !goes_by_tma(io, &a);
     choose_tile(*dev, ep.M, ep.N, a.k_blocks, a.k_blocks > a.pass_blocks || narrow ? 128 : mx ? kMxMostN : 256, mx ? kMxStepN : 32,
                 out_mx ? 1 : kMaxParts, a.x_rows, mx ? kMxSlabClocks : 0.0, mx ? kMxPairClocks : 0.0, &cg, &a.tile_n, &a.parts);
     a.part_blocks = (a.k_blocks + a.parts - 1) / a.parts;
