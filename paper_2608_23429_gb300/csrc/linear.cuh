@@ -149,16 +149,15 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
 // One element as fp32 bits, or its half of them. Not volatile, as the compiler then keeps such loads, and the branches between them, in
 // line (GB300, 8192 x 8191 x 512 with a fp32 hidden state 146 -> 156 us, 256 x 1152 x 4608 in parts of K 11.4 -> 12.3): the
 // epilogue's pointers come from from_here instead.
-__device__ __forceinline__ uint32_t lin_ld1(const void* p, long long e, int bf16) {
-    uint32_t r = 0;
-    if (bf16) {
-        uint16_t h;
-        asm("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(reinterpret_cast<const uint16_t*>(p) + e));
-        r = (uint32_t)h << 16;
-    } else {
-        asm("ld.global.u32 %0, [%1];" : "=r"(r) : "l"(reinterpret_cast<const uint32_t*>(p) + e));
-    }
+__device__ __forceinline__ uint32_t lin_raw1(const void* p, long long e, int bf16) {  // (bf16 in the lower half)
+    uint32_t r;
+    if (bf16) asm("ld.global.u16 %0, [%1];" : "=r"(r) : "l"(reinterpret_cast<const uint16_t*>(p) + e));
+    else asm("ld.global.u32 %0, [%1];" : "=r"(r) : "l"(reinterpret_cast<const uint32_t*>(p) + e));
     return r;
+}
+__device__ __forceinline__ uint32_t lin_ld1(const void* p, long long e, int bf16) {
+    const uint32_t r = lin_raw1(p, e, bf16);
+    return bf16 ? r << 16 : r;
 }
 
 __device__ __forceinline__ void lin_put1(void* p, long long e, int bf16, float v) {

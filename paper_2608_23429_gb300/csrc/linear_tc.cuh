@@ -509,11 +509,11 @@ __device__ __forceinline__ void look_rows(const LinearEpilogue& E, int row, int 
     if (E.resid_bf16) {
 #pragma unroll
         for (int i = 0; i < 8; ++i, q += step)
-            if (row + i < E.M) asm("ld.global.u16 %0, [%1];" : "=r"(r[i]) : "l"(q));
+            if (row + i < E.M) r[i] = lin_raw1(q, 0, 1);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i, q += step)
-            if (row + i < E.M) asm("ld.global.u32 %0, [%1];" : "=r"(r[i]) : "l"(q));
+            if (row + i < E.M) r[i] = lin_raw1(q, 0, 0);
     }
 }
 
