@@ -1,7 +1,7 @@
 // cb_norm_around: the norm after a branch, its addition to the hidden state, and the norm before the next branch.
 //
 // Bound by HBM: a row is read once and written once, and stays on the SM between its reductions: in registers where it is reached by
-// vectors (norm_around_rows.cuh), in shared memory where it is not (below). A layer norm takes two of them, one after the other:
+// vectors (norm_around_rows.cuh) and up to 8192 elements where it is not, else in shared memory (below). A layer norm takes two of them, one after the other:
 // the squares of what is left when the mean is off lose nothing where the mean is far larger than the deviation, as sums of squares
 // less the mean's square do. GB300, gate and modulation: 16384 x 4096 bf16 97 us (82 % of the copy rate), 8192 x 1152 to 4 bits 16.5, to bf16 16.1; fp32
 // stream, branch normed too, to e4m3 25 us; by elements 8192 x 4097 86 us, 16384 x 1153 to bf16 44, to 4 bits 50, x 250 13.
@@ -14,22 +14,59 @@ namespace {
 
 constexpr int kAroundHeld = 49152;  // elements of a row in shared memory
 
-// Elements t, t + T, ... of a row from p on. The first FULL lie in every row that the kernel is launched for, at places that the compiler knows:
-// a select and an address for each of them took a third of the kernel's instructions. Threads behind the row's end read its start.
-template <int CH, int T, int FULL>
+// Pieces t, t + T, ... of V elements (one, or two on their grid) of a row from p on. The first FULL lie in every row that the kernel is launched
+// for, at places that the compiler knows: a select and an address for each of them took a third of the kernel's instructions. Threads behind the
+// row's end read its start.
+template <int CH, int T, int FULL, int V>
 __device__ __forceinline__ void load_row(const void* p, long long e, int bf16, int t, int hidden, float* v) {
-    auto at = [&](int c) { return c < FULL || c * T + t < hidden ? c * T : -t; };
+    auto at = [&](int c) { return c < FULL || (c * T + t) * V < hidden ? c * T : -t; };
     if (bf16) {
-        const uint16_t* const q = reinterpret_cast<const uint16_t*>(p) + e + t;
-        uint16_t w[CH];
+        const uint16_t* const q = reinterpret_cast<const uint16_t*>(p) + e + t * V;
+        if constexpr (V == 2) {
+            uint32_t w[CH];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) w[c] = q[at(c)];
+            for (int c = 0; c < CH; ++c) w[c] = reinterpret_cast<const uint32_t*>(q)[at(c)];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = __uint_as_float((uint32_t)w[c] << 16);
+            for (int c = 0; c < CH; ++c) v[2 * c] = __uint_as_float(w[c] << 16), v[2 * c + 1] = __uint_as_float(w[c] & 0xFFFF0000u);
+        } else {
+            uint16_t w[CH];
+#pragma unroll
+            for (int c = 0; c < CH; ++c) w[c] = q[at(c)];
+#pragma unroll
+            for (int c = 0; c < CH; ++c) v[c] = __uint_as_float((uint32_t)w[c] << 16);
+        }
     } else {
-        const float* const q = reinterpret_cast<const float*>(p) + e + t;
+        const float* const q = reinterpret_cast<const float*>(p) + e + t * V;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = q[at(c)];
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (V == 2) {
+                const float2 f = reinterpret_cast<const float2*>(q)[at(c)];
+                v[2 * c] = f.x, v[2 * c + 1] = f.y;
+            } else {
+                v[c] = q[at(c)];
+            }
+        }
+    }
+}
+template <int CH, int T, int V>
+__device__ __forceinline__ void store_row(void* p, long long e, int dtype, int t, int hidden, const float* v) {
+    if constexpr (V == 1) {
+        store_all<CH, T>(p, e, dtype, t, hidden, v);
+    } else if (dtype == CB_BF16) {
+        uint32_t* const q = reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(p) + e) + t;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if ((c * T + t) * 2 < hidden) q[c * T] = norm_bf16x2(v[2 * c], v[2 * c + 1]);
+    } else if (dtype == CB_FP32) {
+        float2* const q = reinterpret_cast<float2*>(reinterpret_cast<float*>(p) + e) + t;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if ((c * T + t) * 2 < hidden) q[c * T] = make_float2(v[2 * c], v[2 * c + 1]);
+    } else {
+        uint16_t* const q = reinterpret_cast<uint16_t*>(reinterpret_cast<uint8_t*>(p) + e) + t;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if ((c * T + t) * 2 < hidden) q[c * T] = (uint16_t)norm_e4m3x2(v[2 * c], v[2 * c + 1]);
     }
 }
 
@@ -40,7 +77,7 @@ __device__ __forceinline__ void load_row(const void* p, long long e, int bf16, i
 // rows are bound by their loads' time (999 x 577 4.8 us; a warp each, late, 6.9).
 constexpr int kHeldRows = 4;  // warps of a CTA whose rows have a warp each
 __host__ __device__ constexpr int held_rows(int W) { return W == 1 ? kHeldRows : 1; }
-__host__ __device__ constexpr bool around_early(int CH, int W) { return W > 1 && CH * W <= 20; }
+__host__ __device__ constexpr bool around_early(int CH, int W) { return W > 1 && CH * W <= 24; }
 // CTAs of an SM, by the registers that this leaves a thread: 40 for ten elements, 64 for sixteen, 80 for twenty.
 __host__ __device__ constexpr int around_ctas(int CH, int W) {
     if (around_early(CH, W)) return 0;
@@ -49,54 +86,54 @@ __host__ __device__ constexpr int around_ctas(int CH, int W) {
     return (CH <= 10 ? 1536 : CH <= 16 ? 1024 : 768) / (32 * W);
 }
 
-template <int CH, int W, int FULL>
-__global__ void __launch_bounds__(32 * W * held_rows(W), around_ctas(CH, W)) around_held_kernel(const __grid_constant__ AroundArgs args) {
+template <int CH, int W, int FULL, int V>
+__global__ void __launch_bounds__(32 * W * held_rows(W), around_ctas(CH * V, W)) around_held_kernel(const __grid_constant__ AroundArgs args) {
     __shared__ uint32_t slots[5][W];
-    constexpr int T = 32 * W;
-    constexpr bool EARLY = around_early(CH, W);
+    constexpr int T = 32 * W, N = CH * V;
+    constexpr bool EARLY = around_early(CH * V, W);
     const AroundArgs A = args;  // in registers, as stores would have them read again
     after_previous();
     const unsigned row = W == 1 ? blockIdx.x * kHeldRows + threadIdx.x / T : blockIdx.x;
     const int t = threadIdx.x % T;
     if (W == 1 && row >= A.rows) return;
-    auto on = [&](int c) { return c < FULL || c * T + t < A.hidden; };
+    auto on = [&](int i) { return i / V < FULL || (i / V * T + t) * V < A.hidden; };  // its element i
     const long long line = (long long)(row / A.tokens) * A.line_stride;
-    float early[7][CH];
+    float early[7][CH * V];
     auto look = [&](int i, const void* p, long long at) {
-        if (EARLY && p) load_row<CH, T, FULL>(p, at, A.param_bf16, t, A.hidden, early[i]);
+        if (EARLY && p) load_row<CH, T, FULL, V>(p, at, A.param_bf16, t, A.hidden, early[i]);
     };
     // v = f(v, line), of line i at p
-    auto with_line = [&](int i, const void* p, long long at, float (&v)[CH], auto f) {
+    auto with_line = [&](int i, const void* p, long long at, float (&v)[CH * V], auto f) {
         if (!p) return;
-        float late[CH];
-        if (!EARLY) load_row<CH, T, FULL>(p, at, A.param_bf16, t, A.hidden, late);
+        float late[CH * V];
+        if (!EARLY) load_row<CH, T, FULL, V>(p, at, A.param_bf16, t, A.hidden, late);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = f(v[c], EARLY ? early[i][c] : late[c]);
+        for (int c = 0; c < N; ++c) v[c] = f(v[c], EARLY ? early[i][c] : late[c]);
     };
-    auto normalise = [&](float (&v)[CH], int kind, float eps, uint32_t (*s)[W]) {
+    auto normalise = [&](float (&v)[CH * V], int kind, float eps, uint32_t (*s)[W]) {
         if (kind == CB_NORM_LAYER) {
             float sum = 0.0f;
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < N; ++c)
                 if (on(c)) sum += v[c];
             const float mean = __uint_as_float(row_reduce<W, false>(__float_as_uint(sum), s[0])) * A.inv_hidden;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) v[c] -= mean;
+            for (int c = 0; c < N; ++c) v[c] -= mean;
         }
         float sum = 0.0f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < N; ++c)
             if (on(c)) sum = fmaf(v[c], v[c], sum);
         sum = __uint_as_float(row_reduce<W, false>(__float_as_uint(sum), s[1]));
         const float rstd = 1.0f / sqrtf(fmaf(sum, A.inv_hidden, eps));
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] *= rstd;
+        for (int c = 0; c < N; ++c) v[c] *= rstd;
     };
     const auto times = [](float v, float w) { return v * w; };
     const auto plus = [](float v, float w) { return v + w; };
-    float h[CH], r[CH];
-    load_row<CH, T, FULL>(A.x, row * A.x_stride, A.x_bf16, t, A.hidden, h);
-    if (A.branch) load_row<CH, T, FULL>(A.branch, row * A.branch_stride, A.branch_bf16, t, A.hidden, r);
+    float h[CH * V], r[CH * V];
+    load_row<CH, T, FULL, V>(A.x, row * A.x_stride, A.x_bf16, t, A.hidden, h);
+    if (A.branch) load_row<CH, T, FULL, V>(A.branch, row * A.branch_stride, A.branch_bf16, t, A.hidden, r);
     look(0, A.after_weight, 0);
     look(1, A.after_bias, 0);
     look(2, A.gate, line);
@@ -106,7 +143,7 @@ __global__ void __launch_bounds__(32 * W * held_rows(W), around_ctas(CH, W)) aro
     look(6, A.shift, line);
     if (A.x_factor != 1.0f) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) h[c] *= A.x_factor;
+        for (int c = 0; c < N; ++c) h[c] *= A.x_factor;
     }
     if (A.branch) {
         if (A.after != CB_NORM_NONE) {
@@ -116,9 +153,9 @@ __global__ void __launch_bounds__(32 * W * held_rows(W), around_ctas(CH, W)) aro
         }
         with_line(2, A.gate, line, r, times);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) h[c] = fmaf(r[c], A.branch_factor, h[c]);
+        for (int c = 0; c < N; ++c) h[c] = fmaf(r[c], A.branch_factor, h[c]);
     }
-    if (A.x_out) store_all<CH, T>(A.x_out, row * A.x_out_stride, A.x_bf16 ? CB_BF16 : CB_FP32, t, A.hidden, h);
+    if (A.x_out) store_row<CH, T, V>(A.x_out, row * A.x_out_stride, A.x_bf16 ? CB_BF16 : CB_FP32, t, A.hidden, h);
     if (!A.out) return;
     if (A.before != CB_NORM_NONE) {
         normalise(h, A.before, A.before_eps, slots + 2);
@@ -134,9 +171,11 @@ __global__ void __launch_bounds__(32 * W * held_rows(W), around_ctas(CH, W)) aro
         const int ends = (int)A.out_tiles * kMxTileBlocks * kMxBlock;
         float* const turned = turned_rows + (W == 1 ? threadIdx.x / T * ends : 0);
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
-            if (c * T + t < ends) turned[c * T + t] = on(c) ? h[c] : 0.0f;
-        for (int e = CH * T + t; e < ends; e += T) turned[e] = 0.0f;
+        for (int c = 0; c < N; ++c) {
+            const int e = (c / V * T + t) * V + c % V;
+            if (e < ends) turned[e] = on(c) ? h[c] : 0.0f;
+        }
+        for (int e = N * T + t; e < ends; e += T) turned[e] = 0.0f;
         if (W == 1) __syncwarp();
         else __syncthreads();
         for (int first = t / 32 * 256; first < ends; first += T * 8) {  // (of the warp; it ends with a word of scales, sixteen lanes)
@@ -168,15 +207,15 @@ __global__ void __launch_bounds__(32 * W * held_rows(W), around_ctas(CH, W)) aro
     if (A.out_dtype == CB_E4M3) {
         float amax = 0.0f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < N; ++c)
             if (on(c)) amax = max_abs(amax, h[c]);
         const float s = norm_scale_of(row_reduce<W, true>(__float_as_uint(amax) & 0x7FFFFFFFu, slots[4]));
         if (t == 0) reinterpret_cast<float*>(A.out_scale)[row] = s;
         const float inv = __frcp_rn(s);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) h[c] *= inv;
+        for (int c = 0; c < N; ++c) h[c] *= inv;
     }
-    store_all<CH, T>(A.out, row * A.out_stride, A.out_dtype, t, A.hidden, h);
+    store_row<CH, T, V>(A.out, row * A.out_stride, A.out_dtype, t, A.hidden, h);
 }
 
 // Longer rows by elements; HELD: in shared memory, else read again for each reduction.
@@ -285,12 +324,12 @@ __global__ void __launch_bounds__(32 * W) around_elements_kernel(const __grid_co
     }
 }
 
-template <int CH, int W, int FULL>
+template <int CH, int W, int FULL, int V>
 cudaError_t launch_held(const AroundArgs& a, cudaStream_t s) {
     constexpr int rows = held_rows(W);
     // (33 KB at most)
     const size_t smem = a.out && a.out_dtype == CB_MXFP4 ? (size_t)a.out_tiles * kMxTileBlocks * kMxBlock * 4 * rows : 0;
-    return launch_overlapped(around_held_kernel<CH, W, FULL>, (int)((a.rows + rows - 1) / rows), 32 * W * rows, smem, s, a);
+    return launch_overlapped(around_held_kernel<CH, W, FULL, V>, (int)((a.rows + rows - 1) / rows), 32 * W * rows, smem, s, a);
 }
 template <int W, bool HELD>
 cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
@@ -303,34 +342,41 @@ cudaError_t launch_elements(const AroundArgs& a, cudaStream_t s) {
     return launch_overlapped(k, (int)a.rows, 32 * W, smem, s, a);
 }
 
-cudaError_t launch_row(AroundArgs& a, bool vec, int sms, cudaStream_t s) {
+// Rows of up to 8192 elements, by V at a time: pairs where all rows have them, 16384 x 300 17.5 -> 14.9 us, x 1276 55 -> 45, 8192 x 3380 86 -> 72.
+template <int V>
+cudaError_t launch_held_row(const AroundArgs& a, int sms, cudaStream_t s) {
     const int n = a.hidden;
-    if (vec && n <= 16384) return a.param_bf16 ? launch_around_bf16_lines(a, sms, s) : launch_around_fp32_lines(a, sms, s);
     // A warp a row up to 256 elements (250: 1000 rows 4.4 us, four warps 5.7; 16384 rows 12.9 and 28.8), and up to 768 where the rows are more
     // than CTAs of four warps fit on the SMs, 12 on each (577: 1000 rows 6.9, four warps 4.8; 1500 rows 7.1 and 7.2; 3000 rows 7.4 and 10.3;
     // 16384 rows 29 and 49; 16384 x 700 34 and 47, x 801 44 and 47, x 1153 59 and 54).
     if (n <= 256 || (n <= 768 && a.rows > 12u * sms)) {
-        if (n <= 64) return launch_held<2, 1, 0>(a, s);
-        if (n <= 128) return launch_held<4, 1, 2>(a, s);
-        if (n <= 192) return launch_held<6, 1, 4>(a, s);
-        if (n <= 256) return launch_held<8, 1, 6>(a, s);
-        if (n <= 384) return launch_held<12, 1, 8>(a, s);
-        if (n <= 512) return launch_held<16, 1, 12>(a, s);
-        if (n <= 640) return launch_held<20, 1, 16>(a, s);
-        return launch_held<24, 1, 20>(a, s);
+        if (n <= 64) return launch_held<2 / V, 1, 0 / V, V>(a, s);
+        if (n <= 128) return launch_held<4 / V, 1, 2 / V, V>(a, s);
+        if (n <= 192) return launch_held<6 / V, 1, 4 / V, V>(a, s);
+        if (n <= 256) return launch_held<8 / V, 1, 6 / V, V>(a, s);
+        if (n <= 384) return launch_held<12 / V, 1, 8 / V, V>(a, s);
+        if (n <= 512) return launch_held<16 / V, 1, 12 / V, V>(a, s);
+        if (n <= 640) return launch_held<20 / V, 1, 16 / V, V>(a, s);
+        return launch_held<24 / V, 1, 20 / V, V>(a, s);
     }
-    if (n <= 384) return launch_held<3, 4, 2>(a, s);
-    if (n <= 640) return launch_held<5, 4, 3>(a, s);
+    if (n <= 384) return launch_held<(2 + V) / V, 4, 2 / V, V>(a, s);
+    if (n <= 640) return launch_held<(4 + V) / V, 4, 3 / V, V>(a, s);
     // as few warps as hold the row: twice as many with half the elements each took 8192 x 2047 from 45 to 52 us, x 3383 from 88 to 106, x 5001
     // from 114 to 121; half as many with twice the elements 8192 x 2047 to 49, x 4095 from 92 to 94, x 7001 from 193 to 199
-    if (n <= 1024) return launch_held<8, 4, 5>(a, s);
-    if (n <= 1280) return launch_held<10, 4, 8>(a, s);
-    if (n <= 2048) return launch_held<16, 4, 10>(a, s);
-    if (n <= 2560) return launch_held<10, 8, 8>(a, s);
-    if (n <= 4096) return launch_held<16, 8, 10>(a, s);
-    if (n <= 5120) return launch_held<20, 8, 16>(a, s);
-    if (n <= 6144) return launch_held<12, 16, 10>(a, s);
-    if (n <= 8192) return launch_held<16, 16, 10>(a, s);
+    if (n <= 1024) return launch_held<8 / V, 4, 5 / V, V>(a, s);
+    if (n <= 1280) return launch_held<10 / V, 4, 8 / V, V>(a, s);
+    if (n <= 2048) return launch_held<16 / V, 4, 10 / V, V>(a, s);
+    if (n <= 2560) return launch_held<10 / V, 8, 8 / V, V>(a, s);
+    if (n <= 4096) return launch_held<16 / V, 8, 10 / V, V>(a, s);
+    if (n <= 5120) return launch_held<20 / V, 8, 16 / V, V>(a, s);
+    if (n <= 6144) return launch_held<12 / V, 16, 10 / V, V>(a, s);
+    return launch_held<16 / V, 16, 10 / V, V>(a, s);
+}
+
+cudaError_t launch_row(AroundArgs& a, bool vec, bool pairs, int sms, cudaStream_t s) {
+    const int n = a.hidden;
+    if (vec && n <= 16384) return a.param_bf16 ? launch_around_bf16_lines(a, sms, s) : launch_around_fp32_lines(a, sms, s);
+    if (n <= 8192) return pairs ? launch_held_row<2>(a, sms, s) : launch_held_row<1>(a, sms, s);
     if (n <= kAroundHeld) return launch_elements<16, true>(a, s);
     return launch_elements<16, false>(a, s);
 }
@@ -398,18 +444,19 @@ extern "C" int cb_norm_around(const cb_norm_around_desc* d, const void* x, const
                 {bias, d->param_dtype, 0},              {scale, d->param_dtype, a.line_stride},
                 {shift, d->param_dtype, a.line_stride}, {x_out, d->x_dtype, a.x_out_stride},
                 {mx ? nullptr : out, d->out_dtype, a.out_stride}};
-    bool vec = d->hidden % 8 == 0;
+    bool vec = d->hidden % 8 == 0, pairs = d->hidden % 2 == 0;
     for (const auto& u : used) {
         const size_t es = bytes_of(u.dtype), grid = es == 1 ? 8 : 16;
         if (!u.p) continue;
         if (!on_grid(u.p, es)) return CB_ERR_ALIGN;
         vec = vec && on_grid(u.p, grid) && (size_t)u.stride * es % grid == 0;
+        pairs = pairs && on_grid(u.p, 2 * es) && u.stride % 2 == 0;
     }
     if (mx && (!on_grid(out, 16) || !on_grid(out_scale, 16))) return CB_ERR_ALIGN;
     if (!on_grid(out_scale, 4)) return CB_ERR_ALIGN;
     int device = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = launch_row(a, vec, sms, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = launch_row(a, vec, pairs, sms, (cudaStream_t)stream);
     return e == cudaSuccess ? CB_OK : cuda_error(e, "norm launch");
 }

@@ -179,7 +179,17 @@ def test_sizes(lib, hidden):
             check(lib, case(rows, hidden, after, before, x, out=out, tokens=50))
 
 
-@pytest.mark.parametrize("hidden", [255, 257, 383, 385, 511, 577, 640, 641, 767, 768, 769])
+@pytest.mark.parametrize("hidden", [2, 62, 66, 130, 194, 258, 382, 390, 514, 642, 770, 1026, 1282, 2050, 2562, 4098, 5122, 6146, 8190, 8194])
+def test_rows_by_pairs(lib, hidden):
+    """Even rows off the 16-byte grid: lengths off it, starts off it, and starts and strides that are odd, which go one by one."""
+    rows = 141 if hidden < 3000 else 9
+    for after, before, out, x, gap in (("rms", "layer", "mx", "bf16", 0), ("layer", "rms", "bf16", "fp32", 2), ("none", "layer", "e4m3", "bf16", 6),
+                                       ("layer", "layer", "fp32", "fp32", 3)):
+        if hidden > 2 or before != "layer":  # (two elements are their mean and as much off it on each side)
+            check(lib, case(rows, hidden, after, before, x, out=out, tokens=50, pad=gap, off=gap))
+
+
+@pytest.mark.parametrize("hidden", [254, 255, 257, 258, 382, 383, 385, 386, 511, 577, 638, 640, 641, 642, 766, 767, 768, 769, 770])
 def test_many_short_rows_by_elements(lib, hidden):
     """More rows than have four warps each at once, in a number that fills no CTA."""
     pad = 1 if hidden % 8 == 0 else 0
