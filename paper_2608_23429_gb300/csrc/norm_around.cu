@@ -72,12 +72,12 @@ __device__ __forceinline__ void store_row(void* p, long long e, int dtype, int t
 
 // A row by elements, in registers: CH of them in each thread of its W warps. Short rows have a warp each, four to a CTA: there is nothing to wait
 // for but the row's own loads, and a CTA is launched for four rows (17300 x 220, layer norms, to fp32: 11.7 us, with four warps a row 25.9).
-// Their lines, and those of rows above 640 elements, are loaded when they are wanted, which leaves registers for more warps (220 elements 18.3 us
-// with the lines loaded early, 16384 x 1153 to 4 bits 93 instead of 51); four warps and up to 640 elements load them with the row, as few such
-// rows are bound by their loads' time (999 x 577 4.8 us; a warp each, late, 6.9).
+// Their lines, and those of many rows above 640 elements, are loaded when they are wanted, which leaves registers for more warps (220 elements 18.3 us
+// with the lines loaded early, 16384 x 1153 to 4 bits 93 instead of 51); four warps and up to 640 elements, and 16 and 32 warps of few rows, load them with
+// the row, as such rows are bound by their loads' time (999 x 577 4.8 us; a warp each, late, 6.9).
 constexpr int kHeldRows = 4;  // warps of a CTA whose rows have a warp each
 __host__ __device__ constexpr int held_rows(int W) { return W == 1 ? kHeldRows : 1; }
-__host__ __device__ constexpr bool around_early(int CH, int W) { return W > 1 && CH * W <= 24; }
+__host__ __device__ constexpr bool around_early(int CH, int W) { return W > 1 && (CH * W <= 24 || (CH <= 4 && W >= 16)); }
 // CTAs of an SM, by the registers that this leaves a thread: 40 for ten elements, 64 for sixteen, 80 for twenty.
 __host__ __device__ constexpr int around_ctas(int CH, int W) {
     if (around_early(CH, W)) return 0;
@@ -361,6 +361,10 @@ cudaError_t launch_held_row(const AroundArgs& a, int sms, cudaStream_t s) {
     }
     if (n <= 384) return launch_held<(2 + V) / V, 4, 2 / V, V>(a, s);
     if (n <= 640) return launch_held<(4 + V) / V, 4, 3 / V, V>(a, s);
+    // few long rows by as many warps as an SM has room for, lines early: 300 x 2047 7.4 -> 5.1 us (310 rows 7.6, with four warps each), 150 x 3383 8.1 -> 5.6
+    // (300 rows 8.1, with eight)
+    if (n > 1280 && n <= 2048 && a.rows <= 2u * sms) return launch_held<4 / V, 16, 2 / V, V>(a, s);
+    if (n > 2048 && n <= 4096 && a.rows <= 1u * sms) return launch_held<4 / V, 32, 2 / V, V>(a, s);
     // as few warps as hold the row: twice as many with half the elements each took 8192 x 2047 from 45 to 52 us, x 3383 from 88 to 106, x 5001
     // from 114 to 121; half as many with twice the elements 8192 x 2047 to 49, x 4095 from 92 to 94, x 7001 from 193 to 199
     if (n <= 1024) return launch_held<8 / V, 4, 5 / V, V>(a, s);

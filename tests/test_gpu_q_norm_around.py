@@ -179,6 +179,14 @@ def test_sizes(lib, hidden):
             check(lib, case(rows, hidden, after, before, x, out=out, tokens=50))
 
 
+@pytest.mark.parametrize("rows,hidden", [(3, 1281), (141, 1500), (300, 2047), (310, 2047), (150, 2049), (150, 2500), (141, 3383), (160, 3383), (3, 4095), (150, 4096)])
+def test_few_long_rows(lib, rows, hidden):
+    """Off the 16-byte grid, as many as have an SM's warps between them at once, and a few more."""
+    gap = 1 if hidden == 4096 else 0
+    for after, before, out, x in (("rms", "layer", "mx", "bf16"), ("layer", "rms", "bf16", "fp32"), ("layer", "layer", "e4m3", "bf16")):
+        check(lib, case(rows, hidden, after, before, x, out=out, tokens=47, pad=gap, off=gap))
+
+
 @pytest.mark.parametrize("hidden", [2, 62, 66, 130, 194, 258, 382, 390, 514, 642, 770, 1026, 1282, 2050, 2562, 4098, 5122, 6146, 8190, 8194])
 def test_rows_by_pairs(lib, hidden):
     """Even rows off the 16-byte grid: lengths off it, starts off it, and starts and strides that are odd, which go one by one."""
