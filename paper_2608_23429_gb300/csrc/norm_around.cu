@@ -70,12 +70,13 @@ __device__ __forceinline__ void store_row(void* p, long long e, int dtype, int t
     }
 }
 
-// A row by elements, in registers: CH of them in each thread of its W warps. Short rows have a warp each, four to a CTA: there is nothing to wait
-// for but the row's own loads, and a CTA is launched for four rows (17300 x 220, layer norms, to fp32: 11.7 us, with four warps a row 25.9).
+// A row by elements, in registers: CH pieces of V of them in each thread of its W warps. Short rows have a warp each, four to a CTA: there is nothing to wait
+// for but the row's own loads, and a CTA is launched for four rows (17300 x 220 one by one, layer norms, to fp32: 11.7 us, with four warps a row 25.9).
 // Their lines, and those of many rows above 640 elements, are loaded when they are wanted, which leaves registers for more warps (220 elements 18.3 us
 // with the lines loaded early, 16384 x 1153 to 4 bits 93 instead of 51); four warps and up to 640 elements, and 16 and 32 warps of few rows, load them with
 // the row, as such rows are bound by their loads' time (999 x 577 4.8 us; a warp each, late, 6.9).
 constexpr int kHeldRows = 4;  // warps of a CTA whose rows have a warp each
+// (CH: elements of a thread)
 __host__ __device__ constexpr int held_rows(int W) { return W == 1 ? kHeldRows : 1; }
 __host__ __device__ constexpr bool around_early(int CH, int W) { return W > 1 && (CH * W <= 24 || (CH <= 4 && W >= 16)); }
 // CTAs of an SM, by the registers that this leaves a thread: 40 for ten elements, 64 for sixteen, 80 for twenty.
