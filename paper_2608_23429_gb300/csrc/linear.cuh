@@ -46,6 +46,17 @@ __host__ __device__ constexpr int epi_warps(Results r, bool mx = false) {
     if (mx) return r == Results::kDirect ? 16 : r == Results::kHiddenLong ? 8 : r == Results::kQuant ? 16 : 12;
     return r == Results::kDirect ? 16 : 8;
 }
+// Which chunks of 32 columns of a tile are a warp's of the epilogue: its first one (`share`: the warp's place among those of its quarter of the
+// lanes), the one behind chunk c, and the first one of the next tile. Outputs in 4 bits go by pairs of neighbours, three pairs for four warps, of which
+// each one in turn has none; in passes over K a chunk has the same warp in every tile, as the sum of its passes is kept in one place of TMEM
+// that nothing but the warp's own order guards.
+__host__ __device__ constexpr int epi_first_chunk(Results r, int share) { return r == Results::kQuant ? 2 * share : share; }
+__host__ __device__ constexpr int epi_chunk_behind(Results r, bool mx, int c) {
+    return r != Results::kQuant ? c + epi_warps(r, mx) / 4 : c % 2 == 0 ? c + 1 : c + epi_warps(r, mx) / 2 - 1;
+}
+__host__ __device__ constexpr int epi_next_first_chunk(Results r, bool passes, int begin) {
+    return r == Results::kQuant && !passes ? (begin + 6) % 8 : begin;
+}
 constexpr int kTurnBytes = 32 * 32 * 4;  // bytes of an epilogue's warp to turn sums in, or two boxes of results
 
 struct LinearArgs {

@@ -638,9 +638,8 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
         const LinearEpilogue E = from_here(A.e);
         float* const turn = reinterpret_cast<float*>(turns + warp * turn_bytes);
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
-        // Its first one. Outputs in 4 bits go by pairs of neighbours, three pairs for four warps, of which each one in turn has none.
-        int begin = QUANT ? 2 * half : half;
-        auto behind = [](int c) { return !QUANT ? c + EPI / 4 : c % 2 == 0 ? c + 1 : c + EPI / 2 - 1; };
+        int begin = epi_first_chunk(RESULTS, half);
+        auto behind = [](int c) { return epi_chunk_behind(RESULTS, MX, c); };
         const bool whole = QUANT && ((uintptr_t)E.out | (uintptr_t)E.out_stride / 2) % 32 == 0;
         int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken
         auto first_row = [&](const Tile& tile) { return (tile.m * CG + (int)rank) * kRows + quarter * 32; };
@@ -777,7 +776,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
             if (!ok || !all(wait(acc_full + 8 * (pass & 1), (pass >> 1) & 1, limit, CB_DEV_CONSUMER_TIMEOUT))) break;
             fence_after();
             const uint32_t acc_at = lanes + (pass & 1) * stride;
-            const int next_begin = QUANT ? (begin + 6) % 8 : begin;
+            const int next_begin = epi_next_first_chunk(RESULTS, PASSES, begin);
             const int next_col = next.n * A.tile_n + next_begin * 32 + lane;
             if (begin >= chunks) {
                 if (BIAS) look_bias(next_col, next_sample);
