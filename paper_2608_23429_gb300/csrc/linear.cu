@@ -353,7 +353,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     int cg = 1;
     a.k_blocks = (a.k_bytes + 127) / 128;
     // fp32 results: passes over K (see linear_tc.cuh)
-    const bool fp32 = (out && !ep.out_bf16) || (resid_out && !ep.resid_bf16);
+    const bool fp32 = (out && io->out_dtype == CB_FP32) || (resid_out && !ep.resid_bf16);
     a.pass_blocks = fp32 ? (mx ? kPassMx : d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
     // (4 bits) rows that x does not have are not loaded: what the tensor cores read in their place makes sums that nobody takes
     a.x_rows = mx ? std::min(128, (ep.M + 7) / 8 * 8) : 128;
