@@ -140,7 +140,7 @@ constexpr int kMxShortBoxes[2] = {1, 4};
 // Bytes of a row up to which a box's place in it (and a gate's piece's), and that of the box behind, is a positive int.
 constexpr long long kMaxRowBytes = (1LL << 31) - 1024;
 
-// Results and hidden states whose rows lie on the 16-byte grid go by TMA, in boxes of 32 rows by 64 bytes.
+// Results and hidden states whose rows start on 16-byte boundaries go by TMA, in boxes of 32 rows by 64 bytes.
 struct TmaRows {
     const void* p;
     long long row, es;
@@ -157,10 +157,11 @@ TmaResults tma_results(const cb_linear_io* io, LinearArgs* a) {
 }
 bool goes_by_tma(const cb_linear_io* io, LinearArgs* a) {
     const LinearEpilogue& e = a->e;
-    for (const auto& u : tma_results(io, a).used)
-        // (a store writes whole pieces of 16 bytes, past the end of a row that is not made of them)
-        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40 || e.N * u.es > kMaxRowBytes || e.N * u.es % 16 != 0))
-            return false;
+    for (const auto& u : tma_results(io, a).used) {
+        if (u.p && (!on_grid(u.p, 16) || u.row * u.es % 16 != 0 || u.row * u.es >= 1LL << 40 || e.N * u.es > kMaxRowBytes)) return false;
+        // a store writes whole pieces of 16 bytes: the last one of a row that ends inside it is the threads' (in 4 bits all of the row)
+        if (u.p && e.N * u.es % 16 != 0 && (a->operands == Operands::kMx || e.N < 8)) return false;
+    }
     // a gate's pieces of 16 bytes are read whole
     const long long gs = (long long)bytes_of(io->gate_dtype);
     return !e.gate || (on_grid(e.gate, 16) && e.gate_stride * gs % 16 == 0 && e.N * gs % 16 == 0 && e.N * gs <= kMaxRowBytes);
@@ -170,9 +171,11 @@ int results_by_tma(const cb_linear_io* io, LinearArgs* a) {
     a->results = Results::kDirect;
     const bool mx = a->operands == Operands::kMx;
     if (!goes_by_tma(io, a)) return CB_OK;
+    a->whole = (e.out && e.out_bf16) || (e.resid_out && e.resid_bf16) ? e.N & ~7 : e.N & ~3;
     for (const auto& u : tma_results(io, a).used) {
         if (!u.p) continue;
-        const int rc = operand_map(u.map, u.p, e.M, e.N * u.es, u.row * u.es, 32, 64);
+        // what is read ends with the row, what is written with its last whole piece
+        const int rc = operand_map(u.map, u.p, e.M, (u.map == &a->resid_map ? e.N : a->whole) * u.es, u.row * u.es, 32, 64);
         if (rc != CB_OK) return rc;
     }
     a->results = e.resid_out ? Results::kHidden : Results::kOut;
@@ -392,6 +395,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
         ep = LinearEpilogue{ep.M, ep.N, CB_ACT_NONE, (unsigned)ep.M, 0, 0, 0, 0, row, 0, 0, 0, nullptr, nullptr, nullptr, nullptr, nullptr,
                             const_cast<float*>(join.sums), nullptr};
         a.results = Results::kOut;
+        a.whole = ep.N;  // (rows of sums have room for a whole last piece)
         rc = operand_map(&a.out_map, join.sums, (long long)a.parts * a.part_rows, 4ll * ep.N, 4 * row, 32, 64);
     } else if (out_mx) {
         a.results = Results::kQuant;

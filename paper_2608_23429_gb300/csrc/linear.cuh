@@ -67,6 +67,7 @@ struct LinearArgs {
     unsigned out_tiles;                    // kQuant: tiles of scales of a row of the output
     CUtensorMap x_map, w_map;
     CUtensorMap out_map, resid_map, resid_out_map;
+    int whole;             // columns of results that leave by TMA; up to seven behind them by the threads
     int out_boxes;         // operands in 4 bits: boxes of an output alone, of a warp
     int ring, more_boxes;  // hidden states of chunks that a warp holds; boxes of shared memory that it needs for them besides two
     LinearEpilogue e;

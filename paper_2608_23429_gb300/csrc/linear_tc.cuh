@@ -348,6 +348,25 @@ __device__ __forceinline__ void put_box(uint32_t box, int lane, const Two* x) {
     for (int j = 0; j < 4; ++j) st_shared16(piece_at(box, lane, j), BF16 ? packed8(x + 4 * j) : as_uint4(x[2 * j], x[2 * j + 1]));
 }
 
+// A copy by TMA writes whole pieces of 16 bytes. What a row has behind those that its results leave in, columns `whole` to N (seven at
+// most), goes out of the boxes of its last chunk (box1: its columns from the 16th on in fp32) by the lane that has the row. GB300, 8192 rows of 1160
+// elements, K = 1152, 1154 columns to bf16: 18.4 us, e4m3 12.2, altogether by the threads 20.5 and 16.1 (1160 columns 18.4 and 11.9). Not
+// inlined: in line it took up to 4 % of the time of small products, whose way through the code counts, without being reached.
+__device__ __noinline__ void put_tail(uint32_t box0, uint32_t box1, int lane, void* p, long long stride, int bf16, int row, int whole, int N) {
+#pragma unroll 1
+    for (int c = whole; c < N; ++c) {
+        if (bf16) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(piece_at(box0, lane, c % 32 / 8) + c % 8 * 2) : "memory");
+            reinterpret_cast<uint16_t*>(p)[row * stride + c] = v;
+        } else {
+            uint32_t v;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(piece_at(c % 32 < 16 ? box0 : box1, lane, c % 16 / 4) + c % 4 * 4) : "memory");
+            reinterpret_cast<uint32_t*>(p)[row * stride + c] = v;
+        }
+    }
+}
+
 // The gate of 32 columns as it lies in memory, `row` being this lane's sample's, and its values (1 where there is none). N gates
 // are whole pieces of 16 bytes.
 __device__ __forceinline__ void look_gate(const LinearEpilogue& E, const char* row, int col, uint4* raw) {
@@ -639,6 +658,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
         float* const turn = reinterpret_cast<float*>(turns + warp * turn_bytes);
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
         int begin = epi_first_chunk(RESULTS, half);
+        const int by_tma = A.whole;  // columns of its results
         auto behind = [](int c) { return epi_chunk_behind(RESULTS, MX, c); };
         const bool whole = QUANT && ((uintptr_t)E.out | (uintptr_t)E.out_stride / 2) % 32 == 0;
         int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken
@@ -828,7 +848,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                             else put_box<false>(box, lane, x + 8);
                             fence_generic_to_async();
                             __syncwarp();
-                            if (lane == 0 && col + 16 * h < E.N) store_box(&A.out_map, (col + 16 * h) * (E.out_bf16 ? 2 : 4), row0 + tile.part * A.part_rows, box);
+                            if (lane == 0 && col + 16 * h < by_tma) store_box(&A.out_map, (col + 16 * h) * (E.out_bf16 ? 2 : 4), row0 + tile.part * A.part_rows, box);
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
                     } else {
@@ -856,8 +876,8 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                         ++n_chunks, held.next(A.ring);
                         fence_generic_to_async();
                         __syncwarp();
-                        if (lane == 0) {
-                            const bool more = col + 16 < E.N;
+                        if (lane == 0 && col < by_tma) {
+                            const bool more = col + 16 < by_tma;
                             if (E.out) {
                                 store_box(&A.out_map, col * (E.out_bf16 ? 2 : 4), row0, box_at(0));
                                 if (!E.out_bf16 && more) store_box(&A.out_map, col * 4 + 64, row0, box_at(1));
@@ -891,6 +911,18 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                     finish_rows(E, row0, row0 + row, col, now, r, f);
                 }
                 __syncwarp();
+            }
+            if constexpr (!MX && !DIRECT) {  // (its last chunk's boxes are as they were stored)
+                if (__builtin_expect(by_tma < E.N, 0) && ok && col0 + A.tile_n >= E.N && chunks % 2 != half && row0 + lane < E.M && chunks > 0) {
+                    const int row = row0 + lane;
+                    if constexpr (HIDDEN) {
+                        const int slot = held.s == 0 ? A.ring - 1 : held.s - 1;
+                        if (E.out) put_tail(box_at(0), box_at(1), lane, E.out, E.out_stride, E.out_bf16, row, by_tma, E.N);
+                        put_tail(ring_box(slot), ring_box(slot, 1), lane, E.resid_out, E.resid_out_stride, E.resid_bf16, row, by_tma, E.N);
+                    } else {
+                        put_tail(box_at((n_boxes - out_boxes) & 1), box_at((n_boxes - 1) & 1), lane, E.out, E.out_stride, E.out_bf16, row, by_tma, E.N);
+                    }
+                }
             }
             begin = next_begin;
             if (!ok) break;
