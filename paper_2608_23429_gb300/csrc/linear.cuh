@@ -121,8 +121,8 @@ struct LinearJoinArgs {
 };
 cudaError_t launch_linear_join(const LinearJoinArgs& a, cudaStream_t s);
 
-// The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows. prepare_linear raises the kernels' shared-memory
-// limit and tells how many pairs of CTAs run at once.
+// The tensor-core kernels (linear_tc.cuh): cg CTAs per tile of 128 cg rows. prepare_linear raises the shared-memory
+// limit of those for 16 and 8 bits (launch_linear, at its first use, that of those for 4) and tells how many pairs of CTAs run at once.
 size_t linear_stage_bytes(int cg, int tile_n);
 size_t linear_fixed_bytes(Results r, int more_boxes);  // shared memory besides the stages
 constexpr int kBox = 2048, kMaxRing = 6;
