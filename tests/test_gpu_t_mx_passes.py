@@ -80,3 +80,13 @@ def check(lib, m, n, k, out, resid=None, gate=False, tokens=0):
 def test_outputs_in_4_bits(lib, m, n, k):
     """Half of the warps have no chunk of a tile."""
     check(lib, m, n, k, "mx")
+
+
+# (sizes whose way test_mx_passes_cpu.py tells: passes, and more tiles than CTAs)
+@pytest.mark.parametrize("m,n,k,out,resid", [
+    (6000, 2100, 16640, "fp32", None), (6000, 2100, 40000, "fp32", None),  # results by TMA
+    (6000, 2100, 16640, None, "fp32"), (4000, 2100, 33000, "fp32", "fp32"), (4000, 2100, 33000, "bf16", "fp32"),  # hidden states
+    (4000, 2101, 16640, "fp32", None), (4000, 2101, 33000, "bf16", "fp32"),  # by the threads
+    (4000, 2104, 66000, "bf16", None), (4000, 2104, 66000, "bf16", "bf16"), (3000, 2101, 66000, None, "bf16")])
+def test_results_of_every_kind(lib, m, n, k, out, resid):
+    check(lib, m, n, k, out, resid, gate=resid is not None, tokens=100)
