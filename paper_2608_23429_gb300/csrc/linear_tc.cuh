@@ -658,7 +658,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
         float* const turn = reinterpret_cast<float*>(turns + warp * turn_bytes);
         const int quarter = warp % 4, half = warp / 4;  // this warp's rows, and its share of their chunks of 32 columns
         int begin = epi_first_chunk(RESULTS, half);
-        const int by_tma = A.whole;  // columns of its results
+        const int by_tma = MX ? E.N : A.whole;  // columns of its results
         auto behind = [](int c) { return epi_chunk_behind(RESULTS, MX, c); };
         const bool whole = QUANT && ((uintptr_t)E.out | (uintptr_t)E.out_stride / 2) % 32 == 0;
         int n_done = 0, pass = 0, n_boxes = 0;  // tiles, and accumulators, taken
@@ -876,7 +876,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                         ++n_chunks, held.next(A.ring);
                         fence_generic_to_async();
                         __syncwarp();
-                        if (lane == 0 && col < by_tma) {
+                        if (lane == 0 && (MX || col < by_tma)) {
                             const bool more = col + 16 < by_tma;
                             if (E.out) {
                                 store_box(&A.out_map, col * (E.out_bf16 ? 2 : 4), row0, box_at(0));
