@@ -121,7 +121,8 @@ typedef struct {
  * and after_bias go with a norm after, weight and bias with one before, and scale and shift with an out. x_out may be
  * x itself (same stride). Rows that are not finite touch no others; in 4 bits a block with a NaN or an
  * infinity is NaN.
- * Rows and hidden sizes up to 16384 on the 16-byte grid take vector loads, others elements.
+ * Hidden sizes up to 16384 that are multiples of 8, with all pointers and strides on the 16-byte grid (8 bytes for rows in e4m3), take vector
+ * loads; even sizes up to 8192 whose pointers and strides are whole pairs of elements go by pairs; all others, longer ones on the grid too, by elements.
  * Errors: CB_ERR_ARG, CB_ERR_ALIGN (a pointer off its element size; an output in 4 bits or its scales off 16
  * bytes), CB_ERR_LIMIT (rows beyond 2^31 - 1 or hidden beyond 2^31 - 256), CB_ERR_CUDA. */
 int cb_norm_around(const cb_norm_around_desc* desc, const void* x, const void* branch, const void* gate,
@@ -233,7 +234,7 @@ int cb_linear_set_option(cb_linear* layer, int option, int64_t value);
  *     out = round(v)                        the branch output, as cb_cache_push takes it
  *     resid_out = round(resid + gate * v)   the hidden state (gate: a line per sample)
  * with sums, epilogue and hidden state in fp32 and one rounding to each result. The
- * tensor cores cut sums off rather than round them: where a result is fp32 they sum
+ * tensor cores cut sums off rather than round them (CB_BF16 and CB_E4M3 layers): where a result is fp32 they sum
  * parts of 512 features (e4m3: 4096; up to 32 rows: 128 and 256 at most), which are added
  * rounded to nearest. Measured, in the root mean square relative to the sums': 5e-7 with signs
  * mixed, 8e-7 with all terms of one sign, and up to 2^-24 for every part added (of which most
@@ -241,12 +242,14 @@ int cb_linear_set_option(cb_linear* layer, int option, int64_t value);
  * than 32 KB, else one part, which is off by up to 7.2e-5 (16384 features of one sign) before
  * the rounding to bf16.
  * CB_MXFP4 layers: x_scale are x's scales, and their factors 2^(e - 127) stand in place of x_scale[m] w_scale[n] within the
- * sum, whose products are exact. out in CB_MXFP4 (no hidden state then): v as cb_mx_quantize makes
+ * sum, whose products are exact. fp32 results are sums of parts of 16384 features, other results of one part up to 65536 features and of parts of
+ * 8192 beyond, whatever the rows are; under scales that differ much (lognormal) a part is off, in the root mean square relative to the sums' with signs
+ * mixed and with all terms of one sign, by 5e-8 and 1.2e-7 at 2048 features, 1.9e-7 and 6.2e-7 at 16384, 3.2e-6 and 6.4e-6 at 65536. out in CB_MXFP4 (no hidden state then): v as cb_mx_quantize makes
  * it of fp32 rows, with io->out_scale.
  * x_scale: one float a row (CB_E4M3, NULL: 1; not for CB_BF16). out may be NULL, resid and resid_out
  * may be NULL together, gate (with resid only) may be NULL: 1; one result at least
  * is wanted. resid_out may be resid itself (same stride). The order of a sum depends
- * on the sizes alone: equal calls give equal bits.
+ * on the sizes, the types and what of it lies on the 16-byte grid alone: equal calls give equal bits.
  * Over 32 rows, operands whose rows do not start on 16-byte boundaries are copied onto
  * them first, and few tiles of long sums are split over in_features, whose parts' sums a
  * second kernel adds in order. Memory for either is allocated and freed in stream order,

@@ -204,7 +204,7 @@ constexpr int kFewRows = 32;
 // narrower tiles and 89 in one; 4 bits under scales that differ, 16384 features 1.9e-7 and 6.2e-7, 65536 3.2e-6 and 6.4e-6; 8192^3 in
 // passes of 4096 features 210 us, in one 170).
 constexpr int kPassBf16 = 8, kPassE4m3 = 32, kPassMx = 64;
-// Results in bf16 alone: one pass up to kOnePass slabs, as tiles of 256 columns are worth more (4608 x 3072 x 15360 227 -> 274 us, 8192 x
+// Results in bf16 (or 4 bits) alone: one pass up to kOnePass slabs, as tiles of 256 columns are worth more (4608 x 3072 x 15360 227 -> 274 us, 8192 x
 // 8192 x 8192 554 -> 648, 8192 x 1152 x 4608 60.2 -> 62.0 with passes of 16) and what the sums lose is small against the rounding that
 // follows, 2e-3 to 4e-3: 7.2e-5 of their size at most (16384 features of bf16, all terms of one sign; 1.9e-5 with signs mixed). Longer sums
 // in passes, as it grows with the length: 3.5e-4 at 65536, 6.5e-3 at 2^20.
@@ -355,7 +355,7 @@ int cb_linear_run(const cb_linear* l, const cb_linear_io* io, const void* x, con
     }
     int cg = 1;
     a.k_blocks = (a.k_bytes + 127) / 128;
-    // fp32 results: passes over K (see linear_tc.cuh)
+    // fp32 results (which those in 4 bits are not: 8192 x 4608 x 20000 to 4 bits in passes 360 us, in one 288): passes over K (see linear_tc.cuh)
     const bool fp32 = (out && io->out_dtype == CB_FP32) || (resid_out && !ep.resid_bf16);
     a.pass_blocks = fp32 ? (mx ? kPassMx : d.type == CB_BF16 ? kPassBf16 : kPassE4m3) : a.k_blocks > kOnePass ? kPassLong : a.k_blocks;
     // (4 bits) rows that x does not have are not loaded: what the tensor cores read in their place makes sums that nobody takes

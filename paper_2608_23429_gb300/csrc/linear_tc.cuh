@@ -21,8 +21,8 @@
 // Operands in 4 bits (OPERANDS = kMx; slabs of 256 features) come with their scales, two tiles of 128 rows by 4 blocks of x and of each 128
 // columns, which one thread copies to TMEM ahead of the products that take them: they leave room for tiles of 192 columns. The
 // products are four times as fast, so the epilogue counts four times as much: each warp brings its own columns' biases and gates (no wait for
-// other warps), tiles are sought without divisions, and there are 12 or 16 warps where the sums are short. GB300: 8192^3 to bf16 149 to 153 us (7.3
-// PFLOP/s, the tensor cores busy 83 % of the time), 8192 x 4608 x 1152 with GELU to 4 bits 29 us, 8192 x 1152 x 4608 with output and gated hidden
+// other warps), tiles are sought without divisions, and there are 12 or 16 warps where the sums are short. GB300: 8192^3 to bf16 149 to 153 us in a loop
+// of its own (7.3 PFLOP/s, the tensor cores busy 83 % of the time) and 169 to 172 among calls on new inputs (6.4), 8192 x 4608 x 1152 with GELU to 4 bits 29 us, 8192 x 1152 x 4608 with output and gated hidden
 // state 26.
 //
 // Bound by the tensor cores where tiles fill the SMs' rounds: GB300, 4608 x 3072 x 15360 bf16 with a gated hidden state 264 us (1.65
@@ -148,7 +148,8 @@ __device__ __forceinline__ void scales_to_tmem(uint32_t at, uint64_t desc) {
     if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory");
     else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(at), "l"(desc) : "memory");
 }
-// 64 features in 4 bits under two scales a row, at a_scale and b_scale in TMEM.
+// 64 features in 4 bits under two scales a row, at a_scale and b_scale in TMEM. (The public PTX ISA has 96 features an instruction of this kind on
+// sm_103a, too, which has not been built here: the products' rate is that of 64.)
 template <int CG>
 __device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t a_scale, uint32_t b_scale, bool add) {
     const uint32_t on = add;
