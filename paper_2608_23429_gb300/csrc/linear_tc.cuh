@@ -914,6 +914,7 @@ __global__ void __launch_bounds__(linear_threads(RESULTS, OPERANDS == Operands::
                 __syncwarp();
             }
             if constexpr (!MX && !DIRECT) {  // (its last chunk's boxes are as they were stored)
+                static_assert(EPI / 4 == 2, "a tile's last chunk is one's of two warps");
                 if (__builtin_expect(by_tma < E.N, 0) && ok && col0 + A.tile_n >= E.N && chunks % 2 != half && row0 + lane < E.M && chunks > 0) {
                     const int row = row0 + lane;
                     if constexpr (HIDDEN) {

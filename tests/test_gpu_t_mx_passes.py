@@ -76,9 +76,9 @@ def check(lib, m, n, k, out, resid=None, gate=False, tokens=0):
     block.cb_linear_destroy(layer)
 
 
-@pytest.mark.parametrize("m,n,k", [(2600, 2600, 66000), (3000, 1000, 131328)])
+@pytest.mark.parametrize("m,n,k", [(2600, 2600, 66000), (3000, 1000, 131328), (5000, 2320, 16416), (3000, 2304, 40000)])
 def test_outputs_in_4_bits(lib, m, n, k):
-    """Half of the warps have no chunk of a tile."""
+    """In passes, where half of the warps have no chunk of a tile; and in one pass over the longer sums that have only one."""
     check(lib, m, n, k, "mx")
 
 

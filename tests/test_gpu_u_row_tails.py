@@ -81,3 +81,32 @@ def test_gates_that_end_on_the_grid(lib, type, out):
     """bf16 results that end inside a piece under fp32 gates that do not; rows of several samples in a warp."""
     for m, n, k, tokens in ((3000, 1156, 512, 1500), (300, 260, 64, 7), (2000, 1156, 4608, 100)):
         check(lib, type, m, n, k, n + 4, out, "bf16", gate=True, tokens=tokens)
+
+
+def test_in_a_graph_and_on_two_streams(lib):
+    """Calls of two streams into columns of one wider tensor, next to each other, captured and replayed: neither touches the other's."""
+    block, cb = lib
+    m, n, k = 1000, 300, 256
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w = (torch.randint(-1, 2, (r, k), generator=g, device="cuda").bfloat16() for r in (m, 2 * n))
+    both = torch.zeros(m, 608, dtype=torch.bfloat16, device="cuda")  # columns 0 to 299 and 304 to 603
+    layers = [block.cb_linear_create(w[i * n:(i + 1) * n], n, k, cb.CB_BF16) for i in range(2)]
+    io = block.cb_linear_io(rows=m, out_stride=608, out_dtype=cb.CB_BF16)
+    want = (x.float() @ w.float().t()).bfloat16()
+    streams, graphs = [torch.cuda.Stream(), torch.cuda.Stream()], [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    torch.cuda.synchronize()
+    for i, (s, graph) in enumerate(zip(streams, graphs)):
+        with torch.cuda.graph(graph, stream=s):
+            block.cb_linear_run(layers[i], io, x, out=both[:, 304 * i:], stream=s)
+    for _ in range(5):
+        both.fill_(9.0)
+        torch.cuda.synchronize()
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(both[:, :n], want[:, :n]) and torch.equal(both[:, 304:304 + n], want[:, n:])
+        assert bool((both[:, n:304] == 9.0).all()) and bool((both[:, 304 + n:] == 9.0).all())
+    assert block.cb_linear_device_status() == 0
+    for layer in layers:
+        block.cb_linear_destroy(layer)
